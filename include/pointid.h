@@ -422,6 +422,131 @@ int pointid_client_classify_patches(pointid_client c, const float *patches,
 int pointid_client_close(pointid_client c);
 
 /*
+ * Layers: dense and gated layers, their gradients, and 8-bit activation
+ * checkpoints (the dense part of the network of paper §2.2 as operators, for
+ * refining it or trying another block in its place).  They need no classifier:
+ * a pointid_layers holds a device and a cache of scratch buffers, which follows
+ * the rules under "Temporary device memory" above; any number of host threads
+ * and streams may use one at once.
+ *
+ * Matrices are row-major device memory of the call's `dtype` (POINTID_FP32,
+ * POINTID_BF16 or POINTID_FP16) with a row pitch of `ld` elements (at least the
+ * columns; rows need no alignment beyond their element's), x [m][k], weights
+ * [k][n], biases and their gradients fp32 [n] whatever the type.  0 <= m < 2^31,
+ * 1 <= k, n <= 2^20.  Products are summed in fp32 and rounded to `dtype` once.
+ * POINTID_FP32 products are of operands cut exactly into three bf16 parts each,
+ * or plain fp32; their inputs must be finite.  In the 16-bit types infinities
+ * and NaNs go through as in fp32 arithmetic.  Outputs must not overlap inputs,
+ * but `y` may be `residual` itself.  Aligned operands (16-byte base, row pitch a
+ * multiple of 8 elements) save a copy.
+ */
+typedef struct pointid_layers_s *pointid_layers;
+
+/* A cache of scratch buffers on `device`.  Errors: EINVAL (NULL out), ENODEV,
+ * ENOMEM.  pointid_layers_destroy synchronises the device; NULL is a no-op.
+ * pointid_layers_trim is pointid_trim for this cache. */
+int pointid_layers_create(int device, pointid_layers *out);
+int pointid_layers_destroy(pointid_layers l);
+int pointid_layers_trim(pointid_layers l, uint64_t keep_bytes, uint64_t *cached_bytes);
+
+/* activations; GELU(z) = z Phi(z) with the normal distribution function Phi;
+ * the slope of RELU at 0 is 0 */
+enum {
+    POINTID_ACT_NONE = 0,
+    POINTID_ACT_RELU = 1,
+    POINTID_ACT_SILU = 2,       /* z sigmoid(z) */
+    POINTID_ACT_GELU = 3,
+    POINTID_ACT_SIGMOID = 4
+};
+
+typedef struct {
+    void *data;
+    int64_t ld;                 /* row pitch in elements */
+} pointid_matrix;
+
+/* An 8-bit checkpoint of a matrix [rows][cols], both arrays contiguous.  The
+ * values of columns 32 j .. 32 j + 31 of a row share a power of two: p is the
+ * largest integer for which their largest finite magnitude times 2^p is at most
+ * 448, at most 126 (0 where all are 0); exponents[row][j] = 127 - p and
+ * codes[row][col] = the value times 2^p rounded to OCP e4m3 (nearest even).  A
+ * value that is not finite becomes NaN. */
+typedef struct {
+    uint8_t *codes;             /* [rows][cols] */
+    uint8_t *exponents;         /* [rows][ceil(cols / 32)] */
+} pointid_checkpoint;
+
+/* Activations kept between the passes: a matrix of the call's dtype
+ * (full.data), or a checkpoint (full.data NULL). */
+typedef struct {
+    pointid_matrix full;
+    pointid_checkpoint packed;
+} pointid_kept;
+
+/*
+ * y = act(x W + bias) + residual, and optionally z = x W + bias kept for the
+ * backward pass (written in the same pass).
+ *   bias, residual, keep_z  optional (NULL)
+ * m == 0 is a successful no-op.
+ * Errors: EINVAL (NULL l, x, w, y or data; both or neither kind in keep_z; a
+ * size, pitch, activation or alignment to the element out of range),
+ * EUNSUPPORTED (dtype), ENOMEM, EHIP.
+ */
+int pointid_dense(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
+                  const pointid_matrix *x, const pointid_matrix *w, const float *bias,
+                  const pointid_matrix *residual, const pointid_matrix *y,
+                  const pointid_kept *keep_z, void *stream);
+
+/*
+ * Gradients of pointid_dense from dy (the residual's gradient is dy itself):
+ *   dz = dy act'(z),  dx = dz W^T,  dw = x^T dz,  db[j] = sum over rows of dz[.][j]
+ *   x       as a matrix or a checkpoint; needed for dw only
+ *   w       needed for dx only
+ *   z       as kept; not needed for POINTID_ACT_NONE
+ *   dx, dw, db  each optional (NULL)
+ * For the products dz is rounded to the 16-bit types (dz of few values is kept in
+ * two parts); db is summed from fp32 in a fixed order.  m == 0 sets dw and db to 0.
+ * Errors: as pointid_dense, EINVAL also for an input that an output needs.
+ */
+int pointid_dense_backward(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
+                           const pointid_matrix *dy, const pointid_kept *x, const pointid_matrix *w,
+                           const pointid_kept *z, const pointid_matrix *dx, const pointid_matrix *dw,
+                           float *db, void *stream);
+
+/*
+ * A gated layer: h = act(g) u with g = x Wg + bias_g and u = x Wu + bias_u,
+ * both products, the activation and the product of the two in one pass; g and u
+ * optionally kept for the backward pass.
+ * Errors as pointid_dense.
+ */
+int pointid_gated(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
+                  const pointid_matrix *x, const pointid_matrix *wg, const pointid_matrix *wu,
+                  const float *bias_g, const float *bias_u, const pointid_matrix *h,
+                  const pointid_kept *keep_g, const pointid_kept *keep_u, void *stream);
+
+/*
+ * Gradients of pointid_gated from dh:
+ *   dg = dh u act'(g),  du = dh act(g),  dx = dg Wg^T + du Wu^T,
+ *   dwg = x^T dg,  dwu = x^T du,  dbg and dbu the column sums of dg and du
+ * x, wg and wu, and the outputs, as in pointid_dense_backward (dwg and dwu are
+ * given both or neither); g and u are always needed.
+ */
+int pointid_gated_backward(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
+                           const pointid_matrix *dh, const pointid_kept *x, const pointid_matrix *wg,
+                           const pointid_matrix *wu, const pointid_kept *g, const pointid_kept *u,
+                           const pointid_matrix *dx, const pointid_matrix *dwg,
+                           const pointid_matrix *dwu, float *dbg, float *dbu, void *stream);
+
+/*
+ * A matrix to a checkpoint and back (the values it stands for, rounded to
+ * `dtype`).  No handle; the current HIP device.  rows >= 0 (0: a no-op),
+ * 1 <= cols <= 2^20.  Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
+ */
+int pointid_checkpoint_save(int dtype, int64_t rows, int64_t cols, const pointid_matrix *x,
+                            const pointid_checkpoint *out, void *stream);
+int pointid_checkpoint_load(int dtype, int64_t rows, int64_t cols, const pointid_checkpoint *in,
+                            const pointid_matrix *out, void *stream);
+
+/*
  * Kernel timing for measurement tools (not needed for classification).  While
  * enabled (process-wide), every kernel a classification or hit-finding call
  * launches carries HIP events on its own dispatch (hipExtLaunchKernel), on the

@@ -32,6 +32,7 @@ POINTID_BF16 = 1
 POINTID_FP16 = 2
 POINTID_FP8 = 3
 MAX_PLANES = 64
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "sigmoid": 4}
 
 _STATUS = {0: "OK", -1: "EINVAL", -2: "ENOMEM", -3: "EHIP", -4: "ENODEV", -5: "EUNSUPPORTED",
            -6: "EIO"}
@@ -62,6 +63,18 @@ class _Request(ctypes.Structure):
                 ("plane", ctypes.c_int32), ("scores", ctypes.c_void_p)]
 
 
+class _Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
+
+
+class _Packed(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("exponents", ctypes.c_void_p)]
+
+
+class _Kept(ctypes.Structure):
+    _fields_ = [("full", _Matrix), ("packed", _Packed)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -69,6 +82,7 @@ def _load():
             "(or __graft_entry__.build()) first")
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, i64, cint = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_int
+    mat, kept = ctypes.POINTER(_Matrix), ctypes.POINTER(_Kept)
     sig = {
         "pointid_create": (cint, [ctypes.POINTER(_Weights), cint, cint, ctypes.POINTER(vp)]),
         "pointid_destroy": (cint, [vp]),
@@ -101,6 +115,18 @@ def _load():
         "pointid_client_classify": (cint, [vp, i32, vp, i64, vp, ctypes.POINTER(i64)]),
         "pointid_client_classify_patches": (cint, [vp, vp, i64, vp, ctypes.POINTER(i64)]),
         "pointid_client_close": (cint, [vp]),
+        "pointid_layers_create": (cint, [cint, ctypes.POINTER(vp)]),
+        "pointid_layers_destroy": (cint, [vp]),
+        "pointid_layers_trim": (cint, [vp, ctypes.c_uint64, ctypes.POINTER(ctypes.c_uint64)]),
+        "pointid_dense": (cint, [vp, cint, cint, i64, i64, i64, mat, mat, vp, mat, mat, kept, vp]),
+        "pointid_dense_backward": (cint, [vp, cint, cint, i64, i64, i64, mat, kept, mat, kept, mat, mat,
+                                          vp, vp]),
+        "pointid_gated": (cint, [vp, cint, cint, i64, i64, i64, mat, mat, mat, vp, vp, mat, kept, kept,
+                                 vp]),
+        "pointid_gated_backward": (cint, [vp, cint, cint, i64, i64, i64, mat, kept, mat, mat, kept, kept,
+                                          mat, mat, mat, vp, vp, vp]),
+        "pointid_checkpoint_save": (cint, [cint, i64, i64, mat, ctypes.POINTER(_Packed), vp]),
+        "pointid_checkpoint_load": (cint, [cint, i64, i64, ctypes.POINTER(_Packed), mat, vp]),
         "pointid_timing_enable": (cint, [cint]),
         "pointid_timing_reset": (cint, []),
         "pointid_timing_query": (cint, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
@@ -126,7 +152,9 @@ EXPORTED = ("pointid_create", "pointid_destroy", "pointid_precision", "pointid_t
             "pointid_gather_planes", "pointid_find_hits", "pointid_classify_planes_ds",
             "pointid_downsample", "pointid_server_start", "pointid_server_stop",
             "pointid_client_connect", "pointid_client_classify", "pointid_client_classify_patches",
-            "pointid_client_close", "pointid_timing_enable", "pointid_timing_reset",
+            "pointid_client_close", "pointid_layers_create", "pointid_layers_destroy", "pointid_layers_trim",
+            "pointid_dense", "pointid_dense_backward", "pointid_gated", "pointid_gated_backward",
+            "pointid_checkpoint_save", "pointid_checkpoint_load", "pointid_timing_enable", "pointid_timing_reset",
             "pointid_timing_query", "pointid_last_error", "pointid_version")
 
 
@@ -566,3 +594,258 @@ class Client:
             self.close()
         except Exception:
             pass
+
+
+# ---- layers
+
+_LAYER_TYPES = {torch.float32: POINTID_FP32, torch.bfloat16: POINTID_BF16, torch.float16: POINTID_FP16}
+
+
+class Layers:
+    """pointid_layers: a device and its cache of scratch buffers; frees itself on
+    garbage collection."""
+
+    def __init__(self, raw: ctypes.c_void_p, device: int):
+        self._raw = raw
+        self.device = device
+
+    @property
+    def raw(self):
+        if not self._raw:
+            raise ValueError("layers handle was destroyed")
+        return self._raw
+
+    def close(self):
+        if self._raw:
+            _check(lib.pointid_layers_destroy(self._raw))
+            self._raw = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Checkpoint:
+    """An 8-bit checkpoint of a matrix [m][n]: e4m3 codes (uint8 [m][n]) and the biased
+    exponents of the blocks of 32 columns (uint8 [m][ceil(n / 32)])."""
+
+    __slots__ = ("codes", "exponents")
+
+    def __init__(self, codes: torch.Tensor, exponents: torch.Tensor):
+        _need(codes, torch.uint8, "codes")
+        _need(exponents, torch.uint8, "exponents", codes.device.index)
+        if codes.dim() != 2 or tuple(exponents.shape) != (codes.shape[0], -(-codes.shape[1] // 32)):
+            raise ValueError("codes must be [m, n] and exponents [m, ceil(n / 32)]")
+        self.codes = codes
+        self.exponents = exponents
+
+    @classmethod
+    def empty(cls, m: int, n: int, device="cuda") -> "Checkpoint":
+        return cls(torch.empty((m, n), dtype=torch.uint8, device=device),
+                   torch.empty((m, -(-n // 32)), dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+def pointid_layers_create(device: int = 0) -> Layers:
+    raw = ctypes.c_void_p()
+    _check(lib.pointid_layers_create(int(device), ctypes.byref(raw)))
+    return Layers(raw, int(device))
+
+
+def pointid_layers_destroy(layers: Layers):
+    layers.close()
+
+
+def pointid_layers_trim(layers: Layers, keep_bytes: int = 0) -> int:
+    """Free the idle scratch buffers down to keep_bytes; returns the bytes still cached."""
+    cached = ctypes.c_uint64()
+    _check(lib.pointid_layers_trim(layers.raw, ctypes.c_uint64(int(keep_bytes)), ctypes.byref(cached)))
+    return int(cached.value)
+
+
+def _matrix(t, name, dtype, shape, device):
+    """The descriptor of a matrix (rows of unit stride, any pitch), or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.device.index != device:
+        raise ValueError(f"{name} is on cuda:{t.device.index}, the call's device is cuda:{device}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    rows, cols = shape
+    pitch, unit = t.stride()
+    if cols > 1 and unit != 1:
+        raise ValueError(f"the rows of {name} must have unit stride")
+    if rows > 1 and pitch < cols:
+        raise ValueError(f"the rows of {name} overlap")
+    return _Matrix(t.data_ptr(), pitch if rows > 1 else cols)
+
+
+def _kept(t, name, dtype, shape, device):
+    if t is None:
+        return None
+    if isinstance(t, Checkpoint):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        if t.device.index != device:
+            raise ValueError(f"{name} is on cuda:{t.device.index}, the call's device is cuda:{device}")
+        return _Kept(_Matrix(None, 0), _Packed(t.codes.data_ptr(), t.exponents.data_ptr()))
+    return _Kept(_matrix(t, name, dtype, shape, device), _Packed(None, None))
+
+
+def _bias(t, name, n, device):
+    if t is None:
+        return None
+    _need(t, torch.float32, name, device)
+    if t.numel() != n or t.dim() != 1:
+        raise ValueError(f"{name} must be [{n}]")
+    return t.data_ptr()
+
+
+def _layer_type(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise TypeError(f"{name} must be a torch tensor of two dimensions")
+    if t.dtype not in _LAYER_TYPES:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return t.dtype
+
+
+def _activation(act) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _ref(s):
+    return ctypes.byref(s) if s is not None else None
+
+
+def _shapes(x, w, name):
+    if w.dim() != 2 or x.shape[1] != w.shape[0]:
+        raise ValueError(f"x is {list(x.shape)} and {name} {list(w.shape)}: their inner sizes differ")
+    return x.shape[0], x.shape[1], w.shape[1]
+
+
+def pointid_dense(layers: Layers, x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
+                  act: str = "none", residual: torch.Tensor | None = None, y: torch.Tensor | None = None,
+                  save=None, stream=None) -> torch.Tensor:
+    """y [m][n] = act(x [m][k] @ w [k][n] + bias) + residual.
+
+    ``save`` (a tensor like y, or a Checkpoint) receives x @ w + bias for the backward pass."""
+    dt, dev = _layer_type(x, "x"), layers.device
+    m, k, n = _shapes(x, w, "w")
+    code = _activation(act)
+    if y is None:
+        y = torch.empty((m, n), dtype=dt, device=x.device)
+    _check(lib.pointid_dense(
+        layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
+        _ref(_matrix(w, "w", dt, (k, n), dev)), _bias(bias, "bias", n, dev),
+        _ref(_matrix(residual, "residual", dt, (m, n), dev)), _ref(_matrix(y, "y", dt, (m, n), dev)),
+        _ref(_kept(save, "save", dt, (m, n), dev)), _stream_ptr(stream, x.device)))
+    return y
+
+
+def pointid_dense_backward(layers: Layers, dy: torch.Tensor, x, w: torch.Tensor, z=None, act: str = "none",
+                           need_dx: bool = True, need_dw: bool = True, need_db: bool = True, stream=None):
+    """(dx, dw, db) of pointid_dense from dy [m][n]; None for what is not needed.
+
+    ``x`` and ``z`` (the saved x @ w + bias) are tensors or Checkpoints; x is not needed
+    without dw, z not with act "none".  db is float32 [n]."""
+    dt, dev = _layer_type(dy, "dy"), layers.device
+    m, n = dy.shape
+    k = w.shape[0]
+    code = _activation(act)
+    dx = torch.empty((m, k), dtype=dt, device=dy.device) if need_dx else None
+    dw = torch.empty((k, n), dtype=dt, device=dy.device) if need_dw else None
+    db = torch.empty((n,), dtype=torch.float32, device=dy.device) if need_db else None
+    _check(lib.pointid_dense_backward(
+        layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dy, "dy", dt, (m, n), dev)),
+        _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(w, "w", dt, (k, n), dev)),
+        _ref(_kept(z, "z", dt, (m, n), dev)), _ref(_matrix(dx, "dx", dt, (m, k), dev)),
+        _ref(_matrix(dw, "dw", dt, (k, n), dev)), _ptr(db), _stream_ptr(stream, dy.device)))
+    return dx, dw, db
+
+
+def pointid_gated(layers: Layers, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
+                  bias_g: torch.Tensor | None = None, bias_u: torch.Tensor | None = None, act: str = "silu",
+                  h: torch.Tensor | None = None, save_g=None, save_u=None, stream=None) -> torch.Tensor:
+    """h [m][n] = act(x @ wg + bias_g) * (x @ wu + bias_u).
+
+    ``save_g`` and ``save_u`` (tensors like h, or Checkpoints) receive the two factors'
+    sums for the backward pass."""
+    dt, dev = _layer_type(x, "x"), layers.device
+    m, k, n = _shapes(x, wg, "wg")
+    code = _activation(act)
+    if h is None:
+        h = torch.empty((m, n), dtype=dt, device=x.device)
+    _check(lib.pointid_gated(
+        layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
+        _ref(_matrix(wg, "wg", dt, (k, n), dev)), _ref(_matrix(wu, "wu", dt, (k, n), dev)),
+        _bias(bias_g, "bias_g", n, dev), _bias(bias_u, "bias_u", n, dev),
+        _ref(_matrix(h, "h", dt, (m, n), dev)), _ref(_kept(save_g, "save_g", dt, (m, n), dev)),
+        _ref(_kept(save_u, "save_u", dt, (m, n), dev)), _stream_ptr(stream, x.device)))
+    return h
+
+
+def pointid_gated_backward(layers: Layers, dh: torch.Tensor, x, wg: torch.Tensor, wu: torch.Tensor, g, u,
+                           act: str = "silu", need_dx: bool = True, need_dw: bool = True, need_db: bool = False,
+                           stream=None):
+    """(dx, dwg, dwu, dbg, dbu) of pointid_gated from dh [m][n]; None for what is not needed.
+
+    ``x``, ``g`` and ``u`` are tensors or Checkpoints."""
+    dt, dev = _layer_type(dh, "dh"), layers.device
+    m, n = dh.shape
+    k = wg.shape[0]
+    code = _activation(act)
+    dx = torch.empty((m, k), dtype=dt, device=dh.device) if need_dx else None
+    dwg, dwu = (torch.empty((k, n), dtype=dt, device=dh.device) if need_dw else None for _ in range(2))
+    dbg, dbu = (torch.empty((n,), dtype=torch.float32, device=dh.device) if need_db else None for _ in range(2))
+    _check(lib.pointid_gated_backward(
+        layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dh, "dh", dt, (m, n), dev)),
+        _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(wg, "wg", dt, (k, n), dev)),
+        _ref(_matrix(wu, "wu", dt, (k, n), dev)), _ref(_kept(g, "g", dt, (m, n), dev)),
+        _ref(_kept(u, "u", dt, (m, n), dev)), _ref(_matrix(dx, "dx", dt, (m, k), dev)),
+        _ref(_matrix(dwg, "dwg", dt, (k, n), dev)), _ref(_matrix(dwu, "dwu", dt, (k, n), dev)),
+        _ptr(dbg), _ptr(dbu), _stream_ptr(stream, dh.device)))
+    return dx, dwg, dwu, dbg, dbu
+
+
+def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stream=None) -> Checkpoint:
+    """The 8-bit checkpoint of a matrix [m][n] (float32, bfloat16 or float16)."""
+    dt = _layer_type(x, "x")
+    m, n = x.shape
+    if out is None:
+        out = Checkpoint.empty(m, n, x.device)
+    kept = _kept(out, "out", dt, (m, n), x.device.index)
+    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, _ref(_matrix(x, "x", dt, (m, n), x.device.index)),
+                                       ctypes.byref(kept.packed), _stream_ptr(stream, x.device)))
+    return out
+
+
+def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.Tensor | None = None,
+                            stream=None) -> torch.Tensor:
+    """The values a checkpoint stands for, as a matrix [m][n] of ``dtype``."""
+    m, n = saved.shape
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=saved.device)
+    dt = _layer_type(out, "out")
+    dev = saved.device.index
+    kept = _kept(saved, "saved", dt, (m, n), dev)
+    _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed),
+                                       _ref(_matrix(out, "out", dt, (m, n), dev)),
+                                       _stream_ptr(stream, saved.device)))
+    return out

@@ -1,0 +1,160 @@
+// Internal interface of the layer operators: dense and gated layers, their
+// gradients, and 8-bit activation checkpoints.
+//
+// Every product is one of three forms of a sum over an inner index:
+//   forward  z[m][n]  = sum over k of x[m][k] W[k][n]
+//   dx       dx[m][k] = sum over n of dz[m][n] W[k][n]
+//   dW       dW[k][n] = sum over m of x[m][k] dz[m][n]
+// "left" is the operand that the result's rows index, "right" the one its columns
+// index.  A gated layer has two right operands (two halves of one result).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "pointid.h"
+
+namespace pointid {
+
+// Values of a 16-bit or fp32 type at p[i * si + k * sk] (i: the result's row or
+// column, k: the inner index), one of the strides 1.
+struct Strided {
+  const void* p;
+  int64_t si, sk;
+  int32_t dtype;               // POINTID_FP32, _BF16 or _FP16
+};
+
+// An 8-bit checkpoint, contiguous: codes [rows][cols], exponents [rows][ceil(cols / 32)].
+struct Packed8 {
+  uint8_t* codes;
+  uint8_t* exponents;
+};
+constexpr int kBlock8 = 32;
+
+// Where activations kept for the backward pass go to or come from: a matrix of the
+// call's type, or a checkpoint (matrix == nullptr).
+struct Kept {
+  void* matrix;
+  int64_t ld;
+  Packed8 packed;
+  bool any() const { return matrix || packed.codes; }
+};
+
+enum EndMode { kEndDense = 0, kEndGated = 1, kEndStore = 2, kEndPartial = 3 };
+
+// What becomes of the finished sums of one result (or of two halves of one).
+//   kEndDense    v = sum + bias0; keep0 <- v; y0 = act(v) + residual
+//   kEndGated    g = sum0 + bias0, u = sum1 + bias1; keep0 <- g; keep1 <- u; y0 = act(g) u
+//   kEndStore    y0 = sum0 (and y1 = sum1)
+//   kEndPartial  sums to part[(split * halves + half) * rows + row][part_ld] in fp32
+struct End {
+  int32_t mode;
+  int32_t act;
+  int32_t dtype;               // of y0, y1, residual, kept matrices
+  int32_t halves;              // 1 or 2
+  int64_t rows;
+  int64_t cols;                // of each half
+  const float* bias0;
+  const float* bias1;
+  const void* residual;
+  int64_t ld_residual;
+  void* y0;
+  int64_t ld0;
+  void* y1;
+  int64_t ld1;
+  Kept keep0, keep1;
+  float* part;
+  int64_t part_ld;             // a multiple of 32
+  // rows of the matrix can be read or written in 16-byte pieces
+  bool vec_residual, vec0, vec1, vec_keep0, vec_keep1;
+};
+
+// One term of the sum: a left operand with one right operand for each half.
+struct Term {
+  const void* left;
+  const void* right0;
+  const void* right1;
+};
+constexpr int kMaxTerms = 12;
+
+// ---- layers_simple.hip: fp32 arithmetic, any type, stride and size
+struct SimpleArgs {
+  Strided left[2];             // summed over `terms`
+  Strided right[2][2];         // [term][half]
+  int32_t terms;
+  int64_t inner;
+  End end;
+};
+hipError_t launch_layers_simple(const SimpleArgs& a, hipStream_t stream);
+
+// ---- layers_rows.hip: forward products of 1..kFewRows rows; the weights
+// [inner][cols] are read once.  splits > 1 leaves partials (end.mode is kEndPartial then).
+constexpr int kFewRows = 8;
+int few_rows_splits(int64_t inner, int64_t cols, int halves, int cus);
+hipError_t launch_layers_rows(const Strided& x, const Strided* w, int64_t inner, const End& end, int splits,
+                              hipStream_t stream);
+
+// ---- layers_mm.h: products on the matrix cores, 16-bit operands.
+enum Form { kForward = 0, kDx = 1, kDw = 2 };
+struct ProductArgs {
+  Term term[kMaxTerms];
+  int32_t terms;
+  int32_t splits;
+  int64_t inner;
+  int64_t ld_left;             // elements; operands are 16-byte aligned, rows too
+  int64_t ld_right;
+  int32_t tiles_m, tiles_n;    // set by the launch
+  End end;
+};
+// The tile of a launch and its splits of the sum.
+constexpr int kTiles = 3;
+constexpr int kTileM[kTiles] = {256, 128, 64}, kTileN[kTiles] = {256, 128, 128};
+struct ProductPlan {
+  int tile;                    // index into kTileM, kTileN (columns of both halves)
+  int splits;
+};
+ProductPlan plan_product(Form form, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus);
+hipError_t launch_product_bf16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream);
+hipError_t launch_product_fp16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream);
+// Partials of `splits` parts added in order, then `end`.
+hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld, int splits, hipStream_t stream);
+
+// ---- layers_pass.hip: passes over one matrix
+// 16-bit planes [rows][ld] of a matrix, zero past its columns: parts == 1 the values
+// (16-bit types, copied), parts == 3 an fp32 value as the sum of three bf16 values.
+hipError_t launch_layers_pack(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, int parts,
+                              uint16_t* out, int64_t ld, int64_t plane, hipStream_t stream);
+// A checkpoint's values as 16-bit (dtype) or fp32 values [rows][ld], zero past the columns up to ld.
+hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
+                                  int64_t fill_to, hipStream_t stream);
+hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
+                                  const Packed8& out, hipStream_t stream);
+hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols, hipStream_t stream);
+// The gradient before the activation, and its column sums.
+//   dense: dz = dy act'(z) (z absent: dy)     gated: dg = dy u act'(g), du = dy act(g)
+// parts: 0 none written, 1 or 2 planes of the 16-bit type (2: value and remainder),
+// 3 bf16 planes, -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each
+// block of kGradRows rows, or nullptr.
+constexpr int kGradRows = 64;
+struct GradArgs {
+  const void* dy;
+  int64_t ld_dy;
+  int32_t dtype;
+  int32_t type16;              // of the planes: POINTID_BF16 or POINTID_FP16
+  int32_t act;
+  int32_t halves;
+  Kept z[2];                   // dense: z; gated: g, u
+  int64_t rows, cols;
+  int32_t parts;
+  void* out[2];                // each half: planes [parts][rows][ld], or fp32 [rows][ld]
+  int64_t ld, plane;
+  float* col_part;
+  bool vec_dy, vec_z[2];
+};
+hipError_t launch_layers_grad(const GradArgs& a, hipStream_t stream);
+// out[i] = sum over blocks of col_part[block][half][i], for each half whose out is given
+hipError_t launch_layers_colsum(const float* col_part, int64_t blocks, int64_t cols, int halves, float* out0,
+                                float* out1, hipStream_t stream);
+
+}  // namespace pointid

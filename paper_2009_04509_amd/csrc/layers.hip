@@ -1,0 +1,760 @@
+// C ABI of the layer operators (declared in include/pointid.h): argument checks, the
+// choice of kernels, scratch, launch sequencing.  Every call only enqueues work.
+#include "layers.h"
+
+#include <cstring>
+#include <exception>
+#include <new>
+
+#include "call.h"
+#include "internal.h"
+
+using namespace pointid;
+
+struct pointid_layers_s {
+  int device;
+  int cus;
+  ScratchPool scratch;
+};
+
+namespace {
+
+constexpr int64_t kMaxSide = int64_t(1) << 20;         // k and n
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;   // m
+constexpr int64_t kMaxPitch = int64_t(1) << 21;        // of an operand that the products read in place
+
+// Products of up to this many multiplications and inner indices run the plain kernel: one
+// launch, where the others take passes over unaligned or fp32 operands and a join.
+constexpr int64_t kSimpleWork = int64_t(1) << 22, kSimpleInner = 1024;
+// dz of up to this many values is kept in two 16-bit parts: the rounding of so few does not
+// average out in a gradient, and such products are bound by the bytes of the weights.
+constexpr int64_t kTwoPartValues = int64_t(1) << 16;
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int size_of(int dtype) { return dtype == POINTID_FP32 ? 4 : 2; }
+bool rows_in_16(const void* p, int64_t ld, int dtype) {
+  return aligned16(p) && ld % (dtype == POINTID_FP32 ? 4 : 8) == 0;
+}
+
+// No exception crosses the ABI.
+template <class F>
+int guarded(F&& f) noexcept {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return POINTID_ENOMEM;
+  } catch (...) {
+    return POINTID_EHIP;
+  }
+}
+
+// ---- argument checks
+
+int check_call(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n) {
+  if (!l) return set_error(POINTID_EINVAL, "layers is NULL");
+  if (dtype != POINTID_FP32 && dtype != POINTID_BF16 && dtype != POINTID_FP16)
+    return set_error(POINTID_EUNSUPPORTED, "dtype must be POINTID_FP32, POINTID_BF16 or POINTID_FP16");
+  if (act < POINTID_ACT_NONE || act > POINTID_ACT_SIGMOID) return set_error(POINTID_EINVAL, "act is no activation");
+  if (m < 0 || m > kMaxRows) return set_error(POINTID_EINVAL, "m must be in [0, 2^31)");
+  if (k < 1 || k > kMaxSide || n < 1 || n > kMaxSide)
+    return set_error(POINTID_EINVAL, "k and n must be in [1, 2^20]");
+  return POINTID_OK;
+}
+
+// A matrix of the call; `may_miss`: NULL (or NULL data) is allowed.
+int check_matrix(const pointid_matrix* a, const char* name, int dtype, int64_t rows, int64_t cols, bool may_miss = false) {
+  if (!a || !a->data) {
+    if (may_miss || rows == 0) return POINTID_OK;
+    return set_error(POINTID_EINVAL, std::string(name) + " is NULL");
+  }
+  if (reinterpret_cast<uintptr_t>(a->data) % size_of(dtype))
+    return set_error(POINTID_EINVAL, std::string(name) + " is not aligned to its elements");
+  if (rows > 1 && a->ld < cols)
+    return set_error(POINTID_EINVAL, std::string(name) + ": row pitch below its columns");
+  if (rows > 1 && a->ld > INT64_MAX / 8 / rows)
+    return set_error(POINTID_EINVAL, std::string(name) + ": row pitch out of range");
+  return POINTID_OK;
+}
+
+int check_packed(const pointid_checkpoint& c, const char* name) {
+  if (!c.codes || !c.exponents) return set_error(POINTID_EINVAL, std::string(name) + ": codes or exponents is NULL");
+  return POINTID_OK;
+}
+
+int check_kept(const pointid_kept* a, const char* name, int dtype, int64_t rows, int64_t cols, bool may_miss) {
+  if (!a) {
+    if (may_miss || rows == 0) return POINTID_OK;
+    return set_error(POINTID_EINVAL, std::string(name) + " is NULL");
+  }
+  if (a->full.data) {
+    if (a->packed.codes || a->packed.exponents)
+      return set_error(POINTID_EINVAL, std::string(name) + " is both a matrix and a checkpoint");
+    return check_matrix(&a->full, name, dtype, rows, cols);
+  }
+  if (rows == 0) return POINTID_OK;
+  return check_packed(a->packed, name);
+}
+
+int check_floats(const float* p, const char* name) {
+  if (p && reinterpret_cast<uintptr_t>(p) % 4)
+    return set_error(POINTID_EINVAL, std::string(name) + " is not aligned to its elements");
+  return POINTID_OK;
+}
+
+// The pitch of one row is never used: any value stands for its columns.
+pointid_matrix matrix_of(const pointid_matrix* a, int64_t rows, int64_t cols) {
+  pointid_matrix r = {nullptr, cols};
+  if (a && a->data) r = *a;
+  if (rows <= 1 || !r.data) r.ld = round_up(cols, 8);
+  return r;
+}
+Kept kept_of(const pointid_kept* a, int64_t rows, int64_t cols) {
+  Kept k;
+  std::memset(&k, 0, sizeof(k));
+  if (!a) return k;
+  const pointid_matrix f = matrix_of(&a->full, rows, cols);
+  k.matrix = f.data;
+  k.ld = f.ld;
+  if (!k.matrix) k.packed = {a->packed.codes, a->packed.exponents};
+  return k;
+}
+
+// ---- a call: scratch pieces sized before any is taken, launches with their timer
+
+class Call {
+ public:
+  Call(pointid_layers l, hipStream_t stream) : ws_(&l->scratch, stream), stream_(stream) {}
+
+  // a piece of the call's scratch, taken by reserve()
+  template <class T>
+  void want(T** out, size_t bytes) {
+    if (count_ < kMaxPieces) pieces_[count_++] = {reinterpret_cast<void**>(out), bytes};
+  }
+  int reserve() {
+    size_t total = 0;
+    for (int i = 0; i < count_; ++i) total += pad256(pieces_[i].bytes);
+    if (total == 0) return POINTID_OK;
+    hipError_t e = ws_.reserve(total);
+    if (e != hipSuccess) return hip_fail(e, "scratch buffer");
+    for (int i = 0; i < count_; ++i) {
+      e = ws_.get(pieces_[i].bytes, pieces_[i].out);
+      if (e != hipSuccess) return hip_fail(e, "workspace (layers)");
+    }
+    scratch_ = true;
+    return POINTID_OK;
+  }
+  // f: the launch; `last`: of the call (it also records the scratch's completion)
+  template <class F>
+  int run(const char* name, bool last, F&& f) {
+    KernelTimer kt(name, stream_);
+    hipError_t e;
+    if (last && scratch_) {
+      EndsCall end(ws_);
+      e = f();
+      end.launched(e);
+    } else {
+      e = f();
+    }
+    return e == hipSuccess ? POINTID_OK : hip_fail(e, name);
+  }
+  hipStream_t stream() const { return stream_; }
+
+ private:
+  static constexpr int kMaxPieces = 16;
+  struct Piece {
+    void** out;
+    size_t bytes;
+  };
+  Workspace ws_;
+  hipStream_t stream_;
+  Piece pieces_[kMaxPieces];
+  int count_ = 0;
+  bool scratch_ = false;
+};
+
+// A matrix as the products read it: 16-bit planes with aligned rows, zero past the columns.
+struct Planes {
+  const void* base = nullptr;
+  int64_t ld = 0, plane = 0;       // elements
+  int parts = 1;
+  const void* at(int part) const { return static_cast<const uint16_t*>(base) + part * plane; }
+};
+
+// An operand, and whether it is read in place or made by a pass into scratch.
+struct Source {
+  Kept from;                       // a matrix, or a checkpoint
+  int dtype;
+  int64_t rows, cols;
+  bool in_place = false;
+  uint16_t* made = nullptr;
+  Planes planes;
+
+  void plan(const Kept& k, int type, int64_t r, int64_t c, Call& call) {
+    from = k, dtype = type, rows = r, cols = c;
+    in_place = k.matrix && type != POINTID_FP32 && c % 8 == 0 && rows_in_16(k.matrix, k.ld, type) && k.ld <= kMaxPitch;
+    if (in_place) {
+      planes.base = k.matrix;
+      planes.ld = k.ld;
+      return;
+    }
+    planes.ld = round_up(c, 8);
+    planes.plane = r * planes.ld;
+    planes.parts = k.matrix && type == POINTID_FP32 ? 3 : 1;
+    call.want(&made, 2 * (size_t)planes.plane * planes.parts);
+  }
+  int make(Call& call) {
+    if (in_place) return POINTID_OK;
+    planes.base = made;
+    if (!from.matrix)
+      return call.run("layers_load", false, [&] {
+        return launch_checkpoint_load(from.packed, rows, cols, dtype == POINTID_FP16 ? POINTID_FP16 : POINTID_BF16, made,
+                                      planes.ld, planes.ld, call.stream());
+      });
+    return call.run("layers_pack", false, [&] {
+      return launch_layers_pack(from.matrix, from.ld, dtype, rows, cols, planes.parts, made, planes.ld, planes.plane,
+                                call.stream());
+    });
+  }
+};
+
+// The products of the parts of left and right that count (orders up to that of the most
+// parts), the smallest first.
+int add_terms(ProductArgs* a, const Planes& left, const Planes& right0, const Planes* right1) {
+  const int pl = left.parts, pr = right0.parts, most = (pl > pr ? pl : pr) - 1;
+  for (int order = most; order >= 0; --order)
+    for (int i = pl - 1; i >= 0; --i) {
+      const int j = order - i;
+      if (j < 0 || j >= pr) continue;
+      if (a->terms == kMaxTerms) return set_error(POINTID_EHIP, "too many terms");
+      a->term[a->terms++] = {left.at(i), right0.at(j), right1 ? right1->at(j) : nullptr};
+    }
+  return POINTID_OK;
+}
+
+size_t part_bytes(int splits, const End& e) {
+  return splits > 1 ? sizeof(float) * (size_t)splits * e.halves * e.rows * e.part_ld : 0;
+}
+
+// A product and, where its sum is split, the join.
+int run_product(Call& call, Form form, const ProductPlan& plan, ProductArgs& a, int dtype, float* part, bool last) {
+  const End end = a.end;
+  if (plan.splits > 1) {
+    a.end.mode = kEndPartial;
+    a.end.part = part;
+  }
+  int rc = call.run("layers_product", last && plan.splits == 1, [&] {
+    return dtype == POINTID_FP16 ? launch_product_fp16(form, plan, a, call.stream())
+                                 : launch_product_bf16(form, plan, a, call.stream());
+  });
+  if (rc != POINTID_OK || plan.splits == 1) return rc;
+  return call.run("layers_join", last,
+                  [&] { return launch_layers_join(end, part, end.part_ld, plan.splits, call.stream()); });
+}
+
+End end_of(int mode, int act, int dtype, int halves, int64_t rows, int64_t cols, const pointid_matrix& y0,
+           const pointid_matrix& y1) {
+  End e;
+  std::memset(&e, 0, sizeof(e));
+  e.mode = mode;
+  e.act = act;
+  e.dtype = dtype;
+  e.halves = halves;
+  e.rows = rows;
+  e.cols = cols;
+  e.part_ld = round_up(cols, 32);
+  e.y0 = y0.data, e.ld0 = y0.ld, e.vec0 = rows_in_16(y0.data, y0.ld, dtype);
+  e.y1 = y1.data, e.ld1 = y1.ld, e.vec1 = rows_in_16(y1.data, y1.ld, dtype);
+  return e;
+}
+
+bool simple_work(int64_t rows, int64_t cols, int64_t inner) {
+  return inner <= kSimpleInner && rows * cols <= kSimpleWork / inner;
+}
+
+// ---- the forward pass of a dense (halves == 1) or gated layer
+
+struct Forward {
+  int dtype, act, halves;
+  int64_t m, k, n;
+  pointid_matrix x, w[2];
+  const float* bias[2];
+  pointid_matrix residual, y;
+  Kept keep[2];
+};
+
+int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
+  DeviceScope dev(l->device);
+  if (dev.error() != hipSuccess) return hip_fail(dev.error(), "hipSetDevice");
+  Call call(l, stream);
+  const pointid_matrix none = {nullptr, 0};
+  End e = end_of(f.halves == 2 ? kEndGated : kEndDense, f.act, f.dtype, f.halves, f.m, f.n, f.y, none);
+  e.bias0 = f.bias[0];
+  e.bias1 = f.bias[1];
+  e.residual = f.residual.data;
+  e.ld_residual = f.residual.ld;
+  e.vec_residual = rows_in_16(f.residual.data, f.residual.ld, f.dtype);
+  e.keep0 = f.keep[0];
+  e.keep1 = f.keep[1];
+  e.vec_keep0 = rows_in_16(e.keep0.matrix, e.keep0.ld, f.dtype);
+  e.vec_keep1 = rows_in_16(e.keep1.matrix, e.keep1.ld, f.dtype);
+  const Strided x = {f.x.data, f.x.ld, 1, f.dtype};
+  Strided w[2];
+  for (int h = 0; h < 2; ++h) w[h] = {f.w[h].data, 1, f.w[h].ld, f.dtype};
+
+  if (f.m <= kFewRows) {
+    const int splits = few_rows_splits(f.k, f.n, f.halves, l->cus);
+    float* part = nullptr;
+    call.want(&part, part_bytes(splits, e));
+    int rc = call.reserve();
+    if (rc != POINTID_OK) return rc;
+    End rows_end = e;
+    if (splits > 1) {
+      rows_end.mode = kEndPartial;
+      rows_end.part = part;
+    }
+    rc = call.run("layers_rows", splits == 1,
+                  [&] { return launch_layers_rows(x, w, f.k, rows_end, splits, stream); });
+    if (rc != POINTID_OK || splits == 1) return rc;
+    return call.run("layers_join", true, [&] { return launch_layers_join(e, part, e.part_ld, splits, stream); });
+  }
+  if (simple_work(f.m, f.n, f.k)) {
+    SimpleArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.left[0] = x;
+    a.right[0][0] = w[0];
+    a.right[0][1] = w[1];
+    a.terms = 1;
+    a.inner = f.k;
+    a.end = e;
+    return call.run("layers_simple", true, [&] { return launch_layers_simple(a, stream); });
+  }
+  Source sx, sw[2];
+  Kept from;
+  std::memset(&from, 0, sizeof(from));
+  from.matrix = f.x.data, from.ld = f.x.ld;
+  sx.plan(from, f.dtype, f.m, f.k, call);
+  // the halves share a pitch: where one is copied, so is the other
+  bool copy = false;
+  for (int h = 0; h < f.halves; ++h)
+    copy = copy || f.dtype == POINTID_FP32 || f.n % 8 || !rows_in_16(f.w[h].data, f.w[h].ld, f.dtype) ||
+           f.w[h].ld > kMaxPitch || f.w[h].ld != f.w[0].ld;
+  for (int h = 0; h < f.halves; ++h) {
+    from.matrix = f.w[h].data, from.ld = f.w[h].ld;
+    sw[h].plan(from, f.dtype, f.k, f.n, call);
+    if (copy && sw[h].in_place) {
+      sw[h].in_place = false;
+      sw[h].planes = Planes();
+      sw[h].planes.ld = round_up(f.n, 8);
+      sw[h].planes.plane = f.k * sw[h].planes.ld;
+      call.want(&sw[h].made, 2 * (size_t)sw[h].planes.plane);
+    }
+  }
+  const int parts = sx.planes.parts == 3 ? 6 : 1;
+  const ProductPlan plan = plan_product(kForward, f.m, f.n, f.halves, f.k, parts, l->cus);
+  float* part = nullptr;
+  call.want(&part, part_bytes(plan.splits, e));
+  int rc = call.reserve();
+  if (rc == POINTID_OK) rc = sx.make(call);
+  for (int h = 0; h < f.halves && rc == POINTID_OK; ++h) rc = sw[h].make(call);
+  if (rc != POINTID_OK) return rc;
+  ProductArgs a;
+  std::memset(&a, 0, sizeof(a));
+  rc = add_terms(&a, sx.planes, sw[0].planes, f.halves == 2 ? &sw[1].planes : nullptr);
+  if (rc != POINTID_OK) return rc;
+  a.inner = f.k;
+  a.ld_left = sx.planes.ld;
+  a.ld_right = sw[0].planes.ld;
+  a.end = e;
+  return run_product(call, kForward, plan, a, f.dtype, part, true);
+}
+
+// ---- the backward pass of a dense (halves == 1) or gated layer
+
+struct Backward {
+  int dtype, act, halves;
+  int64_t m, k, n;
+  pointid_matrix dy;
+  Kept x, z[2];
+  pointid_matrix w[2], dx, dw[2];
+  float* db[2];
+};
+
+int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
+  DeviceScope dev(l->device);
+  if (dev.error() != hipSuccess) return hip_fail(dev.error(), "hipSetDevice");
+  Call call(l, stream);
+  const bool want_dx = b.dx.data, want_dw = b.dw[0].data, want_db = b.db[0] || b.db[1];
+  if (!want_dx && !want_dw && !want_db) return POINTID_OK;
+  const pointid_matrix none = {nullptr, 0};
+  if (b.m == 0) {
+    int rc = POINTID_OK;
+    for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) {
+      if (want_dw)
+        rc = call.run("layers_zero", false,
+                      [&] { return launch_layers_zero(b.dw[h].data, b.dw[h].ld, b.dtype, b.k, b.n, stream); });
+      if (rc == POINTID_OK && b.db[h])
+        rc = call.run("layers_zero", false,
+                      [&] { return launch_layers_zero(b.db[h], b.n, POINTID_FP32, 1, b.n, stream); });
+    }
+    return rc;
+  }
+  const bool simple = simple_work(b.m, b.k, b.n) && simple_work(b.k, b.n, b.m);
+  const bool products = want_dx || want_dw;
+  // dz is dy itself where no activation changes it and the products can read it
+  const bool plain = b.halves == 1 && b.act == POINTID_ACT_NONE;
+  const bool read_dy = plain && (simple || (b.dtype != POINTID_FP32 && b.n % 8 == 0 && b.dy.ld <= kMaxPitch &&
+                                            rows_in_16(b.dy.data, b.dy.ld, b.dtype)));
+  const bool exact16 = b.halves == 1 && (b.act == POINTID_ACT_NONE || b.act == POINTID_ACT_RELU);
+
+  GradArgs g;
+  std::memset(&g, 0, sizeof(g));
+  g.dy = b.dy.data;
+  g.ld_dy = b.dy.ld;
+  g.dtype = b.dtype;
+  g.type16 = b.dtype == POINTID_FP16 ? POINTID_FP16 : POINTID_BF16;
+  g.act = b.act;
+  g.halves = b.halves;
+  g.rows = b.m;
+  g.cols = b.n;
+  g.vec_dy = rows_in_16(b.dy.data, b.dy.ld, b.dtype);
+  for (int h = 0; h < b.halves; ++h) {
+    g.z[h] = b.z[h];
+    g.vec_z[h] = rows_in_16(b.z[h].matrix, b.z[h].ld, b.dtype);
+  }
+  g.parts = !products || read_dy ? 0 : simple ? -1 : b.dtype == POINTID_FP32 ? 3 : !exact16 && b.m * b.n <= kTwoPartValues ? 2 : 1;
+  g.ld = round_up(b.n, 8);
+  g.plane = b.m * g.ld;
+  const size_t dz_bytes = g.parts < 0 ? 4 * (size_t)g.plane : 2 * (size_t)g.plane * g.parts;
+  for (int h = 0; h < b.halves && g.parts != 0; ++h) call.want(&g.out[h], dz_bytes);
+  const int64_t grad_blocks = (b.m + kGradRows - 1) / kGradRows;
+  if (want_db) call.want(&g.col_part, sizeof(float) * (size_t)(grad_blocks * b.halves * b.n));
+
+  // x for dW, the weights for dx
+  Source sx, sw[2];
+  void* x8 = nullptr;                                  // a checkpoint's values for the plain kernel
+  Kept from;
+  std::memset(&from, 0, sizeof(from));
+  if (simple) {
+    if (want_dw && !b.x.matrix) call.want(&x8, (size_t)size_of(b.dtype) * b.m * b.k);
+  } else {
+    if (want_dw) sx.plan(b.x, b.dtype, b.m, b.k, call);
+    for (int h = 0; h < b.halves && want_dx; ++h) {
+      from.matrix = b.w[h].data, from.ld = b.w[h].ld;
+      sw[h].plan(from, b.dtype, b.k, b.n, call);
+    }
+    // the halves share a pitch: where one is copied, so is the other
+    if (want_dx && b.halves == 2 && sw[0].planes.ld != sw[1].planes.ld)
+      for (int h = 0; h < 2; ++h)
+        if (sw[h].in_place) {
+          sw[h].in_place = false;
+          sw[h].planes = Planes();
+          sw[h].planes.ld = round_up(b.n, 8);
+          sw[h].planes.plane = b.k * sw[h].planes.ld;
+          call.want(&sw[h].made, 2 * (size_t)sw[h].planes.plane);
+        }
+  }
+  End dx_end = end_of(kEndStore, POINTID_ACT_NONE, b.dtype, 1, b.m, b.k, b.dx, none);
+  End dw_end = end_of(kEndStore, POINTID_ACT_NONE, b.dtype, b.halves, b.k, b.n, b.dw[0], b.dw[1]);
+  Planes dz[2];
+  for (int h = 0; h < 2; ++h) {
+    dz[h].ld = read_dy ? b.dy.ld : g.ld;
+    dz[h].plane = g.plane;
+    dz[h].parts = read_dy || g.parts < 1 ? 1 : g.parts;
+  }
+  auto count = [](int p, int q) {
+    int c = 0;
+    for (int i = 0; i < p; ++i)
+      for (int j = 0; j < q; ++j) c += i + j < (p > q ? p : q);
+    return c;
+  };
+  ProductPlan dx_plan = {0, 1}, dw_plan = {0, 1};
+  float* part = nullptr;
+  if (!simple) {
+    if (want_dx)
+      dx_plan = plan_product(kDx, b.m, b.k, 1, b.n, b.halves * count(dz[0].parts, sw[0].planes.parts), l->cus);
+    if (want_dw)
+      dw_plan = plan_product(kDw, b.k, b.n, b.halves, b.m, count(sx.planes.parts, dz[0].parts), l->cus);
+    const size_t p = part_bytes(dx_plan.splits, dx_end), q = part_bytes(dw_plan.splits, dw_end);
+    call.want(&part, p > q ? p : q);                   // one after the other
+  }
+  int rc = call.reserve();
+  if (rc != POINTID_OK) return rc;
+
+  if (g.parts != 0 || want_db) {
+    rc = call.run("layers_grad", false, [&] { return launch_layers_grad(g, stream); });
+    if (rc == POINTID_OK && want_db)
+      rc = call.run("layers_colsum", !products, [&] {
+        return launch_layers_colsum(g.col_part, grad_blocks, b.n, b.halves, b.db[0], b.db[1], stream);
+      });
+    if (rc != POINTID_OK) return rc;
+  }
+  for (int h = 0; h < 2; ++h) dz[h].base = read_dy ? b.dy.data : g.out[h];
+
+  if (simple) {
+    SimpleArgs a;
+    std::memset(&a, 0, sizeof(a));
+    const int dz_type = read_dy ? b.dtype : POINTID_FP32;
+    if (want_dx) {
+      a.terms = b.halves;
+      a.inner = b.n;
+      a.end = dx_end;
+      for (int h = 0; h < b.halves; ++h) {
+        a.left[h] = {dz[h].base, dz[h].ld, 1, dz_type};
+        a.right[h][0] = {b.w[h].data, b.w[h].ld, 1, b.dtype};
+      }
+      rc = call.run("layers_simple", !want_dw, [&] { return launch_layers_simple(a, stream); });
+      if (rc != POINTID_OK) return rc;
+    }
+    if (!want_dw) return POINTID_OK;
+    if (x8) {
+      rc = call.run("layers_load", false,
+                    [&] { return launch_checkpoint_load(b.x.packed, b.m, b.k, b.dtype, x8, b.k, b.k, stream); });
+      if (rc != POINTID_OK) return rc;
+    }
+    a.terms = 1;
+    a.inner = b.m;
+    a.end = dw_end;
+    a.left[0] = {x8 ? x8 : b.x.matrix, 1, x8 ? b.k : b.x.ld, b.dtype};
+    for (int h = 0; h < b.halves; ++h) a.right[0][h] = {dz[h].base, 1, dz[h].ld, dz_type};
+    return call.run("layers_simple", true, [&] { return launch_layers_simple(a, stream); });
+  }
+
+  if (want_dx) {
+    for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = sw[h].make(call);
+    if (rc != POINTID_OK) return rc;
+    ProductArgs a;
+    std::memset(&a, 0, sizeof(a));
+    for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = add_terms(&a, dz[h], sw[h].planes, nullptr);
+    if (rc != POINTID_OK) return rc;
+    a.inner = b.n;
+    a.ld_left = dz[0].ld;
+    a.ld_right = sw[0].planes.ld;
+    a.end = dx_end;
+    rc = run_product(call, kDx, dx_plan, a, b.dtype, part, !want_dw);
+    if (rc != POINTID_OK) return rc;
+  }
+  if (!want_dw) return POINTID_OK;
+  rc = sx.make(call);
+  if (rc != POINTID_OK) return rc;
+  ProductArgs a;
+  std::memset(&a, 0, sizeof(a));
+  rc = add_terms(&a, sx.planes, dz[0], b.halves == 2 ? &dz[1] : nullptr);
+  if (rc != POINTID_OK) return rc;
+  a.inner = b.m;
+  a.ld_left = sx.planes.ld;
+  a.ld_right = dz[0].ld;
+  a.end = dw_end;
+  return run_product(call, kDw, dw_plan, a, b.dtype, part, true);
+}
+
+int check_checkpoint_call(int dtype, int64_t rows, int64_t cols, const pointid_matrix* a, const pointid_checkpoint* c) {
+  if (dtype != POINTID_FP32 && dtype != POINTID_BF16 && dtype != POINTID_FP16)
+    return set_error(POINTID_EUNSUPPORTED, "dtype must be POINTID_FP32, POINTID_BF16 or POINTID_FP16");
+  if (rows < 0 || rows > kMaxRows) return set_error(POINTID_EINVAL, "rows must be in [0, 2^31)");
+  if (cols < 1 || cols > kMaxSide) return set_error(POINTID_EINVAL, "cols must be in [1, 2^20]");
+  if (rows == 0) return POINTID_OK;
+  const int rc = check_matrix(a, "the matrix", dtype, rows, cols);
+  if (rc != POINTID_OK) return rc;
+  if (!c) return set_error(POINTID_EINVAL, "the checkpoint is NULL");
+  return check_packed(*c, "the checkpoint");
+}
+
+#define TRY(call)                            \
+  do {                                       \
+    const int rc_ = (call);                  \
+    if (rc_ != POINTID_OK) return rc_;       \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int pointid_layers_create(int device, pointid_layers* out) {
+  if (!out) return set_error(POINTID_EINVAL, "out is NULL");
+  *out = nullptr;
+  return guarded([&] {
+    int count = 0;
+    if (hipGetDeviceCount(&count) != hipSuccess || count <= 0) return set_error(POINTID_ENODEV, "no HIP device visible");
+    if (device < 0 || device >= count) return set_error(POINTID_ENODEV, "device ordinal out of range");
+    hipDeviceProp_t prop;
+    hipError_t e = hipGetDeviceProperties(&prop, device);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDeviceProperties");
+    if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
+      return set_error(POINTID_ENODEV,
+                       std::string("device is ") + prop.gcnArchName + ", library is built for gfx950");
+    auto* l = new (std::nothrow) pointid_layers_s();
+    if (!l) return set_error(POINTID_ENOMEM, "host allocation failed");
+    l->device = device;
+    l->cus = prop.multiProcessorCount;
+    *out = l;
+    return (int)POINTID_OK;
+  });
+}
+
+int pointid_layers_destroy(pointid_layers l) {
+  if (!l) return POINTID_OK;
+  {
+    DeviceScope dev(l->device);
+    (void)hipDeviceSynchronize();
+    free_scratch(&l->scratch);
+  }
+  delete l;
+  return POINTID_OK;
+}
+
+int pointid_layers_trim(pointid_layers l, uint64_t keep_bytes, uint64_t* cached_bytes) {
+  if (!l) return set_error(POINTID_EINVAL, "layers is NULL");
+  return guarded([&] {
+    DeviceScope dev(l->device);
+    if (dev.error() != hipSuccess) return hip_fail(dev.error(), "hipSetDevice");
+    return trim_scratch(&l->scratch, keep_bytes, cached_bytes);
+  });
+}
+
+int pointid_dense(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n, const pointid_matrix* x,
+                  const pointid_matrix* w, const float* bias, const pointid_matrix* residual, const pointid_matrix* y,
+                  const pointid_kept* keep_z, void* stream) {
+  return guarded([&] {
+    TRY(check_call(l, dtype, act, m, k, n));
+    if (m == 0) return (int)POINTID_OK;
+    TRY(check_matrix(x, "x", dtype, m, k));
+    TRY(check_matrix(w, "w", dtype, k, n));
+    TRY(check_floats(bias, "bias"));
+    TRY(check_matrix(residual, "residual", dtype, m, n, true));
+    TRY(check_matrix(y, "y", dtype, m, n));
+    TRY(check_kept(keep_z, "keep_z", dtype, m, n, true));
+    Forward f;
+    std::memset(&f, 0, sizeof(f));
+    f.dtype = dtype, f.act = act, f.halves = 1, f.m = m, f.k = k, f.n = n;
+    f.x = matrix_of(x, m, k);
+    f.w[0] = f.w[1] = matrix_of(w, k, n);
+    f.bias[0] = bias;
+    f.residual = matrix_of(residual, m, n);
+    f.y = matrix_of(y, m, n);
+    f.keep[0] = kept_of(keep_z, m, n);
+    return run_forward(l, f, static_cast<hipStream_t>(stream));
+  });
+}
+
+int pointid_gated(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n, const pointid_matrix* x,
+                  const pointid_matrix* wg, const pointid_matrix* wu, const float* bias_g, const float* bias_u,
+                  const pointid_matrix* h, const pointid_kept* keep_g, const pointid_kept* keep_u, void* stream) {
+  return guarded([&] {
+    TRY(check_call(l, dtype, act, m, k, n));
+    if (m == 0) return (int)POINTID_OK;
+    TRY(check_matrix(x, "x", dtype, m, k));
+    TRY(check_matrix(wg, "wg", dtype, k, n));
+    TRY(check_matrix(wu, "wu", dtype, k, n));
+    TRY(check_floats(bias_g, "bias_g"));
+    TRY(check_floats(bias_u, "bias_u"));
+    TRY(check_matrix(h, "h", dtype, m, n));
+    TRY(check_kept(keep_g, "keep_g", dtype, m, n, true));
+    TRY(check_kept(keep_u, "keep_u", dtype, m, n, true));
+    Forward f;
+    std::memset(&f, 0, sizeof(f));
+    f.dtype = dtype, f.act = act, f.halves = 2, f.m = m, f.k = k, f.n = n;
+    f.x = matrix_of(x, m, k);
+    f.w[0] = matrix_of(wg, k, n);
+    f.w[1] = matrix_of(wu, k, n);
+    f.bias[0] = bias_g;
+    f.bias[1] = bias_u;
+    f.y = matrix_of(h, m, n);
+    f.keep[0] = kept_of(keep_g, m, n);
+    f.keep[1] = kept_of(keep_u, m, n);
+    return run_forward(l, f, static_cast<hipStream_t>(stream));
+  });
+}
+
+int pointid_dense_backward(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
+                           const pointid_matrix* dy, const pointid_kept* x, const pointid_matrix* w,
+                           const pointid_kept* z, const pointid_matrix* dx, const pointid_matrix* dw, float* db,
+                           void* stream) {
+  return guarded([&] {
+    TRY(check_call(l, dtype, act, m, k, n));
+    const bool want_dx = dx && dx->data && m > 0, want_dw = dw && dw->data;
+    TRY(check_matrix(dy, "dy", dtype, m, n));
+    TRY(check_kept(x, "x", dtype, m, k, !want_dw));
+    TRY(check_matrix(w, "w", dtype, k, n, !want_dx));
+    TRY(check_kept(z, "z", dtype, m, n, act == POINTID_ACT_NONE));
+    TRY(check_matrix(dx, "dx", dtype, m, k, true));
+    TRY(check_matrix(dw, "dw", dtype, k, n, true));
+    TRY(check_floats(db, "db"));
+    Backward b;
+    std::memset(&b, 0, sizeof(b));
+    b.dtype = dtype, b.act = act, b.halves = 1, b.m = m, b.k = k, b.n = n;
+    b.dy = matrix_of(dy, m, n);
+    b.x = kept_of(x, m, k);
+    b.w[0] = matrix_of(w, k, n);
+    if (act != POINTID_ACT_NONE) b.z[0] = kept_of(z, m, n);
+    if (want_dx) b.dx = matrix_of(dx, m, k);
+    if (want_dw) b.dw[0] = matrix_of(dw, k, n);
+    b.db[0] = db;
+    return run_backward(l, b, static_cast<hipStream_t>(stream));
+  });
+}
+
+int pointid_gated_backward(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
+                           const pointid_matrix* dh, const pointid_kept* x, const pointid_matrix* wg,
+                           const pointid_matrix* wu, const pointid_kept* g, const pointid_kept* u,
+                           const pointid_matrix* dx, const pointid_matrix* dwg, const pointid_matrix* dwu, float* dbg,
+                           float* dbu, void* stream) {
+  return guarded([&] {
+    TRY(check_call(l, dtype, act, m, k, n));
+    const bool want_dx = dx && dx->data && m > 0, want_dw = dwg && dwg->data;
+    if (want_dw != (dwu && dwu->data)) return set_error(POINTID_EINVAL, "dwg and dwu are given both or neither");
+    TRY(check_matrix(dh, "dh", dtype, m, n));
+    TRY(check_kept(x, "x", dtype, m, k, !want_dw));
+    TRY(check_matrix(wg, "wg", dtype, k, n, !want_dx));
+    TRY(check_matrix(wu, "wu", dtype, k, n, !want_dx));
+    TRY(check_kept(g, "g", dtype, m, n, false));
+    TRY(check_kept(u, "u", dtype, m, n, false));
+    TRY(check_matrix(dx, "dx", dtype, m, k, true));
+    TRY(check_matrix(dwg, "dwg", dtype, k, n, true));
+    TRY(check_matrix(dwu, "dwu", dtype, k, n, true));
+    TRY(check_floats(dbg, "dbg"));
+    TRY(check_floats(dbu, "dbu"));
+    Backward b;
+    std::memset(&b, 0, sizeof(b));
+    b.dtype = dtype, b.act = act, b.halves = 2, b.m = m, b.k = k, b.n = n;
+    b.dy = matrix_of(dh, m, n);
+    b.x = kept_of(x, m, k);
+    b.w[0] = matrix_of(wg, k, n);
+    b.w[1] = matrix_of(wu, k, n);
+    b.z[0] = kept_of(g, m, n);
+    b.z[1] = kept_of(u, m, n);
+    if (want_dx) b.dx = matrix_of(dx, m, k);
+    if (want_dw) {
+      b.dw[0] = matrix_of(dwg, k, n);
+      b.dw[1] = matrix_of(dwu, k, n);
+    }
+    b.db[0] = dbg;
+    b.db[1] = dbu;
+    return run_backward(l, b, static_cast<hipStream_t>(stream));
+  });
+}
+
+int pointid_checkpoint_save(int dtype, int64_t rows, int64_t cols, const pointid_matrix* x,
+                            const pointid_checkpoint* out, void* stream) {
+  return guarded([&] {
+    TRY(check_checkpoint_call(dtype, rows, cols, x, out));
+    if (rows == 0) return (int)POINTID_OK;
+    const pointid_matrix a = matrix_of(x, rows, cols);
+    const hipError_t e = launch_checkpoint_save(a.data, a.ld, dtype, rows, cols, {out->codes, out->exponents},
+                                                static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? (int)POINTID_OK : hip_fail(e, "checkpoint save launch");
+  });
+}
+
+int pointid_checkpoint_load(int dtype, int64_t rows, int64_t cols, const pointid_checkpoint* in,
+                            const pointid_matrix* out, void* stream) {
+  return guarded([&] {
+    TRY(check_checkpoint_call(dtype, rows, cols, out, in));
+    if (rows == 0) return (int)POINTID_OK;
+    const pointid_matrix a = matrix_of(out, rows, cols);
+    const hipError_t e = launch_checkpoint_load({in->codes, in->exponents}, rows, cols, dtype, a.data, a.ld, cols,
+                                                static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? (int)POINTID_OK : hip_fail(e, "checkpoint load launch");
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,272 @@
+// Device parts that the layer kernels share: types, activations, the 8-bit block
+// format, and the end of a product (bias, activation, product of the halves, residual,
+// kept activations).
+#pragma once
+
+#include "layers.h"
+#include "op16.h"
+
+namespace pointid {
+
+__device__ __forceinline__ uint16_t to16(float v, int dtype) {
+  if (dtype == POINTID_FP16) return __builtin_bit_cast(uint16_t, (_Float16)v);
+  return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+__device__ __forceinline__ float from16(uint16_t h, int dtype) {
+  if (dtype == POINTID_FP16) return (float)__builtin_bit_cast(_Float16, h);
+  return __uint_as_float((uint32_t)h << 16);
+}
+__device__ __forceinline__ uint32_t pack16(float a, float b, int dtype) {
+  return dtype == POINTID_FP16 ? Op16<true>::pack(a, b) : Op16<false>::pack(a, b);
+}
+
+__device__ __forceinline__ float load_any(const void* p, int64_t at, int dtype) {
+  if (dtype == POINTID_FP32) return static_cast<const float*>(p)[at];
+  return from16(static_cast<const uint16_t*>(p)[at], dtype);
+}
+__device__ __forceinline__ void store_any(void* p, int64_t at, float v, int dtype) {
+  if (dtype == POINTID_FP32)
+    static_cast<float*>(p)[at] = v;
+  else
+    static_cast<uint16_t*>(p)[at] = to16(v, dtype);
+}
+
+// kN (8 or 16) consecutive values of a row from column `col`, of which the first `n`
+// exist; the rest read as 0 and are not written.  `vec`: the row's pieces of 16 bytes
+// are aligned.
+template <int kN>
+__device__ __forceinline__ void load_cols(const void* p, int64_t at, int dtype, bool vec, int64_t n, float* v) {
+  if (vec && n >= kN) {
+    if (dtype == POINTID_FP32) {
+      const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < kN / 4; ++i) {
+        const float4 f = s[i];
+        v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+      }
+    } else {
+      const uint4* s = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < kN / 8; ++i) {
+        const uint4 u = s[i];
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[8 * i + 2 * j] = from16((uint16_t)w[j], dtype);
+          v[8 * i + 2 * j + 1] = from16((uint16_t)(w[j] >> 16), dtype);
+        }
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] = i < n ? load_any(p, at + i, dtype) : 0.f;
+}
+template <int kN>
+__device__ __forceinline__ void store_cols(void* p, int64_t at, int dtype, bool vec, int64_t n, const float* v) {
+  if (vec && n >= kN) {
+    if (dtype == POINTID_FP32) {
+      float4* s = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < kN / 4; ++i) s[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else {
+      uint4* s = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at);
+#pragma unroll
+      for (int i = 0; i < kN / 8; ++i)
+        s[i] = make_uint4(pack16(v[8 * i], v[8 * i + 1], dtype), pack16(v[8 * i + 2], v[8 * i + 3], dtype),
+                          pack16(v[8 * i + 4], v[8 * i + 5], dtype), pack16(v[8 * i + 6], v[8 * i + 7], dtype));
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    if (i < n) store_any(p, at + i, v[i], dtype);
+}
+
+// ---- activations (fp32).  relu passes a NaN on; its slope at 0 is 0.
+__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+__device__ __forceinline__ float activate(int act, float z) {
+  switch (act) {
+    case POINTID_ACT_RELU: return z <= 0.f ? 0.f : z;
+    case POINTID_ACT_SILU: return z / (1.f + expf(-z));
+    case POINTID_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case POINTID_ACT_SIGMOID: return sigmoid(z);
+  }
+  return z;
+}
+__device__ __forceinline__ void activate16(int act, float* v) {
+  static_for<5>([&](auto a) {                 // the choice outside of the loop
+    if (a != POINTID_ACT_NONE && act == a)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = activate(a, v[i]);
+  });
+}
+// The gradient d of act(z), brought to z: d act'(z).  relu selects, so that an infinity
+// or NaN does not get through where it is off.
+__device__ __forceinline__ float through(int act, float z, float d) {
+  switch (act) {
+    case POINTID_ACT_RELU: return z <= 0.f ? 0.f : d;
+    case POINTID_ACT_SILU: {
+      const float s = sigmoid(z);
+      return d * (s * (1.f + z * (1.f - s)));
+    }
+    case POINTID_ACT_GELU:
+      return d * (0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f);
+    case POINTID_ACT_SIGMOID: {
+      const float s = sigmoid(z);
+      return d * (s * (1.f - s));
+    }
+  }
+  return d;
+}
+
+// ---- the 8-bit block format.  The values of a block of 32 are multiplied by 2^p, p
+// the largest integer with max |v| 2^p <= 448 (at most 126; 0 for a block of zeros), and
+// rounded to e4m3 (nearest even); 127 - p is stored.  A value that is not finite is
+// stored as NaN and does not count for the maximum.
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+  const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+  return b < 0x7F800000u ? b : 0u;
+}
+__device__ __forceinline__ int block_power(uint32_t max_bits) {
+  if (max_bits == 0) return 0;
+  const float a = __uint_as_float(max_bits);             // f 2^e, f in [1/2, 1); 448 = 7/8 2^9
+  const int e = __builtin_amdgcn_frexp_expf(a);
+  const int p = __builtin_amdgcn_frexp_mantf(a) <= 0.875f ? 9 - e : 8 - e;
+  return p < 126 ? p : 126;
+}
+__device__ __forceinline__ float scaled_for_8(float v, int p) {
+  return (__float_as_uint(v) & 0x7FFFFFFFu) < 0x7F800000u ? __builtin_amdgcn_ldexpf(v, p) : __uint_as_float(0x7FC00000u);
+}
+__device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+__device__ __forceinline__ void unpack8(uint32_t w, int p, float* v) {       // times 2^p
+  const floatx2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+  const floatx2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  v[0] = __builtin_amdgcn_ldexpf(a[0], p);
+  v[1] = __builtin_amdgcn_ldexpf(a[1], p);
+  v[2] = __builtin_amdgcn_ldexpf(b[0], p);
+  v[3] = __builtin_amdgcn_ldexpf(b[1], p);
+}
+
+// 8 or 16 codes of a row from column `col` (a multiple of kN), of which n exist.
+template <int kN>
+__device__ __forceinline__ void load_codes(const Packed8& s, int64_t row, int64_t col, int64_t cols, float* v) {
+  const int64_t at = row * cols + col;
+  const int p = (int)s.exponents[row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8] - 127;
+  const int64_t n = cols - col;
+  const uint8_t* c = s.codes + at;
+  uint32_t w[kN / 4];
+  if (n >= kN && (reinterpret_cast<uintptr_t>(c) & (kN - 1)) == 0) {
+    if constexpr (kN == 16) {
+      const uint4 u = *reinterpret_cast<const uint4*>(c);
+      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(c);
+      w[0] = u.x, w[1] = u.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kN / 4; ++i) {
+      w[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (4 * i + j < n) w[i] |= (uint32_t)c[4 * i + j] << (8 * j);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kN / 4; ++i) unpack8(w[i], p, v + 4 * i);
+}
+
+// 16 values of a row from column `col` (a multiple of 16) to a checkpoint.  The lane
+// kPartner away (xor) holds the other half of the block of 32 and calls this too.
+// `live`: the row exists.  Columns past `cols` do not count and are not written.
+template <int kPartner>
+__device__ __forceinline__ void save_codes(const Packed8& d, bool live, int64_t row, int64_t col, int64_t cols,
+                                           const float* v) {
+  const int64_t n = cols - col;
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t b = i < n ? finite_bits(v[i]) : 0u;
+    top = b > top ? b : top;
+  }
+  const uint32_t other = (uint32_t)__shfl_xor((int)top, kPartner, 64);
+  const int p = block_power(top > other ? top : other);
+  if (!live || n <= 0) return;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = pack8(scaled_for_8(v[4 * i], p), scaled_for_8(v[4 * i + 1], p), scaled_for_8(v[4 * i + 2], p),
+                 scaled_for_8(v[4 * i + 3], p));
+  uint8_t* c = d.codes + row * cols + col;
+  if (n >= 16 && (reinterpret_cast<uintptr_t>(c) & 15) == 0) {
+    *reinterpret_cast<uint4*>(c) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < n) c[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+  if (col % kBlock8 == 0)
+    d.exponents[row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8] = (uint8_t)(127 - p);
+}
+
+template <int kPartner>
+__device__ __forceinline__ void keep_cols(const Kept& k, int dtype, bool vec, bool live, int64_t row, int64_t col,
+                                          int64_t cols, const float* v) {
+  if (k.matrix) {
+    if (live) store_cols<16>(k.matrix, row * k.ld + col, dtype, vec, cols - col, v);
+  } else if (k.packed.codes) {
+    save_codes<kPartner>(k.packed, live, row, col, cols, v);
+  }
+}
+
+__device__ __forceinline__ void add_bias(const float* bias, int64_t col, int64_t cols, float* v) {
+  if (!bias) return;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] += col + i < cols ? bias[col + i] : 0.f;
+}
+
+// The end of 16 finished columns of a row (see End); v1: the second half's, with
+// e.halves == 2.  Every lane of the wave calls it; `live` is false past the rows.
+template <int kPartner>
+__device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int64_t col, float* v0, float* v1) {
+  const int64_t n = e.cols - col;
+  if (e.mode == kEndStore) {
+    if (!live || n <= 0) return;
+    store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, e.vec0, n, v0);
+    if (e.halves == 2) store_cols<16>(e.y1, row * e.ld1 + col, e.dtype, e.vec1, n, v1);
+    return;
+  }
+  add_bias(e.bias0, col, e.cols, v0);
+  keep_cols<kPartner>(e.keep0, e.dtype, e.vec_keep0, live && n > 0, row, col, e.cols, v0);
+  if (e.mode == kEndGated) {
+    add_bias(e.bias1, col, e.cols, v1);
+    keep_cols<kPartner>(e.keep1, e.dtype, e.vec_keep1, live && n > 0, row, col, e.cols, v1);
+  }
+  if (!live || n <= 0) return;
+  activate16(e.act, v0);
+  if (e.mode == kEndGated) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v0[i] *= v1[i];
+  } else if (e.residual) {
+    float r[16];
+    load_cols<16>(e.residual, row * e.ld_residual + col, e.dtype, e.vec_residual, n, r);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v0[i] += r[i];
+  }
+  store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, e.vec0, n, v0);
+}
+
+// 16 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)
+__device__ __forceinline__ void store_partial(const End& e, int split, int half, bool live, int64_t row, int64_t col,
+                                              const float* v) {
+  if (!live || col >= e.part_ld) return;
+  float4* p = reinterpret_cast<float4*>(e.part + (((int64_t)split * e.halves + half) * e.rows + row) * e.part_ld + col);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+}
+
+}  // namespace pointid

@@ -1,0 +1,10 @@
+// The matrix-core products of fp16 operands.
+#include "layers_mm.h"
+
+namespace pointid {
+
+hipError_t launch_product_fp16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream) {
+  return mm::launch<true>(form, plan, a, stream);
+}
+
+}  // namespace pointid

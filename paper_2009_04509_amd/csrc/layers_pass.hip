@@ -1,0 +1,277 @@
+// Passes over one matrix: operands laid out for the product kernels, 8-bit checkpoints
+// written and read, the gradient before an activation with its column sums.  All are
+// bound by the bytes they move.
+#include "internal.h"
+#include "layers_end.h"
+
+namespace pointid {
+namespace {
+
+// v as the sum of three bf16 values: each part is the remainder so far, rounded (8 + 8 + 8
+// bits hold fp32's 24).  A value that rounds past the largest bf16 is cut instead; one
+// that is not finite stays in the first part.
+__device__ __forceinline__ void three_parts(float v, uint16_t* o) {
+  __bf16 a = (__bf16)v;
+  if ((__float_as_uint((float)a) & 0x7FFFFFFFu) >= 0x7F800000u) {
+    if ((__float_as_uint(v) & 0x7FFFFFFFu) >= 0x7F800000u) {
+      o[0] = __builtin_bit_cast(uint16_t, a);
+      o[1] = o[2] = 0;
+      return;
+    }
+    a = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(v) >> 16));
+  }
+  const float r = v - (float)a;
+  const __bf16 b = (__bf16)r;
+  const __bf16 c = (__bf16)(r - (float)b);
+  o[0] = __builtin_bit_cast(uint16_t, a);
+  o[1] = __builtin_bit_cast(uint16_t, b);
+  o[2] = __builtin_bit_cast(uint16_t, c);
+}
+
+__device__ __forceinline__ void store8(uint16_t* p, const uint16_t* h) {      // 16-byte aligned
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// the thread's piece of 8 columns, grid-strided over rows x pieces
+template <class F>
+__device__ __forceinline__ void each_piece(int64_t rows, int64_t pieces, F&& f) {
+  const int64_t total = rows * pieces, step = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step) {
+    const int64_t row = i / pieces;
+    f(row, (i - row * pieces) * 8);
+  }
+}
+
+__global__ void __launch_bounds__(256) pack_kernel(const void* src, int64_t ld_src, int dtype, bool vec, int64_t rows,
+                                                   int64_t cols, int parts, uint16_t* out, int64_t ld, int64_t plane) {
+  each_piece(rows, ld / 8, [&](int64_t row, int64_t col) {
+    float v[8];
+    load_cols<8>(src, row * ld_src + col, dtype, vec, cols - col, v);
+    uint16_t h[3][8];
+    if (parts == 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[0][i] = to16(v[i], dtype);
+      store8(out + row * ld + col, h[0]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint16_t p[3];
+      three_parts(v[i], p);
+      h[0][i] = p[0], h[1][i] = p[1], h[2][i] = p[2];
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) store8(out + q * plane + row * ld + col, h[q]);
+  });
+}
+
+__global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64_t rows, int64_t cols, int dtype,
+                                                              void* out, int64_t ld, bool vec, int64_t fill_to) {
+  each_piece(rows, (fill_to + 7) / 8, [&](int64_t row, int64_t col) {
+    float v[8] = {};
+    if (col < cols) load_codes<8>(src, row, col, cols, v);
+    store_cols<8>(out, row * ld + col, dtype, vec, fill_to - col, v);
+  });
+}
+
+// A block of 32 values by a pair of neighbouring lanes.
+__global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, int64_t ld, int dtype, bool vec,
+                                                              int64_t rows, int64_t cols, Packed8 out) {
+  const int64_t pairs = (cols + kBlock8 - 1) / kBlock8, total = rows * pairs * 2;
+  const int64_t step = (int64_t)gridDim.x * blockDim.x;
+  // every lane of a wave takes the same number of turns, as the exchange needs both of a pair
+  const int64_t last = (total + 63) / 64 * 64;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < last; i += step) {
+    const bool live = i < total;
+    const int64_t row = live ? i / (2 * pairs) : 0, col = live ? (i - row * 2 * pairs) * 16 : 0;
+    float v[16];
+    load_cols<16>(src, row * ld + col, dtype, vec, live ? cols - col : 0, v);
+    save_codes<1>(out, live, row, col, cols, v);
+  }
+}
+
+// Each block: kGradRows rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time.
+template <int kHalves>
+__global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
+  __shared__ float sums[8][256 + 8];
+  const int piece = threadIdx.x % 32, sub = threadIdx.x / 32;
+  const int64_t col = (int64_t)blockIdx.y * 256 + piece * 8, n = a.cols - col;
+  const int64_t row0 = (int64_t)blockIdx.x * kGradRows;
+  float total[kHalves][8] = {};
+  for (int s = 0; s < kGradRows / 8; ++s) {
+    const int64_t row = row0 + 8 * s + sub;
+    if (row >= a.rows || (n <= 0 && col >= a.ld)) continue;
+    float d[kHalves][8] = {};
+    if (n > 0) {
+      float dy[8], z[2][8];
+      load_cols<8>(a.dy, row * a.ld_dy + col, a.dtype, a.vec_dy, n, dy);
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        if (a.z[h].matrix)
+          load_cols<8>(a.z[h].matrix, row * a.z[h].ld + col, a.dtype, a.vec_z[h], n, z[h]);
+        else if (a.z[h].packed.codes)
+          load_codes<8>(a.z[h].packed, row, col, a.cols, z[h]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i >= n) continue;
+        if constexpr (kHalves == 2) {
+          d[0][i] = through(a.act, z[0][i], dy[i] * z[1][i]);
+          d[1][i] = dy[i] * activate(a.act, z[0][i]);
+        } else {
+          d[0][i] = through(a.act, z[0][i], dy[i]);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) total[h][i] += d[h][i];
+    }
+    if (a.parts == 0 || col >= a.ld) continue;
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      if (a.parts < 0) {
+        store_cols<8>(a.out[h], row * a.ld + col, POINTID_FP32, true, 8, d[h]);
+        continue;
+      }
+      uint16_t* o = static_cast<uint16_t*>(a.out[h]) + row * a.ld + col;
+      uint16_t p[3][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (a.parts == 3) {
+          uint16_t t[3];
+          three_parts(d[h][i], t);
+          p[0][i] = t[0], p[1][i] = t[1], p[2][i] = t[2];
+        } else {
+          p[0][i] = to16(d[h][i], a.type16);
+          const float rest = d[h][i] - from16(p[0][i], a.type16);
+          p[1][i] = (__float_as_uint(rest) & 0x7FFFFFFFu) < 0x7F800000u ? to16(rest, a.type16) : 0;
+        }
+      }
+      store8(o, p[0]);
+      if (a.parts >= 2) store8(o + a.plane, p[1]);
+      if (a.parts >= 3) store8(o + 2 * a.plane, p[2]);
+    }
+  }
+  if (!a.col_part) return;
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[sub][piece * 8 + i] = total[h][i];
+    __syncthreads();
+    const int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x;
+    float t = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) t += sums[s][threadIdx.x];
+    if (c < a.cols) a.col_part[((int64_t)blockIdx.x * kHalves + h) * a.cols + c] = t;
+    __syncthreads();
+  }
+}
+
+// Sums of `blocks` rows of the columns of a half (blockIdx.y): 32 columns by 8 lanes of blocks.
+__global__ void __launch_bounds__(256) colsum_kernel(const float* part, int64_t blocks, int64_t cols, float* out0,
+                                                     float* out1) {
+  __shared__ float sums[8][33];
+  const int c = threadIdx.x % 32, sub = threadIdx.x / 32;
+  const int64_t col = (int64_t)blockIdx.x * 32 + c;
+  float* out = blockIdx.y ? out1 : out0;
+  if (!out) return;
+  float t = 0.f;
+  if (col < cols)
+    for (int64_t b = sub; b < blocks; b += 8) t += part[(b * gridDim.y + blockIdx.y) * cols + col];
+  sums[sub][c] = t;
+  __syncthreads();
+  if (sub != 0 || col >= cols) return;
+  float v = 0.f;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) v += sums[s][c];
+  out[col] = v;
+}
+
+// 16 columns of a row of partials by a lane, in the order of the parts.
+template <int kHalves>
+__global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int64_t part_ld, int splits) {
+  const int64_t units = part_ld / 16, total = e.rows * units;
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const bool live = i < total;
+  const int64_t row = live ? i / units : 0, col = live ? (i - row * units) * 16 : 0;
+  float v[kHalves][16] = {};
+  if (live) {
+    for (int s = 0; s < splits; ++s)
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const float4* p = reinterpret_cast<const float4*>(part + (((int64_t)s * kHalves + h) * e.rows + row) * part_ld + col);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 f = p[j];
+          v[h][4 * j] += f.x, v[h][4 * j + 1] += f.y, v[h][4 * j + 2] += f.z, v[h][4 * j + 3] += f.w;
+        }
+      }
+  }
+  finish<1>(e, live, row, col, v[0], v[kHalves - 1]);
+}
+
+__global__ void __launch_bounds__(256) zero_kernel(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols) {
+  const int64_t total = rows * cols, step = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step)
+    store_any(out, i / cols * ld + i % cols, 0.f, dtype);
+}
+
+bool aligned_rows(const void* p, int64_t ld, int dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % (dtype == POINTID_FP32 ? 4 : 8) == 0;
+}
+
+// blocks for `items` lanes of work, at most 8 rounds of the card's 256 CUs of 8 blocks
+unsigned pass_blocks(int64_t items) {
+  const int64_t b = (items + 255) / 256;
+  return (unsigned)(b < 16384 ? (b > 0 ? b : 1) : 16384);
+}
+
+}  // namespace
+
+hipError_t launch_layers_pack(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, int parts,
+                              uint16_t* out, int64_t ld, int64_t plane, hipStream_t stream) {
+  return launch_kernel(pack_kernel, dim3(pass_blocks(rows * (ld / 8))), dim3(256), 0, stream, src, ld_src, dtype,
+                       aligned_rows(src, ld_src, dtype), rows, cols, parts, out, ld, plane);
+}
+
+hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
+                                  int64_t fill_to, hipStream_t stream) {
+  return launch_kernel(checkpoint_load_kernel, dim3(pass_blocks(rows * ((fill_to + 7) / 8))), dim3(256), 0, stream, src,
+                       rows, cols, dtype, out, ld, aligned_rows(out, ld, dtype), fill_to);
+}
+
+hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
+                                  const Packed8& out, hipStream_t stream) {
+  return launch_kernel(checkpoint_save_kernel, dim3(pass_blocks(rows * ((cols + 31) / 32) * 2)), dim3(256), 0, stream,
+                       src, ld, dtype, aligned_rows(src, ld, dtype), rows, cols, out);
+}
+
+hipError_t launch_layers_grad(const GradArgs& a, hipStream_t stream) {
+  const int64_t width = a.parts != 0 && a.ld > a.cols ? a.ld : a.cols;
+  const dim3 grid((unsigned)((a.rows + kGradRows - 1) / kGradRows), (unsigned)((width + 255) / 256));
+  return a.halves == 2 ? launch_kernel(grad_kernel<2>, grid, dim3(256), 0, stream, a)
+                       : launch_kernel(grad_kernel<1>, grid, dim3(256), 0, stream, a);
+}
+
+hipError_t launch_layers_colsum(const float* col_part, int64_t blocks, int64_t cols, int halves, float* out0,
+                                float* out1, hipStream_t stream) {
+  return launch_kernel(colsum_kernel, dim3((unsigned)((cols + 31) / 32), (unsigned)halves), dim3(256), 0, stream,
+                       col_part, blocks, cols, out0, out1);
+}
+
+hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols, hipStream_t stream) {
+  return launch_kernel(zero_kernel, dim3(pass_blocks(rows * cols)), dim3(256), 0, stream, out, ld, dtype, rows, cols);
+}
+
+hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld, int splits, hipStream_t stream) {
+  const unsigned blocks = (unsigned)((end.rows * (part_ld / 16) + 255) / 256);
+  return end.halves == 2
+             ? launch_kernel(join_kernel<2>, dim3(blocks), dim3(256), 0, stream, end, part, part_ld, splits)
+             : launch_kernel(join_kernel<1>, dim3(blocks), dim3(256), 0, stream, end, part, part_ld, splits);
+}
+
+}  // namespace pointid
