@@ -66,8 +66,6 @@ struct End {
   Kept keep0, keep1;
   float* part;
   int64_t part_ld;             // a multiple of 32
-  // rows of the matrix can be read or written in 16-byte pieces
-  bool vec_residual, vec0, vec1, vec_keep0, vec_keep1;
 };
 
 // One term of the sum: a left operand with one right operand for each half.
@@ -136,7 +134,7 @@ hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, in
 // parts: 0 none written, 1 or 2 planes of the 16-bit type (2: value and remainder),
 // 3 bf16 planes, -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each
 // block of kGradRows rows, or nullptr.
-constexpr int kGradRows = 64;
+constexpr int kGradRows = 32;
 struct GradArgs {
   const void* dy;
   int64_t ld_dy;
@@ -150,7 +148,6 @@ struct GradArgs {
   void* out[2];                // each half: planes [parts][rows][ld], or fp32 [rows][ld]
   int64_t ld, plane;
   float* col_part;
-  bool vec_dy, vec_z[2];
 };
 hipError_t launch_layers_grad(const GradArgs& a, hipStream_t stream);
 // out[i] = sum over blocks of col_part[block][half][i], for each half whose out is given

@@ -262,8 +262,8 @@ End end_of(int mode, int act, int dtype, int halves, int64_t rows, int64_t cols,
   e.rows = rows;
   e.cols = cols;
   e.part_ld = round_up(cols, 32);
-  e.y0 = y0.data, e.ld0 = y0.ld, e.vec0 = rows_in_16(y0.data, y0.ld, dtype);
-  e.y1 = y1.data, e.ld1 = y1.ld, e.vec1 = rows_in_16(y1.data, y1.ld, dtype);
+  e.y0 = y0.data, e.ld0 = y0.ld;
+  e.y1 = y1.data, e.ld1 = y1.ld;
   return e;
 }
 
@@ -292,11 +292,8 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   e.bias1 = f.bias[1];
   e.residual = f.residual.data;
   e.ld_residual = f.residual.ld;
-  e.vec_residual = rows_in_16(f.residual.data, f.residual.ld, f.dtype);
   e.keep0 = f.keep[0];
   e.keep1 = f.keep[1];
-  e.vec_keep0 = rows_in_16(e.keep0.matrix, e.keep0.ld, f.dtype);
-  e.vec_keep1 = rows_in_16(e.keep1.matrix, e.keep1.ld, f.dtype);
   const Strided x = {f.x.data, f.x.ld, 1, f.dtype};
   Strided w[2];
   for (int h = 0; h < 2; ++h) w[h] = {f.w[h].data, 1, f.w[h].ld, f.dtype};
@@ -416,11 +413,7 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   g.halves = b.halves;
   g.rows = b.m;
   g.cols = b.n;
-  g.vec_dy = rows_in_16(b.dy.data, b.dy.ld, b.dtype);
-  for (int h = 0; h < b.halves; ++h) {
-    g.z[h] = b.z[h];
-    g.vec_z[h] = rows_in_16(b.z[h].matrix, b.z[h].ld, b.dtype);
-  }
+  for (int h = 0; h < b.halves; ++h) g.z[h] = b.z[h];
   g.parts = !products || read_dy ? 0 : simple ? -1 : b.dtype == POINTID_FP32 ? 3 : !exact16 && b.m * b.n <= kTwoPartValues ? 2 : 1;
   g.ld = round_up(b.n, 8);
   g.plane = b.m * g.ld;

@@ -31,30 +31,21 @@ __device__ __forceinline__ void store_any(void* p, int64_t at, float v, int dtyp
     static_cast<uint16_t*>(p)[at] = to16(v, dtype);
 }
 
-// kN (8 or 16) consecutive values of a row from column `col`, of which the first `n`
-// exist; the rest read as 0 and are not written.  `vec`: the row's pieces of 16 bytes
-// are aligned.
+// kN (4, 8 or 16) consecutive values of a row, of which the first `n` exist; the rest
+// read as 0 and are not written.  Pieces of 16 bytes at any alignment (the hardware
+// takes them; aligned ones are faster).
 template <int kN>
-__device__ __forceinline__ void load_cols(const void* p, int64_t at, int dtype, bool vec, int64_t n, float* v) {
-  if (vec && n >= kN) {
+__device__ __forceinline__ void load_cols(const void* p, int64_t at, int dtype, int64_t n, float* v) {
+  if (n >= kN) {
     if (dtype == POINTID_FP32) {
-      const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-#pragma unroll
-      for (int i = 0; i < kN / 4; ++i) {
-        const float4 f = s[i];
-        v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
-      }
+      __builtin_memcpy(v, static_cast<const float*>(p) + at, 4 * kN);
     } else {
-      const uint4* s = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at);
+      uint32_t w[kN / 2];
+      __builtin_memcpy(w, static_cast<const uint16_t*>(p) + at, 2 * kN);
 #pragma unroll
-      for (int i = 0; i < kN / 8; ++i) {
-        const uint4 u = s[i];
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[8 * i + 2 * j] = from16((uint16_t)w[j], dtype);
-          v[8 * i + 2 * j + 1] = from16((uint16_t)(w[j] >> 16), dtype);
-        }
+      for (int i = 0; i < kN / 2; ++i) {
+        v[2 * i] = from16((uint16_t)w[i], dtype);
+        v[2 * i + 1] = from16((uint16_t)(w[i] >> 16), dtype);
       }
     }
     return;
@@ -63,18 +54,15 @@ __device__ __forceinline__ void load_cols(const void* p, int64_t at, int dtype, 
   for (int i = 0; i < kN; ++i) v[i] = i < n ? load_any(p, at + i, dtype) : 0.f;
 }
 template <int kN>
-__device__ __forceinline__ void store_cols(void* p, int64_t at, int dtype, bool vec, int64_t n, const float* v) {
-  if (vec && n >= kN) {
+__device__ __forceinline__ void store_cols(void* p, int64_t at, int dtype, int64_t n, const float* v) {
+  if (n >= kN) {
     if (dtype == POINTID_FP32) {
-      float4* s = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
-#pragma unroll
-      for (int i = 0; i < kN / 4; ++i) s[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      __builtin_memcpy(static_cast<float*>(p) + at, v, 4 * kN);
     } else {
-      uint4* s = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at);
+      uint32_t w[kN / 2];
 #pragma unroll
-      for (int i = 0; i < kN / 8; ++i)
-        s[i] = make_uint4(pack16(v[8 * i], v[8 * i + 1], dtype), pack16(v[8 * i + 2], v[8 * i + 3], dtype),
-                          pack16(v[8 * i + 4], v[8 * i + 5], dtype), pack16(v[8 * i + 6], v[8 * i + 7], dtype));
+      for (int i = 0; i < kN / 2; ++i) w[i] = pack16(v[2 * i], v[2 * i + 1], dtype);
+      __builtin_memcpy(static_cast<uint16_t*>(p) + at, w, 2 * kN);
     }
     return;
   }
@@ -83,13 +71,29 @@ __device__ __forceinline__ void store_cols(void* p, int64_t at, int dtype, bool 
     if (i < n) store_any(p, at + i, v[i], dtype);
 }
 
-// ---- activations (fp32).  relu passes a NaN on; its slope at 0 is 0.
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+// ---- activations (fp32), from the hardware's 2^x and 1 / x (each within an ulp).
+// sigmoid is off by 1e-7 |z| of itself at most.  Phi, the normal distribution function, is
+// Hastings' approximation of erfc (Abramowitz and Stegun 7.1.26), off by at most 1e-7.
+// A NaN passes through all of them; relu's slope at 0 is 0.
+__device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + two_to(-1.44269504088896341f * z));
+}
+// density: e^(-z^2 / 2)
+__device__ __forceinline__ float normal_below(float z, float* density) {
+  const float e = two_to(-0.72134752044448170f * z * z);
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678118654752f * __builtin_fabsf(z));
+  const float q = 0.5f * e * t *
+                  (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  *density = e;
+  return z < 0.f ? q : 1.f - q;
+}
 __device__ __forceinline__ float activate(int act, float z) {
+  float e;
   switch (act) {
     case POINTID_ACT_RELU: return z <= 0.f ? 0.f : z;
-    case POINTID_ACT_SILU: return z / (1.f + expf(-z));
-    case POINTID_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case POINTID_ACT_SILU: return z * sigmoid(z);
+    case POINTID_ACT_GELU: return z * normal_below(z, &e);
     case POINTID_ACT_SIGMOID: return sigmoid(z);
   }
   return z;
@@ -101,22 +105,31 @@ __device__ __forceinline__ void activate16(int act, float* v) {
       for (int i = 0; i < 16; ++i) v[i] = activate(a, v[i]);
   });
 }
-// The gradient d of act(z), brought to z: d act'(z).  relu selects, so that an infinity
-// or NaN does not get through where it is off.
-__device__ __forceinline__ float through(int act, float z, float d) {
+// act(z), and the gradient d of it brought to z: d act'(z).  relu selects, so that an
+// infinity or NaN does not get through where it is off.
+__device__ __forceinline__ float through(int act, float z, float d, float* value) {
+  float e;
   switch (act) {
-    case POINTID_ACT_RELU: return z <= 0.f ? 0.f : d;
+    case POINTID_ACT_RELU:
+      *value = z <= 0.f ? 0.f : z;
+      return z <= 0.f ? 0.f : d;
     case POINTID_ACT_SILU: {
       const float s = sigmoid(z);
+      *value = z * s;
       return d * (s * (1.f + z * (1.f - s)));
     }
-    case POINTID_ACT_GELU:
-      return d * (0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f);
+    case POINTID_ACT_GELU: {
+      const float below = normal_below(z, &e);
+      *value = z * below;
+      return d * (below + z * e * 0.39894228040143268f);
+    }
     case POINTID_ACT_SIGMOID: {
       const float s = sigmoid(z);
+      *value = s;
       return d * (s * (1.f - s));
     }
   }
+  *value = z;
   return d;
 }
 
@@ -214,10 +227,10 @@ __device__ __forceinline__ void save_codes(const Packed8& d, bool live, int64_t 
 }
 
 template <int kPartner>
-__device__ __forceinline__ void keep_cols(const Kept& k, int dtype, bool vec, bool live, int64_t row, int64_t col,
+__device__ __forceinline__ void keep_cols(const Kept& k, int dtype, bool live, int64_t row, int64_t col,
                                           int64_t cols, const float* v) {
   if (k.matrix) {
-    if (live) store_cols<16>(k.matrix, row * k.ld + col, dtype, vec, cols - col, v);
+    if (live) store_cols<16>(k.matrix, row * k.ld + col, dtype, cols - col, v);
   } else if (k.packed.codes) {
     save_codes<kPartner>(k.packed, live, row, col, cols, v);
   }
@@ -236,15 +249,15 @@ __device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int
   const int64_t n = e.cols - col;
   if (e.mode == kEndStore) {
     if (!live || n <= 0) return;
-    store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, e.vec0, n, v0);
-    if (e.halves == 2) store_cols<16>(e.y1, row * e.ld1 + col, e.dtype, e.vec1, n, v1);
+    store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, n, v0);
+    if (e.halves == 2) store_cols<16>(e.y1, row * e.ld1 + col, e.dtype, n, v1);
     return;
   }
   add_bias(e.bias0, col, e.cols, v0);
-  keep_cols<kPartner>(e.keep0, e.dtype, e.vec_keep0, live && n > 0, row, col, e.cols, v0);
+  keep_cols<kPartner>(e.keep0, e.dtype, live && n > 0, row, col, e.cols, v0);
   if (e.mode == kEndGated) {
     add_bias(e.bias1, col, e.cols, v1);
-    keep_cols<kPartner>(e.keep1, e.dtype, e.vec_keep1, live && n > 0, row, col, e.cols, v1);
+    keep_cols<kPartner>(e.keep1, e.dtype, live && n > 0, row, col, e.cols, v1);
   }
   if (!live || n <= 0) return;
   activate16(e.act, v0);
@@ -253,11 +266,11 @@ __device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int
     for (int i = 0; i < 16; ++i) v0[i] *= v1[i];
   } else if (e.residual) {
     float r[16];
-    load_cols<16>(e.residual, row * e.ld_residual + col, e.dtype, e.vec_residual, n, r);
+    load_cols<16>(e.residual, row * e.ld_residual + col, e.dtype, n, r);
 #pragma unroll
     for (int i = 0; i < 16; ++i) v0[i] += r[i];
   }
-  store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, e.vec0, n, v0);
+  store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, n, v0);
 }
 
 // 16 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)

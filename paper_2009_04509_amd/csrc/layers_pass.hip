@@ -40,16 +40,16 @@ template <class F>
 __device__ __forceinline__ void each_piece(int64_t rows, int64_t pieces, F&& f) {
   const int64_t total = rows * pieces, step = (int64_t)gridDim.x * blockDim.x;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step) {
-    const int64_t row = i / pieces;
+    const int64_t row = total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)pieces) : i / pieces;
     f(row, (i - row * pieces) * 8);
   }
 }
 
-__global__ void __launch_bounds__(256) pack_kernel(const void* src, int64_t ld_src, int dtype, bool vec, int64_t rows,
+__global__ void __launch_bounds__(256) pack_kernel(const void* src, int64_t ld_src, int dtype, int64_t rows,
                                                    int64_t cols, int parts, uint16_t* out, int64_t ld, int64_t plane) {
   each_piece(rows, ld / 8, [&](int64_t row, int64_t col) {
     float v[8];
-    load_cols<8>(src, row * ld_src + col, dtype, vec, cols - col, v);
+    load_cols<8>(src, row * ld_src + col, dtype, cols - col, v);
     uint16_t h[3][8];
     if (parts == 1) {
 #pragma unroll
@@ -69,16 +69,16 @@ __global__ void __launch_bounds__(256) pack_kernel(const void* src, int64_t ld_s
 }
 
 __global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64_t rows, int64_t cols, int dtype,
-                                                              void* out, int64_t ld, bool vec, int64_t fill_to) {
+                                                              void* out, int64_t ld, int64_t fill_to) {
   each_piece(rows, (fill_to + 7) / 8, [&](int64_t row, int64_t col) {
     float v[8] = {};
     if (col < cols) load_codes<8>(src, row, col, cols, v);
-    store_cols<8>(out, row * ld + col, dtype, vec, fill_to - col, v);
+    store_cols<8>(out, row * ld + col, dtype, fill_to - col, v);
   });
 }
 
 // A block of 32 values by a pair of neighbouring lanes.
-__global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, int64_t ld, int dtype, bool vec,
+__global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, int64_t ld, int dtype,
                                                               int64_t rows, int64_t cols, Packed8 out) {
   const int64_t pairs = (cols + kBlock8 - 1) / kBlock8, total = rows * pairs * 2;
   const int64_t step = (int64_t)gridDim.x * blockDim.x;
@@ -86,74 +86,87 @@ __global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, i
   const int64_t last = (total + 63) / 64 * 64;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < last; i += step) {
     const bool live = i < total;
-    const int64_t row = live ? i / (2 * pairs) : 0, col = live ? (i - row * 2 * pairs) * 16 : 0;
+    const int64_t row = !live ? 0 : total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)(2 * pairs)) : i / (2 * pairs);
+    const int64_t col = live ? (i - row * 2 * pairs) * 16 : 0;
     float v[16];
-    load_cols<16>(src, row * ld + col, dtype, vec, live ? cols - col : 0, v);
+    load_cols<16>(src, row * ld + col, dtype, live ? cols - col : 0, v);
     save_codes<1>(out, live, row, col, cols, v);
   }
 }
 
-// Each block: kGradRows rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time.
+// Each block: kGradRows rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time,
+// two such turns' reads in flight.
 template <int kHalves>
 __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
   __shared__ float sums[8][256 + 8];
   const int piece = threadIdx.x % 32, sub = threadIdx.x / 32;
   const int64_t col = (int64_t)blockIdx.y * 256 + piece * 8, n = a.cols - col;
-  const int64_t row0 = (int64_t)blockIdx.x * kGradRows;
+  const int64_t row0 = (int64_t)blockIdx.x * kGradRows + sub;
   float total[kHalves][8] = {};
-  for (int s = 0; s < kGradRows / 8; ++s) {
-    const int64_t row = row0 + 8 * s + sub;
-    if (row >= a.rows || (n <= 0 && col >= a.ld)) continue;
-    float d[kHalves][8] = {};
-    if (n > 0) {
-      float dy[8], z[2][8];
-      load_cols<8>(a.dy, row * a.ld_dy + col, a.dtype, a.vec_dy, n, dy);
+  constexpr int kTurns = kGradRows / 8, kAhead = 2;
+  if (n > 0) {
+    for (int s = 0; s < kTurns; s += kAhead) {
+      float dy[kAhead][8], z[kAhead][2][8];
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) {
-        if (a.z[h].matrix)
-          load_cols<8>(a.z[h].matrix, row * a.z[h].ld + col, a.dtype, a.vec_z[h], n, z[h]);
-        else if (a.z[h].packed.codes)
-          load_codes<8>(a.z[h].packed, row, col, a.cols, z[h]);
-      }
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t row = row0 + 8 * (s + u);
+        const int64_t here = row < a.rows ? n : 0;
+        load_cols<8>(a.dy, row * a.ld_dy + col, a.dtype, here, dy[u]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i >= n) continue;
-        if constexpr (kHalves == 2) {
-          d[0][i] = through(a.act, z[0][i], dy[i] * z[1][i]);
-          d[1][i] = dy[i] * activate(a.act, z[0][i]);
-        } else {
-          d[0][i] = through(a.act, z[0][i], dy[i]);
+        for (int h = 0; h < kHalves; ++h) {
+          if (a.z[h].matrix)
+            load_cols<8>(a.z[h].matrix, row * a.z[h].ld + col, a.dtype, here, z[u][h]);
+          else if (a.z[h].packed.codes && here)
+            load_codes<8>(a.z[h].packed, row, col, a.cols, z[u][h]);
         }
       }
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h)
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t row = row0 + 8 * (s + u);
+        if (row >= a.rows) continue;
+        float d[kHalves][8];
+        static_for<5>([&](auto act) {               // the choice outside of the loop
+          if (a.act == act) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) total[h][i] += d[h][i];
-    }
-    if (a.parts == 0 || col >= a.ld) continue;
+            for (int i = 0; i < 8; ++i) {
+              float value;
+              if constexpr (kHalves == 2) {
+                d[0][i] = i < n ? through(act, z[u][0][i], dy[u][i] * z[u][1][i], &value) : 0.f;
+                d[1][i] = i < n ? dy[u][i] * value : 0.f;
+              } else {
+                d[0][i] = i < n ? through(act, act == POINTID_ACT_NONE ? 0.f : z[u][0][i], dy[u][i], &value) : 0.f;
+              }
+            }
+          }
+        });
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-      if (a.parts < 0) {
-        store_cols<8>(a.out[h], row * a.ld + col, POINTID_FP32, true, 8, d[h]);
-        continue;
-      }
-      uint16_t* o = static_cast<uint16_t*>(a.out[h]) + row * a.ld + col;
-      uint16_t p[3][8];
+        for (int h = 0; h < kHalves; ++h) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (a.parts == 3) {
-          uint16_t t[3];
-          three_parts(d[h][i], t);
-          p[0][i] = t[0], p[1][i] = t[1], p[2][i] = t[2];
-        } else {
-          p[0][i] = to16(d[h][i], a.type16);
-          const float rest = d[h][i] - from16(p[0][i], a.type16);
-          p[1][i] = (__float_as_uint(rest) & 0x7FFFFFFFu) < 0x7F800000u ? to16(rest, a.type16) : 0;
+          for (int i = 0; i < 8; ++i) total[h][i] += d[h][i];
+          if (a.parts == 0) continue;
+          if (a.parts < 0) {
+            store_cols<8>(a.out[h], row * a.ld + col, POINTID_FP32, 8, d[h]);
+            continue;
+          }
+          uint16_t* o = static_cast<uint16_t*>(a.out[h]) + row * a.ld + col;
+          uint16_t p[3][8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (a.parts == 3) {
+              uint16_t t[3];
+              three_parts(d[h][i], t);
+              p[0][i] = t[0], p[1][i] = t[1], p[2][i] = t[2];
+            } else {
+              p[0][i] = to16(d[h][i], a.type16);
+              const float rest = d[h][i] - from16(p[0][i], a.type16);
+              p[1][i] = (__float_as_uint(rest) & 0x7FFFFFFFu) < 0x7F800000u ? to16(rest, a.type16) : 0;
+            }
+          }
+          store8(o, p[0]);
+          if (a.parts >= 2) store8(o + a.plane, p[1]);
+          if (a.parts >= 3) store8(o + 2 * a.plane, p[2]);
         }
       }
-      store8(o, p[0]);
-      if (a.parts >= 2) store8(o + a.plane, p[1]);
-      if (a.parts >= 3) store8(o + 2 * a.plane, p[2]);
     }
   }
   if (!a.col_part) return;
@@ -191,16 +204,21 @@ __global__ void __launch_bounds__(256) colsum_kernel(const float* part, int64_t 
   out[col] = v;
 }
 
-// 16 columns of a row of partials by a lane, in the order of the parts.
-template <int kHalves>
+// Units of 16 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
+// order.  kSub == 8, for many parts: 8 lanes of a unit take every eighth part each, and
+// their sums are added in order.
+template <int kHalves, int kSub>
 __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int64_t part_ld, int splits) {
+  constexpr int kUnits = 256 / kSub;
+  __shared__ float sums[kSub > 1 ? kSub : 1][kHalves][kSub > 1 ? kUnits : 1][kSub > 1 ? 17 : 1];
   const int64_t units = part_ld / 16, total = e.rows * units;
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int unit = threadIdx.x % kUnits, sub = threadIdx.x / kUnits;
+  const int64_t i = (int64_t)blockIdx.x * kUnits + unit;
   const bool live = i < total;
   const int64_t row = live ? i / units : 0, col = live ? (i - row * units) * 16 : 0;
   float v[kHalves][16] = {};
   if (live) {
-    for (int s = 0; s < splits; ++s)
+    for (int s = sub; s < splits; s += kSub)
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
         const float4* p = reinterpret_cast<const float4*>(part + (((int64_t)s * kHalves + h) * e.rows + row) * part_ld + col);
@@ -211,6 +229,19 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
         }
       }
   }
+  if constexpr (kSub > 1) {
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sums[sub][h][unit][j] = v[h][j];
+    __syncthreads();
+    if (sub != 0) return;
+    for (int s = 1; s < kSub; ++s)
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[h][j] += sums[s][h][unit][j];
+  }
   finish<1>(e, live, row, col, v[0], v[kHalves - 1]);
 }
 
@@ -218,10 +249,6 @@ __global__ void __launch_bounds__(256) zero_kernel(void* out, int64_t ld, int dt
   const int64_t total = rows * cols, step = (int64_t)gridDim.x * blockDim.x;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step)
     store_any(out, i / cols * ld + i % cols, 0.f, dtype);
-}
-
-bool aligned_rows(const void* p, int64_t ld, int dtype) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % (dtype == POINTID_FP32 ? 4 : 8) == 0;
 }
 
 // blocks for `items` lanes of work, at most 8 rounds of the card's 256 CUs of 8 blocks
@@ -235,19 +262,19 @@ unsigned pass_blocks(int64_t items) {
 hipError_t launch_layers_pack(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, int parts,
                               uint16_t* out, int64_t ld, int64_t plane, hipStream_t stream) {
   return launch_kernel(pack_kernel, dim3(pass_blocks(rows * (ld / 8))), dim3(256), 0, stream, src, ld_src, dtype,
-                       aligned_rows(src, ld_src, dtype), rows, cols, parts, out, ld, plane);
+                       rows, cols, parts, out, ld, plane);
 }
 
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
                                   int64_t fill_to, hipStream_t stream) {
   return launch_kernel(checkpoint_load_kernel, dim3(pass_blocks(rows * ((fill_to + 7) / 8))), dim3(256), 0, stream, src,
-                       rows, cols, dtype, out, ld, aligned_rows(out, ld, dtype), fill_to);
+                       rows, cols, dtype, out, ld, fill_to);
 }
 
 hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
                                   const Packed8& out, hipStream_t stream) {
   return launch_kernel(checkpoint_save_kernel, dim3(pass_blocks(rows * ((cols + 31) / 32) * 2)), dim3(256), 0, stream,
-                       src, ld, dtype, aligned_rows(src, ld, dtype), rows, cols, out);
+                       src, ld, dtype, rows, cols, out);
 }
 
 hipError_t launch_layers_grad(const GradArgs& a, hipStream_t stream) {
@@ -268,10 +295,14 @@ hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, in
 }
 
 hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld, int splits, hipStream_t stream) {
-  const unsigned blocks = (unsigned)((end.rows * (part_ld / 16) + 255) / 256);
-  return end.halves == 2
-             ? launch_kernel(join_kernel<2>, dim3(blocks), dim3(256), 0, stream, end, part, part_ld, splits)
-             : launch_kernel(join_kernel<1>, dim3(blocks), dim3(256), 0, stream, end, part, part_ld, splits);
+  const int64_t units = end.rows * (part_ld / 16);
+  const int sub = splits >= 8 ? 8 : 1;
+  const int64_t blocks = (units + 256 / sub - 1) / (256 / sub);
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
+  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, end, part, part_ld, splits); };
+  if (end.halves == 2) return sub == 8 ? go(join_kernel<2, 8>) : go(join_kernel<2, 1>);
+  return sub == 8 ? go(join_kernel<1, 8>) : go(join_kernel<1, 1>);
 }
 
 }  // namespace pointid

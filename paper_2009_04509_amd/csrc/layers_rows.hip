@@ -20,7 +20,7 @@ struct RowsArgs {
 // A wave reads kRowsPer rows of 64 columns of the weights at a time, 16 bytes a lane; the
 // block's 4 waves take turns along the inner index.  The lanes of a column are added in a
 // fixed order at the end: lanes, then waves, then (elsewhere) splits.
-template <int kM, int kType, int kHalves, bool kVec>
+template <int kM, int kType, int kHalves>
 __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   constexpr int kCols = kType == POINTID_FP32 ? 4 : 8;                  // of a lane
   constexpr int kLanes = kStrip / kCols;
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
         const int k = base + u * kStep;
 #pragma unroll
         for (int h = 0; h < kHalves; ++h)
-          load_cols<kCols>(a.w[h].p, (k0 + k) * a.w[h].sk + col, kType, kVec,
+          load_cols<kCols>(a.w[h].p, (k0 + k) * a.w[h].sk + col, kType,
                            k < len ? n : 0, w[h][u]);
       }
 #pragma unroll
@@ -101,26 +101,21 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   finish<1>(a.end, live, row, col0 + unit * 16, v[0], v[kHalves - 1]);
 }
 
-template <int kM, int kHalves, int kType>
-hipError_t launch_vec(const RowsArgs& a, bool vec, dim3 grid, hipStream_t stream) {
-  return vec ? launch_kernel(rows_kernel<kM, kType, kHalves, true>, grid, dim3(256), 0, stream, a)
-             : launch_kernel(rows_kernel<kM, kType, kHalves, false>, grid, dim3(256), 0, stream, a);
-}
 template <int kM, int kHalves>
-hipError_t launch_type(const RowsArgs& a, bool vec, dim3 grid, hipStream_t stream) {
+hipError_t launch_type(const RowsArgs& a, dim3 grid, hipStream_t stream) {
   switch (a.w[0].dtype) {
-    case POINTID_FP32: return launch_vec<kM, kHalves, POINTID_FP32>(a, vec, grid, stream);
-    case POINTID_BF16: return launch_vec<kM, kHalves, POINTID_BF16>(a, vec, grid, stream);
+    case POINTID_FP32: return launch_kernel(rows_kernel<kM, POINTID_FP32, kHalves>, grid, dim3(256), 0, stream, a);
+    case POINTID_BF16: return launch_kernel(rows_kernel<kM, POINTID_BF16, kHalves>, grid, dim3(256), 0, stream, a);
   }
-  return launch_vec<kM, kHalves, POINTID_FP16>(a, vec, grid, stream);
+  return launch_kernel(rows_kernel<kM, POINTID_FP16, kHalves>, grid, dim3(256), 0, stream, a);
 }
 
 template <int kHalves>
-hipError_t launch_rows(const RowsArgs& a, bool vec, dim3 grid, hipStream_t stream) {
-  if (a.end.rows <= 1) return launch_type<1, kHalves>(a, vec, grid, stream);
-  if (a.end.rows <= 2) return launch_type<2, kHalves>(a, vec, grid, stream);
-  if (a.end.rows <= 4) return launch_type<4, kHalves>(a, vec, grid, stream);
-  return launch_type<8, kHalves>(a, vec, grid, stream);
+hipError_t launch_rows(const RowsArgs& a, dim3 grid, hipStream_t stream) {
+  if (a.end.rows <= 1) return launch_type<1, kHalves>(a, grid, stream);
+  if (a.end.rows <= 2) return launch_type<2, kHalves>(a, grid, stream);
+  if (a.end.rows <= 4) return launch_type<4, kHalves>(a, grid, stream);
+  return launch_type<8, kHalves>(a, grid, stream);
 }
 
 int64_t rows_per_split(int64_t inner, int splits) { return ((inner + splits - 1) / splits + 31) / 32 * 32; }
@@ -148,12 +143,8 @@ hipError_t launch_layers_rows(const Strided& x, const Strided* w, int64_t inner,
   a.inner = inner;
   a.per_split = rows_per_split(inner, splits);
   a.end = end;
-  bool vec = true;
-  for (int h = 0; h < end.halves; ++h)
-    vec = vec && (reinterpret_cast<uintptr_t>(a.w[h].p) & 15) == 0 &&
-          a.w[h].sk % (a.w[h].dtype == POINTID_FP32 ? 4 : 8) == 0;
   const dim3 grid((unsigned)((end.cols + kStrip - 1) / kStrip), (unsigned)splits);
-  return end.halves == 2 ? launch_rows<2>(a, vec, grid, stream) : launch_rows<1>(a, vec, grid, stream);
+  return end.halves == 2 ? launch_rows<2>(a, grid, stream) : launch_rows<1>(a, grid, stream);
 }
 
 }  // namespace pointid
