@@ -93,36 +93,41 @@ int few_rows_splits(int64_t inner, int64_t cols, int halves, int cus);
 hipError_t launch_layers_rows(const Strided& x, const Strided* w, int64_t inner, const End& end, int splits,
                               hipStream_t stream);
 
-// ---- layers_mm.h: products on the matrix cores, 16-bit operands.
+// ---- layers_mm.h: products on the matrix cores.
 enum Form { kForward = 0, kDx = 1, kDw = 2 };
 struct ProductArgs {
   Term term[kMaxTerms];
   int32_t terms;
   int32_t splits;
-  int64_t inner;
-  int64_t ld_left;             // elements; operands are 16-byte aligned, rows too
+  int32_t inner;
+  int64_t ld_left;             // elements; 16-bit operands are 16-byte aligned, rows too
   int64_t ld_right;
-  int32_t tiles_m, tiles_n;    // set by the launch
+  // set by the launch: tiles, how the blocks spread over the XCDs, stages a split
+  int32_t tiles_m, tiles_n;
+  int32_t xcd_each, xcd_more;
+  int32_t stages, split_each, split_more;
   End end;
 };
 // The tile of a launch and its splits of the sum.
-constexpr int kTiles = 3;
-constexpr int kTileM[kTiles] = {256, 128, 64}, kTileN[kTiles] = {256, 128, 128};
+constexpr int kTiles = 2, kTiles32 = 3;
+constexpr int kTileM[kTiles] = {256, 64}, kTileN[kTiles] = {256, 128};
+constexpr int kTileM32[kTiles32] = {256, 128, 64}, kTileN32[kTiles32] = {128, 128, 128};
 struct ProductPlan {
-  int tile;                    // index into kTileM, kTileN (columns of both halves)
+  int tile;                    // index into kTileM, kTileN (fp32: kTileM32, kTileN32; columns of both halves)
   int splits;
 };
-ProductPlan plan_product(Form form, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus);
+ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus);
 hipError_t launch_product_bf16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream);
 hipError_t launch_product_fp16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream);
+// fp32 operands (4-byte aligned), in three bf16 parts each
+hipError_t launch_product_f32(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream);
 // Partials of `splits` parts added in order, then `end`.
 hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld, int splits, hipStream_t stream);
 
 // ---- layers_pass.hip: passes over one matrix
-// 16-bit planes [rows][ld] of a matrix, zero past its columns: parts == 1 the values
-// (16-bit types, copied), parts == 3 an fp32 value as the sum of three bf16 values.
-hipError_t launch_layers_pack(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, int parts,
-                              uint16_t* out, int64_t ld, int64_t plane, hipStream_t stream);
+// A matrix copied to rows of `ld` values (a multiple of 8), zero past its columns.
+hipError_t launch_layers_copy(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, void* out,
+                              int64_t ld, hipStream_t stream);
 // A checkpoint's values as 16-bit (dtype) or fp32 values [rows][ld], zero past the columns up to ld.
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
                                   int64_t fill_to, hipStream_t stream);
@@ -132,14 +137,13 @@ hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, in
 // The gradient before the activation, and its column sums.
 //   dense: dz = dy act'(z) (z absent: dy)     gated: dg = dy u act'(g), du = dy act(g)
 // parts: 0 none written, 1 or 2 planes of the 16-bit type (2: value and remainder),
-// 3 bf16 planes, -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each
+// -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each
 // block of kGradRows rows, or nullptr.
 constexpr int kGradRows = 32;
 struct GradArgs {
   const void* dy;
   int64_t ld_dy;
   int32_t dtype;
-  int32_t type16;              // of the planes: POINTID_BF16 or POINTID_FP16
   int32_t act;
   int32_t halves;
   Kept z[2];                   // dense: z; gated: g, u

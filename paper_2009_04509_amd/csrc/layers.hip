@@ -172,7 +172,8 @@ class Call {
   bool scratch_ = false;
 };
 
-// A matrix as the products read it: 16-bit planes with aligned rows, zero past the columns.
+// A matrix as the products read it: 16-bit planes with aligned rows, zero past the columns
+// up to a whole piece of 8, or fp32 values.
 struct Planes {
   const void* base = nullptr;
   int64_t ld = 0, plane = 0;       // elements
@@ -180,54 +181,63 @@ struct Planes {
   const void* at(int part) const { return static_cast<const uint16_t*>(base) + part * plane; }
 };
 
+bool read_in_place(const void* p, int64_t ld, int dtype, int64_t cols) {
+  return ld <= kMaxPitch && (dtype == POINTID_FP32 || (cols % 8 == 0 && ld % 8 == 0 && aligned16(p)));
+}
+
 // An operand, and whether it is read in place or made by a pass into scratch.
 struct Source {
   Kept from;                       // a matrix, or a checkpoint
   int dtype;
   int64_t rows, cols;
   bool in_place = false;
-  uint16_t* made = nullptr;
+  void* made = nullptr;
   Planes planes;
 
-  void plan(const Kept& k, int type, int64_t r, int64_t c, Call& call) {
+  void plan(const Kept& k, int type, int64_t r, int64_t c, Call& call, bool copy = false) {
     from = k, dtype = type, rows = r, cols = c;
-    in_place = k.matrix && type != POINTID_FP32 && c % 8 == 0 && rows_in_16(k.matrix, k.ld, type) && k.ld <= kMaxPitch;
-    if (in_place) {
-      planes.base = k.matrix;
-      planes.ld = k.ld;
-      return;
-    }
+    in_place = !copy && k.matrix && read_in_place(k.matrix, k.ld, type, c);
+    planes.base = k.matrix;
+    planes.ld = k.ld;
+    if (in_place) return;
     planes.ld = round_up(c, 8);
-    planes.plane = r * planes.ld;
-    planes.parts = k.matrix && type == POINTID_FP32 ? 3 : 1;
-    call.want(&made, 2 * (size_t)planes.plane * planes.parts);
+    call.want(&made, (size_t)size_of(dtype) * r * planes.ld);
   }
   int make(Call& call) {
     if (in_place) return POINTID_OK;
     planes.base = made;
     if (!from.matrix)
       return call.run("layers_load", false, [&] {
-        return launch_checkpoint_load(from.packed, rows, cols, dtype == POINTID_FP16 ? POINTID_FP16 : POINTID_BF16, made,
-                                      planes.ld, planes.ld, call.stream());
+        return launch_checkpoint_load(from.packed, rows, cols, dtype, made, planes.ld, planes.ld, call.stream());
       });
-    return call.run("layers_pack", false, [&] {
-      return launch_layers_pack(from.matrix, from.ld, dtype, rows, cols, planes.parts, made, planes.ld, planes.plane,
-                                call.stream());
+    return call.run("layers_copy", false, [&] {
+      return launch_layers_copy(from.matrix, from.ld, dtype, rows, cols, made, planes.ld, call.stream());
     });
   }
 };
 
-// The products of the parts of left and right that count (orders up to that of the most
-// parts), the smallest first.
+// The weights of one or both halves: these share a pitch, so that where one is copied, so
+// is the other.
+void plan_weights(Source* s, const pointid_matrix* w, int halves, int dtype, int64_t k, int64_t n, Call& call) {
+  bool copy = false;
+  for (int h = 0; h < halves; ++h)
+    copy = copy || !read_in_place(w[h].data, w[h].ld, dtype, n) || w[h].ld != w[0].ld;
+  for (int h = 0; h < halves; ++h) {
+    Kept from;
+    std::memset(&from, 0, sizeof(from));
+    from.matrix = w[h].data, from.ld = w[h].ld;
+    s[h].plan(from, dtype, k, n, call, copy);
+  }
+}
+
+// The products of the parts of an operand with the other's one, the remainder's first.
 int add_terms(ProductArgs* a, const Planes& left, const Planes& right0, const Planes* right1) {
-  const int pl = left.parts, pr = right0.parts, most = (pl > pr ? pl : pr) - 1;
-  for (int order = most; order >= 0; --order)
-    for (int i = pl - 1; i >= 0; --i) {
-      const int j = order - i;
-      if (j < 0 || j >= pr) continue;
-      if (a->terms == kMaxTerms) return set_error(POINTID_EHIP, "too many terms");
-      a->term[a->terms++] = {left.at(i), right0.at(j), right1 ? right1->at(j) : nullptr};
-    }
+  const int parts = left.parts > right0.parts ? left.parts : right0.parts;
+  for (int p = parts - 1; p >= 0; --p) {
+    if (a->terms == kMaxTerms) return set_error(POINTID_EHIP, "too many terms");
+    const int i = left.parts > 1 ? p : 0, j = right0.parts > 1 ? p : 0;
+    a->term[a->terms++] = {left.at(i), right0.at(j), right1 ? right1->at(j) : nullptr};
+  }
   return POINTID_OK;
 }
 
@@ -243,8 +253,9 @@ int run_product(Call& call, Form form, const ProductPlan& plan, ProductArgs& a, 
     a.end.part = part;
   }
   int rc = call.run("layers_product", last && plan.splits == 1, [&] {
-    return dtype == POINTID_FP16 ? launch_product_fp16(form, plan, a, call.stream())
-                                 : launch_product_bf16(form, plan, a, call.stream());
+    return dtype == POINTID_FP32   ? launch_product_f32(form, plan, a, call.stream())
+           : dtype == POINTID_FP16 ? launch_product_fp16(form, plan, a, call.stream())
+                                   : launch_product_bf16(form, plan, a, call.stream());
   });
   if (rc != POINTID_OK || plan.splits == 1) return rc;
   return call.run("layers_join", last,
@@ -330,24 +341,8 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   std::memset(&from, 0, sizeof(from));
   from.matrix = f.x.data, from.ld = f.x.ld;
   sx.plan(from, f.dtype, f.m, f.k, call);
-  // the halves share a pitch: where one is copied, so is the other
-  bool copy = false;
-  for (int h = 0; h < f.halves; ++h)
-    copy = copy || f.dtype == POINTID_FP32 || f.n % 8 || !rows_in_16(f.w[h].data, f.w[h].ld, f.dtype) ||
-           f.w[h].ld > kMaxPitch || f.w[h].ld != f.w[0].ld;
-  for (int h = 0; h < f.halves; ++h) {
-    from.matrix = f.w[h].data, from.ld = f.w[h].ld;
-    sw[h].plan(from, f.dtype, f.k, f.n, call);
-    if (copy && sw[h].in_place) {
-      sw[h].in_place = false;
-      sw[h].planes = Planes();
-      sw[h].planes.ld = round_up(f.n, 8);
-      sw[h].planes.plane = f.k * sw[h].planes.ld;
-      call.want(&sw[h].made, 2 * (size_t)sw[h].planes.plane);
-    }
-  }
-  const int parts = sx.planes.parts == 3 ? 6 : 1;
-  const ProductPlan plan = plan_product(kForward, f.m, f.n, f.halves, f.k, parts, l->cus);
+  plan_weights(sw, f.w, f.halves, f.dtype, f.k, f.n, call);
+  const ProductPlan plan = plan_product(f.dtype == POINTID_FP32, f.m, f.n, f.halves, f.k, 1, l->cus);
   float* part = nullptr;
   call.want(&part, part_bytes(plan.splits, e));
   int rc = call.reserve();
@@ -358,7 +353,7 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   std::memset(&a, 0, sizeof(a));
   rc = add_terms(&a, sx.planes, sw[0].planes, f.halves == 2 ? &sw[1].planes : nullptr);
   if (rc != POINTID_OK) return rc;
-  a.inner = f.k;
+  a.inner = (int32_t)f.k;
   a.ld_left = sx.planes.ld;
   a.ld_right = sw[0].planes.ld;
   a.end = e;
@@ -399,8 +394,7 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   const bool products = want_dx || want_dw;
   // dz is dy itself where no activation changes it and the products can read it
   const bool plain = b.halves == 1 && b.act == POINTID_ACT_NONE;
-  const bool read_dy = plain && (simple || (b.dtype != POINTID_FP32 && b.n % 8 == 0 && b.dy.ld <= kMaxPitch &&
-                                            rows_in_16(b.dy.data, b.dy.ld, b.dtype)));
+  const bool read_dy = plain && (simple || read_in_place(b.dy.data, b.dy.ld, b.dtype, b.n));
   const bool exact16 = b.halves == 1 && (b.act == POINTID_ACT_NONE || b.act == POINTID_ACT_RELU);
 
   GradArgs g;
@@ -408,13 +402,15 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   g.dy = b.dy.data;
   g.ld_dy = b.dy.ld;
   g.dtype = b.dtype;
-  g.type16 = b.dtype == POINTID_FP16 ? POINTID_FP16 : POINTID_BF16;
   g.act = b.act;
   g.halves = b.halves;
   g.rows = b.m;
   g.cols = b.n;
   for (int h = 0; h < b.halves; ++h) g.z[h] = b.z[h];
-  g.parts = !products || read_dy ? 0 : simple ? -1 : b.dtype == POINTID_FP32 ? 3 : !exact16 && b.m * b.n <= kTwoPartValues ? 2 : 1;
+  g.parts = !products || read_dy                          ? 0
+            : simple || b.dtype == POINTID_FP32             ? -1
+            : !exact16 && b.m * b.n <= kTwoPartValues ? 2
+                                                            : 1;
   g.ld = round_up(b.n, 8);
   g.plane = b.m * g.ld;
   const size_t dz_bytes = g.parts < 0 ? 4 * (size_t)g.plane : 2 * (size_t)g.plane * g.parts;
@@ -425,26 +421,11 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   // x for dW, the weights for dx
   Source sx, sw[2];
   void* x8 = nullptr;                                  // a checkpoint's values for the plain kernel
-  Kept from;
-  std::memset(&from, 0, sizeof(from));
   if (simple) {
     if (want_dw && !b.x.matrix) call.want(&x8, (size_t)size_of(b.dtype) * b.m * b.k);
   } else {
     if (want_dw) sx.plan(b.x, b.dtype, b.m, b.k, call);
-    for (int h = 0; h < b.halves && want_dx; ++h) {
-      from.matrix = b.w[h].data, from.ld = b.w[h].ld;
-      sw[h].plan(from, b.dtype, b.k, b.n, call);
-    }
-    // the halves share a pitch: where one is copied, so is the other
-    if (want_dx && b.halves == 2 && sw[0].planes.ld != sw[1].planes.ld)
-      for (int h = 0; h < 2; ++h)
-        if (sw[h].in_place) {
-          sw[h].in_place = false;
-          sw[h].planes = Planes();
-          sw[h].planes.ld = round_up(b.n, 8);
-          sw[h].planes.plane = b.k * sw[h].planes.ld;
-          call.want(&sw[h].made, 2 * (size_t)sw[h].planes.plane);
-        }
+    if (want_dx) plan_weights(sw, b.w, b.halves, b.dtype, b.k, b.n, call);
   }
   End dx_end = end_of(kEndStore, POINTID_ACT_NONE, b.dtype, 1, b.m, b.k, b.dx, none);
   End dw_end = end_of(kEndStore, POINTID_ACT_NONE, b.dtype, b.halves, b.k, b.n, b.dw[0], b.dw[1]);
@@ -454,19 +435,12 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
     dz[h].plane = g.plane;
     dz[h].parts = read_dy || g.parts < 1 ? 1 : g.parts;
   }
-  auto count = [](int p, int q) {
-    int c = 0;
-    for (int i = 0; i < p; ++i)
-      for (int j = 0; j < q; ++j) c += i + j < (p > q ? p : q);
-    return c;
-  };
   ProductPlan dx_plan = {0, 1}, dw_plan = {0, 1};
   float* part = nullptr;
   if (!simple) {
-    if (want_dx)
-      dx_plan = plan_product(kDx, b.m, b.k, 1, b.n, b.halves * count(dz[0].parts, sw[0].planes.parts), l->cus);
-    if (want_dw)
-      dw_plan = plan_product(kDw, b.k, b.n, b.halves, b.m, count(sx.planes.parts, dz[0].parts), l->cus);
+    const bool f32 = b.dtype == POINTID_FP32;
+    if (want_dx) dx_plan = plan_product(f32, b.m, b.k, 1, b.n, b.halves * dz[0].parts, l->cus);
+    if (want_dw) dw_plan = plan_product(f32, b.k, b.n, b.halves, b.m, dz[0].parts, l->cus);
     const size_t p = part_bytes(dx_plan.splits, dx_end), q = part_bytes(dw_plan.splits, dw_end);
     call.want(&part, p > q ? p : q);                   // one after the other
   }
@@ -519,7 +493,7 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
     std::memset(&a, 0, sizeof(a));
     for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = add_terms(&a, dz[h], sw[h].planes, nullptr);
     if (rc != POINTID_OK) return rc;
-    a.inner = b.n;
+    a.inner = (int32_t)b.n;
     a.ld_left = dz[0].ld;
     a.ld_right = sw[0].planes.ld;
     a.end = dx_end;
@@ -533,7 +507,7 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   std::memset(&a, 0, sizeof(a));
   rc = add_terms(&a, sx.planes, dz[0], b.halves == 2 ? &dz[1] : nullptr);
   if (rc != POINTID_OK) return rc;
-  a.inner = b.m;
+  a.inner = (int32_t)b.m;
   a.ld_left = sx.planes.ld;
   a.ld_right = dz[0].ld;
   a.end = dw_end;

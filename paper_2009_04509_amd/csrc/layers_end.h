@@ -98,11 +98,11 @@ __device__ __forceinline__ float activate(int act, float z) {
   }
   return z;
 }
-__device__ __forceinline__ void activate16(int act, float* v) {
+__device__ __forceinline__ void activate8(int act, float* v) {
   static_for<5>([&](auto a) {                 // the choice outside of the loop
     if (a != POINTID_ACT_NONE && act == a)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = activate(a, v[i]);
+      for (int i = 0; i < 8; ++i) v[i] = activate(a, v[i]);
   });
 }
 // act(z), and the gradient d of it brought to z: d act'(z).  relu selects, so that an
@@ -164,122 +164,123 @@ __device__ __forceinline__ void unpack8(uint32_t w, int p, float* v) {       // 
   v[3] = __builtin_amdgcn_ldexpf(b[1], p);
 }
 
-// 8 or 16 codes of a row from column `col` (a multiple of kN), of which n exist.
-template <int kN>
+// 8 codes of a row from column `col` (a multiple of 8), of which cols - col exist.
 __device__ __forceinline__ void load_codes(const Packed8& s, int64_t row, int64_t col, int64_t cols, float* v) {
-  const int64_t at = row * cols + col;
   const int p = (int)s.exponents[row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8] - 127;
   const int64_t n = cols - col;
-  const uint8_t* c = s.codes + at;
-  uint32_t w[kN / 4];
-  if (n >= kN && (reinterpret_cast<uintptr_t>(c) & (kN - 1)) == 0) {
-    if constexpr (kN == 16) {
-      const uint4 u = *reinterpret_cast<const uint4*>(c);
-      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-    } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(c);
-      w[0] = u.x, w[1] = u.y;
-    }
+  const uint8_t* c = s.codes + row * cols + col;
+  uint32_t w[2] = {0, 0};
+  if (n >= 8) {
+    __builtin_memcpy(w, c, 8);
   } else {
 #pragma unroll
-    for (int i = 0; i < kN / 4; ++i) {
-      w[i] = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (4 * i + j < n) w[i] |= (uint32_t)c[4 * i + j] << (8 * j);
-    }
+    for (int i = 0; i < 8; ++i)
+      if (i < n) w[i / 4] |= (uint32_t)c[i] << (8 * (i % 4));
   }
-#pragma unroll
-  for (int i = 0; i < kN / 4; ++i) unpack8(w[i], p, v + 4 * i);
+  unpack8(w[0], p, v);
+  unpack8(w[1], p, v + 4);
 }
 
-// 16 values of a row from column `col` (a multiple of 16) to a checkpoint.  The lane
-// kPartner away (xor) holds the other half of the block of 32 and calls this too.
-// `live`: the row exists.  Columns past `cols` do not count and are not written.
-template <int kPartner>
+// 8 values of a row from column `col` (a multiple of 8) to a checkpoint.  The 4 lanes of
+// an aligned group hold a block of 32 and all call this.  `live`: the row and column
+// exist.  Columns past `cols` do not count and are not written.
 __device__ __forceinline__ void save_codes(const Packed8& d, bool live, int64_t row, int64_t col, int64_t cols,
                                            const float* v) {
   const int64_t n = cols - col;
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 8; ++i) {
     const uint32_t b = i < n ? finite_bits(v[i]) : 0u;
     top = b > top ? b : top;
   }
-  const uint32_t other = (uint32_t)__shfl_xor((int)top, kPartner, 64);
-  const int p = block_power(top > other ? top : other);
-  if (!live || n <= 0) return;
-  uint32_t w[4];
+  uint32_t other = (uint32_t)__shfl_xor((int)top, 1, 64);
+  top = other > top ? other : top;
+  other = (uint32_t)__shfl_xor((int)top, 2, 64);
+  top = other > top ? other : top;
+  const int p = block_power(top);
+  if (!live) return;
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 2; ++i)
     w[i] = pack8(scaled_for_8(v[4 * i], p), scaled_for_8(v[4 * i + 1], p), scaled_for_8(v[4 * i + 2], p),
                  scaled_for_8(v[4 * i + 3], p));
   uint8_t* c = d.codes + row * cols + col;
-  if (n >= 16 && (reinterpret_cast<uintptr_t>(c) & 15) == 0) {
-    *reinterpret_cast<uint4*>(c) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (n >= 8) {
+    __builtin_memcpy(c, w, 8);
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < 8; ++i)
       if (i < n) c[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
   }
   if (col % kBlock8 == 0)
     d.exponents[row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8] = (uint8_t)(127 - p);
 }
 
-template <int kPartner>
-__device__ __forceinline__ void keep_cols(const Kept& k, int dtype, bool live, int64_t row, int64_t col,
-                                          int64_t cols, const float* v) {
+__device__ __forceinline__ void keep_cols(int dtype, const Kept& k, bool live, int64_t row, int64_t col, int64_t cols,
+                                          const float* v) {
   if (k.matrix) {
-    if (live) store_cols<16>(k.matrix, row * k.ld + col, dtype, cols - col, v);
+    if (live) store_cols<8>(k.matrix, row * k.ld + col, dtype, cols - col, v);
   } else if (k.packed.codes) {
-    save_codes<kPartner>(k.packed, live, row, col, cols, v);
+    save_codes(k.packed, live, row, col, cols, v);
   }
 }
 
-__device__ __forceinline__ void add_bias(const float* bias, int64_t col, int64_t cols, float* v) {
-  if (!bias) return;
+__device__ __forceinline__ void add_bias(const float* bias, int64_t col, int64_t n, float* v) {
+  if (!bias || n <= 0) return;
+  float b[8];
+  load_cols<8>(bias, col, POINTID_FP32, n, b);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] += col + i < cols ? bias[col + i] : 0.f;
+  for (int i = 0; i < 8; ++i) v[i] += b[i];
 }
 
-// The end of 16 finished columns of a row (see End); v1: the second half's, with
-// e.halves == 2.  Every lane of the wave calls it; `live` is false past the rows.
-template <int kPartner>
-__device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int64_t col, float* v0, float* v1) {
+// The residual of 8 columns, if the end has one (finish adds it).
+__device__ __forceinline__ void load_residual(int dtype, const End& e, bool live, int64_t row, int64_t col, float* r) {
+  if (e.residual && live)
+    load_cols<8>(e.residual, row * e.ld_residual + col, dtype, e.cols - col, r);
+  else
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = 0.f;
+}
+
+// The end of 8 finished columns of a row (see End) from `col`, a multiple of 8; v1: the
+// second half's, with e.halves == 2; r: load_residual's.  The 4 lanes of an aligned group
+// hold 32 columns of one row, from a multiple of 32 on, and all call it; `live` is false
+// where the row or the columns do not exist.  dtype: the call's type (a constant where the
+// kernel knows it).
+__device__ __forceinline__ void finish(int dtype, const End& e, bool live, int64_t row, int64_t col, float* v0,
+                                       float* v1, const float* r) {
   const int64_t n = e.cols - col;
   if (e.mode == kEndStore) {
-    if (!live || n <= 0) return;
-    store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, n, v0);
-    if (e.halves == 2) store_cols<16>(e.y1, row * e.ld1 + col, e.dtype, n, v1);
+    if (!live) return;
+    store_cols<8>(e.y0, row * e.ld0 + col, dtype, n, v0);
+    if (e.halves == 2) store_cols<8>(e.y1, row * e.ld1 + col, dtype, n, v1);
     return;
   }
-  add_bias(e.bias0, col, e.cols, v0);
-  keep_cols<kPartner>(e.keep0, e.dtype, live && n > 0, row, col, e.cols, v0);
+  add_bias(e.bias0, col, n, v0);
+  keep_cols(dtype, e.keep0, live, row, col, e.cols, v0);
   if (e.mode == kEndGated) {
-    add_bias(e.bias1, col, e.cols, v1);
-    keep_cols<kPartner>(e.keep1, e.dtype, live && n > 0, row, col, e.cols, v1);
+    add_bias(e.bias1, col, n, v1);
+    keep_cols(dtype, e.keep1, live, row, col, e.cols, v1);
   }
-  if (!live || n <= 0) return;
-  activate16(e.act, v0);
+  if (!live) return;
+  activate8(e.act, v0);
   if (e.mode == kEndGated) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v0[i] *= v1[i];
+    for (int i = 0; i < 8; ++i) v0[i] *= v1[i];
   } else if (e.residual) {
-    float r[16];
-    load_cols<16>(e.residual, row * e.ld_residual + col, e.dtype, n, r);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v0[i] += r[i];
+    for (int i = 0; i < 8; ++i) v0[i] += r[i];
   }
-  store_cols<16>(e.y0, row * e.ld0 + col, e.dtype, n, v0);
+  store_cols<8>(e.y0, row * e.ld0 + col, dtype, n, v0);
 }
 
-// 16 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)
+// 8 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)
 __device__ __forceinline__ void store_partial(const End& e, int split, int half, bool live, int64_t row, int64_t col,
                                               const float* v) {
   if (!live || col >= e.part_ld) return;
   float4* p = reinterpret_cast<float4*>(e.part + (((int64_t)split * e.halves + half) * e.rows + row) * e.part_ld + col);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) p[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  p[0] = make_float4(v[0], v[1], v[2], v[3]);
+  p[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
 }  // namespace pointid

@@ -8,13 +8,14 @@
 // indexed by the inner index (W of the forward form, both of dW) with the transposing
 // read, 4 x 16 values at a time, so no form needs a transposed copy of anything.
 //
-// The results come out with the right operand as the MFMA's first, so a lane holds one
-// row's columns: after a swap of halves 16 consecutive ones, and a lane and the one 32
-// away a whole block of 32 for the 8-bit checkpoint.
+// The results come out with the right operand as the MFMA's first, so a lane holds 4
+// consecutive columns of one row at a time; the end passes them through shared memory to
+// where 8 lanes hold 64 columns of a row (two halves: 4 lanes 32 columns of both).
 //
 // Pieces of 16 bytes stand in shared memory in a permuted order that the loads apply to
 // their global addresses.  Rows of 64 inner indices (128 bytes): piece p of row r at
-// p ^ (r / 2 % 8), so that 16 lanes reading one piece of 16 rows touch all banks.  Rows of
+// p ^ (r / 2 % 8), so that 16 lanes reading one piece of 16 rows touch all banks (rows of
+// 32 inner indices, in the fp32 kernel: p ^ (r / 4 % 4)).  Rows of
 // columns: the 64-byte group g of row r at g ^ (r % 4) (rows of 128 bytes: g ^ (r / 2 % 2)),
 // so that the 4 rows of a transposing read do.
 #pragma once
@@ -35,7 +36,7 @@ constexpr uint32_t kNowhere = 0x80000000u;  // an offset past the resource's ran
 // The piece's place in a row of kPieces pieces of 16 bytes; kInner: rows along the inner index.
 template <bool kInner, int kPieces>
 __device__ __forceinline__ int place(int row, int piece) {
-  if constexpr (kInner) return piece ^ ((row >> 1) & 7);
+  if constexpr (kInner) return kPieces == 8 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3);
   if constexpr (kPieces >= 16) return piece ^ ((row & 3) << 2);
   return piece ^ (((row >> 1) & 1) << 2);
 }
@@ -80,41 +81,43 @@ struct Tile {
       offset[i] = side0 + side < sides ? (uint32_t)((row * ld + piece * 8) * 2) : kNowhere;
     }
   }
-  // The stage from inner index k0 of `inners` on; `origin` points at (side0, 0).
-  __device__ __forceinline__ void load(const char* origin, int64_t k0, int64_t inners, int64_t ld, uint32_t lds,
-                                       int wave) const {
-    const intx4 r = resource(origin + (kInner ? k0 : k0 * ld) * 2);
-    const int left = inners - k0 < kBK ? (int)(inners - k0) : kBK;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      load_to_lds(r, inner[i] < left ? offset[i] : kNowhere, lds + (i * kThreads + wave * 64) * 16);
+  // Load i of the stage at `from`, `left` inner indices of it there.
+  __device__ __forceinline__ void load(int i, intx4 from, int left, uint32_t lds, int wave) const {
+    load_to_lds(from, inner[i] < left ? offset[i] : kNowhere, lds + (i * kThreads + wave * 64) * 16);
   }
 };
 
 // Fragments: 8 consecutive inner indices of one row or column a lane (lane % 32; lanes of
-// 32 and more the next 8), for kFrags groups of 32 rows or columns from side0 on.
-template <bool kInner, int kSide, int kFrags>
+// 32 and more the next 8).  kInner: group i of 32 stands i * 32 rows on; else each group
+// has an address of its own.
+template <bool kInner, int kSide, int kFrags, int kInners = kBK>
 struct Frags {
-  int base[kInner ? 4 : kFrags];
-  __device__ __forceinline__ void init(int lane, int side0) {
+  static constexpr int kSteps = kInners / 16, kRow = kInners * 2;
+  int base[kInner ? kSteps : kFrags];
+  // of group i: its first row or column, and the offset of its tile
+  template <class F>
+  __device__ __forceinline__ void init(int lane, F&& side0) {
     if constexpr (kInner) {
-      const int row = side0 + lane % 32;
+      int tile;
+      const int row = side0(0, &tile) + lane % 32;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) base[s] = row * 128 + place<true, 8>(row, 2 * s + lane / 32) * 16;
+      for (int s = 0; s < kSteps; ++s)
+        base[s] = tile + row * kRow + place<true, kInners / 8>(row, 2 * s + lane / 32) * 16;
     } else {
       // the lane's address in a read of 4 rows x 16 columns by 16 lanes
       const int row = lane / 32 * 8 + lane % 16 / 4;
 #pragma unroll
       for (int i = 0; i < kFrags; ++i) {
-        const int col = side0 + 32 * i + lane / 16 % 2 * 16 + lane % 4 * 4;
-        base[i] = row * (kSide * 2) + place<false, kSide / 8>(row, col / 8) * 16 + col % 8 * 2;
+        int tile;
+        const int col = side0(i, &tile) + lane / 16 % 2 * 16 + lane % 4 * 4;
+        base[i] = tile + row * (kSide * 2) + place<false, kSide / 8>(row, col / 8) * 16 + col % 8 * 2;
       }
     }
   }
   // inner indices 16 s .. 16 s + 15 of group i
   __device__ __forceinline__ uint4 read(const char* tile, int i, int s) const {
     if constexpr (kInner) {
-      return *reinterpret_cast<const uint4*>(tile + base[s] + i * 32 * 128);
+      return *reinterpret_cast<const uint4*>(tile + base[s] + i * 32 * kRow);
     } else {
       typedef __attribute__((address_space(3))) shortx4 LdsShort4;
       const char* p = tile + base[i] + s * 16 * kSide * 2;
@@ -134,55 +137,110 @@ __device__ __forceinline__ floatx16 mfma(const uint4& a, const uint4& b, const f
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// A lane's 16 sums of a 32 x 32 result (columns 8 j + 4 (lane / 32) + t of row lane % 32) ->
-// columns 16 (lane / 32) .. + 15 of that row.
-__device__ __forceinline__ void consecutive(const floatx16& c, float* v) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[4 * j + t]), __float_as_uint(c[4 * j + 8 + t]),
-                                                      false, false);
-      v[8 * j + t] = __uint_as_float(q[0]);
-      v[8 * j + 4 + t] = __uint_as_float(q[1]);
-    }
-}
-
 // All loads to shared memory of this wave done, then the block's barrier.
 __device__ __forceinline__ void stage_ready() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The block's tile and split.
+struct Place {
+  uint32_t split;
+  int64_t tm, tn;
+};
+__device__ __forceinline__ Place block_place(const ProductArgs& a) {
+  // Blocks go to the 8 XCDs in turn: each XCD takes a contiguous stretch of the tiles, in
+  // groups of 8 rows of tiles walked column by column, so that the blocks which run
+  // together on an XCD share operands in its L2.
+  const uint32_t xcd = blockIdx.x % 8;
+  uint32_t id = xcd * a.xcd_each + (xcd < (uint32_t)a.xcd_more ? xcd : a.xcd_more) + blockIdx.x / 8;
+  uint32_t split = 0;
+  if (a.splits > 1) {
+    const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n;
+    split = id / tiles;
+    id -= split * tiles;
+  }
+  constexpr uint32_t kGroup = 8;
+  const uint32_t group = id / (kGroup * a.tiles_n), in = id - group * kGroup * a.tiles_n;
+  const uint32_t rows_here = a.tiles_m - group * kGroup < kGroup ? a.tiles_m - group * kGroup : kGroup;
+  const uint32_t tn = in / rows_here;
+  return {split, group * kGroup + (in - tn * rows_here), tn};
+}
+
+// The end of a wave's results: rows from `row0` of kFragsM groups of 32, columns from `col0`
+// (of each half).  One copy of the end's code: 32 rows x 64 columns a turn (two halves: 32
+// columns of each) through the wave's kEndWave bytes of shared memory, from a lane's 4
+// columns of one row to 16 bytes and more a lane along the rows.
+constexpr int kEndPitch = 64 + 4;
+constexpr int kEndWave = 32 * kEndPitch * 4;
+template <int kType, int kHalves, int kFragsM, int kFragsN>
+__device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFragsM][kFragsN], float* es, int lane,
+                                         int split, int64_t row0, int64_t col0) {
+  constexpr int kPairs = kFragsN / 2, kTurns = kFragsM * kPairs;
+  constexpr int kLanes = kHalves == 2 ? 4 : 8;           // of a row
+#pragma nounroll
+  for (int turn = 0; turn < kTurns; ++turn) {
+    floatx16 c[2] = {};
+    static_for<kTurns>([&](auto t) {
+      constexpr int i = t / kPairs, pair = t % kPairs;
+      if (turn == t) {
+        c[0] = acc[i][kHalves == 2 ? pair : 2 * pair];
+        c[1] = acc[i][kHalves == 2 ? pair + kPairs : 2 * pair + 1];
+      }
+    });
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(es + lane % 32 * kEndPitch + f * 32 + 8 * j + lane / 32 * 4) =
+            make_float4(c[f][4 * j], c[f][4 * j + 1], c[f][4 * j + 2], c[f][4 * j + 3]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int64_t col = col0 + turn % kPairs * (kHalves == 2 ? 32 : 64) + lane % kLanes * 8;
+    const bool live_col = col < e.cols;
+    int64_t row = row0 + 32 * (turn / kPairs) + lane / kLanes;
+    const float* at = es + lane / kLanes * kEndPitch + lane % kLanes * 8;
+    constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes;
+    float res[8], next[8];
+    load_residual(kType, e, live_col && row < e.rows, row, col, next);
+#pragma nounroll
+    for (int s = 0; s < kSteps; ++s, row += kRows, at += kRows * kEndPitch) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) res[i] = next[i];
+      if (s + 1 < kSteps) load_residual(kType, e, live_col && row + kRows < e.rows, row + kRows, col, next);
+      float v[kHalves][8];
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], at + h * 32, 32);
+      if (e.mode == kEndPartial) {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) store_partial(e, split, h, row < e.rows, row, col, v[h]);
+      } else {
+        finish(kType, e, live_col && row < e.rows, row, col, v[0], v[kHalves - 1], res);
+      }
+    }
+  }
+}
+
 template <bool kFp16, int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>
 __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) {
   constexpr int kThreads = 64 * kWM * kWN;
+  constexpr int kType = kFp16 ? POINTID_FP16 : POINTID_BF16;
   constexpr bool kLeftInner = kForm != kDw, kRightInner = kForm == kDx;
+  static_assert(!kRightInner || kHalves == 1, "dx has one half");
   constexpr int kHN = kBN / 2;                           // columns of each half of the tile
-  constexpr int kFragsM = kBM / kWM / 32;
-  static_assert(kHN / kWN == 32, "a wave takes 32 columns of each half");
+  constexpr int kFragsM = kBM / kWM / 32, kFragsN = kBN / kWN / 32;
   using Left = Tile<kLeftInner, kBM, kThreads>;
   using Right = Tile<kRightInner, kHN, kThreads>;
   constexpr int kStage = Left::kBytes + 2 * Right::kBytes;
+  static_assert(kWM * kWN * kEndWave <= 2 * kStage, "the end fits where the stages were");
   __shared__ __align__(1024) char smem[2 * kStage];
 
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = wave / kWN, wn = wave % kWN;
 
-  // Blocks go to the 8 XCDs in turn: each XCD takes a contiguous stretch of the tiles, in
-  // groups of 8 rows of tiles walked column by column, so that the blocks which run
-  // together on an XCD share operands in its L2.
-  const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
-  const int64_t all = tiles * a.splits;
-  const int64_t each = all / 8, more = all % 8, xcd = blockIdx.x % 8;
-  int64_t id = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
-  const int split = (int)(id / tiles);
-  id -= split * tiles;
-  constexpr int kGroup = 8;
-  const int64_t group = id / ((int64_t)kGroup * a.tiles_n), in = id - group * kGroup * a.tiles_n;
-  const int64_t rows_here = a.tiles_m - group * kGroup < kGroup ? a.tiles_m - group * kGroup : kGroup;
-  const int64_t tm = group * kGroup + in % rows_here, tn = in / rows_here;
-
+  const Place at = block_place(a);
+  const uint32_t split = at.split;
+  const int64_t tm = at.tm, tn = at.tn;
   const int64_t row0 = tm * kBM;
   const int64_t col0 = tn * (kHalves == 2 ? kHN : kBN), col1 = kHalves == 2 ? col0 : col0 + kHN;
   Left left;
@@ -190,101 +248,146 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   left.init(tid, row0, a.end.rows, a.ld_left);
   right0.init(tid, col0, a.end.cols, a.ld_right);
   right1.init(tid, col1, a.end.cols, a.ld_right);
+  // A wave's columns: with two halves kFragsN / 2 groups of 32 of each; with one, kFragsN
+  // groups side by side (they lie in one half of the tile).
   Frags<kLeftInner, kBM, kFragsM> lf;
-  Frags<kRightInner, kHN, 1> rf;
-  lf.init(lane, wm * (kBM / kWM));
-  rf.init(lane, wn * 32);
+  Frags<kRightInner, kHN, kFragsN> rf;
+  lf.init(lane, [&](int i, int* tile) {
+    *tile = 0;
+    return wm * (kBM / kWM) + 32 * i;
+  });
+  rf.init(lane, [&](int i, int* tile) {
+    const int half = kHalves == 2 ? i / (kFragsN / 2) : wn * 32 * kFragsN / kHN;
+    *tile = Left::kBytes + half * Right::kBytes;
+    return kHalves == 2 ? wn * (kHN / kWN) + i % (kFragsN / 2) * 32 : wn * 32 * kFragsN % kHN + 32 * i;
+  });
 
-  const int64_t its = (a.inner + kBK - 1) / kBK, total = its * a.terms;
-  int64_t it = total * split / a.splits;
-  const int64_t end = total * (split + 1) / a.splits;
-  int term = (int)(it / its);
-  int64_t k0 = (it - term * its) * kBK;
+  // the split's stages, and where the next one to load is
+  int to_load = a.split_each + (split < (uint32_t)a.split_more);
+  const uint32_t first = split * a.split_each + (split < (uint32_t)a.split_more ? split : a.split_more);
+  int term = 0;
+  if (a.splits > 1) term = (int)(first / (uint32_t)a.stages);
+  int k0 = (int)(first - (uint32_t)term * a.stages) * kBK;
+  const int stages = to_load;
+  const int64_t left_step = (kLeftInner ? kBK : kBK * a.ld_left) * 2;
+  const int64_t right_step = (kRightInner ? kBK : kBK * a.ld_right) * 2;
   const int64_t left_at = (kLeftInner ? row0 * a.ld_left : row0) * 2;
   const int64_t right_at0 = (kRightInner ? col0 * a.ld_right : col0) * 2;
   const int64_t right_at1 = (kRightInner ? col1 * a.ld_right : col1) * 2;
+  const char *lp, *rp0, *rp1;
+  auto enter = [&](int k) {
+    const Term& t = a.term[term];
+    const int64_t s = k / kBK;
+    lp = static_cast<const char*>(t.left) + left_at + s * left_step;
+    rp0 = static_cast<const char*>(t.right0) + right_at0 + s * right_step;
+    rp1 = static_cast<const char*>(kHalves == 2 ? t.right1 : t.right0) + right_at1 + s * right_step;
+  };
+  enter(k0);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
-  auto issue = [&](int stage) {
-    const uint32_t at = lds0 + stage * kStage;
-    const Term& t = a.term[term];
-    left.load(static_cast<const char*>(t.left) + left_at, k0, a.inner, a.ld_left, at, wave);
-    right0.load(static_cast<const char*>(t.right0) + right_at0, k0, a.inner, a.ld_right, at + Left::kBytes, wave);
-    right1.load(static_cast<const char*>(kHalves == 2 ? t.right1 : t.right0) + right_at1, k0, a.inner, a.ld_right,
-                at + Left::kBytes + Right::kBytes, wave);
-    k0 += kBK;
-    if (k0 >= a.inner) k0 = 0, ++term;
-  };
-
-  floatx16 acc[kFragsM][2] = {};
-  auto compute = [&](int stage) {
-    const char* tl = smem + stage * kStage;
-    const char* t0 = tl + Left::kBytes;
-    const char* t1 = t0 + Right::kBytes;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const uint4 r0 = rf.read(t0, 0, s), r1 = rf.read(t1, 0, s);
-#pragma unroll
-      for (int i = 0; i < kFragsM; ++i) {
-        const uint4 l = lf.read(tl, i, s);
-        acc[i][0] = mfma<kFp16>(r0, l, acc[i][0]);
-        acc[i][1] = mfma<kFp16>(r1, l, acc[i][1]);
-      }
-    }
-  };
-
-  int stage = 0;
-  if (it < end) {
-    issue(0);
-    stage_ready();
-    for (; it + 1 < end; ++it) {
-      issue(stage ^ 1);
-      compute(stage);
-      stage_ready();
-      stage ^= 1;
-    }
-    compute(stage);
-  }
-
-  // One copy of the end's code: the sums of each turn are moved to where it takes them from.
-  constexpr int kTurns = kHalves == 2 ? kFragsM : 2 * kFragsM;
-#pragma nounroll
-  for (int turn = 0; turn < kTurns; ++turn) {
-    floatx16 c0 = {}, c1 = {};
-    static_for<kTurns>([&](auto t) {
-      if (turn == t) {
-        c0 = acc[kHalves == 2 ? t : t / 2][kHalves == 2 ? 0 : t % 2];
-        if constexpr (kHalves == 2) c1 = acc[t][1];
+  // part q of kFragsM of the loads of the next stage (a compile-time constant)
+  auto issue = [&](auto q, int stage) {
+    constexpr int kLoads = Left::kLoads + 2 * Right::kLoads;
+    const uint32_t to = lds0 + stage * kStage;
+    const int left_of = a.inner - k0;
+    static_for<kLoads>([&](auto n) {
+      if constexpr (n * kFragsM / kLoads == q) {
+        if constexpr (n < Left::kLoads)
+          left.load(n, resource(lp), left_of, to, wave);
+        else if constexpr (n < Left::kLoads + Right::kLoads)
+          right0.load(n - Left::kLoads, resource(rp0), left_of, to + Left::kBytes, wave);
+        else
+          right1.load(n - Left::kLoads - Right::kLoads, resource(rp1), left_of, to + Left::kBytes + Right::kBytes, wave);
       }
     });
-    const int64_t row = row0 + wm * (kBM / kWM) + 32 * (kHalves == 2 ? turn : turn / 2) + lane % 32;
-    const int64_t col = (kHalves == 2 || turn % 2 == 0 ? col0 : col1) + wn * 32 + lane / 32 * 16;
-    const bool live = row < a.end.rows;
-    float v[kHalves][16];
-    consecutive(c0, v[0]);
-    if constexpr (kHalves == 2) consecutive(c1, v[1]);
-    if (a.end.mode == kEndPartial) {
+    if constexpr (q == kFragsM - 1) {
+      k0 += kBK;
+      lp += left_step, rp0 += right_step, rp1 += right_step;
+      if (k0 >= a.inner && --to_load > 0) {
+        k0 = 0;
+        ++term;
+        enter(0);
+      } else if (k0 < a.inner) {
+        --to_load;
+      }
+    }
+  };
+
+  // Fragments of one step of 16 inner indices are read while the step before multiplies.
+  // The stage's last step multiplies after the barrier that makes the next stage ready and
+  // this one free, so that the next stage's first fragments and the loads of the stage after
+  // it are under way meanwhile.
+  floatx16 acc[kFragsM][kFragsN] = {};
+  uint4 l[2][kFragsM], r[2][kFragsN];
+  auto read = [&](int buf, const char* tile, int s) {
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) store_partial(a.end, split, h, live, row, col, v[h]);
-    } else {
-      finish<32>(a.end, live, row, col, v[0], v[kHalves - 1]);
+    for (int j = 0; j < kFragsN; ++j) r[buf][j] = rf.read(tile, j, s);
+#pragma unroll
+    for (int i = 0; i < kFragsM; ++i) l[buf][i] = lf.read(tile, i, s);
+  };
+  auto multiply_row = [&](int buf, int i) {
+#pragma unroll
+    for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<kFp16>(r[buf][j], l[buf][i], acc[i][j]);
+  };
+  if (stages > 0) {
+    static_for<kFragsM>([&](auto q) { issue(q, 0); });
+    stage_ready();
+    if (to_load > 0) static_for<kFragsM>([&](auto q) { issue(q, 1); });
+    read(0, smem, 0);
+    int stage = 0;
+    for (int it = stages; it > 0; --it, stage ^= 1) {
+      const char* tile = smem + stage * kStage;
+#pragma unroll
+      for (int s = 0; s < 3; ++s) {
+        read((s + 1) % 2, tile, s + 1);
+#pragma unroll
+        for (int i = 0; i < kFragsM; ++i) multiply_row(s % 2, i);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      stage_ready();
+      if (it > 1) read(0, smem + (stage ^ 1) * kStage, 0);
+      const bool more = to_load > 0;
+      static_for<kFragsM>([&](auto q) {
+        __builtin_amdgcn_sched_barrier(0);
+        multiply_row(1, q);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) issue(q, stage);
+      });
     }
   }
+  stage_ready();                                         // the stages are free for the end
+
+  end_tile<kType, kHalves, kFragsM, kFragsN>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4, lane, split,
+                                             row0 + wm * (kBM / kWM),
+                                             col0 + wn * (kHalves == 2 ? kHN / kWN : 32 * kFragsN));
+}
+
+// What a launch works out for its blocks; returns their number, or 0.
+inline int64_t spread(ProductArgs& a, int64_t rows, int64_t cols, int inners) {
+  const int64_t tm = (a.end.rows + rows - 1) / rows, tn = (a.end.cols + cols - 1) / cols;
+  if (tm < 1 || tn < 1 || a.splits < 1 || a.terms < 1 || tm > INT32_MAX / tn || tm * tn > INT32_MAX / a.splits) return 0;
+  a.tiles_m = (int32_t)tm;
+  a.tiles_n = (int32_t)tn;
+  const int64_t blocks = tm * tn * a.splits;
+  a.xcd_each = (int32_t)(blocks / 8);
+  a.xcd_more = (int32_t)(blocks % 8);
+  a.stages = (int32_t)(((int64_t)a.inner + inners - 1) / inners);
+  const int64_t total = (int64_t)a.stages * a.terms;
+  a.split_each = (int32_t)(total / a.splits);
+  a.split_more = (int32_t)(total % a.splits);
+  return blocks;
 }
 
 // The tile shapes, by ProductPlan::tile.
 template <bool kFp16, int kForm, int kHalves>
 hipError_t launch_tile(int tile, ProductArgs& a, hipStream_t stream) {
   const int bm = kTileM[tile], bn = kTileN[tile] / (kHalves == 2 ? 2 : 1);
-  a.tiles_m = (int32_t)((a.end.rows + bm - 1) / bm);
-  a.tiles_n = (int32_t)((a.end.cols + bn - 1) / bn);
-  const int64_t blocks = (int64_t)a.tiles_m * a.tiles_n * a.splits;
-  if (blocks < 1 || blocks > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t blocks = spread(a, bm, bn, kBK);
+  if (blocks < 1 || a.end.dtype != (kFp16 ? POINTID_FP16 : POINTID_BF16)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   switch (tile) {
     case 0: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 256, 256, 2, 4>, grid, dim3(512), 0, stream, a);
-    case 1: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 128, 128, 2, 2>, grid, dim3(256), 0, stream, a);
-    case 2: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+    case 1: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
   }
   return hipErrorInvalidValue;
 }

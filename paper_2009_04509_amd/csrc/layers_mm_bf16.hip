@@ -2,23 +2,48 @@
 // choice of their tiles and splits.
 #include "layers_mm.h"
 
+#include <algorithm>
+#include <cmath>
+
 namespace pointid {
 
-ProductPlan plan_product(Form form, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
-  ProductPlan p;
-  const int64_t its = (inner + mm::kBK - 1) / mm::kBK * terms;
-  auto tiles = [&](int t) {
-    const int64_t n = kTileN[t] / halves;
-    return ((rows + kTileM[t] - 1) / kTileM[t]) * ((cols + n - 1) / n);
-  };
-  p.tile = 0;
-  while (p.tile < kTiles - 1 && tiles(p.tile) < cus) ++p.tile;
-  // fewer tiles than CUs: the sum is split, each part at least 4 stages long
-  const int64_t t = tiles(p.tile);
-  int64_t s = t < cus ? cus / t : 1;
-  if (s > its / 4) s = its / 4;
-  p.splits = (int)(s < 1 ? 1 : s);
-  return p;
+namespace {
+
+// us of a tile shape, fitted to sweeps of tiles and splits over 20 sizes from 16 x 8192 x
+// 8192 to 4096^3 (the fit chose the fastest or one within 6 %): a stage of 64 inner indices
+// when `resident` blocks share a CU (each) and of a block alone, and a block's start and end.
+struct TileCost {
+  double stage, alone, ends;
+  int resident;
+};
+constexpr TileCost kCost[kTiles] = {{1.45, 1.45, 7.3, 1}, {0.27, 0.405, 3.0, 3}};
+constexpr TileCost kCost32[kTiles32] = {{4.47, 4.47, 2.5, 1}, {2.9, 2.9, 2.0, 1}, {1.56, 2.5, 1.9, 2}};
+
+}  // namespace
+
+// The tile and split that the costs above put first.  Large tiles read their operands
+// fewer times (4096 x 4096 x 1024 in 256 x 256 tiles 41 us, in 64 x 128 ones 53); small
+// ones fill the CUs where there are few (2048^3: 29 against 44 in split large tiles).
+ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
+  static constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+  const double stages = (double)((inner + 63) / 64) * terms;
+  const double part_mb = 8e-6 * (double)rows * (double)cols * halves;          // written and read
+  ProductPlan best = {0, 1};
+  double least = 1e300;
+  for (int t = 0; t < (f32 ? kTiles32 : kTiles); ++t) {
+    const TileCost& c = f32 ? kCost32[t] : kCost[t];
+    const int64_t bm = f32 ? kTileM32[t] : kTileM[t], bn = (f32 ? kTileN32[t] : kTileN[t]) / halves;
+    const double tiles = (double)((rows + bm - 1) / bm) * (double)((cols + bn - 1) / bn);
+    for (int s : kSplits) {
+      if (s > 1 && (2 * s > stages || tiles * s > 8.0 * cus)) break;
+      const double per = std::ceil(stages / s), blocks = std::ceil(tiles * s / cus);
+      const double rounds = std::ceil(blocks / c.resident);
+      double us = std::max(blocks * c.stage, rounds * c.alone) * per + rounds * c.ends;
+      if (s > 1) us += f32 ? 2.1 + 0.2 * part_mb * s : 4.6 + 0.13 * part_mb * s;
+      if (us < least) least = us, best = {t, s};
+    }
+  }
+  return best;
 }
 
 hipError_t launch_product_bf16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream) {

@@ -1,0 +1,230 @@
+// The matrix-core products of fp32 operands: every value is the sum of three bf16 values
+// (its rounding, the remainder's rounding, and the rest: 8 + 8 + 8 bits), and a product is
+// the 6 products of parts whose orders add up to less than 3, the smallest first; what is
+// left out is below 2^-26 of a product.
+//
+// Values are read as fp32, 32 inner indices at a time, while the stage before multiplies,
+// cut in registers and written to shared memory as three planes laid out as in the 16-bit
+// kernels (layers_mm.h); two stages.  A stage's 6 products share its fragments, so they
+// read half of what 6 passes over 16-bit planes would, and no pass lays planes out first.
+#include "layers_mm.h"
+
+namespace pointid {
+namespace mm {
+namespace {
+
+constexpr int kBK32 = 32;                   // inner indices of a stage
+
+// One operand's tile: kInner: [kSide][32], else [32][kSide].  A thread reads 4 values at a
+// time along the rows.
+template <bool kInner, int kSide, int kThreads>
+struct Tile32 {
+  static constexpr int kPieces = kInner ? kBK32 / 4 : kSide / 4;     // of 4 values, of a row
+  static constexpr int kRows = kInner ? kSide : kBK32;
+  static constexpr int kPlane = kSide * kBK32 * 2;
+  static constexpr int kLoads = kRows * kPieces / kThreads;
+  static_assert(kLoads * kThreads == kRows * kPieces, "whole loads");
+
+  uint32_t offset[kLoads];                  // of the thread's values from the tile's origin
+  uint16_t to[kLoads];                      // where their parts go in a plane
+  int16_t inner[kLoads];                    // the first's inner index
+  int16_t count[kLoads];                    // kInner: 4, or 0 past the rows; else columns that exist
+
+  __device__ __forceinline__ void init(int tid, int64_t side0, int64_t sides, int64_t ld) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = i * kThreads + tid, row = at / kPieces, piece = at % kPieces;
+      const int64_t side = side0 + (kInner ? row : piece * 4);
+      inner[i] = (int16_t)(kInner ? piece * 4 : row);
+      offset[i] = (uint32_t)((row * ld + piece * 4) * 4);
+      const int64_t n = sides - side;
+      count[i] = (int16_t)(n <= 0 ? 0 : kInner || n > 4 ? 4 : n);
+      const int pitch = kInner ? kBK32 * 2 : kSide * 2;
+      to[i] = (uint16_t)(row * pitch + place<kInner, kInner ? kBK32 / 8 : kSide / 8>(row, piece / 2) * 16 + piece % 2 * 8);
+    }
+  }
+  // whole: every group of 4 values exists as a whole or not at all
+  __device__ __forceinline__ void load(const char* origin, int left, bool whole, float4 (&v)[kLoads]) const {
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(origin), (short)0, (int)kNowhere, 0x00020000);
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        v[i] = __builtin_bit_cast(
+            float4, __builtin_amdgcn_raw_buffer_load_b128(r, count[i] && inner[i] < left ? offset[i] : kNowhere, 0, 0));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      float f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool there = kInner ? count[i] && inner[i] + j < left : j < count[i] && inner[i] < left;
+        f[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, there ? offset[i] + 4 * j : kNowhere, 0, 0));
+      }
+      v[i] = make_float4(f[0], f[1], f[2], f[3]);
+    }
+  }
+  // The parts of the values to the three planes at `tile`.  The first two are cut to the
+  // largest bf16, so that an infinity or NaN stands in the last, which multiplies the first
+  // part of the other operand alone, and goes through as in fp32.
+  template <bool kLast>
+  static __device__ __forceinline__ uint32_t part(float& a, float& b) {
+    if constexpr (kLast) return Op16<false>::pack(a, b);
+    constexpr float kMost = 3.38953139e38f;
+    const uint32_t h = Op16<false>::pack(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
+    a -= __uint_as_float(h << 16);
+    b -= __uint_as_float(h & 0xFFFF0000u);
+    return h;
+  }
+  __device__ __forceinline__ void store(char* tile, float4 (&v)[kLoads]) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      static_for<3>([&](auto p) {
+        const uint32_t x = part<p == 2>(v[i].x, v[i].y), y = part<p == 2>(v[i].z, v[i].w);
+        *reinterpret_cast<uint2*>(tile + p * kPlane + to[i]) = make_uint2(x, y);
+      });
+  }
+};
+
+template <int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>
+__global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs a) {
+  constexpr int kThreads = 64 * kWM * kWN;
+  constexpr bool kLeftInner = kForm != kDw, kRightInner = kForm == kDx;
+  static_assert(!kRightInner || kHalves == 1, "dx has one half");
+  constexpr int kHN = kBN / 2;
+  constexpr int kFragsM = kBM / kWM / 32, kFragsN = kBN / kWN / 32;
+  using Left = Tile32<kLeftInner, kBM, kThreads>;
+  using Right = Tile32<kRightInner, kHN, kThreads>;
+  // a stage: the left operand's planes, then each half's
+  constexpr int kLeftBytes = 3 * Left::kPlane, kRightBytes = 3 * Right::kPlane;
+  constexpr int kStage = kLeftBytes + 2 * kRightBytes;
+  static_assert(kWM * kWN * kEndWave <= 2 * kStage, "the end fits where the stages were");
+  __shared__ __align__(1024) char smem[2 * kStage];
+
+  const int tid = threadIdx.x, lane = tid % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int wm = wave / kWN, wn = wave % kWN;
+  const Place at = block_place(a);
+  const int64_t row0 = at.tm * kBM;
+  const int64_t col0 = at.tn * (kHalves == 2 ? kHN : kBN), col1 = kHalves == 2 ? col0 : col0 + kHN;
+  Left left;
+  Right right0, right1;
+  left.init(tid, row0, a.end.rows, a.ld_left);
+  right0.init(tid, col0, a.end.cols, a.ld_right);
+  right1.init(tid, col1, a.end.cols, a.ld_right);
+  Frags<kLeftInner, kBM, kFragsM, kBK32> lf;
+  Frags<kRightInner, kHN, kFragsN, kBK32> rf;
+  lf.init(lane, [&](int i, int* tile) {
+    *tile = 0;
+    return wm * (kBM / kWM) + 32 * i;
+  });
+  rf.init(lane, [&](int i, int* tile) {
+    const int half = kHalves == 2 ? i / (kFragsN / 2) : wn * 32 * kFragsN / kHN;
+    *tile = kLeftBytes + half * kRightBytes;
+    return kHalves == 2 ? wn * (kHN / kWN) + i % (kFragsN / 2) * 32 : wn * 32 * kFragsN % kHN + 32 * i;
+  });
+
+  int to_load = a.split_each + (at.split < (uint32_t)a.split_more);
+  const uint32_t first = at.split * a.split_each + (at.split < (uint32_t)a.split_more ? at.split : a.split_more);
+  int term = (int)(first / (uint32_t)a.stages);
+  int k0 = (int)(first - (uint32_t)term * a.stages) * kBK32;
+  const int stages = to_load;
+  const int64_t left_step = (kLeftInner ? kBK32 : kBK32 * a.ld_left) * 4;
+  const int64_t right_step = (kRightInner ? kBK32 : kBK32 * a.ld_right) * 4;
+  const bool whole_left = kLeftInner ? a.inner % 4 == 0 : a.end.rows % 4 == 0;
+  const bool whole_right = kRightInner ? a.inner % 4 == 0 : a.end.cols % 4 == 0;
+
+  float4 lv[Left::kLoads], rv0[Right::kLoads], rv1[Right::kLoads];
+  auto load = [&] {
+    const Term& t = a.term[term];
+    const int64_t s = k0 / kBK32;
+    const int left_of = a.inner - k0;
+    left.load(static_cast<const char*>(t.left) + (kLeftInner ? row0 * a.ld_left : row0) * 4 + s * left_step, left_of,
+              whole_left, lv);
+    right0.load(static_cast<const char*>(t.right0) + (kRightInner ? col0 * a.ld_right : col0) * 4 + s * right_step,
+                left_of, whole_right, rv0);
+    right1.load(static_cast<const char*>(kHalves == 2 ? t.right1 : t.right0) +
+                    (kRightInner ? col1 * a.ld_right : col1) * 4 + s * right_step,
+                left_of, whole_right, rv1);
+    k0 += kBK32;
+    if (k0 >= a.inner) k0 = 0, ++term;
+    --to_load;
+  };
+  auto store = [&](int stage) {
+    char* tile = smem + stage * kStage;
+    left.store(tile, lv);
+    right0.store(tile + kLeftBytes, rv0);
+    right1.store(tile + kLeftBytes + kRightBytes, rv1);
+  };
+  floatx16 acc[kFragsM][kFragsN] = {};
+  auto step = [&](int stage, int s) {
+    const char* tile = smem + stage * kStage;
+    uint4 l[3][kFragsM], r[3][kFragsN];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+#pragma unroll
+      for (int i = 0; i < kFragsM; ++i) l[p][i] = lf.read(tile + p * Left::kPlane, i, s);
+#pragma unroll
+      for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * Right::kPlane, j, s);
+    }
+#pragma unroll
+    for (int order = 2; order >= 0; --order)
+#pragma unroll
+      for (int p = order; p >= 0; --p)
+#pragma unroll
+        for (int i = 0; i < kFragsM; ++i)
+#pragma unroll
+          for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[p][i], acc[i][j]);
+  };
+  if (stages > 0) {
+    load();
+    store(0);
+    if (to_load > 0) load();
+    __syncthreads();
+    for (int it = 0; it < stages; ++it) {
+      const int stage = it % 2;
+      step(stage, 0);
+      if (it + 1 < stages) {
+        store(stage ^ 1);
+        if (to_load > 0) load();
+      }
+      step(stage, 1);
+      __syncthreads();
+    }
+  }
+  end_tile<POINTID_FP32, kHalves, kFragsM, kFragsN>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4,
+                                                    lane, at.split, row0 + wm * (kBM / kWM),
+                                                    col0 + wn * (kHalves == 2 ? kHN / kWN : 32 * kFragsN));
+}
+
+template <int kForm, int kHalves>
+hipError_t launch_tile32(int tile, ProductArgs& a, hipStream_t stream) {
+  const int bm = kTileM32[tile], bn = kTileN32[tile] / (kHalves == 2 ? 2 : 1);
+  const int64_t blocks = spread(a, bm, bn, kBK32);
+  if (blocks < 1 || a.end.dtype != POINTID_FP32) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
+  switch (tile) {
+    case 0: return launch_kernel(product_f32_kernel<kForm, kHalves, 256, 128, 4, 2>, grid, dim3(512), 0, stream, a);
+    case 1: return launch_kernel(product_f32_kernel<kForm, kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
+    case 2: return launch_kernel(product_f32_kernel<kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+}  // namespace mm
+
+hipError_t launch_product_f32(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream) {
+  a.splits = plan.splits;
+  const bool two = a.end.halves == 2;
+  switch (form) {
+    case kForward:
+      return two ? mm::launch_tile32<kForward, 2>(plan.tile, a, stream) : mm::launch_tile32<kForward, 1>(plan.tile, a, stream);
+    case kDx: return two ? hipErrorInvalidValue : mm::launch_tile32<kDx, 1>(plan.tile, a, stream);
+    case kDw: return two ? mm::launch_tile32<kDw, 2>(plan.tile, a, stream) : mm::launch_tile32<kDw, 1>(plan.tile, a, stream);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace pointid

@@ -7,27 +7,6 @@
 namespace pointid {
 namespace {
 
-// v as the sum of three bf16 values: each part is the remainder so far, rounded (8 + 8 + 8
-// bits hold fp32's 24).  A value that rounds past the largest bf16 is cut instead; one
-// that is not finite stays in the first part.
-__device__ __forceinline__ void three_parts(float v, uint16_t* o) {
-  __bf16 a = (__bf16)v;
-  if ((__float_as_uint((float)a) & 0x7FFFFFFFu) >= 0x7F800000u) {
-    if ((__float_as_uint(v) & 0x7FFFFFFFu) >= 0x7F800000u) {
-      o[0] = __builtin_bit_cast(uint16_t, a);
-      o[1] = o[2] = 0;
-      return;
-    }
-    a = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(v) >> 16));
-  }
-  const float r = v - (float)a;
-  const __bf16 b = (__bf16)r;
-  const __bf16 c = (__bf16)(r - (float)b);
-  o[0] = __builtin_bit_cast(uint16_t, a);
-  o[1] = __builtin_bit_cast(uint16_t, b);
-  o[2] = __builtin_bit_cast(uint16_t, c);
-}
-
 __device__ __forceinline__ void store8(uint16_t* p, const uint16_t* h) {      // 16-byte aligned
   uint32_t w[4];
 #pragma unroll
@@ -45,26 +24,12 @@ __device__ __forceinline__ void each_piece(int64_t rows, int64_t pieces, F&& f) 
   }
 }
 
-__global__ void __launch_bounds__(256) pack_kernel(const void* src, int64_t ld_src, int dtype, int64_t rows,
-                                                   int64_t cols, int parts, uint16_t* out, int64_t ld, int64_t plane) {
+__global__ void __launch_bounds__(256) copy_kernel(const void* src, int64_t ld_src, int dtype, int64_t rows,
+                                                   int64_t cols, void* out, int64_t ld) {
   each_piece(rows, ld / 8, [&](int64_t row, int64_t col) {
     float v[8];
     load_cols<8>(src, row * ld_src + col, dtype, cols - col, v);
-    uint16_t h[3][8];
-    if (parts == 1) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[0][i] = to16(v[i], dtype);
-      store8(out + row * ld + col, h[0]);
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint16_t p[3];
-      three_parts(v[i], p);
-      h[0][i] = p[0], h[1][i] = p[1], h[2][i] = p[2];
-    }
-#pragma unroll
-    for (int q = 0; q < 3; ++q) store8(out + q * plane + row * ld + col, h[q]);
+    store_cols<8>(out, row * ld + col, dtype, 8, v);
   });
 }
 
@@ -72,25 +37,25 @@ __global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64
                                                               void* out, int64_t ld, int64_t fill_to) {
   each_piece(rows, (fill_to + 7) / 8, [&](int64_t row, int64_t col) {
     float v[8] = {};
-    if (col < cols) load_codes<8>(src, row, col, cols, v);
+    if (col < cols) load_codes(src, row, col, cols, v);
     store_cols<8>(out, row * ld + col, dtype, fill_to - col, v);
   });
 }
 
-// A block of 32 values by a pair of neighbouring lanes.
-__global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, int64_t ld, int dtype,
-                                                              int64_t rows, int64_t cols, Packed8 out) {
-  const int64_t pairs = (cols + kBlock8 - 1) / kBlock8, total = rows * pairs * 2;
+// A block of 32 values by 4 neighbouring lanes.
+__global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, int64_t ld, int dtype, int64_t rows,
+                                                              int64_t cols, Packed8 out) {
+  const int64_t lanes = (cols + kBlock8 - 1) / kBlock8 * 4, total = rows * lanes;
   const int64_t step = (int64_t)gridDim.x * blockDim.x;
-  // every lane of a wave takes the same number of turns, as the exchange needs both of a pair
+  // every lane of a wave takes the same number of turns, as the exchange needs all 4 of a block
   const int64_t last = (total + 63) / 64 * 64;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < last; i += step) {
-    const bool live = i < total;
-    const int64_t row = !live ? 0 : total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)(2 * pairs)) : i / (2 * pairs);
-    const int64_t col = live ? (i - row * 2 * pairs) * 16 : 0;
-    float v[16];
-    load_cols<16>(src, row * ld + col, dtype, live ? cols - col : 0, v);
-    save_codes<1>(out, live, row, col, cols, v);
+    const bool here = i < total;
+    const int64_t row = !here ? 0 : total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)lanes) : i / lanes;
+    const int64_t col = here ? (i - row * lanes) * 8 : 0;
+    float v[8];
+    load_cols<8>(src, row * ld + col, dtype, here ? cols - col : 0, v);
+    save_codes(out, here && col < cols, row, col, cols, v);
   }
 }
 
@@ -117,7 +82,7 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
           if (a.z[h].matrix)
             load_cols<8>(a.z[h].matrix, row * a.z[h].ld + col, a.dtype, here, z[u][h]);
           else if (a.z[h].packed.codes && here)
-            load_codes<8>(a.z[h].packed, row, col, a.cols, z[u][h]);
+            load_codes(a.z[h].packed, row, col, a.cols, z[u][h]);
         }
       }
 #pragma unroll
@@ -149,22 +114,15 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
             continue;
           }
           uint16_t* o = static_cast<uint16_t*>(a.out[h]) + row * a.ld + col;
-          uint16_t p[3][8];
+          uint16_t p[2][8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            if (a.parts == 3) {
-              uint16_t t[3];
-              three_parts(d[h][i], t);
-              p[0][i] = t[0], p[1][i] = t[1], p[2][i] = t[2];
-            } else {
-              p[0][i] = to16(d[h][i], a.type16);
-              const float rest = d[h][i] - from16(p[0][i], a.type16);
-              p[1][i] = (__float_as_uint(rest) & 0x7FFFFFFFu) < 0x7F800000u ? to16(rest, a.type16) : 0;
-            }
+            p[0][i] = to16(d[h][i], a.dtype);
+            const float rest = d[h][i] - from16(p[0][i], a.dtype);
+            p[1][i] = (__float_as_uint(rest) & 0x7FFFFFFFu) < 0x7F800000u ? to16(rest, a.dtype) : 0;
           }
           store8(o, p[0]);
           if (a.parts >= 2) store8(o + a.plane, p[1]);
-          if (a.parts >= 3) store8(o + 2 * a.plane, p[2]);
         }
       }
     }
@@ -204,45 +162,46 @@ __global__ void __launch_bounds__(256) colsum_kernel(const float* part, int64_t 
   out[col] = v;
 }
 
-// Units of 16 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
+// Units of 8 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
 // order.  kSub == 8, for many parts: 8 lanes of a unit take every eighth part each, and
 // their sums are added in order.
 template <int kHalves, int kSub>
 __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int64_t part_ld, int splits) {
   constexpr int kUnits = 256 / kSub;
-  __shared__ float sums[kSub > 1 ? kSub : 1][kHalves][kSub > 1 ? kUnits : 1][kSub > 1 ? 17 : 1];
-  const int64_t units = part_ld / 16, total = e.rows * units;
+  __shared__ float sums[kSub > 1 ? kSub : 1][kHalves][kSub > 1 ? kUnits : 1][kSub > 1 ? 9 : 1];
+  const int64_t units = part_ld / 8, total = e.rows * units;
   const int unit = threadIdx.x % kUnits, sub = threadIdx.x / kUnits;
   const int64_t i = (int64_t)blockIdx.x * kUnits + unit;
-  const bool live = i < total;
-  const int64_t row = live ? i / units : 0, col = live ? (i - row * units) * 16 : 0;
-  float v[kHalves][16] = {};
-  if (live) {
+  const bool here = i < total;
+  const int64_t row = here ? i / units : 0, col = here ? (i - row * units) * 8 : 0;
+  const bool live = here && col < e.cols;
+  float v[kHalves][8] = {}, r[8];
+  if (sub == 0) load_residual(e.dtype, e, live, row, col, r);
+  if (here) {
+#pragma unroll 4
     for (int s = sub; s < splits; s += kSub)
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
-        const float4* p = reinterpret_cast<const float4*>(part + (((int64_t)s * kHalves + h) * e.rows + row) * part_ld + col);
+        float f[8];
+        __builtin_memcpy(f, part + (((int64_t)s * kHalves + h) * e.rows + row) * part_ld + col, 32);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float4 f = p[j];
-          v[h][4 * j] += f.x, v[h][4 * j + 1] += f.y, v[h][4 * j + 2] += f.z, v[h][4 * j + 3] += f.w;
-        }
+        for (int j = 0; j < 8; ++j) v[h][j] += f[j];
       }
   }
   if constexpr (kSub > 1) {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) sums[sub][h][unit][j] = v[h][j];
+      for (int j = 0; j < 8; ++j) sums[sub][h][unit][j] = v[h][j];
     __syncthreads();
     if (sub != 0) return;
     for (int s = 1; s < kSub; ++s)
 #pragma unroll
       for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[h][j] += sums[s][h][unit][j];
+        for (int j = 0; j < 8; ++j) v[h][j] += sums[s][h][unit][j];
   }
-  finish<1>(e, live, row, col, v[0], v[kHalves - 1]);
+  finish(e.dtype, e, live, row, col, v[0], v[kHalves - 1], r);
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols) {
@@ -259,10 +218,10 @@ unsigned pass_blocks(int64_t items) {
 
 }  // namespace
 
-hipError_t launch_layers_pack(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, int parts,
-                              uint16_t* out, int64_t ld, int64_t plane, hipStream_t stream) {
-  return launch_kernel(pack_kernel, dim3(pass_blocks(rows * (ld / 8))), dim3(256), 0, stream, src, ld_src, dtype,
-                       rows, cols, parts, out, ld, plane);
+hipError_t launch_layers_copy(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, void* out,
+                              int64_t ld, hipStream_t stream) {
+  return launch_kernel(copy_kernel, dim3(pass_blocks(rows * (ld / 8))), dim3(256), 0, stream, src, ld_src, dtype, rows,
+                       cols, out, ld);
 }
 
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
@@ -273,7 +232,7 @@ hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols
 
 hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
                                   const Packed8& out, hipStream_t stream) {
-  return launch_kernel(checkpoint_save_kernel, dim3(pass_blocks(rows * ((cols + 31) / 32) * 2)), dim3(256), 0, stream,
+  return launch_kernel(checkpoint_save_kernel, dim3(pass_blocks(rows * ((cols + 31) / 32) * 4)), dim3(256), 0, stream,
                        src, ld, dtype, rows, cols, out);
 }
 
@@ -295,7 +254,7 @@ hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, in
 }
 
 hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld, int splits, hipStream_t stream) {
-  const int64_t units = end.rows * (part_ld / 16);
+  const int64_t units = end.rows * (part_ld / 8);
   const int sub = splits >= 8 ? 8 : 1;
   const int64_t blocks = (units + 256 / sub - 1) / (256 / sub);
   if (blocks > INT32_MAX) return hipErrorInvalidValue;

@@ -82,23 +82,25 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
       }
   __syncthreads();
   if (wave != 0) return;
-  const int row = lane / 4, unit = lane % 4;           // 16 columns of a row
-  const bool live = row < kM && row < a.end.rows;
-  const int at = row < kM ? row : 0;
-  float v[2][16];
+  const int row = lane / 8, unit = lane % 8;           // 8 columns of a row
+  const int64_t at = col0 + unit * 8;
+  const bool live = row < kM && row < a.end.rows && at < a.end.cols;
+  float v[kHalves][8], residual[8];
 #pragma unroll
   for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      const int i = unit * 16 + c;
-      v[h][c] = ((cs[0][h][at][i] + cs[1][h][at][i]) + cs[2][h][at][i]) + cs[3][h][at][i];
+    for (int c = 0; c < 8; ++c) {
+      const int i = unit * 8 + c, r = row < kM ? row : 0;
+      v[h][c] = ((cs[0][h][r][i] + cs[1][h][r][i]) + cs[2][h][r][i]) + cs[3][h][r][i];
     }
   if (a.end.mode == kEndPartial) {
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) store_partial(a.end, blockIdx.y, h, live, row, col0 + unit * 16, v[h]);
+    for (int h = 0; h < kHalves; ++h)
+      store_partial(a.end, blockIdx.y, h, row < kM && row < a.end.rows, row, at, v[h]);
     return;
   }
-  finish<1>(a.end, live, row, col0 + unit * 16, v[0], v[kHalves - 1]);
+  load_residual(kType, a.end, live, row, at, residual);
+  finish(kType, a.end, live, row, at, v[0], v[kHalves - 1], residual);
 }
 
 template <int kM, int kHalves>

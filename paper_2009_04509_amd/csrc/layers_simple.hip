@@ -60,14 +60,16 @@ __global__ void __launch_bounds__(256) simple_kernel(SimpleArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) cs[h][r][c + j] = acc[h][j];
   __syncthreads();
-  if (tid >= 64) return;
-  float v[2][16];
-  const int fr = tid / 2, fc = tid % 2 * 16;
+  if (tid >= 128) return;
+  float v[kHalves][8], residual[8];
+  const int64_t row = row0 + tid / 4, col = col0 + tid % 4 * 8;
+  const bool live = row < a.end.rows && col < a.end.cols;
+  load_residual(a.end.dtype, a.end, live, row, col, residual);
 #pragma unroll
   for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[h][j] = cs[h][fr][fc + j];
-  finish<1>(a.end, row0 + fr < a.end.rows, row0 + fr, col0 + fc, v[0], v[kHalves - 1]);
+    for (int j = 0; j < 8; ++j) v[h][j] = cs[h][tid / 4][tid % 4 * 8 + j];
+  finish(a.end.dtype, a.end, live, row, col, v[0], v[kHalves - 1], residual);
 }
 
 }  // namespace
