@@ -76,16 +76,6 @@ struct Term {
 };
 constexpr int kMaxTerms = 12;
 
-// ---- layers_simple.hip: fp32 arithmetic, any type, stride and size
-struct SimpleArgs {
-  Strided left[2];             // summed over `terms`
-  Strided right[2][2];         // [term][half]
-  int32_t terms;
-  int64_t inner;
-  End end;
-};
-hipError_t launch_layers_simple(const SimpleArgs& a, hipStream_t stream);
-
 // ---- layers_rows.hip: forward products of 1..kFewRows rows; the weights
 // [inner][cols] are read once.  splits > 1 leaves partials (end.mode is kEndPartial then).
 constexpr int kFewRows = 8;
@@ -109,8 +99,8 @@ struct ProductArgs {
   End end;
 };
 // The tile of a launch and its splits of the sum.
-constexpr int kTiles = 2, kTiles32 = 3;
-constexpr int kTileM[kTiles] = {256, 64}, kTileN[kTiles] = {256, 128};
+constexpr int kTiles = 3, kTiles32 = 3;
+constexpr int kTileM[kTiles] = {256, 128, 64}, kTileN[kTiles] = {256, 128, 128};
 constexpr int kTileM32[kTiles32] = {256, 128, 64}, kTileN32[kTiles32] = {128, 128, 128};
 struct ProductPlan {
   int tile;                    // index into kTileM, kTileN (fp32: kTileM32, kTileN32; columns of both halves)

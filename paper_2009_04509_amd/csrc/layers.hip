@@ -23,9 +23,6 @@ constexpr int64_t kMaxSide = int64_t(1) << 20;         // k and n
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;   // m
 constexpr int64_t kMaxPitch = int64_t(1) << 21;        // of an operand that the products read in place
 
-// Products of up to this many multiplications and inner indices run the plain kernel: one
-// launch, where the others take passes over unaligned or fp32 operands and a join.
-constexpr int64_t kSimpleWork = int64_t(1) << 22, kSimpleInner = 1024;
 // dz of up to this many values is kept in two 16-bit parts: the rounding of so few does not
 // average out in a gradient, and such products are bound by the bytes of the weights.
 constexpr int64_t kTwoPartValues = int64_t(1) << 16;
@@ -278,10 +275,6 @@ End end_of(int mode, int act, int dtype, int halves, int64_t rows, int64_t cols,
   return e;
 }
 
-bool simple_work(int64_t rows, int64_t cols, int64_t inner) {
-  return inner <= kSimpleInner && rows * cols <= kSimpleWork / inner;
-}
-
 // ---- the forward pass of a dense (halves == 1) or gated layer
 
 struct Forward {
@@ -292,6 +285,19 @@ struct Forward {
   pointid_matrix residual, y;
   Kept keep[2];
 };
+
+// Whether the weights are streamed past the rows.  fp32: up to 8 rows (8192 x 8192, 8 rows:
+// 63 us, on the matrix cores 70).  16 bits: up to 2 (a gated 4096 x 12288, 2 rows: 49 us
+// against 52; 4 rows: 58 against 52, as each value then costs more than its bytes), but up
+// to 8 where the matrix cores would take a copy of the weights first.  A lane reads 16 bytes
+// of a row, so a row has to have them.
+bool few_rows(const Forward& f) {
+  if (f.m > kFewRows || f.n < (f.dtype == POINTID_FP32 ? 4 : 8)) return false;
+  if (f.dtype == POINTID_FP32 || f.m <= 2) return true;
+  for (int h = 0; h < f.halves; ++h)
+    if (!read_in_place(f.w[h].data, f.w[h].ld, f.dtype, f.n) || f.w[h].ld != f.w[0].ld) return true;
+  return false;
+}
 
 int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   DeviceScope dev(l->device);
@@ -309,7 +315,7 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   Strided w[2];
   for (int h = 0; h < 2; ++h) w[h] = {f.w[h].data, 1, f.w[h].ld, f.dtype};
 
-  if (f.m <= kFewRows) {
+  if (few_rows(f)) {
     const int splits = few_rows_splits(f.k, f.n, f.halves, l->cus);
     float* part = nullptr;
     call.want(&part, part_bytes(splits, e));
@@ -324,17 +330,6 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
                   [&] { return launch_layers_rows(x, w, f.k, rows_end, splits, stream); });
     if (rc != POINTID_OK || splits == 1) return rc;
     return call.run("layers_join", true, [&] { return launch_layers_join(e, part, e.part_ld, splits, stream); });
-  }
-  if (simple_work(f.m, f.n, f.k)) {
-    SimpleArgs a;
-    std::memset(&a, 0, sizeof(a));
-    a.left[0] = x;
-    a.right[0][0] = w[0];
-    a.right[0][1] = w[1];
-    a.terms = 1;
-    a.inner = f.k;
-    a.end = e;
-    return call.run("layers_simple", true, [&] { return launch_layers_simple(a, stream); });
   }
   Source sx, sw[2];
   Kept from;
@@ -390,11 +385,10 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
     }
     return rc;
   }
-  const bool simple = simple_work(b.m, b.k, b.n) && simple_work(b.k, b.n, b.m);
   const bool products = want_dx || want_dw;
   // dz is dy itself where no activation changes it and the products can read it
   const bool plain = b.halves == 1 && b.act == POINTID_ACT_NONE;
-  const bool read_dy = plain && (simple || read_in_place(b.dy.data, b.dy.ld, b.dtype, b.n));
+  const bool read_dy = plain && read_in_place(b.dy.data, b.dy.ld, b.dtype, b.n);
   const bool exact16 = b.halves == 1 && (b.act == POINTID_ACT_NONE || b.act == POINTID_ACT_RELU);
 
   GradArgs g;
@@ -407,10 +401,10 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   g.rows = b.m;
   g.cols = b.n;
   for (int h = 0; h < b.halves; ++h) g.z[h] = b.z[h];
-  g.parts = !products || read_dy                          ? 0
-            : simple || b.dtype == POINTID_FP32             ? -1
+  g.parts = !products || read_dy                      ? 0
+            : b.dtype == POINTID_FP32                 ? -1
             : !exact16 && b.m * b.n <= kTwoPartValues ? 2
-                                                            : 1;
+                                                      : 1;
   g.ld = round_up(b.n, 8);
   g.plane = b.m * g.ld;
   const size_t dz_bytes = g.parts < 0 ? 4 * (size_t)g.plane : 2 * (size_t)g.plane * g.parts;
@@ -420,13 +414,8 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
 
   // x for dW, the weights for dx
   Source sx, sw[2];
-  void* x8 = nullptr;                                  // a checkpoint's values for the plain kernel
-  if (simple) {
-    if (want_dw && !b.x.matrix) call.want(&x8, (size_t)size_of(b.dtype) * b.m * b.k);
-  } else {
-    if (want_dw) sx.plan(b.x, b.dtype, b.m, b.k, call);
-    if (want_dx) plan_weights(sw, b.w, b.halves, b.dtype, b.k, b.n, call);
-  }
+  if (want_dw) sx.plan(b.x, b.dtype, b.m, b.k, call);
+  if (want_dx) plan_weights(sw, b.w, b.halves, b.dtype, b.k, b.n, call);
   End dx_end = end_of(kEndStore, POINTID_ACT_NONE, b.dtype, 1, b.m, b.k, b.dx, none);
   End dw_end = end_of(kEndStore, POINTID_ACT_NONE, b.dtype, b.halves, b.k, b.n, b.dw[0], b.dw[1]);
   Planes dz[2];
@@ -437,13 +426,11 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   }
   ProductPlan dx_plan = {0, 1}, dw_plan = {0, 1};
   float* part = nullptr;
-  if (!simple) {
-    const bool f32 = b.dtype == POINTID_FP32;
-    if (want_dx) dx_plan = plan_product(f32, b.m, b.k, 1, b.n, b.halves * dz[0].parts, l->cus);
-    if (want_dw) dw_plan = plan_product(f32, b.k, b.n, b.halves, b.m, dz[0].parts, l->cus);
-    const size_t p = part_bytes(dx_plan.splits, dx_end), q = part_bytes(dw_plan.splits, dw_end);
-    call.want(&part, p > q ? p : q);                   // one after the other
-  }
+  const bool f32 = b.dtype == POINTID_FP32;
+  if (want_dx) dx_plan = plan_product(f32, b.m, b.k, 1, b.n, b.halves * dz[0].parts, l->cus);
+  if (want_dw) dw_plan = plan_product(f32, b.k, b.n, b.halves, b.m, dz[0].parts, l->cus);
+  const size_t dx_part = part_bytes(dx_plan.splits, dx_end), dw_part = part_bytes(dw_plan.splits, dw_end);
+  call.want(&part, dx_part > dw_part ? dx_part : dw_part);       // one after the other
   int rc = call.reserve();
   if (rc != POINTID_OK) return rc;
 
@@ -456,35 +443,6 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
     if (rc != POINTID_OK) return rc;
   }
   for (int h = 0; h < 2; ++h) dz[h].base = read_dy ? b.dy.data : g.out[h];
-
-  if (simple) {
-    SimpleArgs a;
-    std::memset(&a, 0, sizeof(a));
-    const int dz_type = read_dy ? b.dtype : POINTID_FP32;
-    if (want_dx) {
-      a.terms = b.halves;
-      a.inner = b.n;
-      a.end = dx_end;
-      for (int h = 0; h < b.halves; ++h) {
-        a.left[h] = {dz[h].base, dz[h].ld, 1, dz_type};
-        a.right[h][0] = {b.w[h].data, b.w[h].ld, 1, b.dtype};
-      }
-      rc = call.run("layers_simple", !want_dw, [&] { return launch_layers_simple(a, stream); });
-      if (rc != POINTID_OK) return rc;
-    }
-    if (!want_dw) return POINTID_OK;
-    if (x8) {
-      rc = call.run("layers_load", false,
-                    [&] { return launch_checkpoint_load(b.x.packed, b.m, b.k, b.dtype, x8, b.k, b.k, stream); });
-      if (rc != POINTID_OK) return rc;
-    }
-    a.terms = 1;
-    a.inner = b.m;
-    a.end = dw_end;
-    a.left[0] = {x8 ? x8 : b.x.matrix, 1, x8 ? b.k : b.x.ld, b.dtype};
-    for (int h = 0; h < b.halves; ++h) a.right[0][h] = {dz[h].base, 1, dz[h].ld, dz_type};
-    return call.run("layers_simple", true, [&] { return launch_layers_simple(a, stream); });
-  }
 
   if (want_dx) {
     for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = sw[h].make(call);

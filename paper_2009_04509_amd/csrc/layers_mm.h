@@ -231,8 +231,9 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   using Left = Tile<kLeftInner, kBM, kThreads>;
   using Right = Tile<kRightInner, kHN, kThreads>;
   constexpr int kStage = Left::kBytes + 2 * Right::kBytes;
-  static_assert(kWM * kWN * kEndWave <= 2 * kStage, "the end fits where the stages were");
-  __shared__ __align__(1024) char smem[2 * kStage];
+  // the end uses the stages' memory, and a little more with many small waves
+  constexpr int kShared = kWM * kWN * kEndWave > 2 * kStage ? kWM * kWN * kEndWave : 2 * kStage;
+  __shared__ __align__(1024) char smem[kShared];
 
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -387,7 +388,8 @@ hipError_t launch_tile(int tile, ProductArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)blocks);
   switch (tile) {
     case 0: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 256, 256, 2, 4>, grid, dim3(512), 0, stream, a);
-    case 1: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+    case 1: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
+    case 2: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
   }
   return hipErrorInvalidValue;
 }

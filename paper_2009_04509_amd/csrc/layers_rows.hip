@@ -6,19 +6,20 @@
 namespace pointid {
 namespace {
 
-constexpr int kStrip = 64;       // columns of a block
-constexpr int kChunk = 1024;     // inner indices whose x values are in shared memory at once
+constexpr int kStrip = 256;      // columns of a block
+constexpr int kChunk = 512;      // inner indices whose x values are in shared memory at once
 
 struct RowsArgs {
   Strided x;
   Strided w[2];
   int64_t inner;
-  int64_t per_split;             // inner indices of a split, a multiple of 32
+  int64_t per_split;             // inner indices of a split
   End end;
 };
 
-// A wave reads kRowsPer rows of 64 columns of the weights at a time, 16 bytes a lane; the
-// block's 4 waves take turns along the inner index.  The lanes of a column are added in a
+// A wave reads 256 columns of kRowsPer rows of the weights at a time, 16 bytes a lane (long
+// stretches of a row: 64 columns took a third more time at 4 rows), the next reads under way
+// while it multiplies; the block's 4 waves take turns along the inner index.  The lanes of a column are added in a
 // fixed order at the end: lanes, then waves, then (elsewhere) splits.
 template <int kM, int kType, int kHalves>
 __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
@@ -26,81 +27,142 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   constexpr int kLanes = kStrip / kCols;
   constexpr int kRowsPer = 64 / kLanes;
   constexpr int kStep = 4 * kRowsPer;
-  constexpr int kAhead = kHalves == 2 ? 4 : 8;         // reads in flight a lane
+  constexpr int kAhead = (kHalves == 2 ? 4 : 8)/2;        // reads in flight a lane
   __shared__ float xs[kChunk * kM];
-  __shared__ float cs[4][kHalves][kM][kStrip];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  __shared__ float cs[kHalves][kM][kStrip];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int64_t col0 = (int64_t)blockIdx.x * kStrip;
-  const int64_t col = col0 + lane % kLanes * kCols, n = a.end.cols - col;
+  const int64_t col = col0 + lane % kLanes * kCols;
   const int64_t first = a.per_split * blockIdx.y;
   const int64_t last = first + a.per_split < a.inner ? first + a.per_split : a.inner;
   float acc[kHalves][kM][kCols] = {};
 
+  // A lane whose columns do not all exist reads the row's last ones instead (cols >= kCols).
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+  constexpr uint32_t kNowhere = 0x80000000u;           // past the resource's range: reads 0
+  const int64_t from = col < a.end.cols - kCols ? col : a.end.cols - kCols;
+  const char* wp[kHalves];
+  uint32_t offset[kHalves], step[kHalves];
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h) {
+    const int64_t pitch = a.w[h].sk * kSize;
+    wp[h] = static_cast<const char*>(a.w[h].p) + (first + wave * kRowsPer) * pitch + col0 * kSize;
+    offset[h] = (uint32_t)((lane / kLanes) * pitch + (from - col0) * kSize);
+    step[h] = (uint32_t)(kStep * pitch);
+  }
+  auto values = [](const uint4& r, float* w) {
+    const uint32_t v[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (kSize == 4) {
+        w[i] = __uint_as_float(v[i]);
+      } else {
+        w[2 * i] = from16((uint16_t)v[i], kType);
+        w[2 * i + 1] = from16((uint16_t)(v[i] >> 16), kType);
+      }
+    }
+  };
   for (int64_t k0 = first; k0 < last; k0 += kChunk) {
     const int len = (int)(last - k0 < kChunk ? last - k0 : kChunk);
     __syncthreads();
     for (int i = tid; i < len * kM; i += 256) {
       const int r = i / len, k = i - r * len;
-      xs[k * kM + r] = r < a.end.rows ? load_any(a.x.p, r * a.x.si + k0 + k, a.x.dtype) : 0.f;
+      xs[k * kM + r] = r < a.end.rows ? load_any(a.x.p, r * a.x.si + k0 + k, kType) : 0.f;
     }
     __syncthreads();
-    for (int base = wave * kRowsPer + lane / kLanes; base - lane / kLanes < len; base += kStep * kAhead) {
-      float w[kHalves][kAhead][kCols];
+    // turns of kAhead reads: those of the next turn are under way while this one multiplies
+    const int mine = wave * kRowsPer + lane / kLanes;
+    uint4 raw[2][kHalves][kAhead];
+    auto fetch = [&](int buf, int base) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const int k = base + u * kStep;
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-          load_cols<kCols>(a.w[h].p, (k0 + k) * a.w[h].sk + col, kType,
-                           k < len ? n : 0, w[h][u]);
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int k = base + u * kStep;
-        if (k >= len) continue;
-#pragma unroll
-        for (int r = 0; r < kM; ++r) {
-          const float x = xs[k * kM + r];
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) acc[h][r][c] += x * w[h][u][c];
+        for (int h = 0; h < kHalves; ++h) {
+          const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+              const_cast<char*>(wp[h]), (short)0, (int)kNowhere, 0x00020000);
+          raw[buf][h][u] = __builtin_bit_cast(
+              uint4, __builtin_amdgcn_raw_buffer_load_b128(r, k < len ? offset[h] : kNowhere, u * step[h], 0));
         }
       }
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) wp[h] += (int64_t)kAhead * step[h];
+    };
+    auto multiply = [&](int buf, int base) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int k = base + u * kStep < len ? base + u * kStep : len - 1;     // past the end: times 0
+        float x[kM];
+#pragma unroll
+        for (int r = 0; r < kM; ++r) x[r] = xs[k * kM + r];
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          float w[kCols];
+          values(raw[buf][h][u], w);
+#pragma unroll
+          for (int r = 0; r < kM; ++r)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) acc[h][r][c] += x[r] * w[c];
+        }
+      }
+    };
+    constexpr int kTurn = kStep * kAhead;
+    const char* at[kHalves];
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) at[h] = wp[h];
+    fetch(0, mine);
+    for (int base = mine; base - mine < len; base += 2 * kTurn) {
+      fetch(1, base + kTurn);
+      multiply(0, base);
+      if (base + kTurn - mine >= len) break;
+      fetch(0, base + 2 * kTurn);
+      multiply(1, base + kTurn);
     }
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) wp[h] = at[h] + (int64_t)(kChunk / kStep) * step[h];
   }
 #pragma unroll
   for (int h = 0; h < kHalves; ++h)
 #pragma unroll
     for (int r = 0; r < kM; ++r)
 #pragma unroll
-      for (int c = 0; c < kCols; ++c) {
-        float t = acc[h][r][c];
+      for (int c = 0; c < kCols; ++c)
 #pragma unroll
-        for (int x = kLanes; x < 64; x *= 2) t += __shfl_xor(t, x, 64);
-        if (lane < kLanes) cs[wave][h][r][lane * kCols + c] = t;
-      }
-  __syncthreads();
-  if (wave != 0) return;
-  const int row = lane / 8, unit = lane % 8;           // 8 columns of a row
-  const int64_t at = col0 + unit * 8;
-  const bool live = row < kM && row < a.end.rows && at < a.end.cols;
-  float v[kHalves][8], residual[8];
+        for (int x = kLanes; x < 64; x *= 2) acc[h][r][c] += __shfl_xor(acc[h][r][c], x, 64);
+  for (int turn = 0; turn < 4; ++turn) {
+    if (wave == turn && lane < kLanes) {
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h)
+      for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const int i = unit * 8 + c, r = row < kM ? row : 0;
-      v[h][c] = ((cs[0][h][r][i] + cs[1][h][r][i]) + cs[2][h][r][i]) + cs[3][h][r][i];
+        for (int r = 0; r < kM; ++r)
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            if (from + c < col) continue;              // the lane before has it
+            float* const p = &cs[h][r][from + c - col0];
+            *p = turn == 0 ? acc[h][r][c] : *p + acc[h][r][c];
+          }
     }
-  if (a.end.mode == kEndPartial) {
+    __syncthreads();
+  }
+  // 8 columns of a row a lane, whole waves at a time
+  constexpr int kUnits = kStrip / 8;
+  for (int i = tid; i < (kM * kUnits + 63) / 64 * 64; i += 256) {
+    const int row = i / kUnits, unit = i % kUnits, r = row < kM ? row : 0;
+    const int64_t at = col0 + unit * 8;
+    const bool here = row < kM && row < a.end.rows, live = here && at < a.end.cols;
+    float v[kHalves][8], residual[8];
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
-      store_partial(a.end, blockIdx.y, h, row < kM && row < a.end.rows, row, at, v[h]);
-    return;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[h][c] = cs[h][r][unit * 8 + c];
+    if (a.end.mode == kEndPartial) {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) store_partial(a.end, blockIdx.y, h, here, row, at, v[h]);
+    } else {
+      load_residual(kType, a.end, live, row, at, residual);
+      finish(kType, a.end, live, row, at, v[0], v[kHalves - 1], residual);
+    }
   }
-  load_residual(kType, a.end, live, row, at, residual);
-  finish(kType, a.end, live, row, at, v[0], v[kHalves - 1], residual);
 }
 
 template <int kM, int kHalves>
@@ -120,14 +182,14 @@ hipError_t launch_rows(const RowsArgs& a, dim3 grid, hipStream_t stream) {
   return launch_type<8, kHalves>(a, grid, stream);
 }
 
-int64_t rows_per_split(int64_t inner, int splits) { return ((inner + splits - 1) / splits + 31) / 32 * 32; }
+int64_t rows_per_split(int64_t inner, int splits) { return ((inner + splits - 1) / splits + 7) / 8 * 8; }
 
 }  // namespace
 
-// About 4 blocks a CU, each over at least 128 inner indices.
+// About 3 blocks a CU, each over at least 64 inner indices.
 int few_rows_splits(int64_t inner, int64_t cols, int halves, int cus) {
   const int64_t strips = (cols + kStrip - 1) / kStrip;
-  int64_t s = 4 * (int64_t)cus / strips, most = (inner + 127) / 128;
+  int64_t s = 3 * (int64_t)cus / strips, most = (inner + 63) / 64;
   s = s < 1 ? 1 : s;
   s = s > most ? most : s;
   s = s > 4096 ? 4096 : s;
