@@ -131,6 +131,10 @@ class Call {
     size_t total = 0;
     for (int i = 0; i < count_; ++i) total += pad256(pieces_[i].bytes);
     if (total == 0) return POINTID_OK;
+    // a graph would use the buffer again whenever it is replayed, past the cache's care
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(stream_, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
+      return set_error(POINTID_EINVAL, "the call takes scratch, which a captured stream cannot");
     hipError_t e = ws_.reserve(total);
     if (e != hipSuccess) return hip_fail(e, "scratch buffer");
     for (int i = 0; i < count_; ++i) {
