@@ -225,53 +225,77 @@ __device__ __forceinline__ void keep_cols(int dtype, const Kept& k, bool live, i
   }
 }
 
-__device__ __forceinline__ void add_bias(const float* bias, int64_t col, int64_t n, float* v) {
-  if (!bias || n <= 0) return;
-  float b[8];
-  load_cols<8>(bias, col, POINTID_FP32, n, b);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] += b[i];
+// What the end of 8 columns from `col` adds to their sums, zeros where there is none.
+__device__ __forceinline__ void load_bias(const float* bias, int64_t col, int64_t cols, float* b) {
+  load_cols<8>(bias, col, POINTID_FP32, bias && col < cols ? cols - col : 0, b);
 }
-
-// The residual of 8 columns, if the end has one (finish adds it).
-__device__ __forceinline__ void load_residual(int dtype, const End& e, bool live, int64_t row, int64_t col, float* r) {
-  if (e.residual && live)
-    load_cols<8>(e.residual, row * e.ld_residual + col, dtype, e.cols - col, r);
-  else
+// The residual of 8 columns as it stands in memory, zeros where there is none.
+template <int kType>
+struct Residual {
+  static constexpr int kWords = kType == POINTID_FP32 ? 8 : 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const End& e, bool live, int64_t row, int64_t col) {
+    const int64_t n = e.residual && live ? e.cols - col : 0, at = row * e.ld_residual + col;
+    constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+    if (n >= 8) {
+      __builtin_memcpy(w, static_cast<const char*>(e.residual) + at * kSize, sizeof(w));
+      return;
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = 0.f;
-}
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i >= n) continue;
+      if constexpr (kSize == 4)
+        w[i] = static_cast<const uint32_t*>(e.residual)[at + i];
+      else
+        w[i / 2] |= (uint32_t)static_cast<const uint16_t*>(e.residual)[at + i] << (16 * (i % 2));
+    }
+  }
+  __device__ __forceinline__ void add_to(float* v) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (kType == POINTID_FP32) {
+        v[i] += __uint_as_float(w[i]);
+      } else {
+        v[2 * i] += from16((uint16_t)w[i], kType);
+        v[2 * i + 1] += from16((uint16_t)(w[i] >> 16), kType);
+      }
+    }
+  }
+};
 
-// The end of 8 finished columns of a row (see End) from `col`, a multiple of 8; v1: the
-// second half's, with e.halves == 2; r: load_residual's.  The 4 lanes of an aligned group
-// hold 32 columns of one row, from a multiple of 32 on, and all call it; `live` is false
-// where the row or the columns do not exist.  dtype: the call's type (a constant where the
-// kernel knows it).
-__device__ __forceinline__ void finish(int dtype, const End& e, bool live, int64_t row, int64_t col, float* v0,
-                                       float* v1, const float* r) {
+// The end of 8 finished columns of a row (see End) from `col`, a multiple of 8; v1 and b1:
+// the second half's, with kHalves == 2; b0, b1: load_bias's; r: the residual's.  The 4 lanes
+// of an aligned group hold 32 columns of one row, from a multiple of 32 on, and all call it;
+// `live` is false where the row or the columns do not exist.
+template <int kType, int kHalves>
+__device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int64_t col, float* v0, float* v1,
+                                       const float* b0, const float* b1, const Residual<kType>& r) {
   const int64_t n = e.cols - col;
   if (e.mode == kEndStore) {
     if (!live) return;
-    store_cols<8>(e.y0, row * e.ld0 + col, dtype, n, v0);
-    if (e.halves == 2) store_cols<8>(e.y1, row * e.ld1 + col, dtype, n, v1);
+    store_cols<8>(e.y0, row * e.ld0 + col, kType, n, v0);
+    if (kHalves == 2) store_cols<8>(e.y1, row * e.ld1 + col, kType, n, v1);
     return;
   }
-  add_bias(e.bias0, col, n, v0);
-  keep_cols(dtype, e.keep0, live, row, col, e.cols, v0);
-  if (e.mode == kEndGated) {
-    add_bias(e.bias1, col, n, v1);
-    keep_cols(dtype, e.keep1, live, row, col, e.cols, v1);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v0[i] += b0[i];
+  keep_cols(kType, e.keep0, live, row, col, e.cols, v0);
+  if constexpr (kHalves == 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v1[i] += b1[i];
+    keep_cols(kType, e.keep1, live, row, col, e.cols, v1);
   }
   if (!live) return;
   activate8(e.act, v0);
-  if (e.mode == kEndGated) {
+  if constexpr (kHalves == 2) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v0[i] *= v1[i];
-  } else if (e.residual) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v0[i] += r[i];
+  } else {
+    r.add_to(v0);
   }
-  store_cols<8>(e.y0, row * e.ld0 + col, dtype, n, v0);
+  store_cols<8>(e.y0, row * e.ld0 + col, kType, n, v0);
 }
 
 // 8 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)

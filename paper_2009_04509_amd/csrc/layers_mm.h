@@ -169,24 +169,39 @@ __device__ __forceinline__ Place block_place(const ProductArgs& a) {
 // The end of a wave's results: rows from `row0` of kFragsM groups of 32, columns from `col0`
 // (of each half).  One copy of the end's code: 32 rows x 64 columns a turn (two halves: 32
 // columns of each) through the wave's kEndWave bytes of shared memory, from a lane's 4
-// columns of one row to 16 bytes and more a lane along the rows.
+// columns of one row to 16 bytes and more a lane along the rows.  The residual of a turn is
+// read a turn ahead.
 constexpr int kEndPitch = 64 + 4;
 constexpr int kEndWave = 32 * kEndPitch * 4;
-template <int kType, int kHalves, int kFragsM, int kFragsN>
-__device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFragsM][kFragsN], float* es, int lane,
-                                         int split, int64_t row0, int64_t col0) {
-  constexpr int kPairs = kFragsN / 2, kTurns = kFragsM * kPairs;
+template <int kType, int kHalves, int kFragsM>
+__device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFragsM][2], float* es, int lane, int split,
+                                         int64_t row0, int64_t col0) {
   constexpr int kLanes = kHalves == 2 ? 4 : 8;           // of a row
+  constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes;
+  const int64_t col = col0 + lane % kLanes * 8;
+  const bool live_col = col < e.cols;
+  float b0[8], b1[8];
+  load_bias(e.bias0, col, e.cols, b0);
+  if constexpr (kHalves == 2) load_bias(e.bias1, col, e.cols, b1);
+  const float* const from = es + lane / kLanes * kEndPitch + lane % kLanes * 8;
+  Residual<kType> next[kSteps];
+  auto read = [&](int64_t row) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      if (kHalves == 1) next[s].load(e, live_col && row + s * kRows < e.rows, row + s * kRows, col);
+  };
+  row0 += lane / kLanes;
+  read(row0);
 #pragma nounroll
-  for (int turn = 0; turn < kTurns; ++turn) {
+  for (int turn = 0; turn < kFragsM; ++turn, row0 += 32) {
     floatx16 c[2] = {};
-    static_for<kTurns>([&](auto t) {
-      constexpr int i = t / kPairs, pair = t % kPairs;
-      if (turn == t) {
-        c[0] = acc[i][kHalves == 2 ? pair : 2 * pair];
-        c[1] = acc[i][kHalves == 2 ? pair + kPairs : 2 * pair + 1];
-      }
+    static_for<kFragsM>([&](auto t) {
+      if (turn == t) c[0] = acc[t][0], c[1] = acc[t][1];
     });
+    Residual<kType> now[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) now[s] = next[s];
+    if (turn + 1 < kFragsM) read(row0 + 32);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int f = 0; f < 2; ++f)
@@ -195,26 +210,21 @@ __device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFr
         *reinterpret_cast<float4*>(es + lane % 32 * kEndPitch + f * 32 + 8 * j + lane / 32 * 4) =
             make_float4(c[f][4 * j], c[f][4 * j + 1], c[f][4 * j + 2], c[f][4 * j + 3]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int64_t col = col0 + turn % kPairs * (kHalves == 2 ? 32 : 64) + lane % kLanes * 8;
-    const bool live_col = col < e.cols;
-    int64_t row = row0 + 32 * (turn / kPairs) + lane / kLanes;
-    const float* at = es + lane / kLanes * kEndPitch + lane % kLanes * 8;
-    constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes;
-    float res[8], next[8];
-    load_residual(kType, e, live_col && row < e.rows, row, col, next);
 #pragma nounroll
-    for (int s = 0; s < kSteps; ++s, row += kRows, at += kRows * kEndPitch) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) res[i] = next[i];
-      if (s + 1 < kSteps) load_residual(kType, e, live_col && row + kRows < e.rows, row + kRows, col, next);
+    for (int s = 0; s < kSteps; ++s) {
+      const int64_t row = row0 + s * kRows;
       float v[kHalves][8];
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], at + h * 32, 32);
+      for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], from + s * kRows * kEndPitch + h * 32, 32);
       if (e.mode == kEndPartial) {
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) store_partial(e, split, h, row < e.rows, row, col, v[h]);
       } else {
-        finish(kType, e, live_col && row < e.rows, row, col, v[0], v[kHalves - 1], res);
+        Residual<kType> r = now[0];
+        static_for<kSteps>([&](auto t) {
+          if (s == t) r = now[t];
+        });
+        finish<kType, kHalves>(e, live_col && row < e.rows, row, col, v[0], v[kHalves - 1], b0, b1, r);
       }
     }
   }
@@ -228,6 +238,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   static_assert(!kRightInner || kHalves == 1, "dx has one half");
   constexpr int kHN = kBN / 2;                           // columns of each half of the tile
   constexpr int kFragsM = kBM / kWM / 32, kFragsN = kBN / kWN / 32;
+  static_assert(kFragsN == 2, "a wave takes 64 columns");
   using Left = Tile<kLeftInner, kBM, kThreads>;
   using Right = Tile<kRightInner, kHN, kThreads>;
   constexpr int kStage = Left::kBytes + 2 * Right::kBytes;
@@ -358,7 +369,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   }
   stage_ready();                                         // the stages are free for the end
 
-  end_tile<kType, kHalves, kFragsM, kFragsN>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4, lane, split,
+  end_tile<kType, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4, lane, split,
                                              row0 + wm * (kBM / kWM),
                                              col0 + wn * (kHalves == 2 ? kHN / kWN : 32 * kFragsN));
 }

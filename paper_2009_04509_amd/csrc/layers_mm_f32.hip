@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
   static_assert(!kRightInner || kHalves == 1, "dx has one half");
   constexpr int kHN = kBN / 2;
   constexpr int kFragsM = kBM / kWM / 32, kFragsN = kBN / kWN / 32;
+  static_assert(kFragsN == 2, "a wave takes 64 columns");
   using Left = Tile32<kLeftInner, kBM, kThreads>;
   using Right = Tile32<kRightInner, kHN, kThreads>;
   // a stage: the left operand's planes, then each half's
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
       __syncthreads();
     }
   }
-  end_tile<POINTID_FP32, kHalves, kFragsM, kFragsN>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4,
+  end_tile<POINTID_FP32, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4,
                                                     lane, at.split, row0 + wm * (kBM / kWM),
                                                     col0 + wn * (kHalves == 2 ? kHN / kWN : 32 * kFragsN));
 }

@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(256) colsum_kernel(const float* part, int64_t 
 // Units of 8 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
 // order.  kSub == 8, for many parts: 8 lanes of a unit take every eighth part each, and
 // their sums are added in order.
-template <int kHalves, int kSub>
+template <int kType, int kHalves, int kSub>
 __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int64_t part_ld, int splits) {
   constexpr int kUnits = 256 / kSub;
   __shared__ float sums[kSub > 1 ? kSub : 1][kHalves][kSub > 1 ? kUnits : 1][kSub > 1 ? 9 : 1];
@@ -175,8 +175,13 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
   const bool here = i < total;
   const int64_t row = here ? i / units : 0, col = here ? (i - row * units) * 8 : 0;
   const bool live = here && col < e.cols;
-  float v[kHalves][8] = {}, r[8];
-  if (sub == 0) load_residual(e.dtype, e, live, row, col, r);
+  float v[kHalves][8] = {}, bias[2][8];
+  Residual<kType> residual;
+  if (sub == 0) {
+    load_bias(e.bias0, col, e.cols, bias[0]);
+    load_bias(e.bias1, col, e.cols, bias[1]);
+    residual.load(e, live, row, col);
+  }
   if (here) {
 #pragma unroll 4
     for (int s = sub; s < splits; s += kSub)
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[h][j] += sums[s][h][unit][j];
   }
-  finish(e.dtype, e, live, row, col, v[0], v[kHalves - 1], r);
+  finish<kType, kHalves>(e, live, row, col, v[0], v[kHalves - 1], bias[0], bias[1], residual);
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols) {
@@ -260,8 +265,16 @@ hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, end, part, part_ld, splits); };
-  if (end.halves == 2) return sub == 8 ? go(join_kernel<2, 8>) : go(join_kernel<2, 1>);
-  return sub == 8 ? go(join_kernel<1, 8>) : go(join_kernel<1, 1>);
+  auto type = [&](auto t) {
+    constexpr int kType = t;
+    if (end.halves == 2) return sub == 8 ? go(join_kernel<kType, 2, 8>) : go(join_kernel<kType, 2, 1>);
+    return sub == 8 ? go(join_kernel<kType, 1, 8>) : go(join_kernel<kType, 1, 1>);
+  };
+  switch (end.dtype) {
+    case POINTID_FP32: return type(std::integral_constant<int, POINTID_FP32>{});
+    case POINTID_BF16: return type(std::integral_constant<int, POINTID_BF16>{});
+  }
+  return type(std::integral_constant<int, POINTID_FP16>{});
 }
 
 }  // namespace pointid

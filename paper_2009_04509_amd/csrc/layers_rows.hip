@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
     const int row = i / kUnits, unit = i % kUnits, r = row < kM ? row : 0;
     const int64_t at = col0 + unit * 8;
     const bool here = row < kM && row < a.end.rows, live = here && at < a.end.cols;
-    float v[kHalves][8], residual[8];
+    float v[kHalves][8];
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
@@ -159,8 +159,12 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) store_partial(a.end, blockIdx.y, h, here, row, at, v[h]);
     } else {
-      load_residual(kType, a.end, live, row, at, residual);
-      finish(kType, a.end, live, row, at, v[0], v[kHalves - 1], residual);
+      float bias[2][8];
+      load_bias(a.end.bias0, at, a.end.cols, bias[0]);
+      load_bias(a.end.bias1, at, a.end.cols, bias[1]);
+      Residual<kType> residual;
+      residual.load(a.end, live, row, at);
+      finish<kType, kHalves>(a.end, live, row, at, v[0], v[kHalves - 1], bias[0], bias[1], residual);
     }
   }
 }
