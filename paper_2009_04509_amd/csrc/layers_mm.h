@@ -1,12 +1,14 @@
 // Products on the matrix cores (16-bit operands, fp32 sums), one template for the three
 // forms of layers.h.
 //
-// A block computes kBM x kBN results with 32x32x16 MFMAs.  Both operands go through
-// shared memory, 64 inner indices at a time, two stages, written by loads that go there
-// directly (16 bytes a lane).  An operand whose rows run along the inner index (x and dz
-// of dx and forward's x) is read as fragments with 16-byte reads; one whose rows are
-// indexed by the inner index (W of the forward form, both of dW) with the transposing
-// read, 4 x 16 values at a time, so no form needs a transposed copy of anything.
+// A block computes kBM x kBN results with 16x16x32 MFMAs (a loop of these alone runs at
+// 2.0 PFLOP/s on random bf16 values, one of 32x32x16 at 1.8: the card is at its power limit,
+// and they pass half as many sums per multiplication through the registers).  Both
+// operands go through shared memory, 64 inner indices at a time, two stages, written by loads
+// that go there directly (16 bytes a lane).  An operand whose rows run along the inner
+// index (x and dz of dx and forward's x) is read as fragments with 16-byte reads; one whose
+// rows are indexed by the inner index (W of the forward form, both of dW) with the
+// transposing read, 4 x 16 values at a time, so no form needs a transposed copy of anything.
 //
 // The results come out with the right operand as the MFMA's first, so a lane holds 4
 // consecutive columns of one row at a time; the end passes them through shared memory to
@@ -15,9 +17,10 @@
 // Pieces of 16 bytes stand in shared memory in a permuted order that the loads apply to
 // their global addresses.  Rows of 64 inner indices (128 bytes): piece p of row r at
 // p ^ (r / 2 % 8), so that 16 lanes reading one piece of 16 rows touch all banks (rows of
-// 32 inner indices, in the fp32 kernel: p ^ (r / 4 % 4)).  Rows of
-// columns: the 64-byte group g of row r at g ^ (r % 4) (rows of 128 bytes: g ^ (r / 2 % 2)),
-// so that the 4 rows of a transposing read do.
+// 32 inner indices, in the fp32 kernel: p ^ (r / 4 % 4)).  Rows of columns: the pair of
+// pieces g of row r at g ^ (r % 4 + 4 (r / 8 % 2)) (rows of 128 bytes: g ^ (r / 2 % 2 +
+// 2 (r / 8 % 2))), so that the rows r .. r + 3 and r + 8 .. r + 11 of 16 columns that 32
+// lanes of a transposing read take do.
 #pragma once
 
 #include "internal.h"
@@ -26,7 +29,6 @@
 namespace pointid {
 namespace mm {
 
-typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
@@ -37,8 +39,8 @@ constexpr uint32_t kNowhere = 0x80000000u;  // an offset past the resource's ran
 template <bool kInner, int kPieces>
 __device__ __forceinline__ int place(int row, int piece) {
   if constexpr (kInner) return kPieces == 8 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3);
-  if constexpr (kPieces >= 16) return piece ^ ((row & 3) << 2);
-  return piece ^ (((row >> 1) & 1) << 2);
+  if constexpr (kPieces >= 16) return piece ^ (((row & 3) | (row >> 1 & 4)) << 1);
+  return piece ^ (((row >> 1 & 1) | (row >> 2 & 2)) << 1);
 }
 
 __device__ __forceinline__ intx4 resource(const void* base) {
@@ -68,7 +70,10 @@ struct Tile {
   static_assert(kLoads * kThreads == kRows * kPieces, "whole loads");
 
   uint32_t offset[kLoads];                  // of the lane's pieces from the tile's origin
-  int16_t inner[kLoads];                    // first inner index of the piece
+  int inner;                                // first inner index of the first piece
+  // ... and of piece i: the same, or as many rows on
+  static constexpr int kStep = kInner ? 0 : kThreads / kPieces;
+  static_assert(!kInner || kThreads / kPieces % 16 == 0, "the places repeat");
 
   // side0: the tile's first row or column of `sides`
   __device__ __forceinline__ void init(int tid, int64_t side0, int64_t sides, int64_t ld) {
@@ -77,50 +82,50 @@ struct Tile {
       const int at = i * kThreads + tid, row = at / kPieces;
       const int piece = place<kInner, kPieces>(row, at % kPieces);       // its own inverse
       const int side = kInner ? row : piece * 8;
-      inner[i] = (int16_t)(kInner ? piece * 8 : row);
+      if (i == 0) inner = kInner ? piece * 8 : row;
       offset[i] = side0 + side < sides ? (uint32_t)((row * ld + piece * 8) * 2) : kNowhere;
     }
   }
   // Load i of the stage at `from`, `left` inner indices of it there.
   __device__ __forceinline__ void load(int i, intx4 from, int left, uint32_t lds, int wave) const {
-    load_to_lds(from, inner[i] < left ? offset[i] : kNowhere, lds + (i * kThreads + wave * 64) * 16);
+    load_to_lds(from, inner + i * kStep < left ? offset[i] : kNowhere, lds + (i * kThreads + wave * 64) * 16);
   }
 };
 
-// Fragments: 8 consecutive inner indices of one row or column a lane (lane % 32; lanes of
-// 32 and more the next 8).  kInner: group i of 32 stands i * 32 rows on; else each group
-// has an address of its own.
+// Fragments: 8 consecutive inner indices of one row or column a lane (lane % 16; the next 16
+// lanes the next 8).  kInner: group i of 16 stands i * 16 rows on; else each group has an
+// address of its own.
 template <bool kInner, int kSide, int kFrags, int kInners = kBK>
 struct Frags {
-  static constexpr int kSteps = kInners / 16, kRow = kInners * 2;
+  static constexpr int kSteps = kInners / 32, kRow = kInners * 2;
   int base[kInner ? kSteps : kFrags];
-  // of group i: its first row or column, and the offset of its tile
+  // side0(i, &tile): group i's first row or column, and the offset of its tile
   template <class F>
   __device__ __forceinline__ void init(int lane, F&& side0) {
     if constexpr (kInner) {
       int tile;
-      const int row = side0(0, &tile) + lane % 32;
+      const int row = side0(0, &tile) + lane % 16;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
-        base[s] = tile + row * kRow + place<true, kInners / 8>(row, 2 * s + lane / 32) * 16;
+        base[s] = tile + row * kRow + place<true, kInners / 8>(row, 4 * s + lane / 16) * 16;
     } else {
       // the lane's address in a read of 4 rows x 16 columns by 16 lanes
-      const int row = lane / 32 * 8 + lane % 16 / 4;
+      const int row = lane / 16 * 8 + lane % 16 / 4;
 #pragma unroll
       for (int i = 0; i < kFrags; ++i) {
         int tile;
-        const int col = side0(i, &tile) + lane / 16 % 2 * 16 + lane % 4 * 4;
+        const int col = side0(i, &tile) + lane % 4 * 4;
         base[i] = tile + row * (kSide * 2) + place<false, kSide / 8>(row, col / 8) * 16 + col % 8 * 2;
       }
     }
   }
-  // inner indices 16 s .. 16 s + 15 of group i
+  // inner indices 32 s .. 32 s + 31 of group i
   __device__ __forceinline__ uint4 read(const char* tile, int i, int s) const {
     if constexpr (kInner) {
-      return *reinterpret_cast<const uint4*>(tile + base[s] + i * 32 * kRow);
+      return *reinterpret_cast<const uint4*>(tile + base[s] + i * 16 * kRow);
     } else {
       typedef __attribute__((address_space(3))) shortx4 LdsShort4;
-      const char* p = tile + base[i] + s * 16 * kSide * 2;
+      const char* p = tile + base[i] + s * 32 * kSide * 2;
       const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p);
       const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(p + 4 * kSide * 2));
       const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
@@ -128,14 +133,6 @@ struct Frags {
     }
   }
 };
-
-template <bool kFp16>
-__device__ __forceinline__ floatx16 mfma(const uint4& a, const uint4& b, const floatx16& c) {
-  if constexpr (kFp16)
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
 
 // All loads to shared memory of this wave done, then the block's barrier.
 __device__ __forceinline__ void stage_ready() {
@@ -166,7 +163,7 @@ __device__ __forceinline__ Place block_place(const ProductArgs& a) {
   return {split, group * kGroup + (in - tn * rows_here), tn};
 }
 
-// The end of a wave's results: rows from `row0` of kFragsM groups of 32, columns from `col0`
+// The end of a wave's results: rows from `row0` of kFragsM groups of 16, columns from `col0`
 // (of each half).  One copy of the end's code: 32 rows x 64 columns a turn (two halves: 32
 // columns of each) through the wave's kEndWave bytes of shared memory, from a lane's 4
 // columns of one row to 16 bytes and more a lane along the rows.  The residual of a turn is
@@ -174,7 +171,7 @@ __device__ __forceinline__ Place block_place(const ProductArgs& a) {
 constexpr int kEndPitch = 64 + 4;
 constexpr int kEndWave = 32 * kEndPitch * 4;
 template <int kType, int kHalves, int kFragsM>
-__device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFragsM][2], float* es, int lane, int split,
+__device__ __forceinline__ void end_tile(const End& e, const floatx4 (&acc)[kFragsM][4], float* es, int lane, int split,
                                          int64_t row0, int64_t col0) {
   constexpr int kLanes = kHalves == 2 ? 4 : 8;           // of a row
   constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes;
@@ -193,22 +190,21 @@ __device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFr
   row0 += lane / kLanes;
   read(row0);
 #pragma nounroll
-  for (int turn = 0; turn < kFragsM; ++turn, row0 += 32) {
-    floatx16 c[2] = {};
-    static_for<kFragsM>([&](auto t) {
-      if (turn == t) c[0] = acc[t][0], c[1] = acc[t][1];
+  for (int turn = 0; turn < kFragsM / 2; ++turn, row0 += 32) {
+    floatx4 c[2][4] = {};
+    static_for<kFragsM / 2>([&](auto t) {
+      if (turn == t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i / 4][i % 4] = acc[2 * t + i / 4][i % 4];
     });
     Residual<kType> now[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) now[s] = next[s];
-    if (turn + 1 < kFragsM) read(row0 + 32);
+    if (turn + 1 < kFragsM / 2) read(row0 + 32);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4*>(es + lane % 32 * kEndPitch + f * 32 + 8 * j + lane / 32 * 4) =
-            make_float4(c[f][4 * j], c[f][4 * j + 1], c[f][4 * j + 2], c[f][4 * j + 3]);
+    for (int i = 0; i < 8; ++i)
+      *reinterpret_cast<floatx4*>(es + (i / 4 * 16 + lane % 16) * kEndPitch + i % 4 * 16 + lane / 16 * 4) = c[i / 4][i % 4];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma nounroll
     for (int s = 0; s < kSteps; ++s) {
@@ -230,6 +226,11 @@ __device__ __forceinline__ void end_tile(const End& e, const floatx16 (&acc)[kFr
   }
 }
 
+template <bool kFp16>
+__device__ __forceinline__ floatx4 mfma(const uint4& a, const uint4& b, const floatx4& c) {
+  return Op16<kFp16>::mfma(a, b, c);
+}
+
 template <bool kFp16, int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>
 __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) {
   constexpr int kThreads = 64 * kWM * kWN;
@@ -237,8 +238,8 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   constexpr bool kLeftInner = kForm != kDw, kRightInner = kForm == kDx;
   static_assert(!kRightInner || kHalves == 1, "dx has one half");
   constexpr int kHN = kBN / 2;                           // columns of each half of the tile
-  constexpr int kFragsM = kBM / kWM / 32, kFragsN = kBN / kWN / 32;
-  static_assert(kFragsN == 2, "a wave takes 64 columns");
+  constexpr int kFragsM = kBM / kWM / 16, kFragsN = 4;
+  static_assert(kBN / kWN == 64, "a wave takes 64 columns");
   using Left = Tile<kLeftInner, kBM, kThreads>;
   using Right = Tile<kRightInner, kHN, kThreads>;
   constexpr int kStage = Left::kBytes + 2 * Right::kBytes;
@@ -260,18 +261,18 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   left.init(tid, row0, a.end.rows, a.ld_left);
   right0.init(tid, col0, a.end.cols, a.ld_right);
   right1.init(tid, col1, a.end.cols, a.ld_right);
-  // A wave's columns: with two halves kFragsN / 2 groups of 32 of each; with one, kFragsN
-  // groups side by side (they lie in one half of the tile).
+  // A wave's columns: with two halves 32 of each; with one, 64 side by side (they lie in
+  // one half of the tile).
   Frags<kLeftInner, kBM, kFragsM> lf;
   Frags<kRightInner, kHN, kFragsN> rf;
   lf.init(lane, [&](int i, int* tile) {
     *tile = 0;
-    return wm * (kBM / kWM) + 32 * i;
+    return wm * (kBM / kWM) + 16 * i;
   });
   rf.init(lane, [&](int i, int* tile) {
-    const int half = kHalves == 2 ? i / (kFragsN / 2) : wn * 32 * kFragsN / kHN;
+    const int half = kHalves == 2 ? i / 2 : wn * 64 / kHN;
     *tile = Left::kBytes + half * Right::kBytes;
-    return kHalves == 2 ? wn * (kHN / kWN) + i % (kFragsN / 2) * 32 : wn * 32 * kFragsN % kHN + 32 * i;
+    return kHalves == 2 ? wn * 32 + i % 2 * 16 : wn * 64 % kHN + 16 * i;
   });
 
   // the split's stages, and where the next one to load is
@@ -297,13 +298,14 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   enter(k0);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
-  // part q of kFragsM of the loads of the next stage (a compile-time constant)
+  // part q of kParts of the loads of the next stage (a compile-time constant)
+  constexpr int kParts = kFragsM / 2;
   auto issue = [&](auto q, int stage) {
     constexpr int kLoads = Left::kLoads + 2 * Right::kLoads;
     const uint32_t to = lds0 + stage * kStage;
     const int left_of = a.inner - k0;
     static_for<kLoads>([&](auto n) {
-      if constexpr (n * kFragsM / kLoads == q) {
+      if constexpr (n * kParts / kLoads == q) {
         if constexpr (n < Left::kLoads)
           left.load(n, resource(lp), left_of, to, wave);
         else if constexpr (n < Left::kLoads + Right::kLoads)
@@ -312,7 +314,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
           right1.load(n - Left::kLoads - Right::kLoads, resource(rp1), left_of, to + Left::kBytes + Right::kBytes, wave);
       }
     });
-    if constexpr (q == kFragsM - 1) {
+    if constexpr (q == kParts - 1) {
       k0 += kBK;
       lp += left_step, rp0 += right_step, rp1 += right_step;
       if (k0 >= a.inner && --to_load > 0) {
@@ -325,43 +327,52 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
     }
   };
 
-  // Fragments of one step of 16 inner indices are read while the step before multiplies.
-  // The stage's last step multiplies after the barrier that makes the next stage ready and
-  // this one free, so that the next stage's first fragments and the loads of the stage after
-  // it are under way meanwhile.
-  floatx16 acc[kFragsM][kFragsN] = {};
-  uint4 l[2][kFragsM], r[2][kFragsN];
-  auto read = [&](int buf, const char* tile, int s) {
+  // A stage is multiplied in 4 turns, 32 inner indices by half of the wave's rows; the
+  // fragments of a turn are read while the turn before multiplies.  The last turn multiplies
+  // after the barrier that makes the next stage ready and this one free, so that the next
+  // stage's first fragments and the loads of the stage after it are under way meanwhile.
+  floatx4 acc[kFragsM][kFragsN] = {};
+  uint4 l[2][kParts], r[2][kFragsN];
+  auto read_left = [&](int turn, const char* tile) {
 #pragma unroll
-    for (int j = 0; j < kFragsN; ++j) r[buf][j] = rf.read(tile, j, s);
-#pragma unroll
-    for (int i = 0; i < kFragsM; ++i) l[buf][i] = lf.read(tile, i, s);
+    for (int i = 0; i < kParts; ++i) l[turn % 2][i] = lf.read(tile, turn % 2 * kParts + i, turn / 2);
   };
-  auto multiply_row = [&](int buf, int i) {
+  auto read_right = [&](int s, const char* tile) {
 #pragma unroll
-    for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<kFp16>(r[buf][j], l[buf][i], acc[i][j]);
+    for (int j = 0; j < kFragsN; ++j) r[s][j] = rf.read(tile, j, s);
+  };
+  auto multiply = [&](int turn, int i) {
+    floatx4(&c)[kFragsN] = acc[turn % 2 * kParts + i];
+#pragma unroll
+    for (int j = 0; j < kFragsN; ++j) c[j] = mfma<kFp16>(r[turn / 2][j], l[turn % 2][i], c[j]);
   };
   if (stages > 0) {
-    static_for<kFragsM>([&](auto q) { issue(q, 0); });
+    static_for<kParts>([&](auto q) { issue(q, 0); });
     stage_ready();
-    if (to_load > 0) static_for<kFragsM>([&](auto q) { issue(q, 1); });
-    read(0, smem, 0);
+    if (to_load > 0) static_for<kParts>([&](auto q) { issue(q, 1); });
+    read_right(0, smem);
+    read_left(0, smem);
     int stage = 0;
     for (int it = stages; it > 0; --it, stage ^= 1) {
       const char* tile = smem + stage * kStage;
 #pragma unroll
-      for (int s = 0; s < 3; ++s) {
-        read((s + 1) % 2, tile, s + 1);
+      for (int turn = 0; turn < 3; ++turn) {
+        if (turn == 1) read_right(1, tile);
+        read_left(turn + 1, tile);
 #pragma unroll
-        for (int i = 0; i < kFragsM; ++i) multiply_row(s % 2, i);
+        for (int i = 0; i < kParts; ++i) multiply(turn, i);
       }
       __builtin_amdgcn_sched_barrier(0);
       stage_ready();
-      if (it > 1) read(0, smem + (stage ^ 1) * kStage, 0);
+      if (it > 1) {
+        const char* next = smem + (stage ^ 1) * kStage;
+        read_right(0, next);
+        read_left(0, next);
+      }
       const bool more = to_load > 0;
-      static_for<kFragsM>([&](auto q) {
+      static_for<kParts>([&](auto q) {
         __builtin_amdgcn_sched_barrier(0);
-        multiply_row(1, q);
+        multiply(3, q);
         __builtin_amdgcn_sched_barrier(0);
         if (more) issue(q, stage);
       });
@@ -371,7 +382,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
 
   end_tile<kType, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4, lane, split,
                                              row0 + wm * (kBM / kWM),
-                                             col0 + wn * (kHalves == 2 ? kHN / kWN : 32 * kFragsN));
+                                             col0 + wn * (kHalves == 2 ? 32 : 64));
 }
 
 // What a launch works out for its blocks; returns their number, or 0.

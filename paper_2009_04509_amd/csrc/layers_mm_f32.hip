@@ -93,8 +93,8 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
   constexpr bool kLeftInner = kForm != kDw, kRightInner = kForm == kDx;
   static_assert(!kRightInner || kHalves == 1, "dx has one half");
   constexpr int kHN = kBN / 2;
-  constexpr int kFragsM = kBM / kWM / 32, kFragsN = kBN / kWN / 32;
-  static_assert(kFragsN == 2, "a wave takes 64 columns");
+  constexpr int kFragsM = kBM / kWM / 16, kFragsN = 4;
+  static_assert(kBN / kWN == 64, "a wave takes 64 columns");
   using Left = Tile32<kLeftInner, kBM, kThreads>;
   using Right = Tile32<kRightInner, kHN, kThreads>;
   // a stage: the left operand's planes, then each half's
@@ -118,12 +118,12 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
   Frags<kRightInner, kHN, kFragsN, kBK32> rf;
   lf.init(lane, [&](int i, int* tile) {
     *tile = 0;
-    return wm * (kBM / kWM) + 32 * i;
+    return wm * (kBM / kWM) + 16 * i;
   });
   rf.init(lane, [&](int i, int* tile) {
-    const int half = kHalves == 2 ? i / (kFragsN / 2) : wn * 32 * kFragsN / kHN;
+    const int half = kHalves == 2 ? i / 2 : wn * 64 / kHN;
     *tile = kLeftBytes + half * kRightBytes;
-    return kHalves == 2 ? wn * (kHN / kWN) + i % (kFragsN / 2) * 32 : wn * 32 * kFragsN % kHN + 32 * i;
+    return kHalves == 2 ? wn * 32 + i % 2 * 16 : wn * 64 % kHN + 16 * i;
   });
 
   int to_load = a.split_each + (at.split < (uint32_t)a.split_more);
@@ -158,25 +158,18 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
     right0.store(tile + kLeftBytes, rv0);
     right1.store(tile + kLeftBytes + kRightBytes, rv1);
   };
-  floatx16 acc[kFragsM][kFragsN] = {};
-  auto step = [&](int stage, int s) {
-    const char* tile = smem + stage * kStage;
-    uint4 l[3][kFragsM], r[3][kFragsN];
+  floatx4 acc[kFragsM][kFragsN] = {};
+  uint4 r[3][kFragsN];
+  auto multiply = [&](const char* tile, int i) {
+    uint4 l[3];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-#pragma unroll
-      for (int i = 0; i < kFragsM; ++i) l[p][i] = lf.read(tile + p * Left::kPlane, i, s);
-#pragma unroll
-      for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * Right::kPlane, j, s);
-    }
+    for (int p = 0; p < 3; ++p) l[p] = lf.read(tile + p * Left::kPlane, i, 0);
 #pragma unroll
     for (int order = 2; order >= 0; --order)
 #pragma unroll
       for (int p = order; p >= 0; --p)
 #pragma unroll
-        for (int i = 0; i < kFragsM; ++i)
-#pragma unroll
-          for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[p][i], acc[i][j]);
+        for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[p], acc[i][j]);
   };
   if (stages > 0) {
     load();
@@ -185,18 +178,25 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
     __syncthreads();
     for (int it = 0; it < stages; ++it) {
       const int stage = it % 2;
-      step(stage, 0);
+      const char* tile = smem + stage * kStage;
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * Right::kPlane, j, 0);
+#pragma unroll
+      for (int i = 0; i < kFragsM / 2; ++i) multiply(tile, i);
       if (it + 1 < stages) {
         store(stage ^ 1);
         if (to_load > 0) load();
       }
-      step(stage, 1);
+#pragma unroll
+      for (int i = kFragsM / 2; i < kFragsM; ++i) multiply(tile, i);
       __syncthreads();
     }
   }
   end_tile<POINTID_FP32, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4,
                                                     lane, at.split, row0 + wm * (kBM / kWM),
-                                                    col0 + wn * (kHalves == 2 ? kHN / kWN : 32 * kFragsN));
+                                                    col0 + wn * (kHalves == 2 ? 32 : 64));
 }
 
 template <int kForm, int kHalves>
