@@ -134,9 +134,13 @@ struct Frags {
   }
 };
 
-// All loads to shared memory of this wave done, then the block's barrier.
+// All reads and loads of this wave done, then the block's barrier.  The reads' wait is the
+// compiler's own instruction, so that it does not wait for them again afterwards; of the
+// loads to shared memory it knows nothing.
 __device__ __forceinline__ void stage_ready() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0)
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // The block's tile and split.
@@ -361,8 +365,8 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
         read_left(turn + 1, tile);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) multiply(turn, i);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_barrier(0);
       stage_ready();
       if (it > 1) {
         const char* next = smem + (stage ^ 1) * kStage;
