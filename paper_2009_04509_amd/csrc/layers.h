@@ -115,21 +115,37 @@ hipError_t launch_product_f32(Form form, const ProductPlan& plan, ProductArgs a,
 hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld, int splits, hipStream_t stream);
 
 // ---- layers_pass.hip: passes over one matrix
-// A matrix copied to rows of `ld` values (a multiple of 8), zero past its columns.
-hipError_t launch_layers_copy(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, void* out,
-                              int64_t ld, hipStream_t stream);
-// A checkpoint's values as 16-bit (dtype) or fp32 values [rows][ld], zero past the columns up to ld.
+// What the products take from scratch: a matrix copied to rows of `ld` values (a multiple of
+// 8), zero past its columns, or a checkpoint's values laid out so; and the column sums of a
+// gradient, from the sums of its blocks of rows (ld_src values from one to the next).
+struct FillJob {
+  enum Kind { kCopy = 0, kLoad = 1, kSums = 2 };
+  int32_t kind;
+  int32_t dtype;
+  const void* src;             // kCopy: the matrix; kSums: the blocks' sums
+  int64_t ld_src;
+  Packed8 packed;              // kLoad
+  int64_t rows, cols;          // kSums: blocks, columns
+  void* out;
+  int64_t ld;
+  uint32_t first;              // set by the launch: the job's first block
+};
+struct FillJobs {
+  FillJob job[5];
+  int32_t count;
+};
+hipError_t launch_layers_fill(FillJobs jobs, hipStream_t stream);
+// A checkpoint's values as a matrix.
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
-                                  int64_t fill_to, hipStream_t stream);
+                                  hipStream_t stream);
 hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
                                   const Packed8& out, hipStream_t stream);
 hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols, hipStream_t stream);
 // The gradient before the activation, and its column sums.
 //   dense: dz = dy act'(z) (z absent: dy)     gated: dg = dy u act'(g), du = dy act(g)
 // parts: 0 none written, 1 or 2 planes of the 16-bit type (2: value and remainder),
-// -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each
-// block of kGradRows rows, or nullptr.
-constexpr int kGradRows = 32;
+// -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each block of rows, or
+// nullptr.
 struct GradArgs {
   const void* dy;
   int64_t ld_dy;
@@ -143,9 +159,8 @@ struct GradArgs {
   int64_t ld, plane;
   float* col_part;
 };
-hipError_t launch_layers_grad(const GradArgs& a, hipStream_t stream);
-// out[i] = sum over blocks of col_part[block][half][i], for each half whose out is given
-hipError_t launch_layers_colsum(const float* col_part, int64_t blocks, int64_t cols, int halves, float* out0,
-                                float* out1, hipStream_t stream);
+// Rows of a block: 32, or 8 where that gives fewer than two blocks a CU.
+int grad_rows(int64_t rows, int64_t cols, int cus);
+hipError_t launch_layers_grad(const GradArgs& a, int block_rows, hipStream_t stream);
 
 }  // namespace pointid

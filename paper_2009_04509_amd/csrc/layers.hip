@@ -204,18 +204,24 @@ struct Source {
     planes.ld = round_up(c, 8);
     call.want(&made, (size_t)size_of(dtype) * r * planes.ld);
   }
-  int make(Call& call) {
-    if (in_place) return POINTID_OK;
+  // The operand as it will stand, and the job that makes it so.
+  void make(FillJobs* jobs) {
+    if (in_place) return;
     planes.base = made;
-    if (!from.matrix)
-      return call.run("layers_load", false, [&] {
-        return launch_checkpoint_load(from.packed, rows, cols, dtype, made, planes.ld, planes.ld, call.stream());
-      });
-    return call.run("layers_copy", false, [&] {
-      return launch_layers_copy(from.matrix, from.ld, dtype, rows, cols, made, planes.ld, call.stream());
-    });
+    FillJob& j = jobs->job[jobs->count++];
+    j.kind = from.matrix ? FillJob::kCopy : FillJob::kLoad;
+    j.dtype = dtype;
+    j.src = from.matrix, j.ld_src = from.ld;
+    j.packed = from.packed;
+    j.rows = rows, j.cols = cols;
+    j.out = made, j.ld = planes.ld;
   }
 };
+
+int run_fill(Call& call, const FillJobs& jobs, bool last) {
+  if (jobs.count == 0) return POINTID_OK;
+  return call.run("layers_fill", last, [&] { return launch_layers_fill(jobs, call.stream()); });
+}
 
 // The weights of one or both halves: these share a pitch, so that where one is copied, so
 // is the other.
@@ -345,8 +351,12 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   float* part = nullptr;
   call.want(&part, part_bytes(plan.splits, e));
   int rc = call.reserve();
-  if (rc == POINTID_OK) rc = sx.make(call);
-  for (int h = 0; h < f.halves && rc == POINTID_OK; ++h) rc = sw[h].make(call);
+  if (rc != POINTID_OK) return rc;
+  FillJobs jobs;
+  std::memset(&jobs, 0, sizeof(jobs));
+  sx.make(&jobs);
+  for (int h = 0; h < f.halves; ++h) sw[h].make(&jobs);
+  rc = run_fill(call, jobs, false);
   if (rc != POINTID_OK) return rc;
   ProductArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -413,7 +423,8 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   g.plane = b.m * g.ld;
   const size_t dz_bytes = g.parts < 0 ? 4 * (size_t)g.plane : 2 * (size_t)g.plane * g.parts;
   for (int h = 0; h < b.halves && g.parts != 0; ++h) call.want(&g.out[h], dz_bytes);
-  const int64_t grad_blocks = (b.m + kGradRows - 1) / kGradRows;
+  const int block_rows = grad_rows(b.m, b.n, l->cus);
+  const int64_t grad_blocks = (b.m + block_rows - 1) / block_rows;
   if (want_db) call.want(&g.col_part, sizeof(float) * (size_t)(grad_blocks * b.halves * b.n));
 
   // x for dW, the weights for dx
@@ -439,18 +450,26 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   if (rc != POINTID_OK) return rc;
 
   if (g.parts != 0 || want_db) {
-    rc = call.run("layers_grad", false, [&] { return launch_layers_grad(g, stream); });
-    if (rc == POINTID_OK && want_db)
-      rc = call.run("layers_colsum", !products, [&] {
-        return launch_layers_colsum(g.col_part, grad_blocks, b.n, b.halves, b.db[0], b.db[1], stream);
-      });
+    rc = call.run("layers_grad", false, [&] { return launch_layers_grad(g, block_rows, stream); });
     if (rc != POINTID_OK) return rc;
   }
+  FillJobs jobs;
+  std::memset(&jobs, 0, sizeof(jobs));
+  for (int h = 0; h < b.halves; ++h) {
+    if (!b.db[h]) continue;
+    FillJob& j = jobs.job[jobs.count++];
+    j.kind = FillJob::kSums;
+    j.src = g.col_part + h * b.n, j.ld_src = b.halves * b.n;
+    j.rows = grad_blocks, j.cols = b.n;
+    j.out = b.db[h];
+  }
+  for (int h = 0; h < b.halves && want_dx; ++h) sw[h].make(&jobs);
+  if (want_dw) sx.make(&jobs);
+  rc = run_fill(call, jobs, !products);
+  if (rc != POINTID_OK) return rc;
   for (int h = 0; h < 2; ++h) dz[h].base = read_dy ? b.dy.data : g.out[h];
 
   if (want_dx) {
-    for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = sw[h].make(call);
-    if (rc != POINTID_OK) return rc;
     ProductArgs a;
     std::memset(&a, 0, sizeof(a));
     for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = add_terms(&a, dz[h], sw[h].planes, nullptr);
@@ -463,8 +482,6 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
     if (rc != POINTID_OK) return rc;
   }
   if (!want_dw) return POINTID_OK;
-  rc = sx.make(call);
-  if (rc != POINTID_OK) return rc;
   ProductArgs a;
   std::memset(&a, 0, sizeof(a));
   rc = add_terms(&a, sx.planes, dz[0], b.halves == 2 ? &dz[1] : nullptr);
@@ -680,7 +697,7 @@ int pointid_checkpoint_load(int dtype, int64_t rows, int64_t cols, const pointid
     TRY(check_checkpoint_call(dtype, rows, cols, out, in));
     if (rows == 0) return (int)POINTID_OK;
     const pointid_matrix a = matrix_of(out, rows, cols);
-    const hipError_t e = launch_checkpoint_load({in->codes, in->exponents}, rows, cols, dtype, a.data, a.ld, cols,
+    const hipError_t e = launch_checkpoint_load({in->codes, in->exponents}, rows, cols, dtype, a.data, a.ld,
                                                 static_cast<hipStream_t>(stream));
     return e == hipSuccess ? (int)POINTID_OK : hip_fail(e, "checkpoint load launch");
   });

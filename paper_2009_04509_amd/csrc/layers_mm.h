@@ -143,6 +143,13 @@ __device__ __forceinline__ void stage_ready() {
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// All but the newest kCount loads to shared memory of this wave done, then the block's barrier.
+template <int kCount>
+__device__ __forceinline__ void loads_left() {
+  static_assert(kCount < 16, "one field of the wait");
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kCount) : "memory");
+}
+
 // The block's tile and split.
 struct Place {
   uint32_t split;
@@ -352,8 +359,12 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   };
   if (stages > 0) {
     static_for<kParts>([&](auto q) { issue(q, 0); });
-    stage_ready();
-    if (to_load > 0) static_for<kParts>([&](auto q) { issue(q, 1); });
+    if (to_load > 0) {
+      static_for<kParts>([&](auto q) { issue(q, 1); });
+      loads_left<Left::kLoads + 2 * Right::kLoads>();      // the second stage's
+    } else {
+      loads_left<0>();
+    }
     read_right(0, smem);
     read_left(0, smem);
     int stage = 0;

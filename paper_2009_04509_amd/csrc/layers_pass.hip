@@ -7,38 +7,64 @@
 namespace pointid {
 namespace {
 
-__device__ __forceinline__ void store8(uint16_t* p, const uint16_t* h) {      // 16-byte aligned
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = (uint32_t)h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// the thread's piece of 8 columns, grid-strided over rows x pieces
+// Pieces of 8 columns of a row, from piece `first` on, every `step`-th.
 template <class F>
-__device__ __forceinline__ void each_piece(int64_t rows, int64_t pieces, F&& f) {
-  const int64_t total = rows * pieces, step = (int64_t)gridDim.x * blockDim.x;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step) {
+__device__ __forceinline__ void each_piece(int64_t rows, int64_t pieces, int64_t first, int64_t step, F&& f) {
+  const int64_t total = rows * pieces;
+  for (int64_t i = first; i < total; i += step) {
     const int64_t row = total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)pieces) : i / pieces;
     f(row, (i - row * pieces) * 8);
   }
 }
 
-__global__ void __launch_bounds__(256) copy_kernel(const void* src, int64_t ld_src, int dtype, int64_t rows,
-                                                   int64_t cols, void* out, int64_t ld) {
-  each_piece(rows, ld / 8, [&](int64_t row, int64_t col) {
+__global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64_t rows, int64_t cols, int dtype,
+                                                              void* out, int64_t ld) {
+  each_piece(rows, (cols + 7) / 8, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256,
+             [&](int64_t row, int64_t col) {
     float v[8];
-    load_cols<8>(src, row * ld_src + col, dtype, cols - col, v);
-    store_cols<8>(out, row * ld + col, dtype, 8, v);
+    load_codes(src, row, col, cols, v);
+    store_cols<8>(out, row * ld + col, dtype, cols - col, v);
   });
 }
 
-__global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64_t rows, int64_t cols, int dtype,
-                                                              void* out, int64_t ld, int64_t fill_to) {
-  each_piece(rows, (fill_to + 7) / 8, [&](int64_t row, int64_t col) {
+// Sums of `blocks` rows of 32 columns from `col` on, every `pitch` values: 8 lanes a column.
+__device__ __forceinline__ void sum_columns(const float* part, int64_t blocks, int64_t pitch, int64_t col, int64_t cols,
+                                            float* out) {
+  __shared__ float sums[8][33];
+  const int c = threadIdx.x % 32, sub = threadIdx.x / 32;
+  float t = 0.f;
+  if (col + c < cols)
+#pragma unroll 4
+    for (int64_t b = sub; b < blocks; b += 8) t += part[b * pitch + col + c];
+  sums[sub][c] = t;
+  __syncthreads();
+  if (sub != 0 || col + c >= cols) return;
+  float v = 0.f;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) v += sums[s][c];
+  out[col + c] = v;
+}
+
+// The jobs that stand between the gradient and the products, by one launch: each takes the
+// blocks from its first to the next job's.
+__global__ void __launch_bounds__(256) fill_kernel(FillJobs a) {
+  int j = 0;
+  while (j + 1 < a.count && blockIdx.x >= a.job[j + 1].first) ++j;
+  const FillJob& job = a.job[j];
+  const uint32_t block = blockIdx.x - job.first, blocks = (j + 1 < a.count ? a.job[j + 1].first : gridDim.x) - job.first;
+  if (job.kind == FillJob::kSums) {
+    sum_columns(static_cast<const float*>(job.src), job.rows, job.ld_src, (int64_t)block * 32, job.cols,
+                static_cast<float*>(job.out));
+    return;
+  }
+  each_piece(job.rows, job.ld / 8, (int64_t)block * 256 + threadIdx.x, (int64_t)blocks * 256,
+             [&](int64_t row, int64_t col) {
     float v[8] = {};
-    if (col < cols) load_codes(src, row, col, cols, v);
-    store_cols<8>(out, row * ld + col, dtype, fill_to - col, v);
+    if (job.kind == FillJob::kCopy)
+      load_cols<8>(job.src, row * job.ld_src + col, job.dtype, job.cols - col, v);
+    else if (col < job.cols)
+      load_codes(job.packed, row, col, job.cols, v);
+    store_cols<8>(job.out, row * job.ld + col, job.dtype, 8, v);
   });
 }
 
@@ -59,16 +85,16 @@ __global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, i
   }
 }
 
-// Each block: kGradRows rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time,
-// two such turns' reads in flight.
-template <int kHalves>
+// Each block: 8 kTurns rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time, two
+// such turns' reads in flight.
+template <int kHalves, int kTurns>
 __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
   __shared__ float sums[8][256 + 8];
   const int piece = threadIdx.x % 32, sub = threadIdx.x / 32;
   const int64_t col = (int64_t)blockIdx.y * 256 + piece * 8, n = a.cols - col;
-  const int64_t row0 = (int64_t)blockIdx.x * kGradRows + sub;
+  const int64_t row0 = (int64_t)blockIdx.x * (8 * kTurns) + sub;
   float total[kHalves][8] = {};
-  constexpr int kTurns = kGradRows / 8, kAhead = 2;
+  constexpr int kAhead = kTurns < 2 ? kTurns : 2;
   if (n > 0) {
     for (int s = 0; s < kTurns; s += kAhead) {
       float dy[kAhead][8], z[kAhead][2][8];
@@ -113,16 +139,19 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
             store_cols<8>(a.out[h], row * a.ld + col, POINTID_FP32, 8, d[h]);
             continue;
           }
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack16(d[h][2 * i], d[h][2 * i + 1], a.dtype);
           uint16_t* o = static_cast<uint16_t*>(a.out[h]) + row * a.ld + col;
-          uint16_t p[2][8];
+          *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+          if (a.parts < 2) continue;
+          float rest[8];                               // none beside an infinity or NaN
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            p[0][i] = to16(d[h][i], a.dtype);
-            const float rest = d[h][i] - from16(p[0][i], a.dtype);
-            p[1][i] = (__float_as_uint(rest) & 0x7FFFFFFFu) < 0x7F800000u ? to16(rest, a.dtype) : 0;
+            rest[i] = d[h][i] - from16((uint16_t)(w[i / 2] >> (16 * (i % 2))), a.dtype);
+            if ((__float_as_uint(rest[i]) & 0x7FFFFFFFu) >= 0x7F800000u) rest[i] = 0.f;
           }
-          store8(o, p[0]);
-          if (a.parts >= 2) store8(o + a.plane, p[1]);
+          store_cols<8>(o + a.plane, 0, a.dtype, 8, rest);
         }
       }
     }
@@ -140,26 +169,6 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
     if (c < a.cols) a.col_part[((int64_t)blockIdx.x * kHalves + h) * a.cols + c] = t;
     __syncthreads();
   }
-}
-
-// Sums of `blocks` rows of the columns of a half (blockIdx.y): 32 columns by 8 lanes of blocks.
-__global__ void __launch_bounds__(256) colsum_kernel(const float* part, int64_t blocks, int64_t cols, float* out0,
-                                                     float* out1) {
-  __shared__ float sums[8][33];
-  const int c = threadIdx.x % 32, sub = threadIdx.x / 32;
-  const int64_t col = (int64_t)blockIdx.x * 32 + c;
-  float* out = blockIdx.y ? out1 : out0;
-  if (!out) return;
-  float t = 0.f;
-  if (col < cols)
-    for (int64_t b = sub; b < blocks; b += 8) t += part[(b * gridDim.y + blockIdx.y) * cols + col];
-  sums[sub][c] = t;
-  __syncthreads();
-  if (sub != 0 || col >= cols) return;
-  float v = 0.f;
-#pragma unroll
-  for (int s = 0; s < 8; ++s) v += sums[s][c];
-  out[col] = v;
 }
 
 // Units of 8 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
@@ -223,16 +232,21 @@ unsigned pass_blocks(int64_t items) {
 
 }  // namespace
 
-hipError_t launch_layers_copy(const void* src, int64_t ld_src, int dtype, int64_t rows, int64_t cols, void* out,
-                              int64_t ld, hipStream_t stream) {
-  return launch_kernel(copy_kernel, dim3(pass_blocks(rows * (ld / 8))), dim3(256), 0, stream, src, ld_src, dtype, rows,
-                       cols, out, ld);
+hipError_t launch_layers_fill(FillJobs jobs, hipStream_t stream) {
+  uint32_t blocks = 0;
+  for (int j = 0; j < jobs.count; ++j) {
+    FillJob& job = jobs.job[j];
+    job.first = blocks;
+    blocks += job.kind == FillJob::kSums ? (uint32_t)((job.cols + 31) / 32) : pass_blocks(job.rows * (job.ld / 8));
+  }
+  if (blocks == 0) return hipSuccess;
+  return launch_kernel(fill_kernel, dim3(blocks), dim3(256), 0, stream, jobs);
 }
 
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
-                                  int64_t fill_to, hipStream_t stream) {
-  return launch_kernel(checkpoint_load_kernel, dim3(pass_blocks(rows * ((fill_to + 7) / 8))), dim3(256), 0, stream, src,
-                       rows, cols, dtype, out, ld, fill_to);
+                                  hipStream_t stream) {
+  return launch_kernel(checkpoint_load_kernel, dim3(pass_blocks(rows * ((cols + 7) / 8))), dim3(256), 0, stream, src,
+                       rows, cols, dtype, out, ld);
 }
 
 hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
@@ -241,17 +255,16 @@ hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_
                        src, ld, dtype, rows, cols, out);
 }
 
-hipError_t launch_layers_grad(const GradArgs& a, hipStream_t stream) {
-  const int64_t width = a.parts != 0 && a.ld > a.cols ? a.ld : a.cols;
-  const dim3 grid((unsigned)((a.rows + kGradRows - 1) / kGradRows), (unsigned)((width + 255) / 256));
-  return a.halves == 2 ? launch_kernel(grad_kernel<2>, grid, dim3(256), 0, stream, a)
-                       : launch_kernel(grad_kernel<1>, grid, dim3(256), 0, stream, a);
+int grad_rows(int64_t rows, int64_t cols, int cus) {
+  return ((rows + 31) / 32) * ((cols + 255) / 256) < 2 * cus ? 8 : 32;
 }
 
-hipError_t launch_layers_colsum(const float* col_part, int64_t blocks, int64_t cols, int halves, float* out0,
-                                float* out1, hipStream_t stream) {
-  return launch_kernel(colsum_kernel, dim3((unsigned)((cols + 31) / 32), (unsigned)halves), dim3(256), 0, stream,
-                       col_part, blocks, cols, out0, out1);
+hipError_t launch_layers_grad(const GradArgs& a, int block_rows, hipStream_t stream) {
+  const int64_t width = a.parts != 0 && a.ld > a.cols ? a.ld : a.cols;
+  const dim3 grid((unsigned)((a.rows + block_rows - 1) / block_rows), (unsigned)((width + 255) / 256));
+  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, a); };
+  if (block_rows == 8) return a.halves == 2 ? go(grad_kernel<2, 1>) : go(grad_kernel<1, 1>);
+  return a.halves == 2 ? go(grad_kernel<2, 4>) : go(grad_kernel<1, 4>);
 }
 
 hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols, hipStream_t stream) {
