@@ -38,7 +38,7 @@ struct Kept {
   void* matrix;
   int64_t ld;
   Packed8 packed;
-  bool any() const { return matrix || packed.codes; }
+  __host__ __device__ bool any() const { return matrix || packed.codes; }
 };
 
 enum EndMode { kEndDense = 0, kEndGated = 1, kEndStore = 2, kEndPartial = 3 };

@@ -181,12 +181,11 @@ __device__ __forceinline__ void load_codes(const Packed8& s, int64_t row, int64_
   unpack8(w[1], p, v + 4);
 }
 
-// 8 values of a row from column `col` (a multiple of 8) to a checkpoint.  The 4 lanes of
-// an aligned group hold a block of 32 and all call this.  `live`: the row and column
-// exist.  Columns past `cols` do not count and are not written.
-__device__ __forceinline__ void save_codes(const Packed8& d, bool live, int64_t row, int64_t col, int64_t cols,
-                                           const float* v) {
-  const int64_t n = cols - col;
+// 8 values of a row (of which the first n exist) to a checkpoint's codes at `c`, and by the
+// first lane of a block its exponent to `x`.  The 4 lanes of an aligned group hold a block
+// of 32 and all call this; values that do not exist do not count and are not written.
+// `live`: the row and the first column exist.
+__device__ __forceinline__ void save_codes(uint8_t* c, uint8_t* x, bool live, bool first, int n, const float* v) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -204,7 +203,6 @@ __device__ __forceinline__ void save_codes(const Packed8& d, bool live, int64_t 
   for (int i = 0; i < 2; ++i)
     w[i] = pack8(scaled_for_8(v[4 * i], p), scaled_for_8(v[4 * i + 1], p), scaled_for_8(v[4 * i + 2], p),
                  scaled_for_8(v[4 * i + 3], p));
-  uint8_t* c = d.codes + row * cols + col;
   if (n >= 8) {
     __builtin_memcpy(c, w, 8);
   } else {
@@ -212,45 +210,79 @@ __device__ __forceinline__ void save_codes(const Packed8& d, bool live, int64_t 
     for (int i = 0; i < 8; ++i)
       if (i < n) c[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
   }
-  if (col % kBlock8 == 0)
-    d.exponents[row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8] = (uint8_t)(127 - p);
+  if (first) *x = (uint8_t)(127 - p);
 }
 
-__device__ __forceinline__ void keep_cols(int dtype, const Kept& k, bool live, int64_t row, int64_t col, int64_t cols,
-                                          const float* v) {
-  if (k.matrix) {
-    if (live) store_cols<8>(k.matrix, row * k.ld + col, dtype, cols - col, v);
-  } else if (k.packed.codes) {
-    save_codes(k.packed, live, row, col, cols, v);
+// Where 8 columns of a row of a result go; moved down by whole rows without multiplying.
+template <int kType, int kHalves>
+struct Targets {
+  static constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+  char* y[kHalves];
+  char* kept[kHalves];           // the matrix or the codes
+  uint8_t* exponent[kHalves];
+
+  __device__ __forceinline__ void init(const End& e, int64_t row, int64_t col) {
+    y[0] = static_cast<char*>(e.y0) + (row * e.ld0 + col) * kSize;
+    if constexpr (kHalves == 2)
+      if (e.mode == kEndStore) y[1] = static_cast<char*>(e.y1) + (row * e.ld1 + col) * kSize;
+    each(e, [&](int h, const Kept& k) {
+      if (k.matrix) {
+        kept[h] = static_cast<char*>(k.matrix) + (row * k.ld + col) * kSize;
+      } else {
+        kept[h] = reinterpret_cast<char*>(k.packed.codes) + row * e.cols + col;
+        exponent[h] = k.packed.exponents + row * blocks(e) + col / kBlock8;
+      }
+    });
   }
-}
+  __device__ __forceinline__ void down(const End& e, int rows) {
+    y[0] += rows * e.ld0 * kSize;
+    if constexpr (kHalves == 2)
+      if (e.mode == kEndStore) y[1] += rows * e.ld1 * kSize;
+    each(e, [&](int h, const Kept& k) {
+      kept[h] += k.matrix ? rows * k.ld * kSize : rows * e.cols;
+      exponent[h] += rows * blocks(e);
+    });
+  }
+
+ private:
+  static __device__ __forceinline__ int64_t blocks(const End& e) { return (e.cols + kBlock8 - 1) / kBlock8; }
+  template <class F>
+  static __device__ __forceinline__ void each(const End& e, F&& f) {
+    if (e.mode == kEndStore) return;
+    if (e.keep0.any()) f(0, e.keep0);
+    if constexpr (kHalves == 2)
+      if (e.keep1.any()) f(1, e.keep1);
+  }
+};
 
 // What the end of 8 columns from `col` adds to their sums, zeros where there is none.
 __device__ __forceinline__ void load_bias(const float* bias, int64_t col, int64_t cols, float* b) {
   load_cols<8>(bias, col, POINTID_FP32, bias && col < cols ? cols - col : 0, b);
 }
-// The residual of 8 columns as it stands in memory, zeros where there is none.
+// The residual of 8 columns (n exist) as it stands in memory at p, zeros where there is none.
 template <int kType>
 struct Residual {
   static constexpr int kWords = kType == POINTID_FP32 ? 8 : 4;
   uint32_t w[kWords];
-  __device__ __forceinline__ void load(const End& e, bool live, int64_t row, int64_t col) {
-    const int64_t n = e.residual && live ? e.cols - col : 0, at = row * e.ld_residual + col;
-    constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+  __device__ __forceinline__ void load(const char* p, int n) {
     if (n >= 8) {
-      __builtin_memcpy(w, static_cast<const char*>(e.residual) + at * kSize, sizeof(w));
+      __builtin_memcpy(w, p, sizeof(w));
       return;
     }
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
+    if (n <= 0) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i >= n) continue;
-      if constexpr (kSize == 4)
-        w[i] = static_cast<const uint32_t*>(e.residual)[at + i];
+      if constexpr (kType == POINTID_FP32)
+        w[i] = reinterpret_cast<const uint32_t*>(p)[i];
       else
-        w[i / 2] |= (uint32_t)static_cast<const uint16_t*>(e.residual)[at + i] << (16 * (i % 2));
+        w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
     }
+  }
+  static __device__ __forceinline__ const char* at(const End& e, int64_t row, int64_t col) {
+    return static_cast<const char*>(e.residual) + (row * e.ld_residual + col) * (kType == POINTID_FP32 ? 4 : 2);
   }
   __device__ __forceinline__ void add_to(float* v) const {
 #pragma unroll
@@ -265,27 +297,34 @@ struct Residual {
   }
 };
 
-// The end of 8 finished columns of a row (see End) from `col`, a multiple of 8; v1 and b1:
+// The end of 8 finished columns of a row (see End), of which the first n exist; v1 and b1:
 // the second half's, with kHalves == 2; b0, b1: load_bias's; r: the residual's.  The 4 lanes
-// of an aligned group hold 32 columns of one row, from a multiple of 32 on, and all call it;
-// `live` is false where the row or the columns do not exist.
+// of an aligned group hold 32 columns of one row, from a multiple of 32 on (the lane `first`
+// the first of them), and all call it; `live` is false where the row or the columns do not
+// exist.
 template <int kType, int kHalves>
-__device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int64_t col, float* v0, float* v1,
-                                       const float* b0, const float* b1, const Residual<kType>& r) {
-  const int64_t n = e.cols - col;
+__device__ __forceinline__ void finish(const End& e, const Targets<kType, kHalves>& to, bool live, bool first, int n,
+                                       float* v0, float* v1, const float* b0, const float* b1, const Residual<kType>& r) {
   if (e.mode == kEndStore) {
     if (!live) return;
-    store_cols<8>(e.y0, row * e.ld0 + col, kType, n, v0);
-    if (kHalves == 2) store_cols<8>(e.y1, row * e.ld1 + col, kType, n, v1);
+    store_cols<8>(to.y[0], 0, kType, n, v0);
+    if constexpr (kHalves == 2) store_cols<8>(to.y[1], 0, kType, n, v1);
     return;
   }
+  auto keep = [&](int h, const Kept& k, const float* v) {
+    if (k.matrix) {
+      if (live) store_cols<8>(to.kept[h], 0, kType, n, v);
+    } else if (k.packed.codes) {
+      save_codes(reinterpret_cast<uint8_t*>(to.kept[h]), to.exponent[h], live, first, n, v);
+    }
+  };
 #pragma unroll
   for (int i = 0; i < 8; ++i) v0[i] += b0[i];
-  keep_cols(kType, e.keep0, live, row, col, e.cols, v0);
+  keep(0, e.keep0, v0);
   if constexpr (kHalves == 2) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v1[i] += b1[i];
-    keep_cols(kType, e.keep1, live, row, col, e.cols, v1);
+    keep(1, e.keep1, v1);
   }
   if (!live) return;
   activate8(e.act, v0);
@@ -295,7 +334,11 @@ __device__ __forceinline__ void finish(const End& e, bool live, int64_t row, int
   } else {
     r.add_to(v0);
   }
-  store_cols<8>(e.y0, row * e.ld0 + col, kType, n, v0);
+  store_cols<8>(to.y[0], 0, kType, n, v0);
+}
+// the columns of a piece of 8 that exist, from `col` of `cols`
+__device__ __forceinline__ int piece_cols(int64_t cols, int64_t col) {
+  return cols - col < 8 ? (cols - col < 0 ? 0 : (int)(cols - col)) : 8;
 }
 
 // 8 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)

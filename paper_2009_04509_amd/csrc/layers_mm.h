@@ -187,52 +187,86 @@ __device__ __forceinline__ void end_tile(const End& e, const floatx4 (&acc)[kFra
   constexpr int kLanes = kHalves == 2 ? 4 : 8;           // of a row
   constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes;
   const int64_t col = col0 + lane % kLanes * 8;
-  const bool live_col = col < e.cols;
-  float b0[8], b1[8];
-  load_bias(e.bias0, col, e.cols, b0);
-  if constexpr (kHalves == 2) load_bias(e.bias1, col, e.cols, b1);
-  const float* const from = es + lane / kLanes * kEndPitch + lane % kLanes * 8;
-  Residual<kType> next[kSteps];
-  auto read = [&](int64_t row) {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      if (kHalves == 1) next[s].load(e, live_col && row + s * kRows < e.rows, row + s * kRows, col);
-  };
+  const int n = piece_cols(e.cols, col);
   row0 += lane / kLanes;
-  read(row0);
-#pragma nounroll
-  for (int turn = 0; turn < kFragsM / 2; ++turn, row0 += 32) {
-    floatx4 c[2][4] = {};
+  // rows of the result from the lane's first on
+  int left = (int)(e.rows - row0 < kFragsM * 16 ? e.rows - row0 : kFragsM * 16);
+  const float* const from = es + lane / kLanes * kEndPitch + lane % kLanes * 8;
+  float* const into = es + lane % 16 * kEndPitch + lane / 16 * 4;
+  auto pass = [&](const floatx4(&c)[2][4]) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<floatx4*>(into + i / 4 * 16 * kEndPitch + i % 4 * 16) = c[i / 4][i % 4];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  auto take = [&](int s, float(&v)[kHalves][8]) {
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], from + s * kRows * kEndPitch + h * 32, 32);
+  };
+  auto sums = [&](int turn, floatx4(&c)[2][4]) {
     static_for<kFragsM / 2>([&](auto t) {
       if (turn == t)
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i / 4][i % 4] = acc[2 * t + i / 4][i % 4];
     });
+  };
+  if (e.mode == kEndPartial) {
+#pragma nounroll
+    for (int turn = 0; turn < kFragsM / 2; ++turn, row0 += 32, left -= 32) {
+      floatx4 c[2][4] = {};
+      sums(turn, c);
+      pass(c);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        float v[kHalves][8];
+        take(s, v);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) store_partial(e, split, h, s * kRows < left, row0 + s * kRows, col, v[h]);
+      }
+    }
+    return;
+  }
+  float b0[8], b1[8];
+  if (e.mode != kEndStore) {
+    load_bias(e.bias0, col, e.cols, b0);
+    if constexpr (kHalves == 2) load_bias(e.bias1, col, e.cols, b1);
+  }
+  Targets<kType, kHalves> to;
+  to.init(e, row0, col);
+  const bool add = kHalves == 1 && e.residual;
+  const char* residual = add ? Residual<kType>::at(e, row0, col) : nullptr;
+  const int64_t residual_step = kRows * e.ld_residual * (kType == POINTID_FP32 ? 4 : 2);
+  Residual<kType> next[kSteps];
+  auto read = [&](int rows) {
+    if (!add) return;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s, residual += residual_step) next[s].load(residual, s * kRows < rows ? n : 0);
+  };
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (uint32_t& w : next[s].w) w = 0;
+  read(left);
+#pragma nounroll
+  for (int turn = 0; turn < kFragsM / 2; ++turn) {
+    floatx4 c[2][4] = {};
+    sums(turn, c);
     Residual<kType> now[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) now[s] = next[s];
-    if (turn + 1 < kFragsM / 2) read(row0 + 32);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      *reinterpret_cast<floatx4*>(es + (i / 4 * 16 + lane % 16) * kEndPitch + i % 4 * 16 + lane / 16 * 4) = c[i / 4][i % 4];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (turn + 1 < kFragsM / 2) read(left - 32);
+    pass(c);
 #pragma nounroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int64_t row = row0 + s * kRows;
+    for (int s = 0; s < kSteps; ++s, left -= kRows) {
       float v[kHalves][8];
-#pragma unroll
-      for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], from + s * kRows * kEndPitch + h * 32, 32);
-      if (e.mode == kEndPartial) {
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h) store_partial(e, split, h, row < e.rows, row, col, v[h]);
-      } else {
-        Residual<kType> r = now[0];
+      take(s, v);
+      Residual<kType> r = now[0];
+      if (add)
         static_for<kSteps>([&](auto t) {
           if (s == t) r = now[t];
         });
-        finish<kType, kHalves>(e, live_col && row < e.rows, row, col, v[0], v[kHalves - 1], b0, b1, r);
-      }
+      finish<kType, kHalves>(e, to, n > 0 && left > 0, lane % 4 == 0, n, v[0], v[kHalves - 1], b0, b1, r);
+      to.down(e, kRows);
     }
   }
 }

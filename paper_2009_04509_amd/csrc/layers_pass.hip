@@ -81,7 +81,8 @@ __global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, i
     const int64_t col = here ? (i - row * lanes) * 8 : 0;
     float v[8];
     load_cols<8>(src, row * ld + col, dtype, here ? cols - col : 0, v);
-    save_codes(out, here && col < cols, row, col, cols, v);
+    save_codes(out.codes + row * cols + col, out.exponents + row * (lanes / 4) + col / kBlock8, here && col < cols,
+               col % kBlock8 == 0, here ? piece_cols(cols, col) : 0, v);
   }
 }
 
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
   if (sub == 0) {
     load_bias(e.bias0, col, e.cols, bias[0]);
     load_bias(e.bias1, col, e.cols, bias[1]);
-    residual.load(e, live, row, col);
+    residual.load(residual.at(e, row, col), e.residual && live ? piece_cols(e.cols, col) : 0);
   }
   if (here) {
 #pragma unroll 4
@@ -215,7 +216,10 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[h][j] += sums[s][h][unit][j];
   }
-  finish<kType, kHalves>(e, live, row, col, v[0], v[kHalves - 1], bias[0], bias[1], residual);
+  Targets<kType, kHalves> to;
+  to.init(e, row, col);
+  finish<kType, kHalves>(e, to, live, col % kBlock8 == 0, piece_cols(e.cols, col), v[0], v[kHalves - 1], bias[0], bias[1],
+                         residual);
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols) {

@@ -162,9 +162,12 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
       float bias[2][8];
       load_bias(a.end.bias0, at, a.end.cols, bias[0]);
       load_bias(a.end.bias1, at, a.end.cols, bias[1]);
+      const int count = piece_cols(a.end.cols, at);
       Residual<kType> residual;
-      residual.load(a.end, live, row, at);
-      finish<kType, kHalves>(a.end, live, row, at, v[0], v[kHalves - 1], bias[0], bias[1], residual);
+      residual.load(residual.at(a.end, r, at), a.end.residual && live ? count : 0);
+      Targets<kType, kHalves> to;
+      to.init(a.end, r, at);
+      finish<kType, kHalves>(a.end, to, live, at % kBlock8 == 0, count, v[0], v[kHalves - 1], bias[0], bias[1], residual);
     }
   }
 }
