@@ -214,44 +214,36 @@ __device__ __forceinline__ void save_codes(uint8_t* c, uint8_t* x, bool live, bo
 }
 
 // Where 8 columns of a row of a result go; moved down by whole rows without multiplying.
+template <int kType>
+struct Target {
+  static constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+  char* y;
+  char* kept;                    // the matrix or the codes
+  uint8_t* exponent;
+
+  static __device__ __forceinline__ int64_t blocks(int64_t cols) { return (cols + kBlock8 - 1) / kBlock8; }
+  __device__ __forceinline__ void init(void* out, int64_t ld, const Kept& k, int64_t cols, int64_t row, int64_t col) {
+    y = static_cast<char*>(out) + (row * ld + col) * kSize;
+    kept = k.matrix ? static_cast<char*>(k.matrix) + (row * k.ld + col) * kSize
+                    : reinterpret_cast<char*>(k.packed.codes) + row * cols + col;
+    exponent = k.packed.exponents + row * blocks(cols) + col / kBlock8;
+  }
+  __device__ __forceinline__ void down(int rows, int64_t ld, const Kept& k, int64_t cols) {
+    y += rows * ld * kSize;
+    kept += k.matrix ? rows * k.ld * kSize : rows * cols;
+    exponent += rows * blocks(cols);
+  }
+};
 template <int kType, int kHalves>
 struct Targets {
-  static constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
-  char* y[kHalves];
-  char* kept[kHalves];           // the matrix or the codes
-  uint8_t* exponent[kHalves];
-
+  Target<kType> t0, t1;
   __device__ __forceinline__ void init(const End& e, int64_t row, int64_t col) {
-    y[0] = static_cast<char*>(e.y0) + (row * e.ld0 + col) * kSize;
-    if constexpr (kHalves == 2)
-      if (e.mode == kEndStore) y[1] = static_cast<char*>(e.y1) + (row * e.ld1 + col) * kSize;
-    each(e, [&](int h, const Kept& k) {
-      if (k.matrix) {
-        kept[h] = static_cast<char*>(k.matrix) + (row * k.ld + col) * kSize;
-      } else {
-        kept[h] = reinterpret_cast<char*>(k.packed.codes) + row * e.cols + col;
-        exponent[h] = k.packed.exponents + row * blocks(e) + col / kBlock8;
-      }
-    });
+    t0.init(e.y0, e.ld0, e.keep0, e.cols, row, col);
+    if constexpr (kHalves == 2) t1.init(e.y1, e.ld1, e.keep1, e.cols, row, col);
   }
   __device__ __forceinline__ void down(const End& e, int rows) {
-    y[0] += rows * e.ld0 * kSize;
-    if constexpr (kHalves == 2)
-      if (e.mode == kEndStore) y[1] += rows * e.ld1 * kSize;
-    each(e, [&](int h, const Kept& k) {
-      kept[h] += k.matrix ? rows * k.ld * kSize : rows * e.cols;
-      exponent[h] += rows * blocks(e);
-    });
-  }
-
- private:
-  static __device__ __forceinline__ int64_t blocks(const End& e) { return (e.cols + kBlock8 - 1) / kBlock8; }
-  template <class F>
-  static __device__ __forceinline__ void each(const End& e, F&& f) {
-    if (e.mode == kEndStore) return;
-    if (e.keep0.any()) f(0, e.keep0);
-    if constexpr (kHalves == 2)
-      if (e.keep1.any()) f(1, e.keep1);
+    t0.down(rows, e.ld0, e.keep0, e.cols);
+    if constexpr (kHalves == 2) t1.down(rows, e.ld1, e.keep1, e.cols);
   }
 };
 
@@ -307,24 +299,24 @@ __device__ __forceinline__ void finish(const End& e, const Targets<kType, kHalve
                                        float* v0, float* v1, const float* b0, const float* b1, const Residual<kType>& r) {
   if (e.mode == kEndStore) {
     if (!live) return;
-    store_cols<8>(to.y[0], 0, kType, n, v0);
-    if constexpr (kHalves == 2) store_cols<8>(to.y[1], 0, kType, n, v1);
+    store_cols<8>(to.t0.y, 0, kType, n, v0);
+    if constexpr (kHalves == 2) store_cols<8>(to.t1.y, 0, kType, n, v1);
     return;
   }
-  auto keep = [&](int h, const Kept& k, const float* v) {
+  auto keep = [&](const Target<kType>& t, const Kept& k, const float* v) {
     if (k.matrix) {
-      if (live) store_cols<8>(to.kept[h], 0, kType, n, v);
+      if (live) store_cols<8>(t.kept, 0, kType, n, v);
     } else if (k.packed.codes) {
-      save_codes(reinterpret_cast<uint8_t*>(to.kept[h]), to.exponent[h], live, first, n, v);
+      save_codes(reinterpret_cast<uint8_t*>(t.kept), t.exponent, live, first, n, v);
     }
   };
 #pragma unroll
   for (int i = 0; i < 8; ++i) v0[i] += b0[i];
-  keep(0, e.keep0, v0);
+  keep(to.t0, e.keep0, v0);
   if constexpr (kHalves == 2) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v1[i] += b1[i];
-    keep(1, e.keep1, v1);
+    keep(to.t1, e.keep1, v1);
   }
   if (!live) return;
   activate8(e.act, v0);
@@ -334,7 +326,7 @@ __device__ __forceinline__ void finish(const End& e, const Targets<kType, kHalve
   } else {
     r.add_to(v0);
   }
-  store_cols<8>(to.y[0], 0, kType, n, v0);
+  store_cols<8>(to.t0.y, 0, kType, n, v0);
 }
 // the columns of a piece of 8 that exist, from `col` of `cols`
 __device__ __forceinline__ int piece_cols(int64_t cols, int64_t col) {
