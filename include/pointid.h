@@ -532,7 +532,8 @@ int pointid_gated(pointid_layers l, int dtype, int act, int64_t m, int64_t k, in
  *   dg = dh u act'(g),  du = dh act(g),  dx = dg Wg^T + du Wu^T,
  *   dwg = x^T dg,  dwu = x^T du,  dbg and dbu the column sums of dg and du
  * x, wg and wu, and the outputs, as in pointid_dense_backward (dwg and dwu are
- * given both or neither); g and u are always needed.
+ * given both or neither); g and u are always needed, both as matrices or both as
+ * checkpoints.
  */
 int pointid_gated_backward(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
                            const pointid_matrix *dh, const pointid_kept *x, const pointid_matrix *wg,

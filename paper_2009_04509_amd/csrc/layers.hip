@@ -654,6 +654,8 @@ int pointid_gated_backward(pointid_layers l, int dtype, int act, int64_t m, int6
     TRY(check_matrix(wu, "wu", dtype, k, n, !want_dx));
     TRY(check_kept(g, "g", dtype, m, n, false));
     TRY(check_kept(u, "u", dtype, m, n, false));
+    if (m > 0 && !g->full.data != !u->full.data)
+      return set_error(POINTID_EINVAL, "g and u are kept alike: two matrices or two checkpoints");
     TRY(check_matrix(dx, "dx", dtype, m, k, true));
     TRY(check_matrix(dwg, "dwg", dtype, k, n, true));
     TRY(check_matrix(dwu, "dwu", dtype, k, n, true));

@@ -164,23 +164,6 @@ __device__ __forceinline__ void unpack8(uint32_t w, int p, float* v) {       // 
   v[3] = __builtin_amdgcn_ldexpf(b[1], p);
 }
 
-// 8 codes of a row from column `col` (a multiple of 8), of which cols - col exist.
-__device__ __forceinline__ void load_codes(const Packed8& s, int64_t row, int64_t col, int64_t cols, float* v) {
-  const int p = (int)s.exponents[row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8] - 127;
-  const int64_t n = cols - col;
-  const uint8_t* c = s.codes + row * cols + col;
-  uint32_t w[2] = {0, 0};
-  if (n >= 8) {
-    __builtin_memcpy(w, c, 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) w[i / 4] |= (uint32_t)c[i] << (8 * (i % 4));
-  }
-  unpack8(w[0], p, v);
-  unpack8(w[1], p, v + 4);
-}
-
 // 8 values of a row (of which the first n exist) to a checkpoint's codes at `c`, and by the
 // first lane of a block its exponent to `x`.  The 4 lanes of an aligned group hold a block
 // of 32 and all call this; values that do not exist do not count and are not written.
@@ -251,9 +234,15 @@ struct Targets {
 __device__ __forceinline__ void load_bias(const float* bias, int64_t col, int64_t cols, float* b) {
   load_cols<8>(bias, col, POINTID_FP32, bias && col < cols ? cols - col : 0, b);
 }
-// The residual of 8 columns (n exist) as it stands in memory at p, zeros where there is none.
+// the columns of a piece of 8 that exist, from `col` of `cols`
+__device__ __forceinline__ int piece_cols(int64_t cols, int64_t col) {
+  return cols - col < 8 ? (cols - col < 0 ? 0 : (int)(cols - col)) : 8;
+}
+
+// 8 values of a row (n exist, the rest are 0) as they stand in memory at p: read now, used
+// later.
 template <int kType>
-struct Residual {
+struct Raw8 {
   static constexpr int kWords = kType == POINTID_FP32 ? 8 : 4;
   uint32_t w[kWords];
   __device__ __forceinline__ void load(const char* p, int n) {
@@ -273,19 +262,52 @@ struct Residual {
         w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
     }
   }
+  __device__ __forceinline__ void values(float* v) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (kType == POINTID_FP32) {
+        v[i] = __uint_as_float(w[i]);
+      } else {
+        v[2 * i] = from16((uint16_t)w[i], kType);
+        v[2 * i + 1] = from16((uint16_t)(w[i] >> 16), kType);
+      }
+    }
+  }
+};
+// The same of a checkpoint: codes at c, the block's exponent at x.
+struct RawCodes {
+  uint32_t w[2];
+  uint32_t exponent;
+  __device__ __forceinline__ void load(const uint8_t* c, const uint8_t* x, int n) {
+    w[0] = w[1] = 0;
+    exponent = 127;
+    if (n <= 0) return;
+    exponent = *x;
+    if (n >= 8) {
+      __builtin_memcpy(w, c, 8);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) w[i / 4] |= (uint32_t)c[i] << (8 * (i % 4));
+  }
+  __device__ __forceinline__ void values(float* v) const {
+    unpack8(w[0], (int)exponent - 127, v);
+    unpack8(w[1], (int)exponent - 127, v + 4);
+  }
+};
+
+// The residual of 8 columns, zeros where there is none.
+template <int kType>
+struct Residual : Raw8<kType> {
   static __device__ __forceinline__ const char* at(const End& e, int64_t row, int64_t col) {
     return static_cast<const char*>(e.residual) + (row * e.ld_residual + col) * (kType == POINTID_FP32 ? 4 : 2);
   }
   __device__ __forceinline__ void add_to(float* v) const {
+    float r[8];
+    this->values(r);
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      if constexpr (kType == POINTID_FP32) {
-        v[i] += __uint_as_float(w[i]);
-      } else {
-        v[2 * i] += from16((uint16_t)w[i], kType);
-        v[2 * i + 1] += from16((uint16_t)(w[i] >> 16), kType);
-      }
-    }
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
   }
 };
 
@@ -328,9 +350,12 @@ __device__ __forceinline__ void finish(const End& e, const Targets<kType, kHalve
   }
   store_cols<8>(to.t0.y, 0, kType, n, v0);
 }
-// the columns of a piece of 8 that exist, from `col` of `cols`
-__device__ __forceinline__ int piece_cols(int64_t cols, int64_t col) {
-  return cols - col < 8 ? (cols - col < 0 ? 0 : (int)(cols - col)) : 8;
+// A checkpoint's 8 values of a row from column `col`, a multiple of 8.
+__device__ __forceinline__ void load_codes(const Packed8& s, int64_t row, int64_t col, int64_t cols, float* v) {
+  RawCodes r;
+  r.load(s.codes + row * cols + col, s.exponents + row * ((cols + kBlock8 - 1) / kBlock8) + col / kBlock8,
+         piece_cols(cols, col));
+  r.values(v);
 }
 
 // 8 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)

@@ -86,47 +86,74 @@ __global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, i
   }
 }
 
+// How the activations of a gradient are kept.
+enum { kKeptNot = 0, kKeptWhole = 1, kKeptPacked = 2 };
+
 // Each block: 8 kTurns rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time, two
-// such turns' reads in flight.
-template <int kHalves, int kTurns>
+// such turns' reads in flight before any is used (a read used at once: 163 us for a gated
+// 8192 x 8192 in bf16).
+template <int kType, int kHalves, int kKept, int kTurns>
 __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
   __shared__ float sums[8][256 + 8];
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
   const int piece = threadIdx.x % 32, sub = threadIdx.x / 32;
-  const int64_t col = (int64_t)blockIdx.y * 256 + piece * 8, n = a.cols - col;
+  const int64_t col = (int64_t)blockIdx.y * 256 + piece * 8;
+  const int n = piece_cols(a.cols, col);
   const int64_t row0 = (int64_t)blockIdx.x * (8 * kTurns) + sub;
+  // rows from row0 on, and where the lane's pieces of them stand
+  const int left = (int)(a.rows - row0 < 8 * kTurns ? a.rows - row0 : 8 * kTurns);
+  const int64_t blocks8 = (a.cols + kBlock8 - 1) / kBlock8;
+  const char* dy_at = static_cast<const char*>(a.dy) + (row0 * a.ld_dy + col) * kSize;
+  const char* z_at[kHalves];
+  const uint8_t* x_at[kHalves];
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h) {
+    if constexpr (kKept == kKeptWhole) z_at[h] = static_cast<const char*>(a.z[h].matrix) + (row0 * a.z[h].ld + col) * kSize;
+    if constexpr (kKept == kKeptPacked) {
+      z_at[h] = reinterpret_cast<const char*>(a.z[h].packed.codes) + row0 * a.cols + col;
+      x_at[h] = a.z[h].packed.exponents + row0 * blocks8 + col / kBlock8;
+    }
+  }
   float total[kHalves][8] = {};
   constexpr int kAhead = kTurns < 2 ? kTurns : 2;
   if (n > 0) {
+#pragma unroll
     for (int s = 0; s < kTurns; s += kAhead) {
-      float dy[kAhead][8], z[kAhead][2][8];
+      Raw8<kType> dy[kAhead], zw[kAhead][kHalves];
+      RawCodes zp[kAhead][kHalves];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int64_t row = row0 + 8 * (s + u);
-        const int64_t here = row < a.rows ? n : 0;
-        load_cols<8>(a.dy, row * a.ld_dy + col, a.dtype, here, dy[u]);
+        const int r = 8 * (s + u), here = r < left ? n : 0;
+        dy[u].load(dy_at + r * a.ld_dy * kSize, here);
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
-          if (a.z[h].matrix)
-            load_cols<8>(a.z[h].matrix, row * a.z[h].ld + col, a.dtype, here, z[u][h]);
-          else if (a.z[h].packed.codes && here)
-            load_codes(a.z[h].packed, row, col, a.cols, z[u][h]);
+          if constexpr (kKept == kKeptWhole) zw[u][h].load(z_at[h] + r * a.z[h].ld * kSize, here);
+          if constexpr (kKept == kKeptPacked)
+            zp[u][h].load(reinterpret_cast<const uint8_t*>(z_at[h]) + r * a.cols, x_at[h] + r * blocks8, here);
         }
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int64_t row = row0 + 8 * (s + u);
-        if (row >= a.rows) continue;
-        float d[kHalves][8];
+        const int r = 8 * (s + u);
+        if (r >= left) continue;
+        float d[kHalves][8], z[kHalves][8] = {}, g[8];
+        dy[u].values(g);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          if constexpr (kKept == kKeptWhole) zw[u][h].values(z[h]);
+          if constexpr (kKept == kKeptPacked) zp[u][h].values(z[h]);
+        }
+        // (what does not exist reads as 0 and stays 0: so does the padding)
         static_for<5>([&](auto act) {               // the choice outside of the loop
           if (a.act == act) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               float value;
               if constexpr (kHalves == 2) {
-                d[0][i] = i < n ? through(act, z[u][0][i], dy[u][i] * z[u][1][i], &value) : 0.f;
-                d[1][i] = i < n ? dy[u][i] * value : 0.f;
+                d[0][i] = through(act, z[0][i], g[i] * z[1][i], &value);
+                d[1][i] = g[i] * value;
               } else {
-                d[0][i] = i < n ? through(act, act == POINTID_ACT_NONE ? 0.f : z[u][0][i], dy[u][i], &value) : 0.f;
+                d[0][i] = through(act, z[0][i], g[i], &value);
               }
             }
           }
@@ -136,23 +163,24 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) total[h][i] += d[h][i];
           if (a.parts == 0) continue;
-          if (a.parts < 0) {
-            store_cols<8>(a.out[h], row * a.ld + col, POINTID_FP32, 8, d[h]);
-            continue;
-          }
-          uint32_t w[4];
+          const int64_t at = (row0 + r) * a.ld + col;
+          if constexpr (kType == POINTID_FP32) {
+            store_cols<8>(a.out[h], at, kType, 8, d[h]);
+          } else {
+            uint32_t w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = pack16(d[h][2 * i], d[h][2 * i + 1], a.dtype);
-          uint16_t* o = static_cast<uint16_t*>(a.out[h]) + row * a.ld + col;
-          *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-          if (a.parts < 2) continue;
-          float rest[8];                               // none beside an infinity or NaN
+            for (int i = 0; i < 4; ++i) w[i] = pack16(d[h][2 * i], d[h][2 * i + 1], kType);
+            uint16_t* o = static_cast<uint16_t*>(a.out[h]) + at;
+            *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (a.parts < 2) continue;
+            float rest[8];                               // none beside an infinity or NaN
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            rest[i] = d[h][i] - from16((uint16_t)(w[i / 2] >> (16 * (i % 2))), a.dtype);
-            if ((__float_as_uint(rest[i]) & 0x7FFFFFFFu) >= 0x7F800000u) rest[i] = 0.f;
+            for (int i = 0; i < 8; ++i) {
+              rest[i] = d[h][i] - from16((uint16_t)(w[i / 2] >> (16 * (i % 2))), kType);
+              if ((__float_as_uint(rest[i]) & 0x7FFFFFFFu) >= 0x7F800000u) rest[i] = 0.f;
+            }
+            store_cols<8>(o + a.plane, 0, kType, 8, rest);
           }
-          store_cols<8>(o + a.plane, 0, a.dtype, 8, rest);
         }
       }
     }
@@ -170,6 +198,15 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
     if (c < a.cols) a.col_part[((int64_t)blockIdx.x * kHalves + h) * a.cols + c] = t;
     __syncthreads();
   }
+}
+
+template <int kType, int kTurns>
+hipError_t launch_grad(const GradArgs& a, dim3 grid, hipStream_t stream) {
+  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, a); };
+  if (a.halves == 2)
+    return a.z[0].matrix ? go(grad_kernel<kType, 2, kKeptWhole, kTurns>) : go(grad_kernel<kType, 2, kKeptPacked, kTurns>);
+  if (a.z[0].matrix) return go(grad_kernel<kType, 1, kKeptWhole, kTurns>);
+  return a.z[0].packed.codes ? go(grad_kernel<kType, 1, kKeptPacked, kTurns>) : go(grad_kernel<kType, 1, kKeptNot, kTurns>);
 }
 
 // Units of 8 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
@@ -266,9 +303,15 @@ int grad_rows(int64_t rows, int64_t cols, int cus) {
 hipError_t launch_layers_grad(const GradArgs& a, int block_rows, hipStream_t stream) {
   const int64_t width = a.parts != 0 && a.ld > a.cols ? a.ld : a.cols;
   const dim3 grid((unsigned)((a.rows + block_rows - 1) / block_rows), (unsigned)((width + 255) / 256));
-  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, a); };
-  if (block_rows == 8) return a.halves == 2 ? go(grad_kernel<2, 1>) : go(grad_kernel<1, 1>);
-  return a.halves == 2 ? go(grad_kernel<2, 4>) : go(grad_kernel<1, 4>);
+  // the halves are kept alike (the caller checks)
+  if (a.halves == 2 && (!a.z[0].matrix != !a.z[1].matrix || !a.z[0].any() || !a.z[1].any())) return hipErrorInvalidValue;
+  switch (a.dtype) {
+    case POINTID_FP32:
+      return block_rows == 8 ? launch_grad<POINTID_FP32, 1>(a, grid, stream) : launch_grad<POINTID_FP32, 4>(a, grid, stream);
+    case POINTID_BF16:
+      return block_rows == 8 ? launch_grad<POINTID_BF16, 1>(a, grid, stream) : launch_grad<POINTID_BF16, 4>(a, grid, stream);
+  }
+  return block_rows == 8 ? launch_grad<POINTID_FP16, 1>(a, grid, stream) : launch_grad<POINTID_FP16, 4>(a, grid, stream);
 }
 
 hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols, hipStream_t stream) {

@@ -111,6 +111,7 @@ def test_gated_backward_refusals(b):
         assert call(**{name: None}) == b.POINTID_EINVAL and name in b.pointid_last_error()
     assert call(dwg=None) == b.POINTID_EINVAL and "both" in b.pointid_last_error()
     assert call(dwu=None) == b.POINTID_EINVAL
+    assert call(u=kept(b, at=None, codes=1, exponents=1)) == b.POINTID_EINVAL and "alike" in b.pointid_last_error()
 
 
 def test_checkpoint_refusals(b):
