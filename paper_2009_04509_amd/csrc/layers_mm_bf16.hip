@@ -9,23 +9,23 @@ namespace pointid {
 
 namespace {
 
-// us of a tile shape, fitted to sweeps of tiles and splits over 23 products of all forms
-// from 16 x 8192 x 8192 to 16384 x 1024 x 1024 (13 in fp32): a stage of 64 inner indices when
+// us of a tile shape, fitted to sweeps of tiles and splits over 32 products of all forms
+// from 4 x 12288 x 4096 to 16384 x 4096 x 1024 (24 in fp32): a stage of 64 inner indices when
 // `resident` blocks share a CU (each) and of a block alone, and a block's start and end.
-// The choice by them is the fastest measured or within 3 % of it.
+// The choice by them is the fastest measured or within 6 % of it, half a percent on average.
 struct TileCost {
   double stage, alone, ends;
   int resident;
 };
-constexpr TileCost kCost[kTiles] = {{1.3, 1.3, 9.0, 1}, {0.57, 0.62, 3.4, 2}, {0.315, 0.435, 2.6, 3}};
-constexpr TileCost kCost32[kTiles32] = {{4.47, 4.47, 2.5, 1}, {2.9, 2.9, 2.0, 1}, {1.56, 2.5, 1.9, 2}};
+constexpr TileCost kCost[kTiles] = {{1.21, 1.21, 6.8, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
+constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 1}, {1.58, 2.79, 0.8, 2}};
 
 }  // namespace
 
 // The tile and split that the costs above put first.  Large tiles read their operands fewer
-// times (bf16 4096 x 1024 x 4096: 43 us in 256 x 256 tiles, 46 in 128 x 128, 55 in 64 x 128);
-// small ones fill the CUs where there are few (2048^3: 29 in 64 x 128, 32 in 128 x 128, 44
-// in split 256 x 256; its gated form 41 in 128 x 128, 55 in both others).
+// times (bf16 4096 x 1024 x 4096: 37 us in 256 x 256 tiles, 41 in 128 x 128, 49 in 64 x 128);
+// small ones fill the CUs where there are few (2048^3: 26 in 64 x 128, 29 in 128 x 128, 44
+// in split 256 x 256; its gated form 37 in 128 x 128, 49 and 51 in the others).
 ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
   static constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
   const double stages = (double)((inner + 63) / 64) * terms;
@@ -41,7 +41,7 @@ ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64
       const double per = std::ceil(stages / s), blocks = std::ceil(tiles * s / cus);
       const double rounds = std::ceil(blocks / c.resident);
       double us = std::max(blocks * c.stage, rounds * c.alone) * per + rounds * c.ends;
-      if (s > 1) us += f32 ? 2.1 + 0.2 * part_mb * s : 5.0 + 0.114 * part_mb * s;
+      if (s > 1) us += f32 ? 6.0 + 0.138 * part_mb * s : 1.4 + 0.142 * part_mb * s;
       if (us < least) least = us, best = {t, s};
     }
   }

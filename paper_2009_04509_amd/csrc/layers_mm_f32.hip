@@ -159,17 +159,18 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
     right1.store(tile + kLeftBytes + kRightBytes, rv1);
   };
   floatx4 acc[kFragsM][kFragsN] = {};
-  uint4 r[3][kFragsN];
-  auto multiply = [&](const char* tile, int i) {
-    uint4 l[3];
+  uint4 r[3][kFragsN], l[2][3];
+  auto read_left = [&](const char* tile, int i) {
 #pragma unroll
-    for (int p = 0; p < 3; ++p) l[p] = lf.read(tile + p * Left::kPlane, i, 0);
+    for (int p = 0; p < 3; ++p) l[i % 2][p] = lf.read(tile + p * Left::kPlane, i, 0);
+  };
+  auto multiply = [&](int i) {
 #pragma unroll
     for (int order = 2; order >= 0; --order)
 #pragma unroll
       for (int p = order; p >= 0; --p)
 #pragma unroll
-        for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[p], acc[i][j]);
+        for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[i % 2][p], acc[i][j]);
   };
   if (stages > 0) {
     load();
@@ -183,14 +184,16 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
       for (int p = 0; p < 3; ++p)
 #pragma unroll
         for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * Right::kPlane, j, 0);
+      read_left(tile, 0);
 #pragma unroll
-      for (int i = 0; i < kFragsM / 2; ++i) multiply(tile, i);
-      if (it + 1 < stages) {
-        store(stage ^ 1);
-        if (to_load > 0) load();
+      for (int i = 0; i < kFragsM; ++i) {
+        if (i + 1 < kFragsM) read_left(tile, i + 1);
+        multiply(i);
+        if (i == kFragsM / 2 - 1 && it + 1 < stages) {
+          store(stage ^ 1);
+          if (to_load > 0) load();
+        }
       }
-#pragma unroll
-      for (int i = kFragsM / 2; i < kFragsM; ++i) multiply(tile, i);
       __syncthreads();
     }
   }
