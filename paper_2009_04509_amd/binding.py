@@ -643,8 +643,10 @@ class Checkpoint:
 
     @classmethod
     def empty(cls, m: int, n: int, device="cuda") -> "Checkpoint":
-        return cls(torch.empty((m, n), dtype=torch.uint8, device=device),
-                   torch.empty((m, -(-n // 32)), dtype=torch.uint8, device=device))
+        c = cls.__new__(cls)
+        c.codes = torch.empty((m, n), dtype=torch.uint8, device=device)
+        c.exponents = torch.empty((m, -(-n // 32)), dtype=torch.uint8, device=device)
+        return c
 
     @property
     def shape(self):
@@ -672,6 +674,16 @@ def pointid_layers_trim(layers: Layers, keep_bytes: int = 0) -> int:
     return int(cached.value)
 
 
+# the current stream's handle without the Stream object around it (2 us a call), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _layer_stream(stream, device: int):
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream_ptr(stream, torch.device("cuda", device))
+
+
 def _matrix(t, name, dtype, shape, device):
     """The descriptor of a matrix (rows of unit stride, any pitch), or None."""
     if t is None:
@@ -682,9 +694,9 @@ def _matrix(t, name, dtype, shape, device):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.device.index != device:
-        raise ValueError(f"{name} is on cuda:{t.device.index}, the call's device is cuda:{device}")
-    if tuple(t.shape) != shape:
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's device is cuda:{device}")
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     rows, cols = shape
     pitch, unit = t.stride()
@@ -755,7 +767,7 @@ def pointid_dense(layers: Layers, x: torch.Tensor, w: torch.Tensor, bias: torch.
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
         _ref(_matrix(w, "w", dt, (k, n), dev)), _bias(bias, "bias", n, dev),
         _ref(_matrix(residual, "residual", dt, (m, n), dev)), _ref(_matrix(y, "y", dt, (m, n), dev)),
-        _ref(_kept(save, "save", dt, (m, n), dev)), _stream_ptr(stream, x.device)))
+        _ref(_kept(save, "save", dt, (m, n), dev)), _layer_stream(stream, dev)))
     return y
 
 
@@ -776,7 +788,7 @@ def pointid_dense_backward(layers: Layers, dy: torch.Tensor, x, w: torch.Tensor,
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dy, "dy", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(w, "w", dt, (k, n), dev)),
         _ref(_kept(z, "z", dt, (m, n), dev)), _ref(_matrix(dx, "dx", dt, (m, k), dev)),
-        _ref(_matrix(dw, "dw", dt, (k, n), dev)), _ptr(db), _stream_ptr(stream, dy.device)))
+        _ref(_matrix(dw, "dw", dt, (k, n), dev)), _ptr(db), _layer_stream(stream, dev)))
     return dx, dw, db
 
 
@@ -797,7 +809,7 @@ def pointid_gated(layers: Layers, x: torch.Tensor, wg: torch.Tensor, wu: torch.T
         _ref(_matrix(wg, "wg", dt, (k, n), dev)), _ref(_matrix(wu, "wu", dt, (k, n), dev)),
         _bias(bias_g, "bias_g", n, dev), _bias(bias_u, "bias_u", n, dev),
         _ref(_matrix(h, "h", dt, (m, n), dev)), _ref(_kept(save_g, "save_g", dt, (m, n), dev)),
-        _ref(_kept(save_u, "save_u", dt, (m, n), dev)), _stream_ptr(stream, x.device)))
+        _ref(_kept(save_u, "save_u", dt, (m, n), dev)), _layer_stream(stream, dev)))
     return h
 
 
@@ -820,19 +832,20 @@ def pointid_gated_backward(layers: Layers, dh: torch.Tensor, x, wg: torch.Tensor
         _ref(_matrix(wu, "wu", dt, (k, n), dev)), _ref(_kept(g, "g", dt, (m, n), dev)),
         _ref(_kept(u, "u", dt, (m, n), dev)), _ref(_matrix(dx, "dx", dt, (m, k), dev)),
         _ref(_matrix(dwg, "dwg", dt, (k, n), dev)), _ref(_matrix(dwu, "dwu", dt, (k, n), dev)),
-        _ptr(dbg), _ptr(dbu), _stream_ptr(stream, dh.device)))
+        _ptr(dbg), _ptr(dbu), _layer_stream(stream, dev)))
     return dx, dwg, dwu, dbg, dbu
 
 
 def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stream=None) -> Checkpoint:
     """The 8-bit checkpoint of a matrix [m][n] (float32, bfloat16 or float16)."""
-    dt = _layer_type(x, "x")
+    dt, dev = _layer_type(x, "x"), x.get_device()
     m, n = x.shape
+    a = _matrix(x, "x", dt, (m, n), dev)
     if out is None:
         out = Checkpoint.empty(m, n, x.device)
-    kept = _kept(out, "out", dt, (m, n), x.device.index)
-    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, _ref(_matrix(x, "x", dt, (m, n), x.device.index)),
-                                       ctypes.byref(kept.packed), _stream_ptr(stream, x.device)))
+    kept = _kept(out, "out", dt, (m, n), dev)
+    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(kept.packed),
+                                       _layer_stream(stream, dev)))
     return out
 
 
@@ -842,10 +855,9 @@ def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.T
     m, n = saved.shape
     if out is None:
         out = torch.empty((m, n), dtype=dtype, device=saved.device)
-    dt = _layer_type(out, "out")
-    dev = saved.device.index
+    dt, dev = _layer_type(out, "out"), saved.codes.get_device()
     kept = _kept(saved, "saved", dt, (m, n), dev)
     _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed),
-                                       _ref(_matrix(out, "out", dt, (m, n), dev)),
-                                       _stream_ptr(stream, saved.device)))
+                                       ctypes.byref(_matrix(out, "out", dt, (m, n), dev)),
+                                       _layer_stream(stream, dev)))
     return out
