@@ -11,6 +11,9 @@ __all__ = [
     "pointid_create", "pointid_destroy", "pointid_classify", "pointid_classify_planes",
     "pointid_classify_patches", "pointid_gather", "pointid_gather_planes",
     "pointid_last_error", "pointid_version", "PointIdError", "Handle",
+    "pointid_layers_create", "pointid_layers_destroy", "pointid_layers_trim", "pointid_dense",
+    "pointid_dense_backward", "pointid_gated", "pointid_gated_backward", "pointid_checkpoint_save",
+    "pointid_checkpoint_load", "Layers", "Checkpoint",
 ]
 
 
