@@ -4,8 +4,9 @@
 // A block computes kBM x kBN results with 16x16x32 MFMAs (a loop of these alone runs at
 // 2.0 PFLOP/s on random bf16 values, one of 32x32x16 at 1.8: the card is at its power limit,
 // and they pass half as many sums per multiplication through the registers).  Both
-// operands go through shared memory, 64 inner indices at a time, two stages, written by loads
-// that go there directly (16 bytes a lane).  An operand whose rows run along the inner
+// operands go through shared memory, 64 inner indices at a time, two stages (three for a
+// tile that a CU holds once and whose multiplications are shorter than the loads' latency),
+// written by loads that go there directly (16 bytes a lane).  An operand whose rows run along the inner
 // index (x and dz of dx and forward's x) is read as fragments with 16-byte reads; one whose
 // rows are indexed by the inner index (W of the forward form, both of dW) with the
 // transposing read, 4 x 16 values at a time, so no form needs a transposed copy of anything.
@@ -134,19 +135,14 @@ struct Frags {
   }
 };
 
-// All reads and loads of this wave done, then the block's barrier.  The reads' wait is the
-// compiler's own instruction, so that it does not wait for them again afterwards; of the
-// loads to shared memory it knows nothing.
+// All reads of this wave from shared memory and all but its newest kCount loads into it done,
+// then the block's barrier.  The reads' wait is the compiler's own instruction, so that it
+// does not wait for them again afterwards; of the loads it knows nothing.
+template <int kCount>
 __device__ __forceinline__ void stage_ready() {
+  static_assert(kCount < 64, "the counter's range");
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0)
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
-// All but the newest kCount loads to shared memory of this wave done, then the block's barrier.
-template <int kCount>
-__device__ __forceinline__ void loads_left() {
-  static_assert(kCount < 16, "one field of the wait");
   asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kCount) : "memory");
 }
 
@@ -276,7 +272,7 @@ __device__ __forceinline__ floatx4 mfma(const uint4& a, const uint4& b, const fl
   return Op16<kFp16>::mfma(a, b, c);
 }
 
-template <bool kFp16, int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>
+template <bool kFp16, int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN, int kStages>
 __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) {
   constexpr int kThreads = 64 * kWM * kWN;
   constexpr int kType = kFp16 ? POINTID_FP16 : POINTID_BF16;
@@ -289,7 +285,8 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   using Right = Tile<kRightInner, kHN, kThreads>;
   constexpr int kStage = Left::kBytes + 2 * Right::kBytes;
   // the end uses the stages' memory, and a little more with many small waves
-  constexpr int kShared = kWM * kWN * kEndWave > 2 * kStage ? kWM * kWN * kEndWave : 2 * kStage;
+  constexpr int kShared = kWM * kWN * kEndWave > kStages * kStage ? kWM * kWN * kEndWave : kStages * kStage;
+  constexpr int kStageLoads = Left::kLoads + 2 * Right::kLoads;
   __shared__ __align__(1024) char smem[kShared];
 
   const int tid = threadIdx.x, lane = tid % 64;
@@ -346,7 +343,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   // part q of kParts of the loads of the next stage (a compile-time constant)
   constexpr int kParts = kFragsM / 2;
   auto issue = [&](auto q, int stage) {
-    constexpr int kLoads = Left::kLoads + 2 * Right::kLoads;
+    constexpr int kLoads = kStageLoads;
     const uint32_t to = lds0 + stage * kStage;
     const int left_of = a.inner - k0;
     static_for<kLoads>([&](auto n) {
@@ -392,17 +389,17 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
     for (int j = 0; j < kFragsN; ++j) c[j] = mfma<kFp16>(r[turn / 2][j], l[turn % 2][i], c[j]);
   };
   if (stages > 0) {
-    static_for<kParts>([&](auto q) { issue(q, 0); });
-    if (to_load > 0) {
-      static_for<kParts>([&](auto q) { issue(q, 1); });
-      loads_left<Left::kLoads + 2 * Right::kLoads>();      // the second stage's
-    } else {
-      loads_left<0>();
-    }
+    static_for<kStages>([&](auto n) {
+      if (n < stages) static_for<kParts>([&](auto q) { issue(q, n); });
+    });
+    if (stages >= kStages)
+      stage_ready<(kStages - 1) * kStageLoads>();
+    else
+      stage_ready<0>();
     read_right(0, smem);
     read_left(0, smem);
     int stage = 0;
-    for (int it = stages; it > 0; --it, stage ^= 1) {
+    for (int it = stages; it > 0; --it) {
       const char* tile = smem + stage * kStage;
 #pragma unroll
       for (int turn = 0; turn < 3; ++turn) {
@@ -412,9 +409,14 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
         for (int i = 0; i < kParts; ++i) multiply(turn, i);
         __builtin_amdgcn_sched_barrier(0);
       }
-      stage_ready();
+      // the next stage: all that is newer may still be under way, as long as that is kStages - 2
+      if (kStages > 2 && it >= kStages)
+        stage_ready<(kStages - 2) * kStageLoads>();
+      else
+        stage_ready<0>();
+      const int after = stage + 1 < kStages ? stage + 1 : 0;
       if (it > 1) {
-        const char* next = smem + (stage ^ 1) * kStage;
+        const char* next = smem + after * kStage;
         read_right(0, next);
         read_left(0, next);
       }
@@ -425,9 +427,10 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
         __builtin_amdgcn_sched_barrier(0);
         if (more) issue(q, stage);
       });
+      stage = after;
     }
   }
-  stage_ready();                                         // the stages are free for the end
+  stage_ready<0>();                                      // the stages are free for the end
 
   end_tile<kType, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4, lane, split,
                                              row0 + wm * (kBM / kWM),
@@ -458,9 +461,10 @@ hipError_t launch_tile(int tile, ProductArgs& a, hipStream_t stream) {
   if (blocks < 1 || a.end.dtype != (kFp16 ? POINTID_FP16 : POINTID_BF16)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   switch (tile) {
-    case 0: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 256, 256, 2, 4>, grid, dim3(512), 0, stream, a);
-    case 1: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
-    case 2: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+    case 0: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 256, 256, 2, 4, 2>, grid, dim3(512), 0, stream, a);
+    case 1: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 128, 128, 4, 2, 3>, grid, dim3(512), 0, stream, a);
+    case 2: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 128, 128, 4, 2, 2>, grid, dim3(512), 0, stream, a);
+    case 3: return launch_kernel(product_kernel<kFp16, kForm, kHalves, 64, 128, 2, 2, 2>, grid, dim3(256), 0, stream, a);
   }
   return hipErrorInvalidValue;
 }

@@ -1,5 +1,4 @@
-// The matrix-core products of bf16 operands (and of fp32 ones in three bf16 parts), and the
-// choice of their tiles and splits.
+// The matrix-core products of bf16 operands, and the choice of tiles and splits of all types.
 #include "layers_mm.h"
 
 #include <algorithm>
@@ -17,15 +16,17 @@ struct TileCost {
   double stage, alone, ends;
   int resident;
 };
-constexpr TileCost kCost[kTiles] = {{1.21, 1.21, 6.8, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
+constexpr TileCost kCost[kTiles] = {
+    {1.21, 1.21, 6.8, 1}, {0.555, 0.555, 2.6, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
 constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 1}, {1.58, 2.79, 0.8, 2}};
 
 }  // namespace
 
 // The tile and split that the costs above put first.  Large tiles read their operands fewer
 // times (bf16 4096 x 1024 x 4096: 37 us in 256 x 256 tiles, 41 in 128 x 128, 49 in 64 x 128);
-// small ones fill the CUs where there are few (2048^3: 26 in 64 x 128, 29 in 128 x 128, 44
-// in split 256 x 256; its gated form 37 in 128 x 128, 49 and 51 in the others).
+// small ones fill the CUs where there are few (2048^3: 26 in 64 x 128, 44 in split 256 x 256;
+// its gated form 37 in 128 x 128, 49 and 51 in the others); three stages hide the loads of
+// one 128 x 128 tile a CU (4096 x 4096 x 1024: 43 against 50), two leave room for a second.
 ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
   static constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
   const double stages = (double)((inner + 63) / 64) * terms;
