@@ -17,7 +17,7 @@ struct TileCost {
   int resident;
 };
 constexpr TileCost kCost[kTiles] = {
-    {1.21, 1.21, 6.8, 1}, {0.555, 0.555, 2.6, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
+    {1.25, 1.25, 8.5, 1}, {0.555, 0.555, 2.6, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
 constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 1}, {1.58, 2.79, 0.8, 2}};
 
 }  // namespace
@@ -42,7 +42,7 @@ ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64
       const double per = std::ceil(stages / s), blocks = std::ceil(tiles * s / cus);
       const double rounds = std::ceil(blocks / c.resident);
       double us = std::max(blocks * c.stage, rounds * c.alone) * per + rounds * c.ends;
-      if (s > 1) us += f32 ? 6.0 + 0.138 * part_mb * s : 1.4 + 0.142 * part_mb * s;
+      if (s > 1) us += f32 ? 6.0 + 0.138 * part_mb * s : 1.4 + 0.16 * part_mb * s;
       if (us < least) least = us, best = {t, s};
     }
   }
