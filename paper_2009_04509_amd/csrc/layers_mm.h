@@ -58,7 +58,7 @@ __device__ __forceinline__ intx4 resource(const void* base) {
 // Nothing is returned; the stage's wait covers it.
 __device__ __forceinline__ void load_to_lds(intx4 rsrc, uint32_t offset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(lds), "v"(offset), "s"(rsrc) : "memory");
+               :: "s"(lds), "v"(offset), "s"(rsrc) : "memory", "m0");
 }
 
 // One operand's tile of kSide rows or columns: kInner: [kSide][64], else [64][kSide].

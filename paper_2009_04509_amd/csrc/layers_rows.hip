@@ -41,13 +41,14 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
   constexpr uint32_t kNowhere = 0x80000000u;           // past the resource's range: reads 0
   const int64_t from = col < a.end.cols - kCols ? col : a.end.cols - kCols;
+  const int64_t origin = col0 < a.end.cols - kCols ? col0 : a.end.cols - kCols;      // the first of any lane's
   const char* wp[kHalves];
   uint32_t offset[kHalves], step[kHalves];
 #pragma unroll
   for (int h = 0; h < kHalves; ++h) {
     const int64_t pitch = a.w[h].sk * kSize;
-    wp[h] = static_cast<const char*>(a.w[h].p) + (first + wave * kRowsPer) * pitch + col0 * kSize;
-    offset[h] = (uint32_t)((lane / kLanes) * pitch + (from - col0) * kSize);
+    wp[h] = static_cast<const char*>(a.w[h].p) + (first + wave * kRowsPer) * pitch + origin * kSize;
+    offset[h] = (uint32_t)((lane / kLanes) * pitch + (from - origin) * kSize);
     step[h] = (uint32_t)(kStep * pitch);
   }
   auto values = [](const uint4& r, float* w) {

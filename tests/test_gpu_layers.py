@@ -172,6 +172,23 @@ def test_gated(pid, layers, dtype, m, k, n):
             near(su, U_, eu + U_.abs() * U[dtype] + TINY[dtype], "u")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("n", [8, 9, 15, 255, 256, 257, 259, 260, 263, 264, 513, 1031])
+def test_few_rows_at_the_edges_of_their_strips(pid, layers, dtype, n):
+    """Widths that end a few columns into the streaming kernel's strip of 256."""
+    g = gen(n)
+    for m in (1, 2, 7):
+        k = 90
+        x, w, w2 = rand(g, m, k, dtype=dtype), rand(g, k, n, dtype=dtype), rand(g, k, n, dtype=dtype)
+        z, tz = sums(x, w, dtype)
+        z2, tz2 = sums(x, w2, dtype)
+        y = pid.pointid_dense(layers, dev(x), dev(w))
+        near(y, z, tz + z.abs() * U[dtype] + TINY[dtype], "y")
+        h = pid.pointid_gated(layers, dev(x), dev(w), dev(w2), act="none")
+        want = z * z2
+        near(h, want, z.abs() * tz2 + (z2.abs() + tz2) * tz + want.abs() * (U[dtype] + E) + TINY[dtype], "h")
+
+
 def kept(pid, v, eight):
     """(what is handed over, its values in 64 bits)"""
     if not eight:
