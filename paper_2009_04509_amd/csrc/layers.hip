@@ -297,13 +297,13 @@ struct Forward {
 };
 
 // Whether the weights are streamed past the rows.  fp32: up to 8 rows (8192 x 8192, 8 rows:
-// 63 us, on the matrix cores 70).  16 bits: up to 2 (a gated 4096 x 12288, 2 rows: 49 us
-// against 52; 4 rows: 58 against 52, as each value then costs more than its bytes), but up
-// to 8 where the matrix cores would take a copy of the weights first.  A lane reads 16 bytes
-// of a row, so a row has to have them.
+// 63 us, on the matrix cores 70).  16 bits: on the matrix cores from 2 rows on, and for one
+// row of up to 2^26 weights (4096 x 4096: 14 us against 16; a gated 4096 x 12288: 51
+// against 46), but up to 8 rows where they would take a copy of the weights first.  A lane
+// reads 16 bytes of a row, so a row has to have them.
 bool few_rows(const Forward& f) {
   if (f.m > kFewRows || f.n < (f.dtype == POINTID_FP32 ? 4 : 8)) return false;
-  if (f.dtype == POINTID_FP32 || f.m <= 2) return true;
+  if (f.dtype == POINTID_FP32 || (f.m == 1 && f.k * f.n * f.halves > int64_t(1) << 26)) return true;
   for (int h = 0; h < f.halves; ++h)
     if (!read_in_place(f.w[h].data, f.w[h].ld, f.dtype, f.n) || f.w[h].ld != f.w[0].ld) return true;
   return false;
