@@ -432,12 +432,13 @@ int pointid_client_close(pointid_client c);
  * Matrices are row-major device memory of the call's `dtype` (POINTID_FP32,
  * POINTID_BF16 or POINTID_FP16) with a row pitch of `ld` elements (at least the
  * columns; rows need no alignment beyond their element's), x [m][k], weights
- * [k][n], biases and their gradients fp32 [n] whatever the type.  0 <= m < 2^31,
+ * [k][n], biases and their gradients fp32 [n] whatever the type.  0 <= m <= 2^28,
  * 1 <= k, n <= 2^20.  Products are summed in fp32 and rounded to `dtype` once.
  * POINTID_FP32 products are those of operands cut exactly into three bf16 parts
  * each, without the terms below 2^-26 of a product (up to 8 rows: plain fp32).
- * Infinities and NaNs go through as in fp32 arithmetic.  Outputs must not
- * overlap inputs, but `y` may be `residual` itself.  16-bit operands whose base
+ * Infinities and NaNs go through as in fp32 arithmetic, but a sum of
+ * POINTID_FP32 values that itself passes the type's range may be a NaN instead of
+ * an infinity.  Outputs must not overlap inputs, but `y` may be `residual` itself.  16-bit operands whose base
  * is aligned to 16 bytes and whose columns and row pitch are multiples of 8, and
  * pitches up to 2^21, save a copy.  Results are the same bits for the same
  * arguments; the order of a sum depends on the sizes.  A call that takes scratch

@@ -20,7 +20,7 @@ struct pointid_layers_s {
 namespace {
 
 constexpr int64_t kMaxSide = int64_t(1) << 20;         // k and n
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;   // m
+constexpr int64_t kMaxRows = int64_t(1) << 28;         // m (a launch has fewer than 2^32 threads)
 constexpr int64_t kMaxPitch = int64_t(1) << 21;        // of an operand that the products read in place
 
 // dz of up to this many values is kept in two 16-bit parts: the rounding of so few does not
@@ -52,7 +52,7 @@ int check_call(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64
   if (dtype != POINTID_FP32 && dtype != POINTID_BF16 && dtype != POINTID_FP16)
     return set_error(POINTID_EUNSUPPORTED, "dtype must be POINTID_FP32, POINTID_BF16 or POINTID_FP16");
   if (act < POINTID_ACT_NONE || act > POINTID_ACT_SIGMOID) return set_error(POINTID_EINVAL, "act is no activation");
-  if (m < 0 || m > kMaxRows) return set_error(POINTID_EINVAL, "m must be in [0, 2^31)");
+  if (m < 0 || m > kMaxRows) return set_error(POINTID_EINVAL, "m must be in [0, 2^28]");
   if (k < 1 || k > kMaxSide || n < 1 || n > kMaxSide)
     return set_error(POINTID_EINVAL, "k and n must be in [1, 2^20]");
   return POINTID_OK;
@@ -303,6 +303,8 @@ struct Forward {
 // reads 16 bytes of a row, so a row has to have them.
 bool few_rows(const Forward& f) {
   if (f.m > kFewRows || f.n < (f.dtype == POINTID_FP32 ? 4 : 8)) return false;
+  for (int h = 0; h < f.halves; ++h)
+    if (f.w[h].ld > kMaxPitch) return false;           // past its 32-bit steps
   if (f.dtype == POINTID_FP32 || (f.m == 1 && f.k * f.n * f.halves > int64_t(1) << 26)) return true;
   for (int h = 0; h < f.halves; ++h)
     if (!read_in_place(f.w[h].data, f.w[h].ld, f.dtype, f.n) || f.w[h].ld != f.w[0].ld) return true;
@@ -496,7 +498,7 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
 int check_checkpoint_call(int dtype, int64_t rows, int64_t cols, const pointid_matrix* a, const pointid_checkpoint* c) {
   if (dtype != POINTID_FP32 && dtype != POINTID_BF16 && dtype != POINTID_FP16)
     return set_error(POINTID_EUNSUPPORTED, "dtype must be POINTID_FP32, POINTID_BF16 or POINTID_FP16");
-  if (rows < 0 || rows > kMaxRows) return set_error(POINTID_EINVAL, "rows must be in [0, 2^31)");
+  if (rows < 0 || rows > INT32_MAX) return set_error(POINTID_EINVAL, "rows must be in [0, 2^31)");
   if (cols < 1 || cols > kMaxSide) return set_error(POINTID_EINVAL, "cols must be in [1, 2^20]");
   if (rows == 0) return POINTID_OK;
   const int rc = check_matrix(a, "the matrix", dtype, rows, cols);

@@ -65,25 +65,34 @@ struct Tile32 {
       v[i] = make_float4(f[0], f[1], f[2], f[3]);
     }
   }
-  // The parts of the values to the three planes at `tile`.  The first two are cut to the
-  // largest bf16, so that an infinity or NaN stands in the last, which multiplies the first
-  // part of the other operand alone, and goes through as in fp32.
-  template <bool kLast>
-  static __device__ __forceinline__ uint32_t part(float& a, float& b) {
-    if constexpr (kLast) return Op16<false>::pack(a, b);
+  // The three parts of two values.  The largest values' first part is cut to the largest
+  // bf16.  kCare: an infinity or NaN stands in the last part (which multiplies the first part
+  // of the other operand alone) behind a 1 of its sign and a 0, and so goes through as in fp32.
+  template <bool kCare>
+  static __device__ __forceinline__ void cut(float a, float b, uint32_t (&part)[3]) {
     constexpr float kMost = 3.38953139e38f;
-    const uint32_t h = Op16<false>::pack(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
-    a -= __uint_as_float(h << 16);
-    b -= __uint_as_float(h & 0xFFFF0000u);
-    return h;
+    const bool fa = !kCare || __builtin_isfinite(a), fb = !kCare || __builtin_isfinite(b);
+    const float most_a = fa ? kMost : 1.f, most_b = fb ? kMost : 1.f;
+    auto rest = [&](uint32_t h) {
+      a -= __uint_as_float(h << 16);
+      b -= __uint_as_float(h & 0xFFFF0000u);
+      return h;
+    };
+    part[0] = rest(Op16<false>::pack(__builtin_amdgcn_fmed3f(a, -most_a, most_a), __builtin_amdgcn_fmed3f(b, -most_b, most_b)));
+    part[1] = rest(Op16<false>::pack(fa ? a : 0.f, fb ? b : 0.f));
+    part[2] = Op16<false>::pack(a, b);
   }
-  __device__ __forceinline__ void store(char* tile, float4 (&v)[kLoads]) const {
+  // The parts of the values to the three planes at `tile`.
+  template <bool kCare>
+  __device__ __forceinline__ void store(char* tile, const float4 (&v)[kLoads]) const {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      static_for<3>([&](auto p) {
-        const uint32_t x = part<p == 2>(v[i].x, v[i].y), y = part<p == 2>(v[i].z, v[i].w);
-        *reinterpret_cast<uint2*>(tile + p * kPlane + to[i]) = make_uint2(x, y);
-      });
+    for (int i = 0; i < kLoads; ++i) {
+      uint32_t x[3], y[3];
+      cut<kCare>(v[i].x, v[i].y, x);
+      cut<kCare>(v[i].z, v[i].w, y);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(tile + p * kPlane + to[i]) = make_uint2(x[p], y[p]);
+    }
   }
 };
 
@@ -126,11 +135,10 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
     return kHalves == 2 ? wn * 32 + i % 2 * 16 : wn * 64 % kHN + 16 * i;
   });
 
-  int to_load = a.split_each + (at.split < (uint32_t)a.split_more);
+  const int stages = a.split_each + (at.split < (uint32_t)a.split_more);
   const uint32_t first = at.split * a.split_each + (at.split < (uint32_t)a.split_more ? at.split : a.split_more);
-  int term = (int)(first / (uint32_t)a.stages);
-  int k0 = (int)(first - (uint32_t)term * a.stages) * kBK32;
-  const int stages = to_load;
+  const int term0 = (int)(first / (uint32_t)a.stages);
+  int to_load, term, k0;
   const int64_t left_step = (kLeftInner ? kBK32 : kBK32 * a.ld_left) * 4;
   const int64_t right_step = (kRightInner ? kBK32 : kBK32 * a.ld_right) * 4;
   const bool whole_left = kLeftInner ? a.inner % 4 == 0 : a.end.rows % 4 == 0;
@@ -152,13 +160,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
     if (k0 >= a.inner) k0 = 0, ++term;
     --to_load;
   };
-  auto store = [&](int stage) {
-    char* tile = smem + stage * kStage;
-    left.store(tile, lv);
-    right0.store(tile + kLeftBytes, rv0);
-    right1.store(tile + kLeftBytes + kRightBytes, rv1);
-  };
-  floatx4 acc[kFragsM][kFragsN] = {};
+  floatx4 acc[kFragsM][kFragsN];
   uint4 r[3][kFragsN], l[2][3];
   auto read_left = [&](const char* tile, int i) {
 #pragma unroll
@@ -172,7 +174,21 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
 #pragma unroll
         for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[i % 2][p], acc[i][j]);
   };
-  if (stages > 0) {
+  auto sum = [&](auto care) {
+    auto store = [&](int stage) {
+      char* tile = smem + stage * kStage;
+      left.template store<care>(tile, lv);
+      right0.template store<care>(tile + kLeftBytes, rv0);
+      right1.template store<care>(tile + kLeftBytes + kRightBytes, rv1);
+    };
+    to_load = stages;
+    term = term0;
+    k0 = (int)(first - (uint32_t)term0 * a.stages) * kBK32;
+#pragma unroll
+    for (int i = 0; i < kFragsM; ++i)
+#pragma unroll
+      for (int j = 0; j < kFragsN; ++j) acc[i][j] = floatx4{};
+    if (stages == 0) return;
     load();
     store(0);
     if (to_load > 0) load();
@@ -196,7 +212,18 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
       }
       __syncthreads();
     }
-  }
+  };
+  sum(std::false_type{});
+  // A value that is not finite makes all sums of its row or column so: these are made again
+  // with care (whole blocks, so that the loop does not pay for it).
+  float all = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFragsM; ++i)
+#pragma unroll
+    for (int j = 0; j < kFragsN; ++j)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) all = __builtin_fmaf(acc[i][j][c], 0.f, all);
+  if (__syncthreads_or(all != 0.f)) sum(std::true_type{});
   end_tile<POINTID_FP32, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4,
                                                     lane, at.split, row0 + wm * (kBM / kWM),
                                                     col0 + wn * (kHalves == 2 ? 32 : 64));

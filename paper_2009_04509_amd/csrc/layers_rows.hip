@@ -27,8 +27,8 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   constexpr int kLanes = kStrip / kCols;
   constexpr int kRowsPer = 64 / kLanes;
   constexpr int kStep = 4 * kRowsPer;
-  constexpr int kAhead = (kHalves == 2 ? 4 : 8)/2;        // reads in flight a lane
-  __shared__ float xs[kChunk * kM];
+  constexpr int kAhead = kHalves == 2 ? 2 : 4;          // reads of a half in flight a lane, and as many again
+  __shared__ float xs[(kChunk + 1) * kM];               // and a row of zeros, for what is past the end
   __shared__ float cs[kHalves][kM][kStrip];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int64_t col0 = (int64_t)blockIdx.x * kStrip;
@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   const int64_t first = a.per_split * blockIdx.y;
   const int64_t last = first + a.per_split < a.inner ? first + a.per_split : a.inner;
   float acc[kHalves][kM][kCols] = {};
+  if (tid < kM) xs[kChunk * kM + tid] = 0.f;
 
   // A lane whose columns do not all exist reads the row's last ones instead (cols >= kCols).
   constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
     auto multiply = [&](int buf, int base) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int k = base + u * kStep < len ? base + u * kStep : len - 1;     // past the end: times 0
+        const int k = base + u * kStep < len ? base + u * kStep : kChunk;
         float x[kM];
 #pragma unroll
         for (int r = 0; r < kM; ++r) x[r] = xs[k * kM + r];
