@@ -116,25 +116,35 @@ hipError_t launch_layers_join(const End& end, const float* part, int64_t part_ld
 
 // ---- layers_pass.hip: passes over one matrix
 // What the products take from scratch: a matrix copied to rows of `ld` values (a multiple of
-// 8), zero past its columns, or a checkpoint's values laid out so; and the column sums of a
-// gradient, from the sums of its blocks of rows (ld_src values from one to the next).
+// 8), zero past its columns, or a checkpoint's values laid out so.
 struct FillJob {
-  enum Kind { kCopy = 0, kLoad = 1, kSums = 2 };
+  enum Kind { kCopy = 0, kLoad = 1 };
   int32_t kind;
   int32_t dtype;
-  const void* src;             // kCopy: the matrix; kSums: the blocks' sums
+  const void* src;             // kCopy
   int64_t ld_src;
   Packed8 packed;              // kLoad
-  int64_t rows, cols;          // kSums: blocks, columns
+  int64_t rows, cols;
   void* out;
   int64_t ld;
   uint32_t first;              // set by the launch: the job's first block
 };
 struct FillJobs {
-  FillJob job[5];
+  FillJob job[3];
   int32_t count;
 };
 hipError_t launch_layers_fill(FillJobs jobs, hipStream_t stream);
+// The column sums of a gradient from the sums of its blocks of rows: 32 columns of a half a
+// block.
+struct SumsJobs {
+  const float* part;           // [rows][halves][cols]
+  int64_t rows, cols;
+  int32_t halves;
+  float* out[2];               // nullptr: not wanted
+  uint32_t half_blocks() const { return (uint32_t)((cols + 31) / 32); }
+  uint32_t blocks() const { return half_blocks() * (uint32_t)halves; }
+};
+hipError_t launch_layers_sums(const SumsJobs& jobs, hipStream_t stream);
 // A checkpoint's values as a matrix.
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
                                   hipStream_t stream);
@@ -158,9 +168,21 @@ struct GradArgs {
   void* out[2];                // each half: planes [parts][rows][ld], or fp32 [rows][ld]
   int64_t ld, plane;
   float* col_part;
+  uint32_t row_blocks, strips;  // set by the launch
 };
 // Rows of a block: 32, or 8 where that gives fewer than two blocks a CU.
 int grad_rows(int64_t rows, int64_t cols, int cus);
-hipError_t launch_layers_grad(const GradArgs& a, int block_rows, hipStream_t stream);
+// `fill`: jobs that the same launch takes.
+hipError_t launch_layers_grad(GradArgs a, int block_rows, FillJobs fill, hipStream_t stream);
+
+// ---- layers_mm.h: the products dx and dW of a gradient by one launch of one tile shape, and
+// its column sums.  splits of each; tile < 0: by launches of their own.
+struct PairPlan {
+  int tile;
+  int dx_splits, dw_splits;
+};
+PairPlan plan_pair(int64_t m, int64_t k, int64_t n, int halves, int parts, int cus);
+hipError_t launch_pair_bf16(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream);
+hipError_t launch_pair_fp16(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream);
 
 }  // namespace pointid

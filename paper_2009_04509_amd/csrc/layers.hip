@@ -218,9 +218,9 @@ struct Source {
   }
 };
 
-int run_fill(Call& call, const FillJobs& jobs, bool last) {
+int run_fill(Call& call, const FillJobs& jobs) {
   if (jobs.count == 0) return POINTID_OK;
-  return call.run("layers_fill", last, [&] { return launch_layers_fill(jobs, call.stream()); });
+  return call.run("layers_fill", false, [&] { return launch_layers_fill(jobs, call.stream()); });
 }
 
 // The weights of one or both halves: these share a pitch, so that where one is copied, so
@@ -267,6 +267,33 @@ int run_product(Call& call, Form form, const ProductPlan& plan, ProductArgs& a, 
   if (rc != POINTID_OK || plan.splits == 1) return rc;
   return call.run("layers_join", last,
                   [&] { return launch_layers_join(end, part, end.part_ld, plan.splits, call.stream()); });
+}
+
+// Both products of a gradient in one launch, and the joins.
+int run_pair(Call& call, const ProductPlan& dx_plan, const ProductPlan& dw_plan, ProductArgs& dx, ProductArgs& dw,
+             const SumsJobs& sums, int dtype, float* dx_part, float* dw_part) {
+  const End dx_end = dx.end, dw_end = dw.end;
+  auto split = [](ProductArgs& a, const ProductPlan& plan, float* part) {
+    a.splits = plan.splits;
+    if (plan.splits == 1) return;
+    a.end.mode = kEndPartial;
+    a.end.part = part;
+  };
+  split(dx, dx_plan, dx_part);
+  split(dw, dw_plan, dw_part);
+  int rc = call.run("layers_product", dx_plan.splits == 1 && dw_plan.splits == 1, [&] {
+    return dtype == POINTID_FP16 ? launch_pair_fp16(dx_plan.tile, dx, dw, sums, call.stream())
+                                 : launch_pair_bf16(dx_plan.tile, dx, dw, sums, call.stream());
+  });
+  if (rc == POINTID_OK && dx_plan.splits > 1)
+    rc = call.run("layers_join", dw_plan.splits == 1, [&] {
+      return launch_layers_join(dx_end, dx_part, dx_end.part_ld, dx_plan.splits, call.stream());
+    });
+  if (rc == POINTID_OK && dw_plan.splits > 1)
+    rc = call.run("layers_join", true, [&] {
+      return launch_layers_join(dw_end, dw_part, dw_end.part_ld, dw_plan.splits, call.stream());
+    });
+  return rc;
 }
 
 End end_of(int mode, int act, int dtype, int halves, int64_t rows, int64_t cols, const pointid_matrix& y0,
@@ -358,7 +385,7 @@ int run_forward(pointid_layers l, const Forward& f, hipStream_t stream) {
   std::memset(&jobs, 0, sizeof(jobs));
   sx.make(&jobs);
   for (int h = 0; h < f.halves; ++h) sw[h].make(&jobs);
-  rc = run_fill(call, jobs, false);
+  rc = run_fill(call, jobs);
   if (rc != POINTID_OK) return rc;
   ProductArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -442,57 +469,73 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
     dz[h].parts = read_dy || g.parts < 1 ? 1 : g.parts;
   }
   ProductPlan dx_plan = {0, 1}, dw_plan = {0, 1};
-  float* part = nullptr;
   const bool f32 = b.dtype == POINTID_FP32;
-  if (want_dx) dx_plan = plan_product(f32, b.m, b.k, 1, b.n, b.halves * dz[0].parts, l->cus);
-  if (want_dw) dw_plan = plan_product(f32, b.k, b.n, b.halves, b.m, dz[0].parts, l->cus);
-  const size_t dx_part = part_bytes(dx_plan.splits, dx_end), dw_part = part_bytes(dw_plan.splits, dw_end);
-  call.want(&part, dx_part > dw_part ? dx_part : dw_part);       // one after the other
+  bool pair = false;
+  if (want_dx && want_dw && !f32) {
+    const PairPlan plan = plan_pair(b.m, b.k, b.n, b.halves, dz[0].parts, l->cus);
+    pair = plan.tile >= 0;
+    dx_plan = {plan.tile, plan.dx_splits};
+    dw_plan = {plan.tile, plan.dw_splits};
+  }
+  if (want_dx && !pair) dx_plan = plan_product(f32, b.m, b.k, 1, b.n, b.halves * dz[0].parts, l->cus);
+  if (want_dw && !pair) dw_plan = plan_product(f32, b.k, b.n, b.halves, b.m, dz[0].parts, l->cus);
+  float *part = nullptr, *dw_part = nullptr;
+  const size_t dx_bytes = part_bytes(dx_plan.splits, dx_end), dw_bytes = part_bytes(dw_plan.splits, dw_end);
+  if (pair) {
+    call.want(&part, dx_bytes);
+    call.want(&dw_part, dw_bytes);
+  } else {
+    call.want(&part, dx_bytes > dw_bytes ? dx_bytes : dw_bytes);       // one after the other
+  }
   int rc = call.reserve();
   if (rc != POINTID_OK) return rc;
 
-  if (g.parts != 0 || want_db) {
-    rc = call.run("layers_grad", false, [&] { return launch_layers_grad(g, block_rows, stream); });
-    if (rc != POINTID_OK) return rc;
-  }
   FillJobs jobs;
   std::memset(&jobs, 0, sizeof(jobs));
-  for (int h = 0; h < b.halves; ++h) {
-    if (!b.db[h]) continue;
-    FillJob& j = jobs.job[jobs.count++];
-    j.kind = FillJob::kSums;
-    j.src = g.col_part + h * b.n, j.ld_src = b.halves * b.n;
-    j.rows = grad_blocks, j.cols = b.n;
-    j.out = b.db[h];
-  }
   for (int h = 0; h < b.halves && want_dx; ++h) sw[h].make(&jobs);
   if (want_dw) sx.make(&jobs);
-  rc = run_fill(call, jobs, !products);
+  if (g.parts != 0 || want_db)
+    rc = call.run("layers_grad", false, [&] { return launch_layers_grad(g, block_rows, jobs, stream); });
+  else
+    rc = run_fill(call, jobs);
   if (rc != POINTID_OK) return rc;
+  SumsJobs sums;
+  std::memset(&sums, 0, sizeof(sums));
+  if (want_db) {
+    sums = {g.col_part, grad_blocks, b.n, b.halves, {b.db[0], b.db[1]}};
+    if (!pair) {
+      rc = call.run("layers_sums", !products, [&] { return launch_layers_sums(sums, stream); });
+      if (rc != POINTID_OK) return rc;
+    }
+  }
   for (int h = 0; h < 2; ++h) dz[h].base = read_dy ? b.dy.data : g.out[h];
 
+  if (!pair) dw_part = part;
+  ProductArgs dx, dw;
+  std::memset(&dx, 0, sizeof(dx));
+  std::memset(&dw, 0, sizeof(dw));
   if (want_dx) {
-    ProductArgs a;
-    std::memset(&a, 0, sizeof(a));
-    for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = add_terms(&a, dz[h], sw[h].planes, nullptr);
+    for (int h = 0; h < b.halves && rc == POINTID_OK; ++h) rc = add_terms(&dx, dz[h], sw[h].planes, nullptr);
     if (rc != POINTID_OK) return rc;
-    a.inner = (int32_t)b.n;
-    a.ld_left = dz[0].ld;
-    a.ld_right = sw[0].planes.ld;
-    a.end = dx_end;
-    rc = run_product(call, kDx, dx_plan, a, b.dtype, part, !want_dw);
+    dx.inner = (int32_t)b.n;
+    dx.ld_left = dz[0].ld;
+    dx.ld_right = sw[0].planes.ld;
+    dx.end = dx_end;
+  }
+  if (want_dw) {
+    rc = add_terms(&dw, sx.planes, dz[0], b.halves == 2 ? &dz[1] : nullptr);
+    if (rc != POINTID_OK) return rc;
+    dw.inner = (int32_t)b.m;
+    dw.ld_left = sx.planes.ld;
+    dw.ld_right = dz[0].ld;
+    dw.end = dw_end;
+  }
+  if (pair) return run_pair(call, dx_plan, dw_plan, dx, dw, sums, b.dtype, part, dw_part);
+  if (want_dx) {
+    rc = run_product(call, kDx, dx_plan, dx, b.dtype, part, !want_dw);
     if (rc != POINTID_OK) return rc;
   }
-  if (!want_dw) return POINTID_OK;
-  ProductArgs a;
-  std::memset(&a, 0, sizeof(a));
-  rc = add_terms(&a, sx.planes, dz[0], b.halves == 2 ? &dz[1] : nullptr);
-  if (rc != POINTID_OK) return rc;
-  a.inner = (int32_t)b.m;
-  a.ld_left = sx.planes.ld;
-  a.ld_right = dz[0].ld;
-  a.end = dw_end;
-  return run_product(call, kDw, dw_plan, a, b.dtype, part, true);
+  return want_dw ? run_product(call, kDw, dw_plan, dw, b.dtype, dw_part, true) : POINTID_OK;
 }
 
 int check_checkpoint_call(int dtype, int64_t rows, int64_t cols, const pointid_matrix* a, const pointid_checkpoint* c) {

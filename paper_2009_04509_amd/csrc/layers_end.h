@@ -358,6 +358,31 @@ __device__ __forceinline__ void load_codes(const Packed8& s, int64_t row, int64_
   r.values(v);
 }
 
+// Block `block` of the column sums, by kThreads threads: 32 of them a row of the partial sums
+// in turn; added in order at the end.  sums: kThreads / 32 * 33 values.
+template <int kThreads>
+__device__ __forceinline__ void sum_columns(const SumsJobs& a, uint32_t block, float* sums) {
+  constexpr int kSubs = kThreads / 32;
+  const uint32_t strips = (uint32_t)((a.cols + 31) / 32);
+  const int h = block >= strips;
+  float* const out = a.out[h];
+  if (!out) return;
+  const int c = threadIdx.x % 32, sub = threadIdx.x / 32;
+  const int64_t col = (int64_t)(block - h * strips) * 32 + c, pitch = a.halves * a.cols;
+  const float* const part = a.part + h * a.cols + col;
+  float t = 0.f;
+  if (col < a.cols)
+#pragma unroll 4
+    for (int64_t b = sub; b < a.rows; b += kSubs) t += part[b * pitch];
+  sums[sub * 33 + c] = t;
+  __syncthreads();
+  if (sub != 0 || col >= a.cols) return;
+  float v = 0.f;
+#pragma unroll
+  for (int s = 0; s < kSubs; ++s) v += sums[s * 33 + c];
+  out[col] = v;
+}
+
 // 8 columns of partial sums (fp32, rows padded to whole blocks of 32 columns)
 __device__ __forceinline__ void store_partial(const End& e, int split, int half, bool live, int64_t row, int64_t col,
                                               const float* v) {

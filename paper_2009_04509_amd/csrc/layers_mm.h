@@ -151,12 +151,12 @@ struct Place {
   uint32_t split;
   int64_t tm, tn;
 };
-__device__ __forceinline__ Place block_place(const ProductArgs& a) {
+__device__ __forceinline__ Place block_place(const ProductArgs& a, uint32_t block) {
   // Blocks go to the 8 XCDs in turn: each XCD takes a contiguous stretch of the tiles, in
   // groups of 8 rows of tiles walked column by column, so that the blocks which run
   // together on an XCD share operands in its L2.
-  const uint32_t xcd = blockIdx.x % 8;
-  uint32_t id = xcd * a.xcd_each + (xcd < (uint32_t)a.xcd_more ? xcd : a.xcd_more) + blockIdx.x / 8;
+  const uint32_t xcd = block % 8;
+  uint32_t id = xcd * a.xcd_each + (xcd < (uint32_t)a.xcd_more ? xcd : a.xcd_more) + block / 8;
   uint32_t split = 0;
   if (a.splits > 1) {
     const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n;
@@ -272,8 +272,16 @@ __device__ __forceinline__ floatx4 mfma(const uint4& a, const uint4& b, const fl
   return Op16<kFp16>::mfma(a, b, c);
 }
 
+// Shared memory of a block: its stages, where the end's takes their place, and a little more
+// for that with many small waves.
+template <int kBM, int kBN, int kWM, int kWN, int kStages>
+constexpr int shared_bytes() {
+  constexpr int kStage = (kBM + kBN) * kBK * 2;
+  return kWM * kWN * kEndWave > kStages * kStage ? kWM * kWN * kEndWave : kStages * kStage;
+}
+
 template <bool kFp16, int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN, int kStages>
-__global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) {
+__device__ __forceinline__ void product_block(const ProductArgs& a, uint32_t block, char* smem) {
   constexpr int kThreads = 64 * kWM * kWN;
   constexpr int kType = kFp16 ? POINTID_FP16 : POINTID_BF16;
   constexpr bool kLeftInner = kForm != kDw, kRightInner = kForm == kDx;
@@ -284,16 +292,13 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
   using Left = Tile<kLeftInner, kBM, kThreads>;
   using Right = Tile<kRightInner, kHN, kThreads>;
   constexpr int kStage = Left::kBytes + 2 * Right::kBytes;
-  // the end uses the stages' memory, and a little more with many small waves
-  constexpr int kShared = kWM * kWN * kEndWave > kStages * kStage ? kWM * kWN * kEndWave : kStages * kStage;
   constexpr int kStageLoads = Left::kLoads + 2 * Right::kLoads;
-  __shared__ __align__(1024) char smem[kShared];
 
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = wave / kWN, wn = wave % kWN;
 
-  const Place at = block_place(a);
+  const Place at = block_place(a, block);
   const uint32_t split = at.split;
   const int64_t tm = at.tm, tn = at.tn;
   const int64_t row0 = tm * kBM;
@@ -437,6 +442,46 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) 
                                              col0 + wn * (kHalves == 2 ? 32 : 64));
 }
 
+template <bool kFp16, int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ void __launch_bounds__(64 * kWM * kWN) product_kernel(ProductArgs a) {
+  __shared__ __align__(1024) char smem[shared_bytes<kBM, kBN, kWM, kWN, kStages>()];
+  product_block<kFp16, kForm, kHalves, kBM, kBN, kWM, kWN, kStages>(a, blockIdx.x, smem);
+}
+
+// Both products of a gradient in one launch, their blocks mixed in units of 8 (one of each
+// XCD).  Those with the longer sums come first: their units are spread evenly over the first
+// half of the launch.  The very first blocks take the column sums.
+struct PairArgs {
+  ProductArgs dx, dw;
+  SumsJobs sums;
+  uint32_t sums_blocks, sums_units;
+  int32_t dx_first;
+  uint32_t first_units;
+  uint64_t ratio;              // 2^32 times their share of that part
+};
+template <bool kFp16, int kHalves, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ void __launch_bounds__(64 * kWM * kWN) pair_kernel(PairArgs a) {
+  __shared__ __align__(1024) char smem[shared_bytes<kBM, kBN, kWM, kWN, kStages>()];
+  if (blockIdx.x < a.sums_units * 8) {
+    if (blockIdx.x < a.sums_blocks) sum_columns<64 * kWM * kWN>(a.sums, blockIdx.x, reinterpret_cast<float*>(smem));
+    return;
+  }
+  const uint32_t unit = blockIdx.x / 8 - a.sums_units, xcd = blockIdx.x % 8;
+  auto first_before = [&](uint32_t u) {
+    const uint64_t n = u * a.ratio >> 32;
+    return n < a.first_units ? (uint32_t)n : a.first_units;
+  };
+  const uint32_t before = first_before(unit);
+  const bool first = first_before(unit + 1) > before;
+  const uint32_t mine = first ? before : unit - before;    // the block's unit of its product
+  auto here = [&](const ProductArgs& p) { return mine < p.xcd_each + (xcd < (uint32_t)p.xcd_more ? 1u : 0u); };
+  if (first == (a.dx_first != 0)) {
+    if (here(a.dx)) product_block<kFp16, kDx, 1, kBM, kBN, kWM, kWN, kStages>(a.dx, mine * 8 + xcd, smem);
+  } else {
+    if (here(a.dw)) product_block<kFp16, kDw, kHalves, kBM, kBN, kWM, kWN, kStages>(a.dw, mine * 8 + xcd, smem);
+  }
+}
+
 // What a launch works out for its blocks; returns their number, or 0.
 inline int64_t spread(ProductArgs& a, int64_t rows, int64_t cols, int inners) {
   const int64_t tm = (a.end.rows + rows - 1) / rows, tn = (a.end.cols + cols - 1) / cols;
@@ -481,6 +526,36 @@ hipError_t launch(Form form, const ProductPlan& plan, ProductArgs& a, hipStream_
       return two ? launch_tile<kFp16, kDw, 2>(plan.tile, a, stream) : launch_tile<kFp16, kDw, 1>(plan.tile, a, stream);
   }
   return hipErrorInvalidValue;
+}
+
+template <bool kFp16, int kHalves>
+hipError_t launch_pair_tile(int tile, PairArgs& a, hipStream_t stream) {
+  const int bm = kTileM[tile], bn = kTileN[tile];
+  const int64_t dx = spread(a.dx, bm, bn, kBK), dw = spread(a.dw, bm, bn / kHalves, kBK);
+  constexpr int kType = kFp16 ? POINTID_FP16 : POINTID_BF16;
+  if (dx < 1 || dw < 1 || a.dx.end.dtype != kType || a.dw.end.dtype != kType) return hipErrorInvalidValue;
+  const uint64_t dx_units = (uint64_t)(dx + 7) / 8, dw_units = (uint64_t)(dw + 7) / 8, units = dx_units + dw_units;
+  if (units > INT32_MAX / 8) return hipErrorInvalidValue;
+  a.dx_first = a.dx.split_each >= a.dw.split_each;
+  const uint64_t first = a.dx_first ? dx_units : dw_units;
+  const uint64_t part = first > units / 2 ? first : units / 2;
+  a.first_units = (uint32_t)first;
+  a.ratio = ((first << 32) + part - 1) / part;
+  a.sums_blocks = a.sums.part ? a.sums.blocks() : 0;
+  a.sums_units = (a.sums_blocks + 7) / 8;
+  const dim3 grid((unsigned)((units + a.sums_units) * 8));
+  switch (tile) {
+    case 1: return launch_kernel(pair_kernel<kFp16, kHalves, 128, 128, 4, 2, 3>, grid, dim3(512), 0, stream, a);
+    case 2: return launch_kernel(pair_kernel<kFp16, kHalves, 128, 128, 4, 2, 2>, grid, dim3(512), 0, stream, a);
+    case 3: return launch_kernel(pair_kernel<kFp16, kHalves, 64, 128, 2, 2, 2>, grid, dim3(256), 0, stream, a);
+  }
+  return hipErrorInvalidValue;
+}
+template <bool kFp16>
+hipError_t launch_pair(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream) {
+  PairArgs a;
+  a.dx = dx, a.dw = dw, a.sums = sums;
+  return dw.end.halves == 2 ? launch_pair_tile<kFp16, 2>(tile, a, stream) : launch_pair_tile<kFp16, 1>(tile, a, stream);
 }
 
 }  // namespace mm

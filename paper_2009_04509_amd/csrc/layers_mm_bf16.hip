@@ -20,6 +20,47 @@ constexpr TileCost kCost[kTiles] = {
     {1.25, 1.25, 8.5, 1}, {0.555, 0.555, 2.6, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
 constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 1}, {1.58, 2.79, 0.8, 2}};
 
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+
+struct Timed {
+  ProductPlan plan;
+  double us;
+};
+
+// A product's tiles of shape t, the stages of each, and the MB of fp32 results that a split
+// of its sum writes and reads.
+struct Sizes {
+  double tiles, stages, part_mb;
+};
+Sizes sizes_of(bool f32, int t, int64_t rows, int64_t cols, int halves, int64_t inner, int terms) {
+  const int64_t bm = f32 ? kTileM32[t] : kTileM[t], bn = (f32 ? kTileN32[t] : kTileN[t]) / halves;
+  return {(double)((rows + bm - 1) / bm) * (double)((cols + bn - 1) / bn), (double)((inner + 63) / 64) * terms,
+          8e-6 * (double)rows * (double)cols * halves};
+}
+// Whether a sum may be split so: two stages each, and not many more blocks than the card holds.
+bool may_split(const Sizes& z, int splits, int cus) {
+  return splits == 1 || (2 * splits <= z.stages && z.tiles * splits <= 8.0 * cus);
+}
+double join_cost(bool f32, const Sizes& z, int splits) {
+  return splits == 1 ? 0 : f32 ? 6.0 + 0.138 * z.part_mb * splits : 1.4 + 0.16 * z.part_mb * splits;
+}
+
+Timed least_cost(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
+  Timed best = {{0, 1}, 1e300};
+  for (int t = 0; t < (f32 ? kTiles32 : kTiles); ++t) {
+    const TileCost& c = f32 ? kCost32[t] : kCost[t];
+    const Sizes z = sizes_of(f32, t, rows, cols, halves, inner, terms);
+    for (int s : kSplits) {
+      if (!may_split(z, s, cus)) break;
+      const double per = std::ceil(z.stages / s), blocks = std::ceil(z.tiles * s / cus);
+      const double rounds = std::ceil(blocks / c.resident);
+      const double us = std::max(blocks * c.stage, rounds * c.alone) * per + rounds * c.ends + join_cost(f32, z, s);
+      if (us < best.us) best = {{t, s}, us};
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 // The tile and split that the costs above put first.  Large tiles read their operands fewer
@@ -28,22 +69,37 @@ constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 
 // its gated form 37 in 128 x 128, 49 and 51 in the others); three stages hide the loads of
 // one 128 x 128 tile a CU (4096 x 4096 x 1024: 43 against 50), two leave room for a second.
 ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
-  static constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
-  const double stages = (double)((inner + 63) / 64) * terms;
-  const double part_mb = 8e-6 * (double)rows * (double)cols * halves;          // written and read
-  ProductPlan best = {0, 1};
-  double least = 1e300;
-  for (int t = 0; t < (f32 ? kTiles32 : kTiles); ++t) {
-    const TileCost& c = f32 ? kCost32[t] : kCost[t];
-    const int64_t bm = f32 ? kTileM32[t] : kTileM[t], bn = (f32 ? kTileN32[t] : kTileN[t]) / halves;
-    const double tiles = (double)((rows + bm - 1) / bm) * (double)((cols + bn - 1) / bn);
+  return least_cost(f32, rows, cols, halves, inner, terms, cus).plan;
+}
+
+// Together, the blocks of one product fill the CUs that the other leaves, and no second
+// launch waits for the first's last blocks (bf16, dx and dW of 1693 x 1024 x 2048: 23 us
+// against 42 by two launches; of 4096 x 1024 x 4096: 72 against 84), and what one writes goes
+// along with what the other reads (1693 x 92928 x 128: 198 against 220).  256 x 256 tiles are
+// better alone (16384 x 1024 x 1024: 86 against 90; 4096^3: 214 against 270 in smaller ones).
+// A CU's time is that of its share of the stages, or of the longest block's: as many stages as
+// the other's blocks have beside them, the rest alone.  Two launches cost 6 us more than their
+// blocks, a second join 3.4 (fitted to 20 shapes; within 5 % of the fastest).
+PairPlan plan_pair(int64_t m, int64_t k, int64_t n, int halves, int parts, int cus) {
+  PairPlan best = {-1, 1, 1};
+  double least = least_cost(false, m, k, 1, n, halves * parts, cus).us +
+                 least_cost(false, k, n, halves, m, parts, cus).us + 6.0;
+  for (int t = 1; t < kTiles; ++t) {
+    const TileCost& c = kCost[t];
+    const Sizes dx = sizes_of(false, t, m, k, 1, n, halves * parts), dw = sizes_of(false, t, k, n, halves, m, parts);
     for (int s : kSplits) {
-      if (s > 1 && (2 * s > stages || tiles * s > 8.0 * cus)) break;
-      const double per = std::ceil(stages / s), blocks = std::ceil(tiles * s / cus);
-      const double rounds = std::ceil(blocks / c.resident);
-      double us = std::max(blocks * c.stage, rounds * c.alone) * per + rounds * c.ends;
-      if (s > 1) us += f32 ? 6.0 + 0.138 * part_mb * s : 1.4 + 0.16 * part_mb * s;
-      if (us < least) least = us, best = {t, s};
+      if (!may_split(dx, s, cus)) break;
+      for (int r : kSplits) {
+        if (!may_split(dw, r, cus)) break;
+        const double x = std::ceil(dx.stages / s), w = std::ceil(dw.stages / r), count = dx.tiles * s + dw.tiles * r;
+        const double blocks = std::ceil(count / cus), beside = std::min(blocks, (double)c.resident);
+        const double work = (dx.tiles * s * x + dw.tiles * r * w) / count * blocks * c.stage;
+        const double longest = blocks > 1 ? std::min(x, w) * std::max(beside * c.stage, c.alone) + std::abs(x - w) * c.alone
+                                          : std::max(x, w) * c.alone;
+        const double us = std::max(work, longest) + std::ceil(blocks / c.resident) * c.ends + join_cost(false, dx, s) +
+                          join_cost(false, dw, r) + 2.0 * (s > 1) + 2.0 * (r > 1);
+        if (us < least) least = us, best = {t, s, r};
+      }
     }
   }
   return best;
@@ -51,6 +107,10 @@ ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64
 
 hipError_t launch_product_bf16(Form form, const ProductPlan& plan, ProductArgs a, hipStream_t stream) {
   return mm::launch<false>(form, plan, a, stream);
+}
+
+hipError_t launch_pair_bf16(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream) {
+  return mm::launch_pair<false>(tile, dx, dw, sums, stream);
 }
 
 }  // namespace pointid

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = wave / kWN, wn = wave % kWN;
-  const Place at = block_place(a);
+  const Place at = block_place(a, blockIdx.x);
   const int64_t row0 = at.tm * kBM;
   const int64_t col0 = at.tn * (kHalves == 2 ? kHN : kBN), col1 = kHalves == 2 ? col0 : col0 + kHN;
   Left left;

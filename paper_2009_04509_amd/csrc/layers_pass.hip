@@ -27,36 +27,14 @@ __global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64
   });
 }
 
-// Sums of `blocks` rows of 32 columns from `col` on, every `pitch` values: 8 lanes a column.
-__device__ __forceinline__ void sum_columns(const float* part, int64_t blocks, int64_t pitch, int64_t col, int64_t cols,
-                                            float* out) {
-  __shared__ float sums[8][33];
-  const int c = threadIdx.x % 32, sub = threadIdx.x / 32;
-  float t = 0.f;
-  if (col + c < cols)
-#pragma unroll 4
-    for (int64_t b = sub; b < blocks; b += 8) t += part[b * pitch + col + c];
-  sums[sub][c] = t;
-  __syncthreads();
-  if (sub != 0 || col + c >= cols) return;
-  float v = 0.f;
-#pragma unroll
-  for (int s = 0; s < 8; ++s) v += sums[s][c];
-  out[col + c] = v;
-}
-
-// The jobs that stand between the gradient and the products, by one launch: each takes the
-// blocks from its first to the next job's.
-__global__ void __launch_bounds__(256) fill_kernel(FillJobs a) {
+// Jobs' blocks from the launch's block `first_block` on, by the blocks up to `end_block`:
+// each job takes those from its first to the next job's.
+__device__ __forceinline__ void run_fill_block(const FillJobs& a, uint32_t first_block, uint32_t end_block) {
+  const uint32_t at = blockIdx.x - first_block;
   int j = 0;
-  while (j + 1 < a.count && blockIdx.x >= a.job[j + 1].first) ++j;
+  while (j + 1 < a.count && at >= a.job[j + 1].first) ++j;
   const FillJob& job = a.job[j];
-  const uint32_t block = blockIdx.x - job.first, blocks = (j + 1 < a.count ? a.job[j + 1].first : gridDim.x) - job.first;
-  if (job.kind == FillJob::kSums) {
-    sum_columns(static_cast<const float*>(job.src), job.rows, job.ld_src, (int64_t)block * 32, job.cols,
-                static_cast<float*>(job.out));
-    return;
-  }
+  const uint32_t block = at - job.first, blocks = (j + 1 < a.count ? a.job[j + 1].first : end_block - first_block) - job.first;
   each_piece(job.rows, job.ld / 8, (int64_t)block * 256 + threadIdx.x, (int64_t)blocks * 256,
              [&](int64_t row, int64_t col) {
     float v[8] = {};
@@ -66,6 +44,11 @@ __global__ void __launch_bounds__(256) fill_kernel(FillJobs a) {
       load_codes(job.packed, row, col, job.cols, v);
     store_cols<8>(job.out, row * job.ld + col, job.dtype, 8, v);
   });
+}
+__global__ void __launch_bounds__(256) fill_kernel(FillJobs a) { run_fill_block(a, 0, gridDim.x); }
+__global__ void __launch_bounds__(256) sums_kernel(SumsJobs a) {
+  __shared__ float sums[256 / 32 * 33];
+  sum_columns<256>(a, blockIdx.x, sums);
 }
 
 // A block of 32 values by 4 neighbouring lanes.
@@ -89,17 +72,24 @@ __global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, i
 // How the activations of a gradient are kept.
 enum { kKeptNot = 0, kKeptWhole = 1, kKeptPacked = 2 };
 
-// Each block: 8 kTurns rows x 256 columns; 8 rows by 32 pieces of 8 columns at a time, two
+// Each block: 8 kTurns rows x 256 columns (the blocks past those take the fill's jobs, which
+// need nothing of the gradient); 8 rows by 32 pieces of 8 columns at a time, two
 // such turns' reads in flight before any is used (a read used at once: 163 us for a gated
 // 8192 x 8192 in bf16).
 template <int kType, int kHalves, int kKept, int kTurns>
-__global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
+__global__ void __launch_bounds__(256) grad_kernel(GradArgs a, FillJobs fill) {
   __shared__ float sums[8][256 + 8];
+  const uint32_t row_blocks = a.row_blocks, grad_blocks = row_blocks * a.strips;
+  if (blockIdx.x >= grad_blocks) {
+    run_fill_block(fill, grad_blocks, gridDim.x);
+    return;
+  }
+  const uint32_t strip = blockIdx.x / row_blocks, row_block = blockIdx.x - strip * row_blocks;
   constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
   const int piece = threadIdx.x % 32, sub = threadIdx.x / 32;
-  const int64_t col = (int64_t)blockIdx.y * 256 + piece * 8;
+  const int64_t col = (int64_t)strip * 256 + piece * 8;
   const int n = piece_cols(a.cols, col);
-  const int64_t row0 = (int64_t)blockIdx.x * (8 * kTurns) + sub;
+  const int64_t row0 = (int64_t)row_block * (8 * kTurns) + sub;
   // rows from row0 on, and where the lane's pieces of them stand
   const int left = (int)(a.rows - row0 < 8 * kTurns ? a.rows - row0 : 8 * kTurns);
   const int64_t blocks8 = (a.cols + kBlock8 - 1) / kBlock8;
@@ -191,18 +181,18 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[sub][piece * 8 + i] = total[h][i];
     __syncthreads();
-    const int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x;
+    const int64_t c = (int64_t)strip * 256 + threadIdx.x;
     float t = 0.f;
 #pragma unroll
     for (int s = 0; s < 8; ++s) t += sums[s][threadIdx.x];
-    if (c < a.cols) a.col_part[((int64_t)blockIdx.x * kHalves + h) * a.cols + c] = t;
+    if (c < a.cols) a.col_part[((int64_t)row_block * kHalves + h) * a.cols + c] = t;
     __syncthreads();
   }
 }
 
 template <int kType, int kTurns>
-hipError_t launch_grad(const GradArgs& a, dim3 grid, hipStream_t stream) {
-  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, a); };
+hipError_t launch_grad(const GradArgs& a, const FillJobs& fill, dim3 grid, hipStream_t stream) {
+  auto go = [&](auto kernel) { return launch_kernel(kernel, grid, dim3(256), 0, stream, a, fill); };
   if (a.halves == 2)
     return a.z[0].matrix ? go(grad_kernel<kType, 2, kKeptWhole, kTurns>) : go(grad_kernel<kType, 2, kKeptPacked, kTurns>);
   if (a.z[0].matrix) return go(grad_kernel<kType, 1, kKeptWhole, kTurns>);
@@ -273,15 +263,27 @@ unsigned pass_blocks(int64_t items) {
 
 }  // namespace
 
-hipError_t launch_layers_fill(FillJobs jobs, hipStream_t stream) {
+namespace {
+// Sets the jobs' first blocks; their number.
+uint32_t spread_fill(FillJobs* jobs) {
   uint32_t blocks = 0;
-  for (int j = 0; j < jobs.count; ++j) {
-    FillJob& job = jobs.job[j];
+  for (int j = 0; j < jobs->count; ++j) {
+    FillJob& job = jobs->job[j];
     job.first = blocks;
-    blocks += job.kind == FillJob::kSums ? (uint32_t)((job.cols + 31) / 32) : pass_blocks(job.rows * (job.ld / 8));
+    blocks += pass_blocks(job.rows * (job.ld / 8));
   }
+  return blocks;
+}
+}  // namespace
+
+hipError_t launch_layers_fill(FillJobs jobs, hipStream_t stream) {
+  const uint32_t blocks = spread_fill(&jobs);
   if (blocks == 0) return hipSuccess;
   return launch_kernel(fill_kernel, dim3(blocks), dim3(256), 0, stream, jobs);
+}
+
+hipError_t launch_layers_sums(const SumsJobs& jobs, hipStream_t stream) {
+  return launch_kernel(sums_kernel, dim3(jobs.blocks()), dim3(256), 0, stream, jobs);
 }
 
 hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols, int dtype, void* out, int64_t ld,
@@ -300,18 +302,25 @@ int grad_rows(int64_t rows, int64_t cols, int cus) {
   return ((rows + 31) / 32) * ((cols + 255) / 256) < 2 * cus ? 8 : 32;
 }
 
-hipError_t launch_layers_grad(const GradArgs& a, int block_rows, hipStream_t stream) {
+hipError_t launch_layers_grad(GradArgs a, int block_rows, FillJobs fill, hipStream_t stream) {
   const int64_t width = a.parts != 0 && a.ld > a.cols ? a.ld : a.cols;
-  const dim3 grid((unsigned)((a.rows + block_rows - 1) / block_rows), (unsigned)((width + 255) / 256));
+  const int64_t row_blocks = (a.rows + block_rows - 1) / block_rows, strips = (width + 255) / 256;
+  const int64_t blocks = row_blocks * strips + spread_fill(&fill);
+  if (blocks > INT32_MAX / 256 * 2) return hipErrorInvalidValue;
+  a.row_blocks = (uint32_t)row_blocks;
+  a.strips = (uint32_t)strips;
+  const dim3 grid((unsigned)blocks);
   // the halves are kept alike (the caller checks)
   if (a.halves == 2 && (!a.z[0].matrix != !a.z[1].matrix || !a.z[0].any() || !a.z[1].any())) return hipErrorInvalidValue;
+  auto go = [&](auto type) {
+    constexpr int kType = type;
+    return block_rows == 8 ? launch_grad<kType, 1>(a, fill, grid, stream) : launch_grad<kType, 4>(a, fill, grid, stream);
+  };
   switch (a.dtype) {
-    case POINTID_FP32:
-      return block_rows == 8 ? launch_grad<POINTID_FP32, 1>(a, grid, stream) : launch_grad<POINTID_FP32, 4>(a, grid, stream);
-    case POINTID_BF16:
-      return block_rows == 8 ? launch_grad<POINTID_BF16, 1>(a, grid, stream) : launch_grad<POINTID_BF16, 4>(a, grid, stream);
+    case POINTID_FP32: return go(std::integral_constant<int, POINTID_FP32>{});
+    case POINTID_BF16: return go(std::integral_constant<int, POINTID_BF16>{});
   }
-  return block_rows == 8 ? launch_grad<POINTID_FP16, 1>(a, grid, stream) : launch_grad<POINTID_FP16, 4>(a, grid, stream);
+  return go(std::integral_constant<int, POINTID_FP16>{});
 }
 
 hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols, hipStream_t stream) {
