@@ -181,8 +181,9 @@ struct PairPlan {
   int tile;
   int dx_splits, dw_splits;
 };
-PairPlan plan_pair(int64_t m, int64_t k, int64_t n, int halves, int parts, int cus);
+PairPlan plan_pair(bool f32, int64_t m, int64_t k, int64_t n, int halves, int parts, int cus);
 hipError_t launch_pair_bf16(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream);
+hipError_t launch_pair_f32(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream);
 hipError_t launch_pair_fp16(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream);
 
 }  // namespace pointid

@@ -282,8 +282,9 @@ int run_pair(Call& call, const ProductPlan& dx_plan, const ProductPlan& dw_plan,
   split(dx, dx_plan, dx_part);
   split(dw, dw_plan, dw_part);
   int rc = call.run("layers_product", dx_plan.splits == 1 && dw_plan.splits == 1, [&] {
-    return dtype == POINTID_FP16 ? launch_pair_fp16(dx_plan.tile, dx, dw, sums, call.stream())
-                                 : launch_pair_bf16(dx_plan.tile, dx, dw, sums, call.stream());
+    return dtype == POINTID_FP32   ? launch_pair_f32(dx_plan.tile, dx, dw, sums, call.stream())
+           : dtype == POINTID_FP16 ? launch_pair_fp16(dx_plan.tile, dx, dw, sums, call.stream())
+                                   : launch_pair_bf16(dx_plan.tile, dx, dw, sums, call.stream());
   });
   if (rc == POINTID_OK && dx_plan.splits > 1)
     rc = call.run("layers_join", dw_plan.splits == 1, [&] {
@@ -471,8 +472,8 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   ProductPlan dx_plan = {0, 1}, dw_plan = {0, 1};
   const bool f32 = b.dtype == POINTID_FP32;
   bool pair = false;
-  if (want_dx && want_dw && !f32) {
-    const PairPlan plan = plan_pair(b.m, b.k, b.n, b.halves, dz[0].parts, l->cus);
+  if (want_dx && want_dw) {
+    const PairPlan plan = plan_pair(f32, b.m, b.k, b.n, b.halves, dz[0].parts, l->cus);
     pair = plan.tile >= 0;
     dx_plan = {plan.tile, plan.dx_splits};
     dw_plan = {plan.tile, plan.dw_splits};

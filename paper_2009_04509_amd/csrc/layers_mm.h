@@ -459,11 +459,11 @@ struct PairArgs {
   uint32_t first_units;
   uint64_t ratio;              // 2^32 times their share of that part
 };
-template <bool kFp16, int kHalves, int kBM, int kBN, int kWM, int kWN, int kStages>
-__global__ void __launch_bounds__(64 * kWM * kWN) pair_kernel(PairArgs a) {
-  __shared__ __align__(1024) char smem[shared_bytes<kBM, kBN, kWM, kWN, kStages>()];
+// The block's part: dx(args, block) or dw(args, block), or column sums in `smem`.
+template <int kThreads, class Dx, class Dw>
+__device__ __forceinline__ void pair_block(const PairArgs& a, char* smem, Dx&& dx, Dw&& dw) {
   if (blockIdx.x < a.sums_units * 8) {
-    if (blockIdx.x < a.sums_blocks) sum_columns<64 * kWM * kWN>(a.sums, blockIdx.x, reinterpret_cast<float*>(smem));
+    if (blockIdx.x < a.sums_blocks) sum_columns<kThreads>(a.sums, blockIdx.x, reinterpret_cast<float*>(smem));
     return;
   }
   const uint32_t unit = blockIdx.x / 8 - a.sums_units, xcd = blockIdx.x % 8;
@@ -476,10 +476,20 @@ __global__ void __launch_bounds__(64 * kWM * kWN) pair_kernel(PairArgs a) {
   const uint32_t mine = first ? before : unit - before;    // the block's unit of its product
   auto here = [&](const ProductArgs& p) { return mine < p.xcd_each + (xcd < (uint32_t)p.xcd_more ? 1u : 0u); };
   if (first == (a.dx_first != 0)) {
-    if (here(a.dx)) product_block<kFp16, kDx, 1, kBM, kBN, kWM, kWN, kStages>(a.dx, mine * 8 + xcd, smem);
+    if (here(a.dx)) dx(a.dx, mine * 8 + xcd);
   } else {
-    if (here(a.dw)) product_block<kFp16, kDw, kHalves, kBM, kBN, kWM, kWN, kStages>(a.dw, mine * 8 + xcd, smem);
+    if (here(a.dw)) dw(a.dw, mine * 8 + xcd);
   }
+}
+template <bool kFp16, int kHalves, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ void __launch_bounds__(64 * kWM * kWN) pair_kernel(PairArgs a) {
+  __shared__ __align__(1024) char smem[shared_bytes<kBM, kBN, kWM, kWN, kStages>()];
+  pair_block<64 * kWM * kWN>(
+      a, smem,
+      [&](const ProductArgs& p, uint32_t block) { product_block<kFp16, kDx, 1, kBM, kBN, kWM, kWN, kStages>(p, block, smem); },
+      [&](const ProductArgs& p, uint32_t block) {
+        product_block<kFp16, kDw, kHalves, kBM, kBN, kWM, kWN, kStages>(p, block, smem);
+      });
 }
 
 // What a launch works out for its blocks; returns their number, or 0.
@@ -528,22 +538,26 @@ hipError_t launch(Form form, const ProductPlan& plan, ProductArgs& a, hipStream_
   return hipErrorInvalidValue;
 }
 
-template <bool kFp16, int kHalves>
-hipError_t launch_pair_tile(int tile, PairArgs& a, hipStream_t stream) {
-  const int bm = kTileM[tile], bn = kTileN[tile];
-  const int64_t dx = spread(a.dx, bm, bn, kBK), dw = spread(a.dw, bm, bn / kHalves, kBK);
-  constexpr int kType = kFp16 ? POINTID_FP16 : POINTID_BF16;
-  if (dx < 1 || dw < 1 || a.dx.end.dtype != kType || a.dw.end.dtype != kType) return hipErrorInvalidValue;
+// The same of a pair of products in bm x bn tiles.
+inline int64_t spread_pair(PairArgs& a, int64_t bm, int64_t bn, int inners) {
+  const int64_t dx = spread(a.dx, bm, bn, inners), dw = spread(a.dw, bm, bn / a.dw.end.halves, inners);
   const uint64_t dx_units = (uint64_t)(dx + 7) / 8, dw_units = (uint64_t)(dw + 7) / 8, units = dx_units + dw_units;
-  if (units > INT32_MAX / 8) return hipErrorInvalidValue;
+  if (dx < 1 || dw < 1 || units > INT32_MAX / 16) return 0;
   a.dx_first = a.dx.split_each >= a.dw.split_each;
-  const uint64_t first = a.dx_first ? dx_units : dw_units;
-  const uint64_t part = first > units / 2 ? first : units / 2;
+  const uint64_t first = a.dx_first ? dx_units : dw_units, part = first > units / 2 ? first : units / 2;
   a.first_units = (uint32_t)first;
   a.ratio = ((first << 32) + part - 1) / part;
   a.sums_blocks = a.sums.part ? a.sums.blocks() : 0;
   a.sums_units = (a.sums_blocks + 7) / 8;
-  const dim3 grid((unsigned)((units + a.sums_units) * 8));
+  return (int64_t)(units + a.sums_units) * 8;
+}
+
+template <bool kFp16, int kHalves>
+hipError_t launch_pair_tile(int tile, PairArgs& a, hipStream_t stream) {
+  const int64_t blocks = spread_pair(a, kTileM[tile], kTileN[tile], kBK);
+  constexpr int kType = kFp16 ? POINTID_FP16 : POINTID_BF16;
+  if (blocks < 1 || a.dx.end.dtype != kType || a.dw.end.dtype != kType) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
   switch (tile) {
     case 1: return launch_kernel(pair_kernel<kFp16, kHalves, 128, 128, 4, 2, 3>, grid, dim3(512), 0, stream, a);
     case 2: return launch_kernel(pair_kernel<kFp16, kHalves, 128, 128, 4, 2, 2>, grid, dim3(512), 0, stream, a);

@@ -74,19 +74,20 @@ ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64
 
 // Together, the blocks of one product fill the CUs that the other leaves, and no second
 // launch waits for the first's last blocks (bf16, dx and dW of 1693 x 1024 x 2048: 23 us
-// against 42 by two launches; of 4096 x 1024 x 4096: 72 against 84), and what one writes goes
-// along with what the other reads (1693 x 92928 x 128: 198 against 220).  256 x 256 tiles are
-// better alone (16384 x 1024 x 1024: 86 against 90; 4096^3: 214 against 270 in smaller ones).
+// against 42 by two launches; of 4096 x 1024 x 4096: 72 against 84; fp32 2048^3: 170 against
+// 201), and what one writes goes along with what the other reads (1693 x 92928 x 128: 198
+// against 220).  16-bit tiles of 256 x 256
+// are better alone (16384 x 1024 x 1024: 86 against 90; 4096^3: 214 against 270 in smaller ones).
 // A CU's time is that of its share of the stages, or of the longest block's: as many stages as
 // the other's blocks have beside them, the rest alone.  Two launches cost 6 us more than their
-// blocks, a second join 3.4 (fitted to 20 shapes; within 5 % of the fastest).
-PairPlan plan_pair(int64_t m, int64_t k, int64_t n, int halves, int parts, int cus) {
+// blocks, a second join 3.4 (fitted to 35 shapes; within 5 % of the fastest).
+PairPlan plan_pair(bool f32, int64_t m, int64_t k, int64_t n, int halves, int parts, int cus) {
   PairPlan best = {-1, 1, 1};
-  double least = least_cost(false, m, k, 1, n, halves * parts, cus).us +
-                 least_cost(false, k, n, halves, m, parts, cus).us + 6.0;
-  for (int t = 1; t < kTiles; ++t) {
-    const TileCost& c = kCost[t];
-    const Sizes dx = sizes_of(false, t, m, k, 1, n, halves * parts), dw = sizes_of(false, t, k, n, halves, m, parts);
+  double least = least_cost(f32, m, k, 1, n, halves * parts, cus).us +
+                 least_cost(f32, k, n, halves, m, parts, cus).us + 6.0;
+  for (int t = f32 ? 0 : 1; t < (f32 ? kTiles32 : kTiles); ++t) {
+    const TileCost& c = f32 ? kCost32[t] : kCost[t];
+    const Sizes dx = sizes_of(f32, t, m, k, 1, n, halves * parts), dw = sizes_of(f32, t, k, n, halves, m, parts);
     for (int s : kSplits) {
       if (!may_split(dx, s, cus)) break;
       for (int r : kSplits) {
@@ -96,8 +97,8 @@ PairPlan plan_pair(int64_t m, int64_t k, int64_t n, int halves, int parts, int c
         const double work = (dx.tiles * s * x + dw.tiles * r * w) / count * blocks * c.stage;
         const double longest = blocks > 1 ? std::min(x, w) * std::max(beside * c.stage, c.alone) + std::abs(x - w) * c.alone
                                           : std::max(x, w) * c.alone;
-        const double us = std::max(work, longest) + std::ceil(blocks / c.resident) * c.ends + join_cost(false, dx, s) +
-                          join_cost(false, dw, r) + 2.0 * (s > 1) + 2.0 * (r > 1);
+        const double us = std::max(work, longest) + std::ceil(blocks / c.resident) * c.ends + join_cost(f32, dx, s) +
+                          join_cost(f32, dw, r) + 2.0 * (s > 1) + 2.0 * (r > 1);
         if (us < least) least = us, best = {t, s, r};
       }
     }

@@ -96,8 +96,16 @@ struct Tile32 {
   }
 };
 
+// Shared memory of a block: two stages of three planes; the end fits where they were.
+template <int kBM, int kBN, int kWM, int kWN>
+constexpr int shared_bytes32() {
+  constexpr int kStages = 2 * 3 * (kBM + kBN) * kBK32 * 2;
+  static_assert(kWM * kWN * kEndWave <= kStages, "the end's part");
+  return kStages;
+}
+
 template <int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>
-__global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs a) {
+__device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t block, char* smem) {
   constexpr int kThreads = 64 * kWM * kWN;
   constexpr bool kLeftInner = kForm != kDw, kRightInner = kForm == kDx;
   static_assert(!kRightInner || kHalves == 1, "dx has one half");
@@ -109,13 +117,11 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
   // a stage: the left operand's planes, then each half's
   constexpr int kLeftBytes = 3 * Left::kPlane, kRightBytes = 3 * Right::kPlane;
   constexpr int kStage = kLeftBytes + 2 * kRightBytes;
-  static_assert(kWM * kWN * kEndWave <= 2 * kStage, "the end fits where the stages were");
-  __shared__ __align__(1024) char smem[2 * kStage];
 
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = wave / kWN, wn = wave % kWN;
-  const Place at = block_place(a, blockIdx.x);
+  const Place at = block_place(a, block);
   const int64_t row0 = at.tm * kBM;
   const int64_t col0 = at.tn * (kHalves == 2 ? kHN : kBN), col1 = kHalves == 2 ? col0 : col0 + kHN;
   Left left;
@@ -229,6 +235,19 @@ __global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs
                                                     col0 + wn * (kHalves == 2 ? 32 : 64));
 }
 
+template <int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>
+__global__ void __launch_bounds__(64 * kWM * kWN) product_f32_kernel(ProductArgs a) {
+  __shared__ __align__(1024) char smem[shared_bytes32<kBM, kBN, kWM, kWN>()];
+  product_f32_block<kForm, kHalves, kBM, kBN, kWM, kWN>(a, blockIdx.x, smem);
+}
+template <int kHalves, int kBM, int kBN, int kWM, int kWN>
+__global__ void __launch_bounds__(64 * kWM * kWN) pair_f32_kernel(PairArgs a) {
+  __shared__ __align__(1024) char smem[shared_bytes32<kBM, kBN, kWM, kWN>()];
+  pair_block<64 * kWM * kWN>(
+      a, smem, [&](const ProductArgs& p, uint32_t block) { product_f32_block<kDx, 1, kBM, kBN, kWM, kWN>(p, block, smem); },
+      [&](const ProductArgs& p, uint32_t block) { product_f32_block<kDw, kHalves, kBM, kBN, kWM, kWN>(p, block, smem); });
+}
+
 template <int kForm, int kHalves>
 hipError_t launch_tile32(int tile, ProductArgs& a, hipStream_t stream) {
   const int bm = kTileM32[tile], bn = kTileN32[tile] / (kHalves == 2 ? 2 : 1);
@@ -239,6 +258,19 @@ hipError_t launch_tile32(int tile, ProductArgs& a, hipStream_t stream) {
     case 0: return launch_kernel(product_f32_kernel<kForm, kHalves, 256, 128, 4, 2>, grid, dim3(512), 0, stream, a);
     case 1: return launch_kernel(product_f32_kernel<kForm, kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
     case 2: return launch_kernel(product_f32_kernel<kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <int kHalves>
+hipError_t launch_pair_tile32(int tile, PairArgs& a, hipStream_t stream) {
+  const int64_t blocks = spread_pair(a, kTileM32[tile], kTileN32[tile], kBK32);
+  if (blocks < 1 || a.dx.end.dtype != POINTID_FP32 || a.dw.end.dtype != POINTID_FP32) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
+  switch (tile) {
+    case 0: return launch_kernel(pair_f32_kernel<kHalves, 256, 128, 4, 2>, grid, dim3(512), 0, stream, a);
+    case 1: return launch_kernel(pair_f32_kernel<kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
+    case 2: return launch_kernel(pair_f32_kernel<kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
   }
   return hipErrorInvalidValue;
 }
@@ -256,6 +288,12 @@ hipError_t launch_product_f32(Form form, const ProductPlan& plan, ProductArgs a,
     case kDw: return two ? mm::launch_tile32<kDw, 2>(plan.tile, a, stream) : mm::launch_tile32<kDw, 1>(plan.tile, a, stream);
   }
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_pair_f32(int tile, const ProductArgs& dx, const ProductArgs& dw, const SumsJobs& sums, hipStream_t stream) {
+  mm::PairArgs a;
+  a.dx = dx, a.dw = dw, a.sums = sums;
+  return dw.end.halves == 2 ? mm::launch_pair_tile32<2>(tile, a, stream) : mm::launch_pair_tile32<1>(tile, a, stream);
 }
 
 }  // namespace pointid
