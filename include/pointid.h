@@ -435,7 +435,7 @@ int pointid_client_close(pointid_client c);
  * [k][n], biases and their gradients fp32 [n] whatever the type.  0 <= m <= 2^28,
  * 1 <= k, n <= 2^20.  Products are summed in fp32 and rounded to `dtype` once.
  * POINTID_FP32 products are those of operands cut exactly into three bf16 parts
- * each, without the terms below 2^-26 of a product (up to 8 rows: plain fp32).
+ * each, without terms of up to 2^-24 of a product (up to 8 rows: plain fp32).
  * Infinities and NaNs go through as in fp32 arithmetic, but a sum of
  * POINTID_FP32 values that itself passes the type's range may be a NaN instead of
  * an infinity.  Outputs must not overlap inputs, but `y` may be `residual` itself.  16-bit operands whose base

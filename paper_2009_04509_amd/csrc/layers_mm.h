@@ -1,15 +1,21 @@
 // Products on the matrix cores (16-bit operands, fp32 sums), one template for the three
-// forms of layers.h.
+// forms of layers.h: x w, dz w^T and x^T dz, the sums over k, n and m.
 //
 // A block computes kBM x kBN results with 16x16x32 MFMAs (a loop of these alone runs at
 // 2.0 PFLOP/s on random bf16 values, one of 32x32x16 at 1.8: the card is at its power limit,
 // and they pass half as many sums per multiplication through the registers).  Both
 // operands go through shared memory, 64 inner indices at a time, two stages (three for a
 // tile that a CU holds once and whose multiplications are shorter than the loads' latency),
-// written by loads that go there directly (16 bytes a lane).  An operand whose rows run along the inner
-// index (x and dz of dx and forward's x) is read as fragments with 16-byte reads; one whose
-// rows are indexed by the inner index (W of the forward form, both of dW) with the
-// transposing read, 4 x 16 values at a time, so no form needs a transposed copy of anything.
+// written by loads that go there directly (16 bytes a lane).  An operand whose rows run
+// along the inner index (x and dz of dx and forward's x) is read as fragments with 16-byte
+// reads; one whose rows are indexed by the inner index (W of the forward form, both of dW)
+// with the transposing read, 4 x 16 values at a time, so no form needs a transposed copy.
+//
+// Bound by power where there is work for all CUs: 16384 x 4096 x 4096 in bf16 412 us, 1.33
+// PFLOP/s (with GELU and a residual 455-470), MFMA 56-66 % busy at 1.9 GHz; 8192 x 16384 x
+// 4096 831 us, its dx 821, its dW 884; a gated 8192 x 4096 x 8192 824, 884 with g and u kept
+// in 8 bits.  Few rows are bound by the bytes of the weights: 4 rows of a gated 4096 x 12288
+// 51 us with the join, 4.0 TB/s.
 //
 // The results come out with the right operand as the MFMA's first, so a lane holds 4
 // consecutive columns of one row at a time; the end passes them through shared memory to
@@ -39,7 +45,7 @@ constexpr uint32_t kNowhere = 0x80000000u;  // an offset past the resource's ran
 // The piece's place in a row of kPieces pieces of 16 bytes; kInner: rows along the inner index.
 template <bool kInner, int kPieces>
 __device__ __forceinline__ int place(int row, int piece) {
-  if constexpr (kInner) return kPieces == 8 ? piece ^ ((row >> 1) & 7) : piece ^ ((row >> 2) & 3);
+  if constexpr (kInner) return kPieces == 8 ? piece ^ ((row >> 1) & 7) : piece ^ (-(row >> 2) & 3);
   if constexpr (kPieces >= 16) return piece ^ (((row & 3) | (row >> 1 & 4)) << 1);
   return piece ^ (((row >> 1 & 1) | (row >> 2 & 2)) << 1);
 }
@@ -170,7 +176,9 @@ __device__ __forceinline__ Place block_place(const ProductArgs& a, uint32_t bloc
   return {split, group * kGroup + (in - tn * rows_here), tn};
 }
 
-// The end of a wave's results: rows from `row0` of kFragsM groups of 16, columns from `col0`
+// The end of a wave's results (bias, activation, product of the halves, residual and kept
+// activations are done here, on the sums in registers: as a pass of its own the GELU and
+// residual of 16384 x 4096 would move 400 MB more, 85 us).  Rows from `row0` of kFragsM groups of 16, columns from `col0`
 // (of each half).  One copy of the end's code: 32 rows x 64 columns a turn (two halves: 32
 // columns of each) through the wave's kEndWave bytes of shared memory, from a lane's 4
 // columns of one row to 16 bytes and more a lane along the rows.  The residual of a turn is

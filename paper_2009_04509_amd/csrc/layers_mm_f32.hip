@@ -1,12 +1,19 @@
 // The matrix-core products of fp32 operands: every value is the sum of three bf16 values
 // (its rounding, the remainder's rounding, and the rest: 8 + 8 + 8 bits), and a product is
 // the 6 products of parts whose orders add up to less than 3, the smallest first; what is
-// left out is below 2^-26 of a product.
+// left out is at most 2^-24 of a product, its root mean square 2^-27.
 //
 // Values are read as fp32, 32 inner indices at a time, while the stage before multiplies,
 // cut in registers and written to shared memory as three planes laid out as in the 16-bit
 // kernels (layers_mm.h); two stages.  A stage's 6 products share its fragments, so they
 // read half of what 6 passes over 16-bit planes would, and no pass lays planes out first.
+//
+// Bound by power where there is work for all CUs (4096^3: 640 us, 215 TFLOP/s, which is
+// 1.29 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
+// multiplying, about 2 us, with one 128 x 128 or 256 x 128 tile a CU (235 x 2304 x (2 x 1021):
+// 28 us and 6 of the join; 44 % MFMA busy in a gradient's pair of products of 1693 x 1024 x
+// (2 x 2048)).  Reading a stage's first fragments during the last products of the one before
+// (as the 16-bit kernels do), and loads two stages ahead, gained nothing.
 #include "layers_mm.h"
 
 namespace pointid {

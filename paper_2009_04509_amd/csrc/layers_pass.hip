@@ -17,6 +17,7 @@ __device__ __forceinline__ void each_piece(int64_t rows, int64_t pieces, int64_t
   }
 }
 
+// code 2^(e - 127), 8 columns a lane.  16384 x 8192 to bf16: 70 us, 5.8 TB/s read and written.
 __global__ void __launch_bounds__(256) checkpoint_load_kernel(Packed8 src, int64_t rows, int64_t cols, int dtype,
                                                               void* out, int64_t ld) {
   each_piece(rows, (cols + 7) / 8, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256,
@@ -51,31 +52,51 @@ __global__ void __launch_bounds__(256) sums_kernel(SumsJobs a) {
   sum_columns<256>(a, blockIdx.x, sums);
 }
 
-// A block of 32 values by 4 neighbouring lanes.
-__global__ void __launch_bounds__(256) checkpoint_save_kernel(const void* src, int64_t ld, int dtype, int64_t rows,
-                                                              int64_t cols, Packed8 out) {
+// A block of 32 values by 4 neighbouring lanes, which exchange its maximum (see save_codes); a
+// lane has two such pieces in flight (one: 82 us for 77).  Bound by the bytes: bf16 16384 x
+// 8192 77 us, 5.3 TB/s read and written (3.8 under a profiler, 106 us).
+template <int kType>
+__global__ void __launch_bounds__(256) checkpoint_save_kernel(const char* src, int64_t ld, int64_t rows, int64_t cols,
+                                                              Packed8 out) {
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
   const int64_t lanes = (cols + kBlock8 - 1) / kBlock8 * 4, total = rows * lanes;
-  const int64_t step = (int64_t)gridDim.x * blockDim.x;
+  const int64_t step = (int64_t)gridDim.x * 256;
   // every lane of a wave takes the same number of turns, as the exchange needs all 4 of a block
   const int64_t last = (total + 63) / 64 * 64;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < last; i += step) {
-    const bool here = i < total;
-    const int64_t row = !here ? 0 : total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)lanes) : i / lanes;
-    const int64_t col = here ? (i - row * lanes) * 8 : 0;
-    float v[8];
-    load_cols<8>(src, row * ld + col, dtype, here ? cols - col : 0, v);
-    save_codes(out.codes + row * cols + col, out.exponents + row * (lanes / 4) + col / kBlock8, here && col < cols,
-               col % kBlock8 == 0, here ? piece_cols(cols, col) : 0, v);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < last; i += 2 * step) {
+    int64_t row[2], col[2];
+    int n[2];
+    Raw8<kType> raw[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t at = i + u * step;
+      const bool here = at < total;
+      row[u] = !here ? 0 : total <= UINT32_MAX ? (int64_t)((uint32_t)at / (uint32_t)lanes) : at / lanes;
+      col[u] = here ? (at - row[u] * lanes) * 8 : 0;
+      n[u] = here ? piece_cols(cols, col[u]) : 0;
+      raw[u].load(src + (row[u] * ld + col[u]) * kSize, n[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float v[8];
+      raw[u].values(v);
+      save_codes(out.codes + row[u] * cols + col[u], out.exponents + row[u] * (lanes / 4) + col[u] / kBlock8, n[u] > 0,
+                 col[u] % kBlock8 == 0, n[u], v);
+    }
   }
 }
 
 // How the activations of a gradient are kept.
 enum { kKeptNot = 0, kKeptWhole = 1, kKeptPacked = 2 };
 
+// dz = dy act'(z), or of a gated layer dg = dh u act'(g) and du = dh act(g), in fp32 and
+// rounded once to the type that the products read; the column sums before the rounding.
 // Each block: 8 kTurns rows x 256 columns (the blocks past those take the fill's jobs, which
-// need nothing of the gradient); 8 rows by 32 pieces of 8 columns at a time, two
-// such turns' reads in flight before any is used (a read used at once: 163 us for a gated
-// 8192 x 8192 in bf16).
+// need nothing of the gradient); 8 rows by 32 pieces of 8 columns at a time, two such turns'
+// reads in flight before any is used (a read used at once: 163 us for a gated 8192 x 8192 in
+// bf16).  Bound by the bytes: that one from 8 bits 120 us, 4.5 TB/s read and written; with x's
+// 8192 x 4096 from 8 bits beside it 153, 4.3 TB/s.  A block's sums are added by the sums' pass
+// in order, not by atomics, so that the bits do not depend on which block is first.
 template <int kType, int kHalves, int kKept, int kTurns>
 __global__ void __launch_bounds__(256) grad_kernel(GradArgs a, FillJobs fill) {
   __shared__ float sums[8][256 + 8];
@@ -199,6 +220,8 @@ hipError_t launch_grad(const GradArgs& a, const FillJobs& fill, dim3 grid, hipSt
   return a.z[0].packed.codes ? go(grad_kernel<kType, 1, kKeptPacked, kTurns>) : go(grad_kernel<kType, 1, kKeptNot, kTurns>);
 }
 
+// The sums of a split product: part 0, 1, ... in order, and then the end that a product
+// without splits has in its own kernel.  A launch's latency, 4 to 8 us, more than its bytes.
 // Units of 8 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
 // order.  kSub == 8, for many parts: 8 lanes of a unit take every eighth part each, and
 // their sums are added in order.
@@ -294,8 +317,15 @@ hipError_t launch_checkpoint_load(const Packed8& src, int64_t rows, int64_t cols
 
 hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_t rows, int64_t cols,
                                   const Packed8& out, hipStream_t stream) {
-  return launch_kernel(checkpoint_save_kernel, dim3(pass_blocks(rows * ((cols + 31) / 32) * 4)), dim3(256), 0, stream,
-                       src, ld, dtype, rows, cols, out);
+  const dim3 grid(pass_blocks((rows * ((cols + 31) / 32) * 4 + 1) / 2));
+  auto go = [&](auto kernel) {
+    return launch_kernel(kernel, grid, dim3(256), 0, stream, static_cast<const char*>(src), ld, rows, cols, out);
+  };
+  switch (dtype) {
+    case POINTID_FP32: return go(checkpoint_save_kernel<POINTID_FP32>);
+    case POINTID_BF16: return go(checkpoint_save_kernel<POINTID_BF16>);
+  }
+  return go(checkpoint_save_kernel<POINTID_FP16>);
 }
 
 int grad_rows(int64_t rows, int64_t cols, int cus) {

@@ -1,5 +1,8 @@
-// Forward products of a few rows (serving): the weights are read once, every value
-// multiplied in fp32 with that of each row.  Bound by the bytes of the weights.
+// Forward products of a few rows (serving): y = x w with the weights read once, every value
+// multiplied in fp32 with that of each row.  Bound by the bytes of the weights: fp32 8192 x
+// 8192, 1 row 53 us (5.0 TB/s), 4 rows 58, 8 rows 63; bf16 gated 4096 x 12288, 1 row 46 (4.4).
+// The inner index is split over blocks until there are about 3 a CU, as one block's reads in
+// flight do not fill the memory; the join adds their sums in order.
 #include "internal.h"
 #include "layers_end.h"
 
@@ -19,8 +22,8 @@ struct RowsArgs {
 
 // A wave reads 256 columns of kRowsPer rows of the weights at a time, 16 bytes a lane (long
 // stretches of a row: 64 columns took a third more time at 4 rows), the next reads under way
-// while it multiplies; the block's 4 waves take turns along the inner index.  The lanes of a column are added in a
-// fixed order at the end: lanes, then waves, then (elsewhere) splits.
+// while it multiplies; the block's 4 waves take turns along the inner index.  The lanes of a
+// column are added in a fixed order at the end: lanes, then waves, then (elsewhere) splits.
 template <int kM, int kType, int kHalves>
 __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
   constexpr int kCols = kType == POINTID_FP32 ? 4 : 8;                  // of a lane
