@@ -8,8 +8,8 @@
 // kernels (layers_mm.h); two stages.  A stage's 6 products share its fragments, so they
 // read half of what 6 passes over 16-bit planes would, and no pass lays planes out first.
 //
-// Bound by power where there is work for all CUs (4096^3: 640 us, 215 TFLOP/s, which is
-// 1.29 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
+// Bound by power where there is work for all CUs (4096^3: 628 us, 219 TFLOP/s, which is
+// 1.31 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
 // multiplying, about 2 us, with one 128 x 128 or 256 x 128 tile a CU (235 x 2304 x (2 x 1021):
 // 28 us and 6 of the join; 44 % MFMA busy in a gradient's pair of products of 1693 x 1024 x
 // (2 x 2048)).  Reading a stage's first fragments during the last products of the one before
@@ -187,6 +187,10 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
 #pragma unroll
         for (int j = 0; j < kFragsN; ++j) acc[i][j] = mfma<false>(r[order - p][j], l[i % 2][p], acc[i][j]);
   };
+  // Of the two waves that share a SIMD one cuts and stores the next stage before it multiplies,
+  // the other halfway, so that one cuts while the other multiplies (both halfway: 2048 x 4096 x
+  // 2048 176 us for 173, its dx 172 for 164; the second at the end: 177).
+  const bool early = kWM * kWN == 8 && wave < 4;
   auto sum = [&](auto care) {
     auto store = [&](int stage) {
       char* tile = smem + stage * kStage;
@@ -214,14 +218,17 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
 #pragma unroll
         for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * Right::kPlane, j, 0);
       read_left(tile, 0);
+      auto next = [&] {
+        if (it + 1 == stages) return;
+        store(stage ^ 1);
+        if (to_load > 0) load();
+      };
+      if (early) next();
 #pragma unroll
       for (int i = 0; i < kFragsM; ++i) {
         if (i + 1 < kFragsM) read_left(tile, i + 1);
         multiply(i);
-        if (i == kFragsM / 2 - 1 && it + 1 < stages) {
-          store(stage ^ 1);
-          if (to_load > 0) load();
-        }
+        if (i == kFragsM / 2 - 1 && !early) next();
       }
       __syncthreads();
     }
