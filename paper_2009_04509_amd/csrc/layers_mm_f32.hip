@@ -8,8 +8,8 @@
 // kernels (layers_mm.h); two stages.  A stage's 6 products share its fragments, so they
 // read half of what 6 passes over 16-bit planes would, and no pass lays planes out first.
 //
-// Bound by power where there is work for all CUs (4096^3: 628 us, 219 TFLOP/s, which is
-// 1.31 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
+// Bound by power where there is work for all CUs (4096^3: 593-628 us by box, 219-232 TFLOP/s,
+// which is 1.31-1.39 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
 // multiplying, about 2 us, with one 128 x 128 or 256 x 128 tile a CU (235 x 2304 x (2 x 1021):
 // 28 us and 6 of the join; 44 % MFMA busy in a gradient's pair of products of 1693 x 1024 x
 // (2 x 2048)).  Reading a stage's first fragments during the last products of the one before
@@ -72,21 +72,27 @@ struct Tile32 {
       v[i] = make_float4(f[0], f[1], f[2], f[3]);
     }
   }
-  // The three parts of two values.  The largest values' first part is cut to the largest
-  // bf16.  kCare: an infinity or NaN stands in the last part (which multiplies the first part
-  // of the other operand alone) behind a 1 of its sign and a 0, and so goes through as in fp32.
+  // The three parts of two values.  kCare: an infinity or NaN stands in the last part (which
+  // multiplies the first part of the other operand alone) behind a 1 of its sign and a 0, and
+  // so goes through as in fp32, and the first part of the largest values, which would round to
+  // an infinity, is the largest bf16.
   template <bool kCare>
   static __device__ __forceinline__ void cut(float a, float b, uint32_t (&part)[3]) {
-    constexpr float kMost = 3.38953139e38f;
-    const bool fa = !kCare || __builtin_isfinite(a), fb = !kCare || __builtin_isfinite(b);
-    const float most_a = fa ? kMost : 1.f, most_b = fb ? kMost : 1.f;
     auto rest = [&](uint32_t h) {
       a -= __uint_as_float(h << 16);
       b -= __uint_as_float(h & 0xFFFF0000u);
       return h;
     };
-    part[0] = rest(Op16<false>::pack(__builtin_amdgcn_fmed3f(a, -most_a, most_a), __builtin_amdgcn_fmed3f(b, -most_b, most_b)));
-    part[1] = rest(Op16<false>::pack(fa ? a : 0.f, fb ? b : 0.f));
+    if constexpr (kCare) {
+      constexpr float kMost = 3.38953139e38f;
+      const bool fa = __builtin_isfinite(a), fb = __builtin_isfinite(b);
+      const float most_a = fa ? kMost : 1.f, most_b = fb ? kMost : 1.f;
+      part[0] = rest(Op16<false>::pack(__builtin_amdgcn_fmed3f(a, -most_a, most_a), __builtin_amdgcn_fmed3f(b, -most_b, most_b)));
+      part[1] = rest(Op16<false>::pack(fa ? a : 0.f, fb ? b : 0.f));
+    } else {
+      part[0] = rest(Op16<false>::pack(a, b));
+      part[1] = rest(Op16<false>::pack(a, b));
+    }
     part[2] = Op16<false>::pack(a, b);
   }
   // The parts of the values to the three planes at `tile`.
@@ -234,8 +240,9 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
     }
   };
   sum(std::false_type{});
-  // A value that is not finite makes all sums of its row or column so: these are made again
-  // with care (whole blocks, so that the loop does not pay for it).
+  // A value whose first part is not finite makes all sums of its row or column so: these are
+  // made again with care (whole blocks, so that the loop does not pay for it: with the clamp
+  // in it 4096^3 took 607 us for 593).
   float all = 0.f;
 #pragma unroll
   for (int i = 0; i < kFragsM; ++i)

@@ -51,6 +51,31 @@ def test_fp32_infinities_times_large_values(pid, layers, m, form):
     same_kind(y.double().cpu(), z)
 
 
+@pytest.mark.parametrize("form", ["forward", "dx", "dw"])
+def test_fp32_values_above_the_largest_bf16(pid, layers, form):
+    """Finite values that round to an infinity in 16 bits, beside an infinity or not."""
+    g = torch.Generator().manual_seed(24)
+    m, k, n = 40, 36, 68
+    left, right = torch.randn((m, k), generator=g), torch.randn((k, n), generator=g) * 2.0 ** -10
+    left[3, 5], left[4, 6], left[5, 7] = 3.4028e38, -3.4e38, 3.39e38
+    left[6, 1] = float("inf")
+    z = left.double() @ right.double()
+    a, b = left.to(DEV), right.to(DEV)
+    if form == "forward":
+        y = pid.pointid_dense(layers, a, b)
+    elif form == "dx":
+        y = pid.pointid_dense_backward(layers, a, None, b.t().contiguous(), need_dw=False, need_db=False)[0]
+    else:
+        y = pid.pointid_dense_backward(layers, b, a.t().contiguous(), torch.empty((m, n), device=DEV),
+                                       need_dx=False, need_db=False)[1]
+    y = y.double().cpu()
+    same_kind(y, z)
+    here = z.isfinite()
+    # 6 k products of parts, each sum rounded to 2^-23 of the magnitudes at most
+    bound = (left.double().abs() @ right.double().abs()) * (6 * k * 2.0 ** -23)
+    assert ((y - z).abs() <= bound)[here].all()
+
+
 @pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("k", [1, 63, 513, 700])
 def test_an_infinity_at_the_end_of_few_rows(pid, layers, dtype, k):
