@@ -707,6 +707,14 @@ def _matrix(t, name, dtype, shape, device):
     return _Matrix(t.data_ptr(), pitch if rows > 1 else cols)
 
 
+def _output(t, like, name, dtype, shape, device):
+    """An output that is given, or made like a tensor of the call, and its descriptor."""
+    if t is not None:
+        return t, _matrix(t, name, dtype, shape, device)
+    t = like.new_empty(shape, dtype=dtype)
+    return t, _Matrix(t.data_ptr(), shape[1])
+
+
 def _kept(t, name, dtype, shape, device):
     if t is None:
         return None
@@ -761,12 +769,11 @@ def pointid_dense(layers: Layers, x: torch.Tensor, w: torch.Tensor, bias: torch.
     dt, dev = _layer_type(x, "x"), layers.device
     m, k, n = _shapes(x, w, "w")
     code = _activation(act)
-    if y is None:
-        y = torch.empty((m, n), dtype=dt, device=x.device)
+    y, out = _output(y, x, "y", dt, (m, n), dev)
     _check(lib.pointid_dense(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
         _ref(_matrix(w, "w", dt, (k, n), dev)), _bias(bias, "bias", n, dev),
-        _ref(_matrix(residual, "residual", dt, (m, n), dev)), _ref(_matrix(y, "y", dt, (m, n), dev)),
+        _ref(_matrix(residual, "residual", dt, (m, n), dev)), ctypes.byref(out),
         _ref(_kept(save, "save", dt, (m, n), dev)), _layer_stream(stream, dev)))
     return y
 
@@ -781,14 +788,14 @@ def pointid_dense_backward(layers: Layers, dy: torch.Tensor, x, w: torch.Tensor,
     m, n = dy.shape
     k = w.shape[0]
     code = _activation(act)
-    dx = torch.empty((m, k), dtype=dt, device=dy.device) if need_dx else None
-    dw = torch.empty((k, n), dtype=dt, device=dy.device) if need_dw else None
-    db = torch.empty((n,), dtype=torch.float32, device=dy.device) if need_db else None
+    dx, to_dx = _output(None, dy, "dx", dt, (m, k), dev) if need_dx else (None, None)
+    dw, to_dw = _output(None, dy, "dw", dt, (k, n), dev) if need_dw else (None, None)
+    db = dy.new_empty((n,), dtype=torch.float32) if need_db else None
     _check(lib.pointid_dense_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dy, "dy", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(w, "w", dt, (k, n), dev)),
-        _ref(_kept(z, "z", dt, (m, n), dev)), _ref(_matrix(dx, "dx", dt, (m, k), dev)),
-        _ref(_matrix(dw, "dw", dt, (k, n), dev)), _ptr(db), _layer_stream(stream, dev)))
+        _ref(_kept(z, "z", dt, (m, n), dev)), _ref(to_dx), _ref(to_dw), _ptr(db),
+        _layer_stream(stream, dev)))
     return dx, dw, db
 
 
@@ -802,13 +809,12 @@ def pointid_gated(layers: Layers, x: torch.Tensor, wg: torch.Tensor, wu: torch.T
     dt, dev = _layer_type(x, "x"), layers.device
     m, k, n = _shapes(x, wg, "wg")
     code = _activation(act)
-    if h is None:
-        h = torch.empty((m, n), dtype=dt, device=x.device)
+    h, out = _output(h, x, "h", dt, (m, n), dev)
     _check(lib.pointid_gated(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
         _ref(_matrix(wg, "wg", dt, (k, n), dev)), _ref(_matrix(wu, "wu", dt, (k, n), dev)),
         _bias(bias_g, "bias_g", n, dev), _bias(bias_u, "bias_u", n, dev),
-        _ref(_matrix(h, "h", dt, (m, n), dev)), _ref(_kept(save_g, "save_g", dt, (m, n), dev)),
+        ctypes.byref(out), _ref(_kept(save_g, "save_g", dt, (m, n), dev)),
         _ref(_kept(save_u, "save_u", dt, (m, n), dev)), _layer_stream(stream, dev)))
     return h
 
@@ -823,16 +829,15 @@ def pointid_gated_backward(layers: Layers, dh: torch.Tensor, x, wg: torch.Tensor
     m, n = dh.shape
     k = wg.shape[0]
     code = _activation(act)
-    dx = torch.empty((m, k), dtype=dt, device=dh.device) if need_dx else None
-    dwg, dwu = (torch.empty((k, n), dtype=dt, device=dh.device) if need_dw else None for _ in range(2))
-    dbg, dbu = (torch.empty((n,), dtype=torch.float32, device=dh.device) if need_db else None for _ in range(2))
+    dx, to_dx = _output(None, dh, "dx", dt, (m, k), dev) if need_dx else (None, None)
+    (dwg, to_dwg), (dwu, to_dwu) = (_output(None, dh, name, dt, (k, n), dev) if need_dw else (None, None)
+                                    for name in ("dwg", "dwu"))
+    dbg, dbu = (dh.new_empty((n,), dtype=torch.float32) if need_db else None for _ in range(2))
     _check(lib.pointid_gated_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dh, "dh", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(wg, "wg", dt, (k, n), dev)),
         _ref(_matrix(wu, "wu", dt, (k, n), dev)), _ref(_kept(g, "g", dt, (m, n), dev)),
-        _ref(_kept(u, "u", dt, (m, n), dev)), _ref(_matrix(dx, "dx", dt, (m, k), dev)),
-        _ref(_matrix(dwg, "dwg", dt, (k, n), dev)), _ref(_matrix(dwu, "dwu", dt, (k, n), dev)),
-        _ptr(dbg), _ptr(dbu), _layer_stream(stream, dev)))
+        _ref(_kept(u, "u", dt, (m, n), dev)), _ref(to_dx), _ref(to_dwg), _ref(to_dwu), _ptr(dbg), _ptr(dbu), _layer_stream(stream, dev)))
     return dx, dwg, dwu, dbg, dbu
 
 
@@ -842,9 +847,13 @@ def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stre
     m, n = x.shape
     a = _matrix(x, "x", dt, (m, n), dev)
     if out is None:
-        out = Checkpoint.empty(m, n, x.device)
-    kept = _kept(out, "out", dt, (m, n), dev)
-    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(kept.packed),
+        out = Checkpoint.__new__(Checkpoint)
+        out.codes = x.new_empty((m, n), dtype=torch.uint8)
+        out.exponents = out.codes.new_empty((m, -(-n // 32)))
+        packed = _Packed(out.codes.data_ptr(), out.exponents.data_ptr())
+    else:
+        packed = _kept(out, "out", dt, (m, n), dev).packed
+    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(packed),
                                        _layer_stream(stream, dev)))
     return out
 
@@ -853,11 +862,11 @@ def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.T
                             stream=None) -> torch.Tensor:
     """The values a checkpoint stands for, as a matrix [m][n] of ``dtype``."""
     m, n = saved.shape
-    if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=saved.device)
-    dt, dev = _layer_type(out, "out"), saved.codes.get_device()
+    dt, dev = dtype if out is None else _layer_type(out, "out"), saved.codes.get_device()
+    if dt not in _LAYER_TYPES:
+        raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dt}")
     kept = _kept(saved, "saved", dt, (m, n), dev)
-    _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed),
-                                       ctypes.byref(_matrix(out, "out", dt, (m, n), dev)),
+    out, a = _output(out, saved.codes, "out", dt, (m, n), dev)
+    _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
                                        _layer_stream(stream, dev)))
     return out
