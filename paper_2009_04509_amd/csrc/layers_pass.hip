@@ -228,7 +228,7 @@ hipError_t launch_grad(const GradArgs& a, const FillJobs& fill, dim3 grid, hipSt
 template <int kType, int kHalves, int kSub>
 __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int64_t part_ld, int splits) {
   constexpr int kUnits = 256 / kSub;
-  __shared__ float sums[kSub > 1 ? kSub : 1][kHalves][kSub > 1 ? kUnits : 1][kSub > 1 ? 9 : 1];
+  __shared__ __align__(16) float sums[kSub > 1 ? kSub : 1][kHalves][kSub > 1 ? kUnits * 8 : 1];
   const int64_t units = part_ld / 8, total = e.rows * units;
   const int unit = threadIdx.x % kUnits, sub = threadIdx.x / kUnits;
   const int64_t i = (int64_t)blockIdx.x * kUnits + unit;
@@ -254,17 +254,21 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
       }
   }
   if constexpr (kSub > 1) {
+    static_assert(kUnits * 8 == 256, "a column of each half a lane");
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h)
+    for (int h = 0; h < kHalves; ++h) __builtin_memcpy(&sums[sub][h][unit * 8], v[h], 32);
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sums[sub][h][unit][j] = v[h][j];
+    for (int h = 0; h < kHalves; ++h) {
+      float t = sums[0][h][threadIdx.x];
+#pragma unroll
+      for (int s = 1; s < kSub; ++s) t += sums[s][h][threadIdx.x];
+      sums[0][h][threadIdx.x] = t;
+    }
     __syncthreads();
     if (sub != 0) return;
-    for (int s = 1; s < kSub; ++s)
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[h][j] += sums[s][h][unit][j];
+    for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], &sums[0][h][unit * 8], 32);
   }
   Targets<kType, kHalves> to;
   to.init(e, row, col);
