@@ -11,10 +11,10 @@
 // reads; one whose rows are indexed by the inner index (W of the forward form, both of dW)
 // with the transposing read, 4 x 16 values at a time, so no form needs a transposed copy.
 //
-// Bound by power where there is work for all CUs: 16384 x 4096 x 4096 in bf16 412 us, 1.33
-// PFLOP/s (with GELU and a residual 455-470), MFMA 56-66 % busy at 1.9 GHz; 8192 x 16384 x
-// 4096 831 us, its dx 821, its dW 884; a gated 8192 x 4096 x 8192 824, 884 with g and u kept
-// in 8 bits.  Few rows are bound by the bytes of the weights: 4 rows of a gated 4096 x 12288
+// Bound by power where there is work for all CUs: 16384 x 4096 x 4096 in bf16 407 us, 1.35
+// PFLOP/s (with GELU and a residual 458), MFMA 55-65 % busy at 1.9 GHz; 8192 x 16384 x 4096
+// 832 us, its dx 826, its dW 874; a gated 8192 x 4096 x 8192 824, 892 with g and u kept in 8
+// bits.  Few rows are bound by the bytes of the weights: 4 rows of a gated 4096 x 12288
 // 51 us with the join, 4.0 TB/s.
 //
 // The results come out with the right operand as the MFMA's first, so a lane holds 4
@@ -24,7 +24,8 @@
 // Pieces of 16 bytes stand in shared memory in a permuted order that the loads apply to
 // their global addresses.  Rows of 64 inner indices (128 bytes): piece p of row r at
 // p ^ (r / 2 % 8), so that 16 lanes reading one piece of 16 rows touch all banks (rows of
-// 32 inner indices, in the fp32 kernel: p ^ (r / 4 % 4)).  Rows of columns: the pair of
+// 32 inner indices, in the fp32 kernel: p ^ (-(r / 4) % 4); without the minus lanes 0-3 and
+// 12-15 met 20-27, which are served with them: 0.22 to 0.36 of the cycles).  Rows of columns: the pair of
 // pieces g of row r at g ^ (r % 4 + 4 (r / 8 % 2)) (rows of 128 bytes: g ^ (r / 2 % 2 +
 // 2 (r / 8 % 2))), so that the rows r .. r + 3 and r + 8 .. r + 11 of 16 columns that 32
 // lanes of a transposing read take do.

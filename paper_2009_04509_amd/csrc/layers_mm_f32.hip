@@ -8,10 +8,10 @@
 // kernels (layers_mm.h); two stages.  A stage's 6 products share its fragments, so they
 // read half of what 6 passes over 16-bit planes would, and no pass lays planes out first.
 //
-// Bound by power where there is work for all CUs (4096^3: 593-628 us by box, 219-232 TFLOP/s,
-// which is 1.31-1.39 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
-// multiplying, about 2 us, with one 128 x 128 or 256 x 128 tile a CU (235 x 2304 x (2 x 1021):
-// 28 us and 6 of the join; 44 % MFMA busy in a gradient's pair of products of 1693 x 1024 x
+// Bound by power where there is work for all CUs (4096^3: 593-597 us, 231 TFLOP/s, which is
+// 1.38 PFLOP/s of bf16 products); below that by a stage's chain of loading, cutting and
+// multiplying, 1 to 2 us, with one 128 x 128 or 256 x 128 tile a CU (235 x 2304 x (2 x 1021):
+// 25 us and 6 of the join; 50 % MFMA busy in a gradient's pair of products of 1693 x 1024 x
 // (2 x 2048)).  Reading a stage's first fragments during the last products of the one before
 // (as the 16-bit kernels do), and loads two stages ahead, gained nothing.
 #include "layers_mm.h"

@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(256) sums_kernel(SumsJobs a) {
 
 // A block of 32 values by 4 neighbouring lanes, which exchange its maximum (see save_codes); a
 // lane has two such pieces in flight (one: 82 us for 77).  Bound by the bytes: bf16 16384 x
-// 8192 77 us, 5.3 TB/s read and written (3.8 under a profiler, 106 us).
+// 8192 74-77 us, 5.3-5.5 TB/s read and written.
 template <int kType>
 __global__ void __launch_bounds__(256) checkpoint_save_kernel(const char* src, int64_t ld, int64_t rows, int64_t cols,
                                                               Packed8 out) {
@@ -221,7 +221,7 @@ hipError_t launch_grad(const GradArgs& a, const FillJobs& fill, dim3 grid, hipSt
 }
 
 // The sums of a split product: part 0, 1, ... in order, and then the end that a product
-// without splits has in its own kernel.  A launch's latency, 4 to 8 us, more than its bytes.
+// without splits has in its own kernel.  A launch's latency, 4 to 6 us, more than its bytes.
 // Units of 8 columns of a row of partials.  kSub == 1: a lane adds a unit's parts in
 // order.  kSub == 8, for many parts: 8 lanes of a unit take every eighth part each, and
 // their sums are added in order.
