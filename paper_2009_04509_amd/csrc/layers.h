@@ -99,9 +99,9 @@ struct ProductArgs {
   End end;
 };
 // The tile of a launch and its splits of the sum.
-constexpr int kTiles = 4, kTiles32 = 3;        // 16-bit: two of 128 x 128, of 3 and 2 stages
+constexpr int kTiles = 4, kTiles32 = 4;        // 16-bit: two of 128 x 128, of 3 and 2 stages
 constexpr int kTileM[kTiles] = {256, 128, 128, 64}, kTileN[kTiles] = {256, 128, 128, 128};
-constexpr int kTileM32[kTiles32] = {256, 128, 64}, kTileN32[kTiles32] = {128, 128, 128};
+constexpr int kTileM32[kTiles32] = {256, 128, 64, 64}, kTileN32[kTiles32] = {128, 128, 128, 64};
 struct ProductPlan {
   int tile;                    // index into kTileM, kTileN (fp32: kTileM32, kTileN32; columns of both halves)
   int splits;

@@ -27,7 +27,7 @@
 // 32 inner indices, in the fp32 kernel: p ^ (-(r / 4) % 4); without the minus lanes 0-3 and
 // 12-15 met 20-27, which are served with them: 0.22 to 0.36 of the cycles).  Rows of columns: the pair of
 // pieces g of row r at g ^ (r % 4 + 4 (r / 8 % 2)) (rows of 128 bytes: g ^ (r / 2 % 2 +
-// 2 (r / 8 % 2))), so that the rows r .. r + 3 and r + 8 .. r + 11 of 16 columns that 32
+// 2 (r / 8 % 2)), of 64: g ^ (r / 8 % 2)), so that the rows r .. r + 3 and r + 8 .. r + 11 of 16 columns that 32
 // lanes of a transposing read take do.
 #pragma once
 
@@ -48,6 +48,7 @@ template <bool kInner, int kPieces>
 __device__ __forceinline__ int place(int row, int piece) {
   if constexpr (kInner) return kPieces == 8 ? piece ^ ((row >> 1) & 7) : piece ^ (-(row >> 2) & 3);
   if constexpr (kPieces >= 16) return piece ^ (((row & 3) | (row >> 1 & 4)) << 1);
+  if constexpr (kPieces == 4) return piece ^ (row >> 3 & 1) << 1;
   return piece ^ (((row >> 1 & 1) | (row >> 2 & 2)) << 1);
 }
 
@@ -190,7 +191,7 @@ template <int kType, int kHalves, int kFragsM>
 __device__ __forceinline__ void end_tile(const End& e, const floatx4 (&acc)[kFragsM][4], float* es, int lane, int split,
                                          int64_t row0, int64_t col0) {
   constexpr int kLanes = kHalves == 2 ? 4 : 8;           // of a row
-  constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes;
+  constexpr int kSteps = kLanes / 2, kRows = 64 / kLanes, kTurns = (kFragsM + 1) / 2;
   const int64_t col = col0 + lane % kLanes * 8;
   const int n = piece_cols(e.cols, col);
   row0 += lane / kLanes;
@@ -209,15 +210,16 @@ __device__ __forceinline__ void end_tile(const End& e, const floatx4 (&acc)[kFra
     for (int h = 0; h < kHalves; ++h) __builtin_memcpy(v[h], from + s * kRows * kEndPitch + h * 32, 32);
   };
   auto sums = [&](int turn, floatx4(&c)[2][4]) {
-    static_for<kFragsM / 2>([&](auto t) {
+    static_for<kTurns>([&](auto t) {
       if (turn == t)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i / 4][i % 4] = acc[2 * t + i / 4][i % 4];
+        for (int i = 0; i < 8; ++i)
+          if (2 * t + i / 4 < kFragsM) c[i / 4][i % 4] = acc[2 * t + i / 4 < kFragsM ? 2 * t + i / 4 : 0][i % 4];
     });
   };
   if (e.mode == kEndPartial) {
 #pragma nounroll
-    for (int turn = 0; turn < kFragsM / 2; ++turn, row0 += 32, left -= 32) {
+    for (int turn = 0; turn < kTurns; ++turn, row0 += 32, left -= 32) {
       floatx4 c[2][4] = {};
       sums(turn, c);
       pass(c);
@@ -253,13 +255,13 @@ __device__ __forceinline__ void end_tile(const End& e, const floatx4 (&acc)[kFra
     for (uint32_t& w : next[s].w) w = 0;
   read(left);
 #pragma nounroll
-  for (int turn = 0; turn < kFragsM / 2; ++turn) {
+  for (int turn = 0; turn < kTurns; ++turn) {
     floatx4 c[2][4] = {};
     sums(turn, c);
     Residual<kType> now[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) now[s] = next[s];
-    if (turn + 1 < kFragsM / 2) read(left - 32);
+    if (turn + 1 < kTurns) read(left - 32);
     pass(c);
 #pragma nounroll
     for (int s = 0; s < kSteps; ++s, left -= kRows) {

@@ -9,16 +9,17 @@ namespace pointid {
 namespace {
 
 // us of a tile shape, fitted to sweeps of tiles and splits over 32 products of all forms
-// from 4 x 12288 x 4096 to 16384 x 4096 x 1024 (24 in fp32): a stage of 64 inner indices when
+// from 4 x 12288 x 4096 to 16384 x 4096 x 1024 (70 in fp32): a stage of 64 inner indices when
 // `resident` blocks share a CU (each) and of a block alone, and a block's start and end.
-// The choice by them is the fastest measured or within 6 % of it, half a percent on average.
+// The choice by them takes half a percent more than the fastest measured on average, at
+// worst 6 % (fp32 15).
 struct TileCost {
   double stage, alone, ends;
   int resident;
 };
 constexpr TileCost kCost[kTiles] = {
     {1.25, 1.25, 8.5, 1}, {0.555, 0.555, 2.6, 1}, {0.515, 0.617, 2.6, 2}, {0.314, 0.463, 1.7, 3}};
-constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 1}, {1.58, 2.79, 0.8, 2}};
+constexpr TileCost kCost32[kTiles32] = {{4.53, 4.53, 3.0, 1}, {2.76, 2.76, 2.4, 1}, {1.58, 2.79, 0.8, 2}, {1.0, 1.8, 0.7, 3}};
 
 constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
 
@@ -68,6 +69,9 @@ Timed least_cost(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner
 // small ones fill the CUs where there are few (2048^3: 26 in 64 x 128, 44 in split 256 x 256;
 // its gated form 37 in 128 x 128, 49 and 51 in the others); three stages hide the loads of
 // one 128 x 128 tile a CU (4096 x 4096 x 1024: 43 against 50), two leave room for a second.
+// fp32: 2048^3 96 in 128 x 128 tiles, 136 in 64 x 64; 308 x 7121 x 944 47 in 64 x 128, 53 in
+// 64 x 64, 57 in 128 x 128; 235 x 128 x 32 8.7 in 64 x 64, 10.4 in 64 x 128 (the chain of a
+// stage is shorter); a gated 3257 x 2532 x 285 82 in 256 x 128, 89 in 64 x 128.
 ProductPlan plan_product(bool f32, int64_t rows, int64_t cols, int halves, int64_t inner, int terms, int cus) {
   return least_cost(f32, rows, cols, halves, inner, terms, cus).plan;
 }

@@ -95,8 +95,8 @@ struct Tile32 {
     }
     part[2] = Op16<false>::pack(a, b);
   }
-  // The parts of the values to the three planes at `tile`.
-  template <bool kCare>
+  // The parts of the values to the three planes at `tile`, kPitch bytes apart.
+  template <bool kCare, int kPitch>
   __device__ __forceinline__ void store(char* tile, const float4 (&v)[kLoads]) const {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -104,7 +104,7 @@ struct Tile32 {
       cut<kCare>(v[i].x, v[i].y, x);
       cut<kCare>(v[i].z, v[i].w, y);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(tile + p * kPlane + to[i]) = make_uint2(x[p], y[p]);
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(tile + p * kPitch + to[i]) = make_uint2(x[p], y[p]);
     }
   }
 };
@@ -127,9 +127,8 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
   static_assert(kBN / kWN == 64, "a wave takes 64 columns");
   using Left = Tile32<kLeftInner, kBM, kThreads>;
   using Right = Tile32<kRightInner, kHN, kThreads>;
-  // a stage: the left operand's planes, then each half's
-  constexpr int kLeftBytes = 3 * Left::kPlane, kRightBytes = 3 * Right::kPlane;
-  constexpr int kStage = kLeftBytes + 2 * kRightBytes;
+  // a stage: the left operand's planes, then the right one's, half after half in each
+  constexpr int kLeftBytes = 3 * Left::kPlane, kStage = kLeftBytes + 6 * Right::kPlane;
 
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -149,9 +148,9 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
     return wm * (kBM / kWM) + 16 * i;
   });
   rf.init(lane, [&](int i, int* tile) {
-    const int half = kHalves == 2 ? i / 2 : wn * 64 / kHN;
-    *tile = kLeftBytes + half * kRightBytes;
-    return kHalves == 2 ? wn * 32 + i % 2 * 16 : wn * 64 % kHN + 16 * i;
+    const int col = kHalves == 2 ? i / 2 * kHN + wn * 32 + i % 2 * 16 : wn * 64 + 16 * i;
+    *tile = kLeftBytes + col / kHN * Right::kPlane;
+    return col % kHN;
   });
 
   const int stages = a.split_each + (at.split < (uint32_t)a.split_more);
@@ -200,9 +199,9 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
   auto sum = [&](auto care) {
     auto store = [&](int stage) {
       char* tile = smem + stage * kStage;
-      left.template store<care>(tile, lv);
-      right0.template store<care>(tile + kLeftBytes, rv0);
-      right1.template store<care>(tile + kLeftBytes + kRightBytes, rv1);
+      left.template store<care, Left::kPlane>(tile, lv);
+      right0.template store<care, 2 * Right::kPlane>(tile + kLeftBytes, rv0);
+      right1.template store<care, 2 * Right::kPlane>(tile + kLeftBytes + Right::kPlane, rv1);
     };
     to_load = stages;
     term = term0;
@@ -222,7 +221,7 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
 #pragma unroll
       for (int p = 0; p < 3; ++p)
 #pragma unroll
-        for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * Right::kPlane, j, 0);
+        for (int j = 0; j < kFragsN; ++j) r[p][j] = rf.read(tile + p * 2 * Right::kPlane, j, 0);
       read_left(tile, 0);
       auto next = [&] {
         if (it + 1 == stages) return;
@@ -234,7 +233,7 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
       for (int i = 0; i < kFragsM; ++i) {
         if (i + 1 < kFragsM) read_left(tile, i + 1);
         multiply(i);
-        if (i == kFragsM / 2 - 1 && !early) next();
+        if (i == (kFragsM - 1) / 2 && !early) next();
       }
       __syncthreads();
     }
@@ -279,6 +278,7 @@ hipError_t launch_tile32(int tile, ProductArgs& a, hipStream_t stream) {
     case 0: return launch_kernel(product_f32_kernel<kForm, kHalves, 256, 128, 4, 2>, grid, dim3(512), 0, stream, a);
     case 1: return launch_kernel(product_f32_kernel<kForm, kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
     case 2: return launch_kernel(product_f32_kernel<kForm, kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+    case 3: return launch_kernel(product_f32_kernel<kForm, kHalves, 64, 64, 4, 1>, grid, dim3(256), 0, stream, a);
   }
   return hipErrorInvalidValue;
 }
@@ -292,6 +292,7 @@ hipError_t launch_pair_tile32(int tile, PairArgs& a, hipStream_t stream) {
     case 0: return launch_kernel(pair_f32_kernel<kHalves, 256, 128, 4, 2>, grid, dim3(512), 0, stream, a);
     case 1: return launch_kernel(pair_f32_kernel<kHalves, 128, 128, 4, 2>, grid, dim3(512), 0, stream, a);
     case 2: return launch_kernel(pair_f32_kernel<kHalves, 64, 128, 2, 2>, grid, dim3(256), 0, stream, a);
+    case 3: return launch_kernel(pair_f32_kernel<kHalves, 64, 64, 4, 1>, grid, dim3(256), 0, stream, a);
   }
   return hipErrorInvalidValue;
 }
