@@ -25,10 +25,10 @@
 // their global addresses.  Rows of 64 inner indices (128 bytes): piece p of row r at
 // p ^ (r / 2 % 8), so that 16 lanes reading one piece of 16 rows touch all banks (rows of
 // 32 inner indices, in the fp32 kernel: p ^ (-(r / 4) % 4); without the minus lanes 0-3 and
-// 12-15 met 20-27, which are served with them: 0.22 to 0.36 of the cycles).  Rows of columns: the pair of
-// pieces g of row r at g ^ (r % 4 + 4 (r / 8 % 2)) (rows of 128 bytes: g ^ (r / 2 % 2 +
-// 2 (r / 8 % 2)), of 64: g ^ (r / 8 % 2)), so that the rows r .. r + 3 and r + 8 .. r + 11 of 16 columns that 32
-// lanes of a transposing read take do.
+// 12-15 met 20-27, which are served with them: 0.22 to 0.36 of the cycles).  Rows of columns:
+// the pair of pieces g of row r at g ^ (r % 4 + 4 (r / 8 % 2)) (rows of 128 bytes: g ^ (r / 2
+// % 2 + 2 (r / 8 % 2)), of 64: g ^ (r / 8 % 2)), so that the rows r .. r + 3 and r + 8 ..
+// r + 11 of 16 columns that 32 lanes of a transposing read take do.
 #pragma once
 
 #include "internal.h"
