@@ -46,7 +46,7 @@ enum EndMode { kEndDense = 0, kEndGated = 1, kEndStore = 2, kEndPartial = 3 };
 // What becomes of the finished sums of one result (or of two halves of one).
 //   kEndDense    v = sum + bias0; keep0 <- v; y0 = act(v) + residual
 //   kEndGated    g = sum0 + bias0, u = sum1 + bias1; keep0 <- g; keep1 <- u; y0 = act(g) u
-//   kEndStore    y0 = sum0 (and y1 = sum1)
+//   kEndStore    y0 = sum0 (and y1 = sum1), fp16 times *unscale where that is given
 //   kEndPartial  sums to part[(split * halves + half) * rows + row][part_ld] in fp32
 struct End {
   int32_t mode;
@@ -64,6 +64,7 @@ struct End {
   void* y1;
   int64_t ld1;
   Kept keep0, keep1;
+  const float* unscale;
   float* part;
   int64_t part_ld;             // a multiple of 32
 };
@@ -155,7 +156,9 @@ hipError_t launch_layers_zero(void* out, int64_t ld, int dtype, int64_t rows, in
 //   dense: dz = dy act'(z) (z absent: dy)     gated: dg = dy u act'(g), du = dy act(g)
 // parts: 0 none written, 1 or 2 planes of the 16-bit type (2: value and remainder),
 // -1 fp32 values.  col_part: [row blocks][halves][cols] sums of each block of rows, or
-// nullptr.
+// nullptr.  maxima: nullptr, or (fp16) what launch_layers_grad_max left: the values written
+// are those times the power of two that brings the largest finite magnitude to [2^14, 2^15),
+// and *unscale <- the power that undoes it.
 struct GradArgs {
   const void* dy;
   int64_t ld_dy;
@@ -168,10 +171,18 @@ struct GradArgs {
   void* out[2];                // each half: planes [parts][rows][ld], or fp32 [rows][ld]
   int64_t ld, plane;
   float* col_part;
+  uint32_t* maxima;
+  uint32_t maxima_count;
+  float* unscale;
   uint32_t row_blocks, strips;  // set by the launch
 };
 // Rows of a block: 32, or 8 where that gives fewer than two blocks a CU.
 int grad_rows(int64_t rows, int64_t cols, int cus);
+// The largest finite magnitudes (their bits) of a fp16 gradient's values, one a block, in
+// grad_max_blocks() words.
+constexpr uint32_t kMostMaxima = 1024;
+uint32_t grad_max_blocks(int64_t rows, int64_t cols);
+hipError_t launch_layers_grad_max(const GradArgs& a, hipStream_t stream);
 // `fill`: jobs that the same launch takes.
 hipError_t launch_layers_grad(GradArgs a, int block_rows, FillJobs fill, hipStream_t stream);
 

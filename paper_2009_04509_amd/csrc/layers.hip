@@ -456,6 +456,13 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   const int block_rows = grad_rows(b.m, b.n, l->cus);
   const int64_t grad_blocks = (b.m + block_rows - 1) / block_rows;
   if (want_db) call.want(&g.col_part, sizeof(float) * (size_t)(grad_blocks * b.halves * b.n));
+  // what is not dy itself can leave fp16's range
+  const bool scaled = b.dtype == POINTID_FP16 && products && !exact16;
+  if (scaled) {
+    g.maxima_count = grad_max_blocks(b.m, b.n);
+    call.want(&g.maxima, sizeof(uint32_t) * g.maxima_count);
+    call.want(&g.unscale, sizeof(float));
+  }
 
   // x for dW, the weights for dx
   Source sx, sw[2];
@@ -495,6 +502,11 @@ int run_backward(pointid_layers l, const Backward& b, hipStream_t stream) {
   std::memset(&jobs, 0, sizeof(jobs));
   for (int h = 0; h < b.halves && want_dx; ++h) sw[h].make(&jobs);
   if (want_dw) sx.make(&jobs);
+  if (scaled) {
+    rc = call.run("layers_grad_max", false, [&] { return launch_layers_grad_max(g, stream); });
+    if (rc != POINTID_OK) return rc;
+    dx_end.unscale = dw_end.unscale = g.unscale;
+  }
   if (g.parts != 0 || want_db)
     rc = call.run("layers_grad", false, [&] { return launch_layers_grad(g, block_rows, jobs, stream); });
   else

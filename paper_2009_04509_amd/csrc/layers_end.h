@@ -311,16 +311,29 @@ struct Residual : Raw8<kType> {
   }
 };
 
+// The factor of kEndStore's sums.
+template <int kType>
+__device__ __forceinline__ float unscale_of(const End& e) {
+  if constexpr (kType != POINTID_FP16) return 1.f;
+  return e.unscale ? *e.unscale : 1.f;
+}
+
 // The end of 8 finished columns of a row (see End), of which the first n exist; v1 and b1:
 // the second half's, with kHalves == 2; b0, b1: load_bias's; r: the residual's.  The 4 lanes
 // of an aligned group hold 32 columns of one row, from a multiple of 32 on (the lane `first`
 // the first of them), and all call it; `live` is false where the row or the columns do not
-// exist.
+// exist.  unscale: unscale_of's.
 template <int kType, int kHalves>
 __device__ __forceinline__ void finish(const End& e, const Targets<kType, kHalves>& to, bool live, bool first, int n,
-                                       float* v0, float* v1, const float* b0, const float* b1, const Residual<kType>& r) {
+                                       float* v0, float* v1, const float* b0, const float* b1, const Residual<kType>& r, float unscale) {
   if (e.mode == kEndStore) {
     if (!live) return;
+    if constexpr (kType == POINTID_FP16)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v0[i] *= unscale;
+        if constexpr (kHalves == 2) v1[i] *= unscale;
+      }
     store_cols<8>(to.t0.y, 0, kType, n, v0);
     if constexpr (kHalves == 2) store_cols<8>(to.t1.y, 0, kType, n, v1);
     return;

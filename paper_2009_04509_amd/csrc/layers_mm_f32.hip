@@ -252,7 +252,7 @@ __device__ __forceinline__ void product_f32_block(const ProductArgs& a, uint32_t
   if (__syncthreads_or(all != 0.f)) sum(std::true_type{});
   end_tile<POINTID_FP32, kHalves, kFragsM>(a.end, acc, reinterpret_cast<float*>(smem) + wave * kEndWave / 4,
                                                     lane, at.split, row0 + wm * (kBM / kWM),
-                                                    col0 + wn * (kHalves == 2 ? 32 : 64));
+                                                    col0 + wn * (kHalves == 2 ? 32 : 64), 1.f);
 }
 
 template <int kForm, int kHalves, int kBM, int kBN, int kWM, int kWN>

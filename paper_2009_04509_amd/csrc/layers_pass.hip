@@ -89,6 +89,80 @@ __global__ void __launch_bounds__(256) checkpoint_save_kernel(const char* src, i
 // How the activations of a gradient are kept.
 enum { kKeptNot = 0, kKeptWhole = 1, kKeptPacked = 2 };
 
+// 8 values of a gradient brought before the activation: g of dy (dh), z of z (g, u).
+template <int kHalves>
+__device__ __forceinline__ void through8(int act, const float (&g)[8], const float (&z)[kHalves][8],
+                                         float (&d)[kHalves][8]) {
+  static_for<5>([&](auto a) {                   // the choice outside of the loop
+    if (act == a) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float value;
+        if constexpr (kHalves == 2) {
+          d[0][i] = through(a, z[0][i], g[i] * z[1][i], &value);
+          d[1][i] = g[i] * value;
+        } else {
+          d[0][i] = through(a, z[0][i], g[i], &value);
+        }
+      }
+    }
+  });
+}
+
+// The largest of 256 threads' values.
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t (&waves)[4]) {
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    const uint32_t other = (uint32_t)__shfl_xor((int)v, x, 64);
+    v = other > v ? other : v;
+  }
+  if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v = waves[w] > v ? waves[w] : v;
+  return v;
+}
+
+// dz = dy act'(z) (dg, du) reaches past fp16's largest value, and below its smallest, where
+// the products are in range: it is kept times a power of two, which this pass is for.  It
+// computes what the gradient pass does and leaves the largest finite magnitude of each block
+// (the gradient pass takes the largest of these, so that no word is shared and cleared).  Bound
+// by the bytes: a gated 8192 x 8192 75-85 us of 1,930 (about 5 TB/s read), from 8 bits 70-80;
+// 1693 x 2048 8, most of it the launch and the next pass's wait for the maxima.
+template <int kHalves, bool kPacked>
+__global__ void __launch_bounds__(256) grad_max_kernel(GradArgs a) {
+  __shared__ uint32_t waves[4];
+  uint32_t top = 0;
+  each_piece(a.rows, (a.cols + 7) / 8, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256,
+             [&](int64_t row, int64_t col) {
+    const int n = piece_cols(a.cols, col);
+    Raw8<POINTID_FP16> dy;
+    dy.load(static_cast<const char*>(a.dy) + (row * a.ld_dy + col) * 2, n);
+    float g[8], z[kHalves][8], d[kHalves][8];
+    dy.values(g);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      if constexpr (kPacked) {
+        load_codes(a.z[h].packed, row, col, a.cols, z[h]);
+      } else {
+        Raw8<POINTID_FP16> w;
+        w.load(static_cast<const char*>(a.z[h].matrix) + (row * a.z[h].ld + col) * 2, n);
+        w.values(z[h]);
+      }
+    }
+    through8<kHalves>(a.act, g, z, d);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t b = finite_bits(d[h][i]);
+        top = b > top ? b : top;
+      }
+  });
+  top = block_max(top, waves);
+  if (threadIdx.x == 0) a.maxima[blockIdx.x] = top;
+}
+
 // dz = dy act'(z), or of a gated layer dg = dh u act'(g) and du = dh act(g), in fp32 and
 // rounded once to the type that the products read; the column sums before the rounding.
 // Each block: 8 kTurns rows x 256 columns (the blocks past those take the fill's jobs, which
@@ -104,6 +178,20 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a, FillJobs fill) {
   if (blockIdx.x >= grad_blocks) {
     run_fill_block(fill, grad_blocks, gridDim.x);
     return;
+  }
+  float scale = 1.f;
+  if constexpr (kType == POINTID_FP16) {
+    if (a.maxima) {
+      __shared__ uint32_t waves[4];
+      uint32_t top = 0;
+      for (uint32_t i = threadIdx.x; i < a.maxima_count; i += 256) top = a.maxima[i] > top ? a.maxima[i] : top;
+      top = block_max(top, waves);
+      // top = f 2^e, f in [1/2, 1): to [2^14, 2^15)
+      int p = top == 0 ? 0 : 15 - __builtin_amdgcn_frexp_expf(__uint_as_float(top));
+      p = p < 126 ? p : 126;
+      scale = __builtin_amdgcn_ldexpf(1.f, p);
+      if (blockIdx.x == 0 && threadIdx.x == 0) *a.unscale = __builtin_amdgcn_ldexpf(1.f, -p);
+    }
   }
   const uint32_t strip = blockIdx.x / row_blocks, row_block = blockIdx.x - strip * row_blocks;
   constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
@@ -155,20 +243,7 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a, FillJobs fill) {
           if constexpr (kKept == kKeptPacked) zp[u][h].values(z[h]);
         }
         // (what does not exist reads as 0 and stays 0: so does the padding)
-        static_for<5>([&](auto act) {               // the choice outside of the loop
-          if (a.act == act) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float value;
-              if constexpr (kHalves == 2) {
-                d[0][i] = through(act, z[0][i], g[i] * z[1][i], &value);
-                d[1][i] = g[i] * value;
-              } else {
-                d[0][i] = through(act, z[0][i], g[i], &value);
-              }
-            }
-          }
-        });
+        through8<kHalves>(a.act, g, z, d);
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
 #pragma unroll
@@ -178,6 +253,9 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs a, FillJobs fill) {
           if constexpr (kType == POINTID_FP32) {
             store_cols<8>(a.out[h], at, kType, 8, d[h]);
           } else {
+            if constexpr (kType == POINTID_FP16)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) d[h][i] *= scale;
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = pack16(d[h][2 * i], d[h][2 * i + 1], kType);
@@ -273,7 +351,7 @@ __global__ void __launch_bounds__(256) join_kernel(End e, const float* part, int
   Targets<kType, kHalves> to;
   to.init(e, row, col);
   finish<kType, kHalves>(e, to, live, col % kBlock8 == 0, piece_cols(e.cols, col), v[0], v[kHalves - 1], bias[0], bias[1],
-                         residual);
+                         residual, unscale_of<kType>(e));
 }
 
 __global__ void __launch_bounds__(256) zero_kernel(void* out, int64_t ld, int dtype, int64_t rows, int64_t cols) {
@@ -330,6 +408,20 @@ hipError_t launch_checkpoint_save(const void* src, int64_t ld, int dtype, int64_
     case POINTID_BF16: return go(checkpoint_save_kernel<POINTID_BF16>);
   }
   return go(checkpoint_save_kernel<POINTID_FP16>);
+}
+
+uint32_t grad_max_blocks(int64_t rows, int64_t cols) {
+  const int64_t blocks = (rows * ((cols + 7) / 8) + 255) / 256;
+  return (uint32_t)(blocks < kMostMaxima ? blocks : kMostMaxima);
+}
+
+hipError_t launch_layers_grad_max(const GradArgs& a, hipStream_t stream) {
+  if (a.dtype != POINTID_FP16 || !a.maxima || a.maxima_count != grad_max_blocks(a.rows, a.cols)) return hipErrorInvalidValue;
+  for (int h = 0; h < a.halves; ++h)
+    if (!a.z[h].any() || !a.z[h].matrix != !a.z[0].matrix) return hipErrorInvalidValue;
+  auto go = [&](auto kernel) { return launch_kernel(kernel, dim3(a.maxima_count), dim3(256), 0, stream, a); };
+  if (a.halves == 2) return a.z[0].matrix ? go(grad_max_kernel<2, false>) : go(grad_max_kernel<2, true>);
+  return a.z[0].matrix ? go(grad_max_kernel<1, false>) : go(grad_max_kernel<1, true>);
 }
 
 int grad_rows(int64_t rows, int64_t cols, int cus) {

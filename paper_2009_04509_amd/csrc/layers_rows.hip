@@ -172,7 +172,8 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a) {
       residual.load(residual.at(a.end, r, at), a.end.residual && live ? count : 0);
       Targets<kType, kHalves> to;
       to.init(a.end, r, at);
-      finish<kType, kHalves>(a.end, to, live, at % kBlock8 == 0, count, v[0], v[kHalves - 1], bias[0], bias[1], residual);
+      finish<kType, kHalves>(a.end, to, live, at % kBlock8 == 0, count, v[0], v[kHalves - 1], bias[0], bias[1], residual,
+                              1.f);
     }
   }
 }

@@ -1,0 +1,181 @@
+"""GPU: gradients of fp16 layers whose values before the activation leave fp16's range
+while their products stay in it, against the definition in 64 bits.
+
+Tolerances.  dz (dg, du) is rounded once, to 11 bits (2^-11 of it), after a power of two has
+brought its largest finite magnitude M to [2^14, 2^15): what falls below fp16's normal range
+there is off by at most 2^-25 of those, 2^-39 M.  In two parts: 2^-22 of it and 2^-39 M.  An
+activation's slope is computed to 1e-6 of max(1, |z|), a sum of L terms in fp32 to L 2^-23 of
+its magnitudes, and the result is rounded to fp16 (2^-11, or 2^-25).
+"""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -11
+E = 2.0 ** -23
+F16 = torch.float16
+
+
+@pytest.fixture(scope="module")
+def pid():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2009_04509_amd import binding
+    return binding
+
+
+@pytest.fixture(scope="module")
+def layers(pid):
+    h = pid.pointid_layers_create(0)
+    yield h
+    h.close()
+
+
+def act64(name, z):
+    return {"none": z, "relu": z.clamp(min=0), "silu": z * torch.sigmoid(z), "gelu": z * torch.special.ndtr(z),
+            "sigmoid": torch.sigmoid(z)}[name]
+
+
+def slope64(name, z):
+    s = torch.sigmoid(z)
+    return {"none": torch.ones_like(z), "relu": (z > 0).double(), "silu": s * (1 + z * (1 - s)),
+            "gelu": torch.special.ndtr(z) + z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5, "sigmoid": s * (1 - s)}[name]
+
+
+def half(g, *shape, scale=1.0):
+    return (torch.randn(shape, generator=g, dtype=torch.float64) * scale).to(F16)
+
+
+def dev(t):
+    return t.to(DEV)
+
+
+def near(got, want, tol, what):
+    got = got.double().cpu()
+    assert want.abs().max() < 65504, "the test's own result has to be in range"
+    bad = ~((got - want).abs() <= tol + want.abs() * U + 2.0 ** -25)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, e.g. at {bad.nonzero()[0].tolist()}: " \
+        f"{got[bad][0].item()} for {want[bad][0].item()}"
+
+
+def kept(pid, v, eight):
+    if not eight:
+        return dev(v), v.double()
+    c = pid.pointid_checkpoint_save(dev(v))
+    return c, pid.pointid_checkpoint_load(c, torch.float32).double().cpu()
+
+
+def product(a, b, ta=None, tb=None):
+    """(a b, its fp32 error and that of its operands)"""
+    t = (a.abs() @ b.abs()) * ((a.shape[1] + 8) * E)
+    return a @ b, t + (ta @ b.abs() if ta is not None else 0) + (a.abs() @ tb if tb is not None else 0)
+
+
+def check_gated(pid, layers, dh, x, w, u, v, act, eight, two):
+    """The gradients of a gated layer at g = u, u = v."""
+    X, x64 = kept(pid, x, eight)
+    (G, g64), (V, u64) = kept(pid, u, eight), kept(pid, v, eight)
+    d = dh.double()
+    dg, du = d * u64 * slope64(act, g64), d * act64(act, g64)
+    most = max(dg.abs().max().item(), du.abs().max().item())
+    slack = 1e-6 * g64.abs().clamp(min=1)
+    eg, eu = ((d * f).abs() * slack + t.abs() * ((U * U if two else U) + 3 * E) + most * 2.0 ** -39
+              for f, t in ((u64, dg), (torch.ones_like(d), du)))
+    dx, dwg, dwu, dbg, dbu = pid.pointid_gated_backward(layers, dev(dh), X, dev(w[0]), dev(w[1]), G, V, act, need_db=True)
+    (a, ta), (b, tb) = (product(t, y.double().t(), ta=e) for t, y, e in ((dg, w[0], eg), (du, w[1], eu)))
+    near(dx, a + b, 2 * (ta + tb), f"dx {act}")
+    for got, t, e, name in ((dwg, dg, eg, "dwg"), (dwu, du, eu, "dwu")):
+        near(got, *product(x64.t(), t, tb=e), f"{name} {act}")
+    # each output alone as well: dx and dW by launches of their own
+    alone = pid.pointid_gated_backward(layers, dev(dh), None, dev(w[0]), dev(w[1]), G, V, act, need_dw=False)
+    near(alone[0], a + b, 2 * (ta + tb), f"dx alone {act}")
+    alone = pid.pointid_gated_backward(layers, dev(dh), X, dev(w[0]), dev(w[1]), G, V, act, need_dx=False)
+    near(alone[1], *product(x64.t(), dg, tb=eg), f"dwg alone {act}")
+
+
+# m n up to and past 2^16: dg and du in two parts and in one
+SHAPES = [(4, 512, 64, True), (40, 72, 100, True), (300, 264, 260, False), (1030, 96, 131, False)]
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("m, k, n, two", SHAPES)
+def test_gated_gradients_past_the_largest_value(pid, layers, m, k, n, two, eight):
+    """One row whose dg is twice fp16's largest value; the products are in range."""
+    g = torch.Generator().manual_seed(m)
+    x, dh, u, v = half(g, m, k, scale=2.0 ** -4), half(g, m, n), half(g, m, n), half(g, m, n)
+    w = [half(g, k, n, scale=0.05).clamp(-0.3, 0.3) for _ in range(2)]
+    dh[1, :], v[1, :] = 0, 0
+    dh[1, n - 2], v[1, n - 2], u[1, n - 2] = 600, 200, 3
+    for act in ("silu", "gelu", "relu", "none"):
+        check_gated(pid, layers, dh, x, w, u, v, act, eight, two)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("m, k, n, two", SHAPES)
+def test_gated_gradients_below_the_smallest_value(pid, layers, m, k, n, two, eight):
+    """dg and du near and below fp16's smallest subnormal; dW sums enough of them, or x is
+    large enough, to stand in the type."""
+    g = torch.Generator().manual_seed(m + 1)
+    x, dh = half(g, m, k, scale=1000.0), half(g, m, n, scale=2.0 ** -14)
+    u, v = half(g, m, n, scale=2.0 ** -9), half(g, m, n, scale=2.0 ** -9)
+    w = [half(g, k, n, scale=100.0) for _ in range(2)]
+    for act in ("silu", "gelu", "none"):
+        check_gated(pid, layers, dh, x, w, u, v, act, eight, two)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("act", ["silu", "gelu", "sigmoid"])
+@pytest.mark.parametrize("scale", [2.0 ** -16, 30000.0])
+@pytest.mark.parametrize("m, k, n, two", SHAPES)
+def test_dense_gradients_at_the_ends_of_the_range(pid, layers, m, k, n, two, scale, act, eight):
+    """dy of a few units of the smallest subnormal, or near the largest value (slopes up to 1.13
+    take it past that)."""
+    g = torch.Generator().manual_seed(m + 2)
+    small = scale < 1
+    dy = half(g, m, n, scale=scale).clamp(-60000, 60000) if small else \
+        torch.where(torch.rand((m, n), generator=g) < 1 / n, scale * 2, 0.0).to(F16)
+    x, w = half(g, m, k, scale=100.0 if small else 2.0 ** -6), half(g, k, n, scale=100.0 if small else 2.0 ** -8)
+    z = half(g, m, n) if small else half(g, m, n, scale=0.1) + 1.5
+    X, x64 = kept(pid, x, eight)
+    Z, z64 = kept(pid, z, eight)
+    dz = dy.double() * slope64(act, z64)
+    e = dy.double().abs() * 1e-6 * z64.abs().clamp(min=1) + dz.abs() * ((U * U if two else U) + 3 * E) + \
+        dz.abs().max() * 2.0 ** -39
+    dx, dw, db = pid.pointid_dense_backward(layers, dev(dy), X, dev(w), Z, act)
+    near(dx, *product(dz, w.double().t(), ta=e), "dx")
+    near(dw, *product(x64.t(), dz, tb=e), "dw")
+    tol = dy.double().abs().sum(0) * 1e-6 * z64.abs().max().clamp(min=1) + dz.abs().sum(0) * (m + 4) * E + 1e-30
+    assert ((db.double().cpu() - dz.sum(0)).abs() <= tol).all()
+
+
+def test_infinities_beside_small_values(pid, layers):
+    """What is not finite does not set the power of two, and stays in its row and column."""
+    g = torch.Generator().manual_seed(9)
+    m, k, n = 300, 64, 264
+    dy, z = half(g, m, n, scale=2.0 ** -16), half(g, m, n)
+    x, w = half(g, m, k, scale=100.0).abs() + 1, half(g, k, n, scale=100.0).abs() + 1
+    dy[7, 11], z[7, 11] = float("inf"), 1
+    dy[9, 13] = float("nan")
+    dz = dy.double() * slope64("silu", z.double())
+    dx, dw, _ = pid.pointid_dense_backward(layers, dev(dy), dev(x), dev(w), dev(z), "silu")
+    for got, want in ((dx, dz @ w.double().t()), (dw, x.double().t() @ dz)):
+        got = got.double().cpu()
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+        here = want.isfinite()
+        # each term is rounded to 2^-11 of it, and so is the result; the terms' magnitudes add up
+        # to at most 300 times the largest of them
+        size = dz.nan_to_num(0, 0, 0).abs().max() * 300 * max(x.double().max().item(), w.double().max().item())
+        assert ((got - want).abs()[here] <= size * 2 * U).all()
+
+
+def test_gradients_of_nothing(pid, layers):
+    """dy of zeros: zeros."""
+    m, k, n = 300, 64, 264
+    g = torch.Generator().manual_seed(10)
+    z = torch.zeros((m, n), dtype=F16, device=DEV)
+    q = pid.pointid_gated_backward(layers, z, dev(half(g, m, k)), dev(half(g, k, n)), dev(half(g, k, n)),
+                                   dev(half(g, m, n)), dev(half(g, m, n)), need_db=True)
+    assert all(not t.any() for t in q)
