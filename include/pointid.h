@@ -504,7 +504,9 @@ int pointid_dense(pointid_layers l, int dtype, int act, int64_t m, int64_t k, in
 /*
  * Gradients of pointid_dense from dy (the residual's gradient is dy itself):
  *   dz = dy act'(z),  dx = dz W^T,  dw = x^T dz,  db[j] = sum over rows of dz[.][j]
- *   x       as a matrix or a checkpoint; needed for dw only
+ *   x       as a matrix or a checkpoint; needed for dw only (fp16: a checkpoint's
+ *           65536, to which values from 63488 on are rounded, counts as 65504, the
+ *           largest value; larger ones are infinities)
  *   w       needed for dx only
  *   z       as kept; not needed for POINTID_ACT_NONE
  *   dx, dw, db  each optional (NULL)

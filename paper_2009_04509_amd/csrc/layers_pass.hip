@@ -43,6 +43,11 @@ __device__ __forceinline__ void run_fill_block(const FillJobs& a, uint32_t first
       load_cols<8>(job.src, row * job.ld_src + col, job.dtype, job.cols - col, v);
     else if (col < job.cols)
       load_codes(job.packed, row, col, job.cols, v);
+    // fp16 values from 63488 on are kept as 65536, which the type would hold as an infinity: the
+    // nearest that it holds is 65504
+    if (job.kind == FillJob::kLoad && job.dtype == POINTID_FP16)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __builtin_fabsf(v[i]) == 65536.f ? __builtin_copysignf(65504.f, v[i]) : v[i];
     store_cols<8>(job.out, row * job.ld + col, job.dtype, 8, v);
   });
 }

@@ -179,3 +179,29 @@ def test_gradients_of_nothing(pid, layers):
     q = pid.pointid_gated_backward(layers, z, dev(half(g, m, k)), dev(half(g, k, n)), dev(half(g, k, n)),
                                    dev(half(g, m, n)), dev(half(g, m, n)), need_db=True)
     assert all(not t.any() for t in q)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("n", [32, 261])
+def test_the_largest_values_in_8_bits(pid, layers, n, gated):
+    """Finite x of fp16 that 8 bits round to 65536: finite in dW, and no NaN beside dz of 0.  A
+    value is off by 2^-11 of it (65504 for 65536) and the roundings of the result."""
+    g = torch.Generator().manual_seed(11)
+    m, k = 300, 70
+    x = half(g, m, k)
+    x[3, 4], x[5, 4], x[7, 66], x[9, 60] = 65504, -63488, 64000, 57344     # the last stands as it is
+    dy, z = half(g, m, n, scale=2.0 ** -6), half(g, m, n)
+    dy[5, :] = 0
+    c = pid.pointid_checkpoint_save(dev(x))
+    x64 = pid.pointid_checkpoint_load(c, torch.float32).double().cpu()
+    assert x64[3, 4] == 65536 and x64[5, 4] == -65536 and x64[7, 66] == 65536 and x64[9, 60] == 57344
+    w = dev(half(g, k, n))
+    if gated:
+        du = dy.double() * act64("silu", z.double())
+        got = pid.pointid_gated_backward(layers, dev(dy), c, w, w, dev(z), dev(z), need_dx=False)[2]
+    else:
+        du = dy.double()
+        got = pid.pointid_dense_backward(layers, dev(dy), c, w, need_dx=False)[1]
+    e = du.abs() * (U + 3 * E) + dy.double().abs() * 1e-6 * z.double().abs().clamp(min=1) + du.abs().max() * 2.0 ** -39
+    want, tol = product(x64.t(), du, ta=x64.t().abs() * (x64.t().abs() == 65536) * U, tb=e)
+    near(got, want, tol, "dW")
