@@ -203,6 +203,13 @@ def _stream_ptr(stream, device=None):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _stream_object(stream, device):
+    """torch's object of a stream given as one or as its handle."""
+    if not isinstance(stream, int):
+        return stream
+    return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+
+
 def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
 
@@ -707,11 +714,20 @@ def _matrix(t, name, dtype, shape, device):
     return _Matrix(t.data_ptr(), pitch if rows > 1 else cols)
 
 
-def _output(t, like, name, dtype, shape, device):
+def _new(like, shape, dtype, stream, device):
+    """An output made like a tensor of the call, of the memory of the call's stream: the current
+    stream may still be using what its own memory had before."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(_stream_object(stream, device)):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def _output(t, like, name, dtype, shape, device, stream):
     """An output that is given, or made like a tensor of the call, and its descriptor."""
     if t is not None:
         return t, _matrix(t, name, dtype, shape, device)
-    t = like.new_empty(shape, dtype=dtype)
+    t = _new(like, shape, dtype, stream, device)
     return t, _Matrix(t.data_ptr(), shape[1])
 
 
@@ -769,7 +785,7 @@ def pointid_dense(layers: Layers, x: torch.Tensor, w: torch.Tensor, bias: torch.
     dt, dev = _layer_type(x, "x"), layers.device
     m, k, n = _shapes(x, w, "w")
     code = _activation(act)
-    y, out = _output(y, x, "y", dt, (m, n), dev)
+    y, out = _output(y, x, "y", dt, (m, n), dev, stream)
     _check(lib.pointid_dense(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
         _ref(_matrix(w, "w", dt, (k, n), dev)), _bias(bias, "bias", n, dev),
@@ -788,9 +804,9 @@ def pointid_dense_backward(layers: Layers, dy: torch.Tensor, x, w: torch.Tensor,
     m, n = dy.shape
     k = w.shape[0]
     code = _activation(act)
-    dx, to_dx = _output(None, dy, "dx", dt, (m, k), dev) if need_dx else (None, None)
-    dw, to_dw = _output(None, dy, "dw", dt, (k, n), dev) if need_dw else (None, None)
-    db = dy.new_empty((n,), dtype=torch.float32) if need_db else None
+    dx, to_dx = _output(None, dy, "dx", dt, (m, k), dev, stream) if need_dx else (None, None)
+    dw, to_dw = _output(None, dy, "dw", dt, (k, n), dev, stream) if need_dw else (None, None)
+    db = _new(dy, (n,), torch.float32, stream, dev) if need_db else None
     _check(lib.pointid_dense_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dy, "dy", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(w, "w", dt, (k, n), dev)),
@@ -809,7 +825,7 @@ def pointid_gated(layers: Layers, x: torch.Tensor, wg: torch.Tensor, wu: torch.T
     dt, dev = _layer_type(x, "x"), layers.device
     m, k, n = _shapes(x, wg, "wg")
     code = _activation(act)
-    h, out = _output(h, x, "h", dt, (m, n), dev)
+    h, out = _output(h, x, "h", dt, (m, n), dev, stream)
     _check(lib.pointid_gated(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(x, "x", dt, (m, k), dev)),
         _ref(_matrix(wg, "wg", dt, (k, n), dev)), _ref(_matrix(wu, "wu", dt, (k, n), dev)),
@@ -829,10 +845,10 @@ def pointid_gated_backward(layers: Layers, dh: torch.Tensor, x, wg: torch.Tensor
     m, n = dh.shape
     k = wg.shape[0]
     code = _activation(act)
-    dx, to_dx = _output(None, dh, "dx", dt, (m, k), dev) if need_dx else (None, None)
-    (dwg, to_dwg), (dwu, to_dwu) = (_output(None, dh, name, dt, (k, n), dev) if need_dw else (None, None)
-                                    for name in ("dwg", "dwu"))
-    dbg, dbu = (dh.new_empty((n,), dtype=torch.float32) if need_db else None for _ in range(2))
+    dx, to_dx = _output(None, dh, "dx", dt, (m, k), dev, stream) if need_dx else (None, None)
+    (dwg, to_dwg), (dwu, to_dwu) = (_output(None, dh, name, dt, (k, n), dev, stream) if need_dw
+                                    else (None, None) for name in ("dwg", "dwu"))
+    dbg, dbu = (_new(dh, (n,), torch.float32, stream, dev) if need_db else None for _ in range(2))
     _check(lib.pointid_gated_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dh, "dh", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(wg, "wg", dt, (k, n), dev)),
@@ -848,8 +864,8 @@ def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stre
     a = _matrix(x, "x", dt, (m, n), dev)
     if out is None:
         out = Checkpoint.__new__(Checkpoint)
-        out.codes = x.new_empty((m, n), dtype=torch.uint8)
-        out.exponents = out.codes.new_empty((m, -(-n // 32)))
+        out.codes = _new(x, (m, n), torch.uint8, stream, dev)
+        out.exponents = _new(x, (m, -(-n // 32)), torch.uint8, stream, dev)
         packed = _Packed(out.codes.data_ptr(), out.exponents.data_ptr())
     else:
         packed = _kept(out, "out", dt, (m, n), dev).packed
@@ -866,7 +882,7 @@ def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.T
     if dt not in _LAYER_TYPES:
         raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dt}")
     kept = _kept(saved, "saved", dt, (m, n), dev)
-    out, a = _output(out, saved.codes, "out", dt, (m, n), dev)
+    out, a = _output(out, saved.codes, "out", dt, (m, n), dev, stream)
     _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
                                        _layer_stream(stream, dev)))
     return out
