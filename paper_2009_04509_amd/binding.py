@@ -210,6 +210,15 @@ def _stream_object(stream, device):
     return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
 
 
+def _empty(shape, dtype, device, stream):
+    """An output of the memory of the call's stream: the current stream may still be using what
+    its own memory had before."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_stream_object(stream, device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
 
@@ -292,7 +301,7 @@ def pointid_classify(h: Handle, image: torch.Tensor, hits: torch.Tensor,
     _need(hits, torch.int32, "hits", h.device, (2,))
     n = hits.shape[0]
     if scores is None:
-        scores = torch.empty((n, 4), dtype=torch.float32, device=image.device)
+        scores = _empty((n, 4), torch.float32, image.device, stream)
     _need(scores, torch.float32, "scores", h.device, (4,))
     _check(lib.pointid_classify(h.raw, _ptr(image), image.shape[0], image.shape[1], _ptr(hits),
                                 n, _ptr(scores), _stream_ptr(stream, image.device)))
@@ -318,7 +327,7 @@ def pointid_classify_planes(h: Handle, images, hits: torch.Tensor,
     _need(hits, torch.int32, "hits", h.device, (3,))
     n = hits.shape[0]
     if scores is None:
-        scores = torch.empty((n, 4), dtype=torch.float32, device=hits.device)
+        scores = _empty((n, 4), torch.float32, hits.device, stream)
     _need(scores, torch.float32, "scores", h.device, (4,))
     _check(lib.pointid_classify_planes(h.raw, arr, len(images), _ptr(hits), n, _ptr(scores),
                                        _stream_ptr(stream, hits.device)))
@@ -332,7 +341,7 @@ def pointid_classify_planes_noalloc(h: Handle, images, hits: torch.Tensor,
     _need(hits, torch.int32, "hits", h.device, (3,))
     n = hits.shape[0]
     if scores is None:
-        scores = torch.empty((n, 4), dtype=torch.float32, device=hits.device)
+        scores = _empty((n, 4), torch.float32, hits.device, stream)
     _need(scores, torch.float32, "scores", h.device, (4,))
     arr = _plane_array(images)
     _check(lib.pointid_classify_planes_noalloc(h.raw, arr, len(images), _ptr(hits), n, _ptr(scores),
@@ -348,7 +357,7 @@ def pointid_classify_planes_ds(h: Handle, images, hits: torch.Tensor, ticks_per_
     _need(hits, torch.int32, "hits", h.device, (3,))
     n = hits.shape[0]
     if scores is None:
-        scores = torch.empty((n, 4), dtype=torch.float32, device=hits.device)
+        scores = _empty((n, 4), torch.float32, hits.device, stream)
     _need(scores, torch.float32, "scores", h.device, (4,))
     _check(lib.pointid_classify_planes_ds(h.raw, arr, len(images), int(ticks_per_column),
                                           _ptr(hits), n, _ptr(scores),
@@ -366,7 +375,7 @@ def pointid_downsample(image: torch.Tensor, ticks_per_column: int,
     W, T = image.shape
     J = -(-T // D) if D >= 1 else 0
     if out is None:
-        out = torch.empty((W, max(J, 1)), dtype=torch.float32, device=image.device)
+        out = _empty((W, max(J, 1)), torch.float32, image.device, stream)
     _need(out, torch.float32, "out")
     if tuple(out.shape) != (W, J):
         raise ValueError(f"out must be [{W}, {J}]")
@@ -391,7 +400,7 @@ def pointid_classify_requests(h: Handle, images, requests, stream=None):
         _need(hits, torch.int32, f"requests[{i}].hits", h.device, (2,) if plane >= 0 else (3,))
         n = hits.shape[0]
         if scores is None:
-            scores = torch.empty((n, 4), dtype=torch.float32, device=hits.device)
+            scores = _empty((n, 4), torch.float32, hits.device, stream)
         _need(scores, torch.float32, f"requests[{i}].scores", h.device, (4,))
         reqs[i] = _Request(hits.data_ptr(), n, plane, scores.data_ptr())
         outs.append(scores)
@@ -427,7 +436,7 @@ class Batcher:
         _need(hits, torch.int32, "hits", self._h.device, (2,) if plane >= 0 else (3,))
         n = hits.shape[0]
         if scores is None:
-            scores = torch.empty((n, 4), dtype=torch.float32, device=hits.device)
+            scores = _empty((n, 4), torch.float32, hits.device, stream)
         _need(scores, torch.float32, "scores", self._h.device, (4,))
         req = _Request(hits.data_ptr(), n, plane, scores.data_ptr())
         ticket = ctypes.c_uint64()
@@ -463,7 +472,7 @@ def pointid_classify_patches(h: Handle, patches: torch.Tensor,
     _need(patches, torch.float32, "patches", h.device, (48, 48))
     n = patches.shape[0]
     if scores is None:
-        scores = torch.empty((n, 4), dtype=torch.float32, device=patches.device)
+        scores = _empty((n, 4), torch.float32, patches.device, stream)
     _need(scores, torch.float32, "scores", h.device, (4,))
     _check(lib.pointid_classify_patches(h.raw, _ptr(patches), n, _ptr(scores),
                                         _stream_ptr(stream, patches.device)))
@@ -479,7 +488,7 @@ def pointid_gather(image: torch.Tensor, hits: torch.Tensor, out_dtype="fp32",
     n = hits.shape[0]
     tdt = torch.float32 if code == POINTID_FP32 else torch.int16
     if out is None:
-        out = torch.empty((n, 48, 48), dtype=tdt, device=image.device)
+        out = _empty((n, 48, 48), tdt, image.device, stream)
     _check(lib.pointid_gather(_ptr(image), image.shape[0], image.shape[1], _ptr(hits), n,
                               _ptr(out), code, _stream_ptr(stream, image.device)))
     return out
@@ -493,7 +502,7 @@ def pointid_gather_planes(images, hits: torch.Tensor, out_dtype="fp32",
     n = hits.shape[0]
     tdt = torch.float32 if code == POINTID_FP32 else torch.int16
     if out is None:
-        out = torch.empty((n, 48, 48), dtype=tdt, device=hits.device)
+        out = _empty((n, 48, 48), tdt, hits.device, stream)
     _check(lib.pointid_gather_planes(arr, len(images), _ptr(hits), n, _ptr(out), code,
                                      _stream_ptr(stream, hits.device)))
     return out
@@ -513,13 +522,13 @@ def pointid_find_hits(h: Handle, images, threshold: float, capacity: int | None 
     dev = images[0].device
     if hits_out is None:
         cap = 65536 if capacity is None else int(capacity)
-        hits_out = torch.empty((cap, 3), dtype=torch.int32, device=dev)
+        hits_out = _empty((cap, 3), torch.int32, dev, stream)
     _need(hits_out, torch.int32, "hits_out", h.device, (3,))
     cap = hits_out.shape[0] if capacity is None else int(capacity)
     if cap > hits_out.shape[0]:
         raise ValueError("capacity exceeds hits_out")
     if n_found is None:
-        n_found = torch.empty((1,), dtype=torch.int64, device=dev)
+        n_found = _empty((1,), torch.int64, dev, stream)
     _need(n_found, torch.int64, "n_found", h.device)
     _check(lib.pointid_find_hits(h.raw, arr, len(images), float(threshold),
                                  _ptr(hits_out) if cap > 0 else ctypes.c_void_p(0), cap,
@@ -714,20 +723,16 @@ def _matrix(t, name, dtype, shape, device):
     return _Matrix(t.data_ptr(), pitch if rows > 1 else cols)
 
 
-def _new(like, shape, dtype, stream, device):
-    """An output made like a tensor of the call, of the memory of the call's stream: the current
-    stream may still be using what its own memory had before."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(_stream_object(stream, device)):
-        return like.new_empty(shape, dtype=dtype)
+def _new(like, shape, dtype, stream):
+    """_empty on the device of a tensor of the call."""
+    return like.new_empty(shape, dtype=dtype) if stream is None else _empty(shape, dtype, like.device, stream)
 
 
 def _output(t, like, name, dtype, shape, device, stream):
     """An output that is given, or made like a tensor of the call, and its descriptor."""
     if t is not None:
         return t, _matrix(t, name, dtype, shape, device)
-    t = _new(like, shape, dtype, stream, device)
+    t = _new(like, shape, dtype, stream)
     return t, _Matrix(t.data_ptr(), shape[1])
 
 
@@ -806,7 +811,7 @@ def pointid_dense_backward(layers: Layers, dy: torch.Tensor, x, w: torch.Tensor,
     code = _activation(act)
     dx, to_dx = _output(None, dy, "dx", dt, (m, k), dev, stream) if need_dx else (None, None)
     dw, to_dw = _output(None, dy, "dw", dt, (k, n), dev, stream) if need_dw else (None, None)
-    db = _new(dy, (n,), torch.float32, stream, dev) if need_db else None
+    db = _new(dy, (n,), torch.float32, stream) if need_db else None
     _check(lib.pointid_dense_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dy, "dy", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(w, "w", dt, (k, n), dev)),
@@ -848,7 +853,7 @@ def pointid_gated_backward(layers: Layers, dh: torch.Tensor, x, wg: torch.Tensor
     dx, to_dx = _output(None, dh, "dx", dt, (m, k), dev, stream) if need_dx else (None, None)
     (dwg, to_dwg), (dwu, to_dwu) = (_output(None, dh, name, dt, (k, n), dev, stream) if need_dw
                                     else (None, None) for name in ("dwg", "dwu"))
-    dbg, dbu = (_new(dh, (n,), torch.float32, stream, dev) if need_db else None for _ in range(2))
+    dbg, dbu = (_new(dh, (n,), torch.float32, stream) if need_db else None for _ in range(2))
     _check(lib.pointid_gated_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dh, "dh", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(wg, "wg", dt, (k, n), dev)),
@@ -864,8 +869,8 @@ def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stre
     a = _matrix(x, "x", dt, (m, n), dev)
     if out is None:
         out = Checkpoint.__new__(Checkpoint)
-        out.codes = _new(x, (m, n), torch.uint8, stream, dev)
-        out.exponents = _new(x, (m, -(-n // 32)), torch.uint8, stream, dev)
+        out.codes = _new(x, (m, n), torch.uint8, stream)
+        out.exponents = _new(x, (m, -(-n // 32)), torch.uint8, stream)
         packed = _Packed(out.codes.data_ptr(), out.exponents.data_ptr())
     else:
         packed = _kept(out, "out", dt, (m, n), dev).packed
