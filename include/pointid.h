@@ -549,8 +549,8 @@ int pointid_gated_backward(pointid_layers l, int dtype, int act, int64_t m, int6
 
 /*
  * A matrix to a checkpoint and back (the values it stands for, rounded to
- * `dtype`).  No handle; the current HIP device.  rows >= 0 (0: a no-op),
- * 1 <= cols <= 2^20.  Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
+ * `dtype`).  No handle; on the current HIP device, which has to be that of the
+ * memory and the stream.  rows >= 0 (0: a no-op), 1 <= cols <= 2^20.  Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
  */
 int pointid_checkpoint_save(int dtype, int64_t rows, int64_t cols, const pointid_matrix *x,
                             const pointid_checkpoint *out, void *stream);

@@ -9,6 +9,7 @@ library's HIP kernels; if the library is not built this module fails to import.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -210,6 +211,14 @@ def _stream_object(stream, device):
     return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
 
 
+_STAYS = contextlib.nullcontext()
+
+
+def _on(device: int):
+    """Makes a device current for a call that has no handle to do so."""
+    return _STAYS if torch.cuda.current_device() == device else torch.cuda.device(device)
+
+
 def _empty(shape, dtype, device, stream):
     """An output of the memory of the call's stream: the current stream may still be using what
     its own memory had before."""
@@ -379,8 +388,9 @@ def pointid_downsample(image: torch.Tensor, ticks_per_column: int,
     _need(out, torch.float32, "out")
     if tuple(out.shape) != (W, J):
         raise ValueError(f"out must be [{W}, {J}]")
-    _check(lib.pointid_downsample(_ptr(image), W, T, D, _ptr(out),
-                                  _stream_ptr(stream, image.device)))
+    with _on(image.get_device()):
+        _check(lib.pointid_downsample(_ptr(image), W, T, D, _ptr(out),
+                                      _stream_ptr(stream, image.device)))
     return out
 
 
@@ -489,8 +499,9 @@ def pointid_gather(image: torch.Tensor, hits: torch.Tensor, out_dtype="fp32",
     tdt = torch.float32 if code == POINTID_FP32 else torch.int16
     if out is None:
         out = _empty((n, 48, 48), tdt, image.device, stream)
-    _check(lib.pointid_gather(_ptr(image), image.shape[0], image.shape[1], _ptr(hits), n,
-                              _ptr(out), code, _stream_ptr(stream, image.device)))
+    with _on(image.get_device()):
+        _check(lib.pointid_gather(_ptr(image), image.shape[0], image.shape[1], _ptr(hits), n,
+                                  _ptr(out), code, _stream_ptr(stream, image.device)))
     return out
 
 
@@ -503,8 +514,9 @@ def pointid_gather_planes(images, hits: torch.Tensor, out_dtype="fp32",
     tdt = torch.float32 if code == POINTID_FP32 else torch.int16
     if out is None:
         out = _empty((n, 48, 48), tdt, hits.device, stream)
-    _check(lib.pointid_gather_planes(arr, len(images), _ptr(hits), n, _ptr(out), code,
-                                     _stream_ptr(stream, hits.device)))
+    with _on(hits.get_device()):
+        _check(lib.pointid_gather_planes(arr, len(images), _ptr(hits), n, _ptr(out), code,
+                                         _stream_ptr(stream, hits.device)))
     return out
 
 
@@ -874,8 +886,9 @@ def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stre
         packed = _Packed(out.codes.data_ptr(), out.exponents.data_ptr())
     else:
         packed = _kept(out, "out", dt, (m, n), dev).packed
-    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(packed),
-                                       _layer_stream(stream, dev)))
+    with _on(dev):
+        _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(packed),
+                                           _layer_stream(stream, dev)))
     return out
 
 
@@ -888,6 +901,7 @@ def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.T
         raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dt}")
     kept = _kept(saved, "saved", dt, (m, n), dev)
     out, a = _output(out, saved.codes, "out", dt, (m, n), dev, stream)
-    _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
-                                       _layer_stream(stream, dev)))
+    with _on(dev):
+        _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
+                                           _layer_stream(stream, dev)))
     return out
