@@ -510,11 +510,12 @@ int pointid_dense(pointid_layers l, int dtype, int act, int64_t m, int64_t k, in
  *   w       needed for dx only
  *   z       as kept; not needed for POINTID_ACT_NONE
  *   dx, dw, db  each optional (NULL)
- * For the products dz is rounded to the 16-bit types (dz of few values is kept in
- * two parts), fp16 after a power of two has brought its largest finite magnitude
- * to [2^14, 2^15), which the results undo in fp32: values below 2^-28 of the largest
- * lose bits, below 2^-40 they vanish.  Where dz is dy or 0 (POINTID_ACT_NONE, _RELU)
- * it is neither scaled nor rounded.  db is summed from fp32 in a fixed order.  m == 0 sets dw and db to 0.
+ * For the products dz is rounded to the 16-bit types, up to 2^16 values of it in
+ * two parts (value and remainder); fp16 after a power of two has brought its largest
+ * finite magnitude to [2^14, 2^15), which the results undo in fp32: values below
+ * 2^-28 of the largest lose bits, below 2^-40 they vanish.  Where dz is dy or 0
+ * (POINTID_ACT_NONE, _RELU) it is neither scaled nor rounded.  db is summed from
+ * fp32 in a fixed order.  m == 0 sets dw and db to 0.
  * Errors: as pointid_dense, EINVAL also for an input that an output needs.
  */
 int pointid_dense_backward(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n,
@@ -550,7 +551,8 @@ int pointid_gated_backward(pointid_layers l, int dtype, int act, int64_t m, int6
 /*
  * A matrix to a checkpoint and back (the values it stands for, rounded to
  * `dtype`).  No handle; on the current HIP device, which has to be that of the
- * memory and the stream.  rows >= 0 (0: a no-op), 1 <= cols <= 2^20.  Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
+ * memory and the stream.  rows >= 0 (0: a no-op), 1 <= cols <= 2^20.
+ * Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
  */
 int pointid_checkpoint_save(int dtype, int64_t rows, int64_t cols, const pointid_matrix *x,
                             const pointid_checkpoint *out, void *stream);

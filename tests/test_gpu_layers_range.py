@@ -205,3 +205,32 @@ def test_the_largest_values_in_8_bits(pid, layers, n, gated):
     e = du.abs() * (U + 3 * E) + dy.double().abs() * 1e-6 * z.double().abs().clamp(min=1) + du.abs().max() * 2.0 ** -39
     want, tol = product(x64.t(), du, ta=x64.t().abs() * (x64.t().abs() == 65536) * U, tb=e)
     near(got, want, tol, "dW")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m, k, n", [(128, 72, 512), (129, 72, 512), (5, 800, 12288), (6, 800, 12288)])
+def test_both_sides_of_the_limit_of_two_parts(pid, layers, dtype, m, k, n):
+    """Up to 2^16 values of dz the results have the error of their own rounding, past that the
+    one of dz's as well.  Half a unit in the last place of 1 is u; the errors of rounding values of
+    any magnitude have the root mean square u sqrt(3 / (8 ln 2) / 3) = 0.425 u of them, two such
+    sqrt(2) times that; 5 % for the number of values (14,000 and more)."""
+    u = torch.finfo(dtype).eps / 2
+    most = 1.05 * 0.4247 * u * (1 if m * n <= 1 << 16 else 2 ** 0.5)
+    g = torch.Generator(device=DEV).manual_seed(m)
+
+    def rand(*shape):
+        return torch.randn(shape, generator=g, device=DEV).to(dtype)
+
+    dy, x, w, w2, z, v = rand(m, n), rand(m, k), rand(k, n), rand(k, n), rand(m, n), rand(m, n)
+    d, z64, v64 = dy.double(), z.double(), v.double()
+    dz = d * slope64("silu", z64)
+    dx, dw, _ = pid.pointid_dense_backward(layers, dy, x, w, z, "silu")
+    dg, du = dz * v64, d * act64("silu", z64)
+    q = pid.pointid_gated_backward(layers, dy, x, w, w2, z, v)
+    for got, want in ((dx, dz @ w.double().t()), (dw, x.double().t() @ dz),
+                      (q[0], dg @ w.double().t() + du @ w2.double().t()), (q[1], x.double().t() @ dg),
+                      (q[2], x.double().t() @ du)):
+        if got.numel() < 14000:
+            continue
+        err = ((got.double() - want).norm() / want.norm()).item()
+        assert err <= most, (err / u, most / u)
