@@ -332,14 +332,18 @@ struct Forward {
 
 // Whether the weights are streamed past the rows.  fp32: up to 8 rows (8192 x 8192, 8 rows:
 // 63 us, on the matrix cores 70).  16 bits: on the matrix cores from 2 rows on, and for one
-// row of up to 2^26 weights (4096 x 4096: 14 us against 16; a gated 4096 x 12288: 51
-// against 46), but up to 8 rows where they would take a copy of the weights first.  A lane
-// reads 16 bytes of a row, so a row has to have them.
+// row of up to 2^27 weights, of a gated layer 2^26.  Streamed against those, bf16, weights
+// out of memory: 4096 x 4096 15.7 us against 14.0, 8192 x 8192 34.2 against 33.2, 8192 x 9216
+// 37.2 against 34.9, 16384 x 8192 57.0 against 55.3, 12288 x 12288 61.2 against 61.8,
+// 16384 x 16384 97.0 against 100.5; gated 4096 x 4096 24.2 against 22.7, 4096 x 8192 34.6
+// against 35.6, 12288 x 4096 47.6 against 46.8, 4096 x 12288 46.2 against 51.8, 12288 x
+// 12288 114 against 137 (fp16 alike).  But streamed up to 8 rows where they would take a copy
+// of the weights first.  A lane reads 16 bytes of a row, so a row has to have them.
 bool few_rows(const Forward& f) {
   if (f.m > kFewRows || f.n < (f.dtype == POINTID_FP32 ? 4 : 8)) return false;
   for (int h = 0; h < f.halves; ++h)
     if (f.w[h].ld > kMaxPitch) return false;           // past its 32-bit steps
-  if (f.dtype == POINTID_FP32 || (f.m == 1 && f.k * f.n * f.halves > int64_t(1) << 26)) return true;
+  if (f.dtype == POINTID_FP32 || (f.m == 1 && f.k * f.n > int64_t(1) << (f.halves == 2 ? 25 : 27))) return true;
   for (int h = 0; h < f.halves; ++h)
     if (!read_in_place(f.w[h].data, f.w[h].ld, f.dtype, f.n) || f.w[h].ld != f.w[0].ld) return true;
   return false;

@@ -1,6 +1,7 @@
 // Forward products of a few rows (serving): y = x w with the weights read once, every value
 // multiplied in fp32 with that of each row.  Bound by the bytes of the weights: fp32 8192 x
-// 8192, 1 row 53 us (5.0 TB/s), 4 rows 58, 8 rows 63; bf16 gated 4096 x 12288, 1 row 46 (4.4).
+// 8192, 1 row 55 us (4.9 TB/s), 4 rows 59, 8 rows 64; gated 104, 112 and 122 (5.2 to 4.4); bf16
+// gated 4096 x 12288, 1 row 46 (4.4).
 // The inner index is split over blocks until there are about 3 a CU, as one block's reads in
 // flight do not fill the memory; the join adds their sums in order.
 #include "internal.h"
