@@ -423,8 +423,10 @@ int pointid_client_close(pointid_client c);
 
 /*
  * Layers: dense and gated layers, their gradients, and 8-bit activation
- * checkpoints (the dense part of the network of paper §2.2 as operators, for
- * refining it or trying another block in its place).  They need no classifier:
+ * checkpoints: what the dense part of the network of paper §2.2 is made of, for
+ * models of the caller's own on patches or on features of them (the classifier
+ * above neither hands out its convolution's features nor serves such a model).
+ * They need no classifier:
  * a pointid_layers holds a device and a cache of scratch buffers, which follows
  * the rules under "Temporary device memory" above; any number of host threads
  * and streams may use one at once.
@@ -434,16 +436,19 @@ int pointid_client_close(pointid_client c);
  * columns; rows need no alignment beyond their element's), x [m][k], weights
  * [k][n], biases and their gradients fp32 [n] whatever the type.  0 <= m <= 2^28,
  * 1 <= k, n <= 2^20.  Products are summed in fp32 and rounded to `dtype` once.
- * POINTID_FP32 products are those of operands cut exactly into three bf16 parts
- * each, without terms of up to 2^-24 of a product (up to 8 rows: plain fp32).
+ * POINTID_FP32 products are those of operands cut into three bf16 parts each,
+ * without terms of up to 2^-24 of a product.  The cut is exact but for values below
+ * 2^-110, which are off by up to 2^-134.  Forward calls of up to 8 rows are plain
+ * fp32 where n >= 4 and no weights' pitch passes 2^21.
  * Infinities and NaNs go through as in fp32 arithmetic, but a sum of
  * POINTID_FP32 values that itself passes the type's range may be a NaN instead of
- * an infinity.  Outputs must not overlap inputs, but `y` may be `residual` itself.  16-bit operands whose base
- * is aligned to 16 bytes and whose columns and row pitch are multiples of 8, and
- * pitches up to 2^21, save a copy.  Results are the same bits for the same
- * arguments; the order of a sum depends on the sizes.  A call that takes scratch
- * (one whose sum is split, that copies an operand, or a backward pass) refuses a
- * stream under capture.
+ * an infinity.  Outputs must not overlap inputs, but `y` may be `residual` itself.
+ * 16-bit operands whose base is aligned to 16 bytes and whose columns and row pitch
+ * are multiples of 8, and pitches up to 2^21, save a copy.  Results are the same
+ * bits for the same arguments; the order of a sum depends on the sizes, on pitches
+ * and alignment, and on which outputs a backward call is asked for.  A call that
+ * takes scratch (one whose sum is split, that copies an operand, or a backward pass)
+ * refuses a stream under capture.
  */
 typedef struct pointid_layers_s *pointid_layers;
 

@@ -1,7 +1,8 @@
 // The matrix-core products of fp32 operands: every value is the sum of three bf16 values
 // (its rounding, the remainder's rounding, and the rest: 8 + 8 + 8 bits), and a product is
 // the 6 products of parts whose orders add up to less than 3, the smallest first; what is
-// left out is at most 2^-24 of a product, its root mean square 2^-27.
+// left out is at most 2^-24 of a product, its root mean square 2^-27.  bf16 ends at 2^-133, so
+// that a value below 2^-110 is off by up to 2^-134.
 //
 // Values are read as fp32, 32 inner indices at a time, while the stage before multiplies,
 // cut in registers and written to shared memory as three planes laid out as in the 16-bit

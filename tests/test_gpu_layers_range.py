@@ -1,5 +1,6 @@
-"""GPU: gradients of fp16 layers whose values before the activation leave fp16's range
-while their products stay in it, against the definition in 64 bits.
+"""GPU: the layers at the ends of their types' ranges, against the definition in 64 bits: gradients
+of fp16 layers whose values before the activation leave fp16's range while their products
+stay in it, the largest fp16 values in 8 bits, the smallest fp32 values.
 
 Tolerances.  dz (dg, du) is rounded once, to 11 bits (2^-11 of it), after a power of two has
 brought its largest finite magnitude M to [2^14, 2^15): what falls below fp16's normal range
@@ -234,3 +235,24 @@ def test_both_sides_of_the_limit_of_two_parts(pid, layers, dtype, m, k, n):
             continue
         err = ((got.double() - want).norm() / want.norm()).item()
         assert err <= most, (err / u, most / u)
+
+
+@pytest.mark.parametrize("power", [-105, -112, -118, -124, -128])
+@pytest.mark.parametrize("form", ["forward", "dx", "dw"])
+def test_fp32_values_near_the_smallest(pid, layers, form, power):
+    """fp32 values whose last part bf16 cannot hold: off by 2^-134 each at most, and the rounding of
+    the 6 k products of parts."""
+    g = torch.Generator().manual_seed(12)
+    m, k, n = 40, 36, 68
+    left, right = torch.randn((m, k), generator=g) * 2.0 ** power, torch.randn((k, n), generator=g) * 2.0 ** 100
+    a, b = dev(left), dev(right)
+    if form == "forward":
+        y = pid.pointid_dense(layers, a, b)
+    elif form == "dx":
+        y = pid.pointid_dense_backward(layers, a, None, b.t().contiguous(), need_dw=False, need_db=False)[0]
+    else:
+        y = pid.pointid_dense_backward(layers, b, a.t().contiguous(), torch.empty((m, n), device=DEV),
+                                       need_dx=False, need_db=False)[1]
+    small = torch.full_like(left, 2.0 ** -134, dtype=torch.float64)
+    bound = left.double().abs() @ right.double().abs() * (6 * k * E) + small @ right.double().abs()
+    assert ((y.double().cpu() - left.double() @ right.double()).abs() <= bound).all()
