@@ -9,7 +9,6 @@ library's HIP kernels; if the library is not built this module fails to import.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -204,28 +203,35 @@ def _stream_ptr(stream, device=None):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
-def _stream_object(stream, device):
-    """torch's object of a stream given as one or as its handle."""
-    if not isinstance(stream, int):
-        return stream
-    return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+# the current stream's handle without the Stream object around it (2 us a call), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-_STAYS = contextlib.nullcontext()
+def _check_on(device: int, call, *args):
+    """A call that has no handle to make its device current."""
+    if torch.cuda.current_device() == device:
+        return _check(call(*args))
+    with torch.cuda.device(device):
+        return _check(call(*args))
 
 
-def _on(device: int):
-    """Makes a device current for a call that has no handle to do so."""
-    return _STAYS if torch.cuda.current_device() == device else torch.cuda.device(device)
+def _make(stream, device: int, outputs):
+    """outputs(), the tensors that a call returns, in its stream's memory: the current stream may
+    still be using what its own memory had before.  (Not called without a stream of their own:
+    0.3 us of a small call's 9.)"""
+    raw = stream if isinstance(stream, int) else stream.cuda_stream
+    if _raw_stream is not None and raw == _raw_stream(device):
+        return outputs()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return outputs()
 
 
 def _empty(shape, dtype, device, stream):
-    """An output of the memory of the call's stream: the current stream may still be using what
-    its own memory had before."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(_stream_object(stream, device)):
-        return torch.empty(shape, dtype=dtype, device=device)
+    return _make(stream, device.index, lambda: torch.empty(shape, dtype=dtype, device=device))
 
 
 def _ptr(t):
@@ -388,9 +394,8 @@ def pointid_downsample(image: torch.Tensor, ticks_per_column: int,
     _need(out, torch.float32, "out")
     if tuple(out.shape) != (W, J):
         raise ValueError(f"out must be [{W}, {J}]")
-    with _on(image.get_device()):
-        _check(lib.pointid_downsample(_ptr(image), W, T, D, _ptr(out),
-                                      _stream_ptr(stream, image.device)))
+    _check_on(image.get_device(), lib.pointid_downsample, _ptr(image), W, T, D, _ptr(out),
+              _stream_ptr(stream, image.device))
     return out
 
 
@@ -499,9 +504,8 @@ def pointid_gather(image: torch.Tensor, hits: torch.Tensor, out_dtype="fp32",
     tdt = torch.float32 if code == POINTID_FP32 else torch.int16
     if out is None:
         out = _empty((n, 48, 48), tdt, image.device, stream)
-    with _on(image.get_device()):
-        _check(lib.pointid_gather(_ptr(image), image.shape[0], image.shape[1], _ptr(hits), n,
-                                  _ptr(out), code, _stream_ptr(stream, image.device)))
+    _check_on(image.get_device(), lib.pointid_gather, _ptr(image), image.shape[0], image.shape[1], _ptr(hits), n,
+              _ptr(out), code, _stream_ptr(stream, image.device))
     return out
 
 
@@ -514,9 +518,8 @@ def pointid_gather_planes(images, hits: torch.Tensor, out_dtype="fp32",
     tdt = torch.float32 if code == POINTID_FP32 else torch.int16
     if out is None:
         out = _empty((n, 48, 48), tdt, hits.device, stream)
-    with _on(hits.get_device()):
-        _check(lib.pointid_gather_planes(arr, len(images), _ptr(hits), n, _ptr(out), code,
-                                         _stream_ptr(stream, hits.device)))
+    _check_on(hits.get_device(), lib.pointid_gather_planes, arr, len(images), _ptr(hits), n, _ptr(out), code,
+              _stream_ptr(stream, hits.device))
     return out
 
 
@@ -702,10 +705,6 @@ def pointid_layers_trim(layers: Layers, keep_bytes: int = 0) -> int:
     return int(cached.value)
 
 
-# the current stream's handle without the Stream object around it (2 us a call), where torch has it
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
 def _layer_stream(stream, device: int):
     if stream is None and _raw_stream is not None:
         return _raw_stream(device)
@@ -735,16 +734,11 @@ def _matrix(t, name, dtype, shape, device):
     return _Matrix(t.data_ptr(), pitch if rows > 1 else cols)
 
 
-def _new(like, shape, dtype, stream):
-    """_empty on the device of a tensor of the call."""
-    return like.new_empty(shape, dtype=dtype) if stream is None else _empty(shape, dtype, like.device, stream)
-
-
-def _output(t, like, name, dtype, shape, device, stream):
+def _output(t, like, name, dtype, shape, device, stream=None):
     """An output that is given, or made like a tensor of the call, and its descriptor."""
     if t is not None:
         return t, _matrix(t, name, dtype, shape, device)
-    t = _new(like, shape, dtype, stream)
+    t = like.new_empty(shape, dtype=dtype) if stream is None else _empty(shape, dtype, like.device, stream)
     return t, _Matrix(t.data_ptr(), shape[1])
 
 
@@ -821,9 +815,13 @@ def pointid_dense_backward(layers: Layers, dy: torch.Tensor, x, w: torch.Tensor,
     m, n = dy.shape
     k = w.shape[0]
     code = _activation(act)
-    dx, to_dx = _output(None, dy, "dx", dt, (m, k), dev, stream) if need_dx else (None, None)
-    dw, to_dw = _output(None, dy, "dw", dt, (k, n), dev, stream) if need_dw else (None, None)
-    db = _new(dy, (n,), torch.float32, stream) if need_db else None
+
+    def outputs():
+        return (_output(None, dy, "dx", dt, (m, k), dev) if need_dx else (None, None),
+                _output(None, dy, "dw", dt, (k, n), dev) if need_dw else (None, None),
+                dy.new_empty((n,), dtype=torch.float32) if need_db else None)
+
+    (dx, to_dx), (dw, to_dw), db = outputs() if stream is None else _make(stream, dev, outputs)
     _check(lib.pointid_dense_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dy, "dy", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(w, "w", dt, (k, n), dev)),
@@ -862,10 +860,13 @@ def pointid_gated_backward(layers: Layers, dh: torch.Tensor, x, wg: torch.Tensor
     m, n = dh.shape
     k = wg.shape[0]
     code = _activation(act)
-    dx, to_dx = _output(None, dh, "dx", dt, (m, k), dev, stream) if need_dx else (None, None)
-    (dwg, to_dwg), (dwu, to_dwu) = (_output(None, dh, name, dt, (k, n), dev, stream) if need_dw
-                                    else (None, None) for name in ("dwg", "dwu"))
-    dbg, dbu = (_new(dh, (n,), torch.float32, stream) if need_db else None for _ in range(2))
+
+    def outputs():
+        return (_output(None, dh, "dx", dt, (m, k), dev) if need_dx else (None, None),
+                *(_output(None, dh, name, dt, (k, n), dev) if need_dw else (None, None) for name in ("dwg", "dwu")),
+                *(dh.new_empty((n,), dtype=torch.float32) if need_db else None for _ in range(2)))
+
+    (dx, to_dx), (dwg, to_dwg), (dwu, to_dwu), dbg, dbu = outputs() if stream is None else _make(stream, dev, outputs)
     _check(lib.pointid_gated_backward(
         layers.raw, _LAYER_TYPES[dt], code, m, k, n, _ref(_matrix(dh, "dh", dt, (m, n), dev)),
         _ref(_kept(x, "x", dt, (m, k), dev)), _ref(_matrix(wg, "wg", dt, (k, n), dev)),
@@ -879,16 +880,21 @@ def pointid_checkpoint_save(x: torch.Tensor, out: Checkpoint | None = None, stre
     dt, dev = _layer_type(x, "x"), x.get_device()
     m, n = x.shape
     a = _matrix(x, "x", dt, (m, n), dev)
+    if torch.cuda.current_device() != dev:              # there is no handle to make it so
+        with torch.cuda.device(dev):
+            return pointid_checkpoint_save(x, out, stream)
     if out is None:
         out = Checkpoint.__new__(Checkpoint)
-        out.codes = _new(x, (m, n), torch.uint8, stream)
-        out.exponents = _new(x, (m, -(-n // 32)), torch.uint8, stream)
+        if stream is None:
+            out.codes = x.new_empty((m, n), dtype=torch.uint8)
+            out.exponents = out.codes.new_empty((m, -(-n // 32)))
+        else:
+            out.codes, out.exponents = (_empty((m, c), torch.uint8, x.device, stream) for c in (n, -(-n // 32)))
         packed = _Packed(out.codes.data_ptr(), out.exponents.data_ptr())
     else:
         packed = _kept(out, "out", dt, (m, n), dev).packed
-    with _on(dev):
-        _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(packed),
-                                           _layer_stream(stream, dev)))
+    _check(lib.pointid_checkpoint_save(_LAYER_TYPES[dt], m, n, ctypes.byref(a), ctypes.byref(packed),
+                                       _layer_stream(stream, dev)))
     return out
 
 
@@ -900,8 +906,10 @@ def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.T
     if dt not in _LAYER_TYPES:
         raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dt}")
     kept = _kept(saved, "saved", dt, (m, n), dev)
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return pointid_checkpoint_load(saved, dtype, out, stream)
     out, a = _output(out, saved.codes, "out", dt, (m, n), dev, stream)
-    with _on(dev):
-        _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
-                                           _layer_stream(stream, dev)))
+    _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
+                                       _layer_stream(stream, dev)))
     return out
