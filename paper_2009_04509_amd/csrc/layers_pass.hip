@@ -131,9 +131,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t (&waves)[4]) 
 // dz = dy act'(z) (dg, du) reaches past fp16's largest value, and below its smallest, where
 // the products are in range: it is kept times a power of two, which this pass is for.  It
 // computes what the gradient pass does and leaves the largest finite magnitude of each block
-// (the gradient pass takes the largest of these, so that no word is shared and cleared).  Bound
-// by the bytes: a gated 8192 x 8192 75-85 us of 1,930 (about 5 TB/s read), from 8 bits 70-80;
-// 1693 x 2048 8, most of it the launch and the next pass's wait for the maxima.
+// (the gradient pass takes the largest of these, so that no word is shared and cleared).  In the
+// trace a gated 8192 x 8192 takes 90 us (4.5 TB/s read), from 8 bits 78-87, 1693 x 2048 7; twice
+// the blocks gained nothing.  A call of those sizes is 70-85 and 8 us longer by it.
 template <int kHalves, bool kPacked>
 __global__ void __launch_bounds__(256) grad_max_kernel(GradArgs a) {
   __shared__ uint32_t waves[4];
