@@ -2,25 +2,13 @@
 // choice of kernels, scratch, launch sequencing.  Every call only enqueues work.
 #include "layers.h"
 
-#include <cstring>
-#include <exception>
-#include <new>
-
-#include "call.h"
-#include "internal.h"
+#include "layers_call.h"
 
 using namespace pointid;
-
-struct pointid_layers_s {
-  int device;
-  int cus;
-  ScratchPool scratch;
-};
 
 namespace {
 
 constexpr int64_t kMaxSide = int64_t(1) << 20;         // k and n
-constexpr int64_t kMaxRows = int64_t(1) << 28;         // m (a launch has fewer than 2^32 threads)
 constexpr int64_t kMaxPitch = int64_t(1) << 21;        // of an operand that the products read in place
 
 // dz of up to this many values is kept in two 16-bit parts.  Rounded once, it makes the error of
@@ -33,24 +21,6 @@ constexpr int64_t kMaxPitch = int64_t(1) << 21;        // of an operand that the
 // 4096 x 12288 147 and 220.
 constexpr int64_t kTwoPartValues = int64_t(1) << 16;
 
-int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-int size_of(int dtype) { return dtype == POINTID_FP32 ? 4 : 2; }
-bool rows_in_16(const void* p, int64_t ld, int dtype) {
-  return aligned16(p) && ld % (dtype == POINTID_FP32 ? 4 : 8) == 0;
-}
-
-// No exception crosses the ABI.
-template <class F>
-int guarded(F&& f) noexcept {
-  try {
-    return f();
-  } catch (const std::bad_alloc&) {
-    return POINTID_ENOMEM;
-  } catch (...) {
-    return POINTID_EHIP;
-  }
-}
-
 // ---- argument checks
 
 int check_call(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64_t n) {
@@ -61,21 +31,6 @@ int check_call(pointid_layers l, int dtype, int act, int64_t m, int64_t k, int64
   if (m < 0 || m > kMaxRows) return set_error(POINTID_EINVAL, "m must be in [0, 2^28]");
   if (k < 1 || k > kMaxSide || n < 1 || n > kMaxSide)
     return set_error(POINTID_EINVAL, "k and n must be in [1, 2^20]");
-  return POINTID_OK;
-}
-
-// A matrix of the call; `may_miss`: NULL (or NULL data) is allowed.
-int check_matrix(const pointid_matrix* a, const char* name, int dtype, int64_t rows, int64_t cols, bool may_miss = false) {
-  if (!a || !a->data) {
-    if (may_miss || rows == 0) return POINTID_OK;
-    return set_error(POINTID_EINVAL, std::string(name) + " is NULL");
-  }
-  if (reinterpret_cast<uintptr_t>(a->data) % size_of(dtype))
-    return set_error(POINTID_EINVAL, std::string(name) + " is not aligned to its elements");
-  if (rows > 1 && a->ld < cols)
-    return set_error(POINTID_EINVAL, std::string(name) + ": row pitch below its columns");
-  if (rows > 1 && a->ld > INT64_MAX / 8 / rows)
-    return set_error(POINTID_EINVAL, std::string(name) + ": row pitch out of range");
   return POINTID_OK;
 }
 
@@ -98,19 +53,6 @@ int check_kept(const pointid_kept* a, const char* name, int dtype, int64_t rows,
   return check_packed(a->packed, name);
 }
 
-int check_floats(const float* p, const char* name) {
-  if (p && reinterpret_cast<uintptr_t>(p) % 4)
-    return set_error(POINTID_EINVAL, std::string(name) + " is not aligned to its elements");
-  return POINTID_OK;
-}
-
-// The pitch of one row is never used: any value stands for its columns.
-pointid_matrix matrix_of(const pointid_matrix* a, int64_t rows, int64_t cols) {
-  pointid_matrix r = {nullptr, cols};
-  if (a && a->data) r = *a;
-  if (rows <= 1 || !r.data) r.ld = round_up(cols, 8);
-  return r;
-}
 Kept kept_of(const pointid_kept* a, int64_t rows, int64_t cols) {
   Kept k;
   std::memset(&k, 0, sizeof(k));
@@ -121,63 +63,6 @@ Kept kept_of(const pointid_kept* a, int64_t rows, int64_t cols) {
   if (!k.matrix) k.packed = {a->packed.codes, a->packed.exponents};
   return k;
 }
-
-// ---- a call: scratch pieces sized before any is taken, launches with their timer
-
-class Call {
- public:
-  Call(pointid_layers l, hipStream_t stream) : ws_(&l->scratch, stream), stream_(stream) {}
-
-  // a piece of the call's scratch, taken by reserve()
-  template <class T>
-  void want(T** out, size_t bytes) {
-    if (count_ < kMaxPieces) pieces_[count_++] = {reinterpret_cast<void**>(out), bytes};
-  }
-  int reserve() {
-    size_t total = 0;
-    for (int i = 0; i < count_; ++i) total += pad256(pieces_[i].bytes);
-    if (total == 0) return POINTID_OK;
-    // a graph would use the buffer again whenever it is replayed, past the cache's care
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(stream_, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
-      return set_error(POINTID_EINVAL, "the call takes scratch, which a captured stream cannot");
-    hipError_t e = ws_.reserve(total);
-    if (e != hipSuccess) return hip_fail(e, "scratch buffer");
-    for (int i = 0; i < count_; ++i) {
-      e = ws_.get(pieces_[i].bytes, pieces_[i].out);
-      if (e != hipSuccess) return hip_fail(e, "workspace (layers)");
-    }
-    scratch_ = true;
-    return POINTID_OK;
-  }
-  // f: the launch; `last`: of the call (it also records the scratch's completion)
-  template <class F>
-  int run(const char* name, bool last, F&& f) {
-    KernelTimer kt(name, stream_);
-    hipError_t e;
-    if (last && scratch_) {
-      EndsCall end(ws_);
-      e = f();
-      end.launched(e);
-    } else {
-      e = f();
-    }
-    return e == hipSuccess ? POINTID_OK : hip_fail(e, name);
-  }
-  hipStream_t stream() const { return stream_; }
-
- private:
-  static constexpr int kMaxPieces = 16;
-  struct Piece {
-    void** out;
-    size_t bytes;
-  };
-  Workspace ws_;
-  hipStream_t stream_;
-  Piece pieces_[kMaxPieces];
-  int count_ = 0;
-  bool scratch_ = false;
-};
 
 // A matrix as the products read it: 16-bit planes with aligned rows, zero past the columns
 // up to a whole piece of 8, or fp32 values.
@@ -572,12 +457,6 @@ int check_checkpoint_call(int dtype, int64_t rows, int64_t cols, const pointid_m
   if (!c) return set_error(POINTID_EINVAL, "the checkpoint is NULL");
   return check_packed(*c, "the checkpoint");
 }
-
-#define TRY(call)                            \
-  do {                                       \
-    const int rc_ = (call);                  \
-    if (rc_ != POINTID_OK) return rc_;       \
-  } while (0)
 
 }  // namespace
 
