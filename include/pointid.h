@@ -565,6 +565,162 @@ int pointid_checkpoint_load(int dtype, int64_t rows, int64_t cols, const pointid
                             const pointid_matrix *out, void *stream);
 
 /*
+ * Around the layers: dropout, the norms at the joint of two residual blocks, and log
+ * probabilities as a loss or an answer, with their gradients: what the layers above need
+ * beside them in a training step, and the last two when a model is served.  They take the
+ * layers' handle and its conventions: matrices of the call's `dtype` with any row pitch,
+ * parameters and statistics fp32, 0 <= m <= 2^28 (m == 0: a no-op, but that gradients of
+ * parameters are set to 0), 1 <= n <= 2^20, sums in fp32 in a fixed order, results rounded
+ * to `dtype` once, the same bits for the same arguments.  Each row's results depend on that
+ * row alone, but for gradients of parameters.
+ *
+ * Calls that may take scratch have `scratch`, memory of the caller's of at least
+ * `scratch_bytes` = pointid_..._scratch() bytes, aligned to 256, or NULL (and 0) for the
+ * handle's cache.  Under stream capture it has to be the caller's, used by nothing else while
+ * the graph may run.  The other calls can be captured as they are.
+ */
+
+/*
+ * Dropout: each element is kept with probability 1 - p and divided by it, else 0 (whatever it
+ * was).  p is rounded to a multiple T / 65536.  The mask is never stored: element (row, col) is
+ * kept if its 16 random bits are at least T, and these are a function of `seed`, the offset,
+ * row and col alone: of the words of Philox4x32-10 for the counter (col / 8, row, offset's
+ * lower 32 bits, its upper) and the key (seed's lower, its upper), word (col % 8) / 2, its
+ * lower half for even columns.  The offset is `offset` plus, where `step` is given, the value
+ * in that device memory, read when the call runs: a captured step draws a new mask each time
+ * it is replayed if the graph counts it up.
+ */
+typedef struct {
+    double p;                   /* in [0, 1]; 0: no dropout */
+    uint64_t seed, offset;
+    const uint64_t *step;       /* device memory, 8-byte aligned, or NULL */
+} pointid_drop;
+
+/*
+ * y = drop(x) + residual.  The gradient of x is the same call on dy, without a residual (whose
+ * gradient is dy).
+ *   residual  optional (NULL)
+ *   y         may be x or residual itself
+ * Errors: EINVAL (NULL l, drop, x or y; p outside [0, 1]; a size, pitch or alignment out of
+ * range), EUNSUPPORTED (dtype), EHIP.
+ */
+int pointid_dropout(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix *x,
+                    const pointid_drop *drop, const pointid_matrix *residual, const pointid_matrix *y,
+                    void *stream);
+
+/* Norms of rows: u w + b with
+ *   RMS    u = x / sqrt(mean(x^2) + eps)
+ *   LAYER  u = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps)
+ * The squares are summed in fp32: rows whose sum of squares passes its range become 0. */
+enum {
+    POINTID_NORM_NONE = 0,
+    POINTID_NORM_RMS = 1,
+    POINTID_NORM_LAYER = 2
+};
+typedef struct {
+    int32_t kind;
+    float eps;                  /* >= 0 */
+    const float *weight;        /* w [n], or NULL: ones */
+    const float *bias;          /* b [n], or NULL: zeros */
+} pointid_norm_of;
+
+/* A residual block's end: its output and how it is added to the block's input x,
+ * scale x + gate * drop(norm(out)). */
+typedef struct {
+    pointid_matrix out;         /* [m][n] */
+    pointid_norm_of norm;       /* the norm after the block, or POINTID_NORM_NONE */
+    const float *gate;          /* [n], or NULL: ones */
+    float scale;                /* of x, finite */
+    pointid_drop drop;          /* p == 0: none */
+} pointid_block;
+
+/*
+ * The joint of two residual blocks in one pass:
+ *   total = scale x + gate * drop(norm_after(out))    (without a block: x itself)
+ *   h     = norm(total)                               the next block's input
+ * h is made of the unrounded total.
+ *   norm   the norm before the next block, or NULL (h is NULL then)
+ *   block  or NULL: h = norm(x)
+ *   total  optional, with a block; it may be x itself
+ *   stats  optional fp32 [m][4], 16-byte aligned: mean and 1 / deviation of the norm after the
+ *          block and of the one before the next (0 and 1 where there is none, or no mean), for
+ *          the backward pass
+ * Errors: EINVAL (NULL l, x, neither total nor h; h without norm or norm without h; total
+ * without block; a kind, eps, p, scale, size, pitch or alignment out of range), EUNSUPPORTED
+ * (dtype), EHIP.
+ */
+int pointid_norm(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix *x,
+                 const pointid_norm_of *norm, const pointid_block *block, const pointid_matrix *total,
+                 const pointid_matrix *h, float *stats, void *stream);
+
+/* Results of pointid_norm_backward, each optional (NULL data, NULL). */
+typedef struct {
+    pointid_matrix dx;          /* [m][n]; may be dtotal itself */
+    pointid_matrix dout;        /* [m][n], with a block */
+    float *dweight, *dbias;     /* [n], of the norm before the next block */
+    float *dblock_weight, *dblock_bias, *dgate;     /* [n], with a block */
+} pointid_norm_grads;
+
+/*
+ * Gradients of pointid_norm from dh and dtotal (what reaches total besides h; NULL: nothing):
+ *   u    = (total - mean) r,  e = dh w,  d = dtotal + r (e - u mean(e u) - [LAYER] mean(e))
+ *   dx   = scale d,  dw = sum dh u,  db = sum dh
+ *   q    = gate * drop(d),  dgate = sum drop(d) norm_after(out)
+ *   dout = the norm after the block's gradient from q, and its parameters', as above
+ * The means are over a row, the sums over the rows, in a fixed order.
+ *   norm, block  as in the forward call (block->out is needed for a norm after the block and
+ *                for dgate)
+ *   dh           needed with norm;  total, stats: those of the forward call (without a block,
+ *                total is x), needed with a norm (total with the one before the next block)
+ * m == 0 sets the parameters' gradients to 0.
+ * Errors: EINVAL (NULL l or grads; an input that is needed; gradients of what the call has not;
+ * scratch too small or not aligned; else as pointid_norm), EUNSUPPORTED, ENOMEM, EHIP.
+ */
+int pointid_norm_backward(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix *dh,
+                          const pointid_matrix *total, const float *stats, const pointid_norm_of *norm,
+                          const pointid_block *block, const pointid_matrix *dtotal,
+                          const pointid_norm_grads *grads, void *scratch, uint64_t scratch_bytes, void *stream);
+/* Scratch that any such call of m rows and n columns fits in (0 for NULL l or sizes out of range). */
+uint64_t pointid_norm_backward_scratch(pointid_layers l, int64_t m, int64_t n);
+
+/*
+ * Log probabilities of the columns of each row of logits, z = scale logits:
+ *   lse     = ln sum_j e^z_j           logp = z_target - lse
+ *   entropy = - sum_j p_j ln p_j       p_j = e^(z_j - lse)
+ *   top     the `top` largest logits' columns in falling order, the lowest column first among
+ *           equals, and their log probabilities
+ *   scale     > 0, finite (one over a temperature)
+ *   targets   device int32 [m], optional; a target outside [0, n) is none: logp is 0
+ *   logp, lse, entropy  optional fp32 [m]; logp needs targets
+ *   top       0..64, at most n; top_ids int32 [m][top], top_logp fp32 [m][top]
+ * A logit of minus infinity is a column that cannot be: p is 0 there, ln p minus infinity.  In a
+ * row of nothing else lse and every ln p are minus infinity, entropy is 0 and the top columns are
+ * the first ones.  Plus infinity or a NaN make a row's lse, logp, entropy and top_logp NaN; a
+ * NaN's place among the top columns is that of minus infinity.
+ * Errors: EINVAL (NULL l, logits or outputs; scale, top, a size, pitch or alignment out of range;
+ * scratch too small or not aligned), EUNSUPPORTED (dtype), ENOMEM, EHIP.
+ */
+int pointid_logprobs(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix *logits, float scale,
+                     const int32_t *targets, float *logp, float *lse, float *entropy, int32_t top,
+                     int32_t *top_ids, float *top_logp, void *scratch, uint64_t scratch_bytes, void *stream);
+/* Scratch that such a call of m rows and n columns fits in; 0 where it takes none. */
+uint64_t pointid_logprobs_scratch(pointid_layers l, int64_t m, int64_t n, int32_t top);
+
+/*
+ * The logits' gradient from those of logp, lse and entropy (fp32 [m], each optional, at least
+ * one given; dlogp of a row without a target is not used):
+ *   dlogits_j = scale (dlogp ([j = target] - p_j) + dlse p_j - dentropy p_j (ln p_j + entropy))
+ *   lse       as the forward call left it; entropy too, needed with dentropy
+ *   targets   needed with dlogp
+ *   dlogits   may be logits itself
+ * 0 in rows whose lse is minus infinity.  Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
+ */
+int pointid_logprobs_backward(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix *logits,
+                              float scale, const float *lse, const int32_t *targets, const float *dlogp,
+                              const float *entropy, const float *dentropy, const float *dlse,
+                              const pointid_matrix *dlogits, void *stream);
+
+/*
  * Kernel timing for measurement tools (not needed for classification).  While
  * enabled (process-wide), every kernel a classification or hit-finding call
  * launches carries HIP events on its own dispatch (hipExtLaunchKernel), on the

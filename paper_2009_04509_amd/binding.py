@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -71,6 +72,29 @@ class _Packed(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("exponents", ctypes.c_void_p)]
 
 
+class _Drop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("step", ctypes.c_void_p)]
+
+
+class _NormOf(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p)]
+
+
+class _Block(ctypes.Structure):
+    """pointid_block, its members' members one after another (they stand so)"""
+    _fields_ = _Matrix._fields_ + _NormOf._fields_ + [("gate", ctypes.c_void_p), ("scale", ctypes.c_float)] + \
+        _Drop._fields_
+
+
+class _NormGrads(ctypes.Structure):
+    """pointid_norm_grads, likewise"""
+    _fields_ = [("dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64), ("dout", ctypes.c_void_p),
+                ("ld_dout", ctypes.c_int64)] + [(name, ctypes.c_void_p) for name in (
+                    "dweight", "dbias", "dblock_weight", "dblock_bias", "dgate")]
+
+
 class _Kept(ctypes.Structure):
     _fields_ = [("full", _Matrix), ("packed", _Packed)]
 
@@ -81,7 +105,7 @@ def _load():
             f"{LIB_PATH} is not built; run `python -m paper_2009_04509_amd.build` "
             "(or __graft_entry__.build()) first")
     lib = ctypes.CDLL(LIB_PATH)
-    vp, i32, i64, cint = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_int
+    vp, i32, i64, u64, cint = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_int
     mat, kept = ctypes.POINTER(_Matrix), ctypes.POINTER(_Kept)
     sig = {
         "pointid_create": (cint, [ctypes.POINTER(_Weights), cint, cint, ctypes.POINTER(vp)]),
@@ -127,6 +151,17 @@ def _load():
                                           mat, mat, mat, vp, vp, vp]),
         "pointid_checkpoint_save": (cint, [cint, i64, i64, mat, ctypes.POINTER(_Packed), vp]),
         "pointid_checkpoint_load": (cint, [cint, i64, i64, ctypes.POINTER(_Packed), mat, vp]),
+        "pointid_dropout": (cint, [vp, cint, i64, i64, mat, ctypes.POINTER(_Drop), mat, mat, vp]),
+        "pointid_norm": (cint, [vp, cint, i64, i64, mat, ctypes.POINTER(_NormOf), ctypes.POINTER(_Block), mat, mat,
+                                vp, vp]),
+        "pointid_norm_backward": (cint, [vp, cint, i64, i64, mat, mat, vp, ctypes.POINTER(_NormOf),
+                                         ctypes.POINTER(_Block), mat, ctypes.POINTER(_NormGrads), vp, u64, vp]),
+        "pointid_norm_backward_scratch": (u64, [vp, i64, i64]),
+        "pointid_logprobs": (cint, [vp, cint, i64, i64, mat, ctypes.c_float, vp, vp, vp, vp, i32, vp, vp, vp, u64,
+                                    vp]),
+        "pointid_logprobs_scratch": (u64, [vp, i64, i64, i32]),
+        "pointid_logprobs_backward": (cint, [vp, cint, i64, i64, mat, ctypes.c_float, vp, vp, vp, vp, vp, vp, mat,
+                                             vp]),
         "pointid_timing_enable": (cint, [cint]),
         "pointid_timing_reset": (cint, []),
         "pointid_timing_query": (cint, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
@@ -154,7 +189,9 @@ EXPORTED = ("pointid_create", "pointid_destroy", "pointid_precision", "pointid_t
             "pointid_client_connect", "pointid_client_classify", "pointid_client_classify_patches",
             "pointid_client_close", "pointid_layers_create", "pointid_layers_destroy", "pointid_layers_trim",
             "pointid_dense", "pointid_dense_backward", "pointid_gated", "pointid_gated_backward",
-            "pointid_checkpoint_save", "pointid_checkpoint_load", "pointid_timing_enable", "pointid_timing_reset",
+            "pointid_checkpoint_save", "pointid_checkpoint_load",
+            "pointid_dropout", "pointid_norm", "pointid_norm_backward", "pointid_norm_backward_scratch",
+            "pointid_logprobs", "pointid_logprobs_scratch", "pointid_logprobs_backward", "pointid_timing_enable", "pointid_timing_reset",
             "pointid_timing_query", "pointid_last_error", "pointid_version")
 
 
@@ -629,6 +666,7 @@ class Client:
 
 # ---- layers
 
+NORMS = {"rms": 1, "layer": 2}
 _LAYER_TYPES = {torch.float32: POINTID_FP32, torch.bfloat16: POINTID_BF16, torch.float16: POINTID_FP16}
 
 
@@ -913,3 +951,247 @@ def pointid_checkpoint_load(saved: Checkpoint, dtype=torch.float32, out: torch.T
     _check(lib.pointid_checkpoint_load(_LAYER_TYPES[dt], m, n, ctypes.byref(kept.packed), ctypes.byref(a),
                                        _layer_stream(stream, dev)))
     return out
+
+
+# ---- around the layers
+
+class Drop(NamedTuple):
+    """A dropout: probability, and what its mask is made of (``step``: an int64 or uint64 device
+    value that is added to the offset when the call runs)."""
+    p: float
+    seed: int
+    offset: int = 0
+    step: torch.Tensor | None = None
+
+
+class Norm(NamedTuple):
+    """A norm of rows, "rms" or "layer", with its parameters (float32 [n])."""
+    kind: str = "rms"
+    weight: torch.Tensor | None = None
+    bias: torch.Tensor | None = None
+    eps: float = 1e-5
+
+
+class Block(NamedTuple):
+    """A residual block's end: its output, and how that is added to the block's input x,
+    scale x + gate * drop(norm(out)); gate float32 [n]."""
+    out: torch.Tensor
+    norm: Norm | None = None
+    gate: torch.Tensor | None = None
+    scale: float = 1.0
+    drop: Drop | None = None
+
+
+class Normed(NamedTuple):
+    h: torch.Tensor | None
+    total: torch.Tensor | None
+    stats: torch.Tensor | None
+
+
+class NormGradients(NamedTuple):
+    dx: torch.Tensor | None
+    dout: torch.Tensor | None
+    dweight: torch.Tensor | None
+    dbias: torch.Tensor | None
+    dblock_weight: torch.Tensor | None
+    dblock_bias: torch.Tensor | None
+    dgate: torch.Tensor | None
+
+
+class LogProbs(NamedTuple):
+    logp: torch.Tensor | None
+    lse: torch.Tensor
+    entropy: torch.Tensor | None
+    top_ids: torch.Tensor | None
+    top_logp: torch.Tensor | None
+
+
+def _drop(d, device):
+    """The fields of a dropout."""
+    if d is None:
+        return 0.0, 0, 0, None
+    if not 0.0 <= d.p <= 1.0:
+        raise ValueError("p must be in [0, 1]")
+    if not (0 <= d.seed < 1 << 64 and 0 <= d.offset < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    step = d.step
+    if step is not None:
+        if not isinstance(step, torch.Tensor) or step.dtype not in (torch.int64, torch.uint64):
+            raise TypeError("step must be a torch tensor of int64 or uint64")
+        if step.numel() != 1 or step.get_device() != device:
+            raise ValueError(f"step must be one value on cuda:{device}")
+        step = step.data_ptr()
+    return d.p, d.seed, d.offset, step
+
+
+def _norm(norm, name, n, device):
+    """The fields of a norm."""
+    if norm is None:
+        return 0, 0.0, None, None
+    if norm.kind not in NORMS:
+        raise ValueError(f"{name}.kind must be one of {', '.join(NORMS)}")
+    return (NORMS[norm.kind], norm.eps, _bias(norm.weight, f"{name}.weight", n, device),
+            _bias(norm.bias, f"{name}.bias", n, device))
+
+
+def _block(block, dt, m, n, device):
+    if block is None:
+        return None
+    out = _matrix(block.out, "block.out", dt, (m, n), device)
+    return _Block(out.data, out.ld, *_norm(block.norm, "block.norm", n, device),
+                  _bias(block.gate, "block.gate", n, device), block.scale, *_drop(block.drop, device))
+
+
+def _vector(t, name, dtype, m, device):
+    """The address of a vector of the rows, or None."""
+    if t is None:
+        return None
+    _need(t, dtype, name, device)
+    if t.dim() != 1 or t.shape[0] != m:
+        raise ValueError(f"{name} must be [{m}]")
+    return t.data_ptr()
+
+
+def _scratch(size, layers, like, *sizes):
+    """(the memory, its bytes) of a call: under capture the graph's own, else the handle's."""
+    if not torch.cuda.is_current_stream_capturing():
+        return None, 0
+    n = size(layers.raw, *sizes)
+    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n else (None, 0)
+
+
+def pointid_dropout(layers: Layers, x: torch.Tensor, drop: Drop, residual: torch.Tensor | None = None,
+                    y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """y [m][n] = drop(x) + residual; its gradient by x is pointid_dropout(dy, drop).
+
+    ``y`` may be x or residual itself."""
+    dt, dev = _layer_type(x, "x"), layers.device
+    shape = x.shape
+    a, r = _matrix(x, "x", dt, shape, dev), _matrix(residual, "residual", dt, shape, dev)
+    d = _Drop(*_drop(drop, dev))
+    y, out = _output(y, x, "y", dt, shape, dev, stream)
+    _check(lib.pointid_dropout(layers.raw, _LAYER_TYPES[dt], shape[0], shape[1], a, d, r, out,
+                               _layer_stream(stream, dev)))
+    return y
+
+
+def pointid_norm(layers: Layers, x: torch.Tensor, norm: Norm | None = None, block: Block | None = None,
+                 keep: bool = False, total: torch.Tensor | None = None, h: torch.Tensor | None = None,
+                 stream=None) -> Normed:
+    """The joint of two residual blocks: total = scale x + gate * drop(block.norm(block.out)), where there is a
+    block, and h = norm(total), where there is a norm.
+
+    Returns (h, total, stats), None for what there is not: total without a block is x itself; with
+    ``keep`` the rows' statistics [m][4] are there for the backward pass.  ``total`` may be x itself."""
+    dt, dev = _layer_type(x, "x"), layers.device
+    m, n = shape = x.shape
+    if norm is None and block is None:
+        raise ValueError("neither norm nor block is given")
+    if (h is not None and norm is None) or (total is not None and block is None):
+        raise ValueError("h needs norm and total needs block")
+    a = _matrix(x, "x", dt, shape, dev)
+    after, end = _NormOf(*_norm(norm, "norm", n, dev)) if norm is not None else None, _block(block, dt, m, n, dev)
+
+    def outputs():
+        return (_output(total, x, "total", dt, shape, dev) if block is not None else (None, None),
+                _output(h, x, "h", dt, shape, dev) if norm is not None else (None, None),
+                x.new_empty((m, 4), dtype=torch.float32) if keep else None)
+
+    (total, to_total), (h, to_h), stats = outputs() if stream is None else _make(stream, dev, outputs)
+    _check(lib.pointid_norm(layers.raw, _LAYER_TYPES[dt], m, n, a, after, end, to_total, to_h,
+                            stats.data_ptr() if keep else None, _layer_stream(stream, dev)))
+    return Normed(h, total, stats)
+
+
+def pointid_norm_backward(layers: Layers, dh: torch.Tensor | None, total: torch.Tensor | None,
+                          stats: torch.Tensor | None, norm: Norm | None = None, block: Block | None = None,
+                          dtotal: torch.Tensor | None = None, need_dx: bool = True, need_dout: bool = True,
+                          need_params: bool = True, dx: torch.Tensor | None = None, stream=None) -> NormGradients:
+    """Gradients of pointid_norm from those of h and total (``dtotal``), with the total (without a
+    block: x) and the stats of the forward call, and its norm and block.
+
+    Parameters' gradients are float32 [n], of those that are given.  ``dx`` may be dtotal itself."""
+    given = dh if norm is not None else dtotal
+    dt, dev = _layer_type(given, "dh" if norm is not None else "dtotal"), layers.device
+    m, n = shape = given.shape
+    a, b = (_matrix(dh, "dh", dt, shape, dev), _matrix(total, "total", dt, shape, dev)) if norm is not None else (None, None)
+    if norm is not None and b is None:
+        raise ValueError("total is needed with norm")
+    c = _matrix(dtotal, "dtotal", dt, shape, dev)
+    before, end = _NormOf(*_norm(norm, "norm", n, dev)) if norm is not None else None, _block(block, dt, m, n, dev)
+    after = block.norm if block is not None else None
+    if norm is not None or after is not None:
+        _need(stats, torch.float32, "stats", dev)
+        if tuple(stats.shape) != (m, 4):
+            raise ValueError(f"stats must be [{m}, 4]")
+    else:
+        stats = None
+    params = [norm and norm.weight, norm and norm.bias, after and after.weight, after and after.bias,
+              block and block.gate] if need_params else [None] * 5
+    params = [p is not None for p in params]
+
+    def outputs():
+        return (_output(dx, given, "dx", dt, shape, dev) if need_dx or dx is not None else (None, None),
+                _output(None, given, "dout", dt, shape, dev) if need_dout and block is not None else (None, None),
+                [given.new_empty((n,), dtype=torch.float32) if p else None for p in params],
+                _scratch(lib.pointid_norm_backward_scratch, layers, given, m, n))
+
+    (dx, to_dx), (dout, to_dout), sums, (scratch, size) = outputs() if stream is None else _make(stream, dev, outputs)
+    grads = _NormGrads(to_dx and to_dx.data, to_dx.ld if to_dx else 0, to_dout and to_dout.data,
+                       to_dout.ld if to_dout else 0, *(p.data_ptr() if p is not None else None for p in sums))
+    _check(lib.pointid_norm_backward(layers.raw, _LAYER_TYPES[dt], m, n, a, b,
+                                     stats.data_ptr() if stats is not None else None, before, end, c, grads,
+                                     scratch.data_ptr() if scratch is not None else None, size,
+                                     _layer_stream(stream, dev)))
+    return NormGradients(dx, dout, *sums)
+
+
+def pointid_logprobs(layers: Layers, logits: torch.Tensor, targets: torch.Tensor | None = None, scale: float = 1.0,
+                     entropy: bool = False, top: int = 0, stream=None) -> LogProbs:
+    """Log probabilities of z = scale logits [m][n]: (logp, lse, entropy, top_ids, top_logp), float32 [m]
+    (int32 and float32 [m][top]), None for what is not asked for.
+
+    logp: the targets' (int32 [m]; 0 for a target outside [0, n)); top: the most likely columns
+    in falling order, the lowest first among equals."""
+    dt, dev = _layer_type(logits, "logits"), layers.device
+    m, n = logits.shape
+    a = _matrix(logits, "logits", dt, (m, n), dev)
+    at = _vector(targets, "targets", torch.int32, m, dev)
+    if not 0 <= top <= min(64, n):
+        raise ValueError("top must be in [0, 64] and at most n")
+
+    def outputs():
+        values = logits.new_empty((1 + (at is not None) + bool(entropy), m), dtype=torch.float32).unbind()
+        best = logits.new_empty((2, m, top), dtype=torch.int32).unbind() if top else None
+        return values, best, _scratch(lib.pointid_logprobs_scratch, layers, logits, m, n, top)
+
+    values, best, (scratch, size) = outputs() if stream is None else _make(stream, dev, outputs)
+    lse, h, logp = values[0], values[1] if entropy else None, values[-1] if at is not None else None
+    ids, best = (best[0], best[1].view(torch.float32)) if top else (None, None)
+    _check(lib.pointid_logprobs(layers.raw, _LAYER_TYPES[dt], m, n, a, scale, at,
+                                logp.data_ptr() if at is not None else None, lse.data_ptr(),
+                                h.data_ptr() if entropy else None, top, ids.data_ptr() if top else None,
+                                best.data_ptr() if top else None,
+                                scratch.data_ptr() if scratch is not None else None, size,
+                                _layer_stream(stream, dev)))
+    return LogProbs(logp, lse, h, ids, best)
+
+
+def pointid_logprobs_backward(layers: Layers, logits: torch.Tensor, lse: torch.Tensor,
+                              targets: torch.Tensor | None = None, dlogp: torch.Tensor | None = None,
+                              entropy: torch.Tensor | None = None, dentropy: torch.Tensor | None = None,
+                              dlse: torch.Tensor | None = None, scale: float = 1.0,
+                              dlogits: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The logits' gradient from those of logp, entropy and lse (float32 [m]), with the lse (and,
+    for dentropy, the entropy) of the forward call.  ``dlogits`` may be logits itself."""
+    dt, dev = _layer_type(logits, "logits"), layers.device
+    m, n = shape = logits.shape
+    a = _matrix(logits, "logits", dt, shape, dev)
+    f32 = torch.float32
+    vectors = [_vector(lse, "lse", f32, m, dev), _vector(targets, "targets", torch.int32, m, dev),
+               _vector(dlogp, "dlogp", f32, m, dev), _vector(entropy, "entropy", f32, m, dev),
+               _vector(dentropy, "dentropy", f32, m, dev), _vector(dlse, "dlse", f32, m, dev)]
+    dlogits, out = _output(dlogits, logits, "dlogits", dt, shape, dev, stream)
+    _check(lib.pointid_logprobs_backward(layers.raw, _LAYER_TYPES[dt], m, n, a, scale, *vectors, out,
+                                         _layer_stream(stream, dev)))
+    return dlogits

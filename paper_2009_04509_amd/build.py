@@ -29,8 +29,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpointid.so")
 
 SOURCES = ["layers_rows.hip", "layers_mm_bf16.hip", "layers_mm_fp16.hip", "layers_mm_f32.hip", "api.hip", "batcher.hip", "gather.hip", "conv_fc1_16.hip",
-           "conv_fc1_8.hip", "conv_fc1_f32.hip", "hits.hip", "layers.hip", "layers_pass.hip",
-           "pack.hip", "server.hip", "tail.hip"]
+           "conv_fc1_8.hip", "conv_fc1_f32.hip", "dropout.hip", "hits.hip", "layers.hip",
+           "layers_pass.hip", "logprobs.hip", "norm.hip", "norm_call.hip", "pack.hip", "server.hip", "tail.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

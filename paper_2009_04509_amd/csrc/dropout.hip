@@ -1,0 +1,46 @@
+// Dropout: y = drop(x) + residual, one pass (see random.h).
+#include "internal.h"
+#include "layers_end.h"
+#include "norm.h"
+
+namespace pointid {
+namespace {
+
+template <int kType>
+__global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+  const DropKey key(a.drop);
+  const int64_t pieces = (a.cols + 7) / 8, total = a.rows * pieces;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)pieces) : i / pieces;
+    const int64_t col = (i - row * pieces) * 8;
+    const int n = piece_cols(a.cols, col);
+    Raw8<kType> x, r;
+    x.load(a.x + (row * a.ld_x + col) * kSize, n);
+    if (a.residual) r.load(a.residual + (row * a.ld_residual + col) * kSize, n);
+    float v[8];
+    x.values(v);
+    drop8(a.drop, key, row, col, v);
+    if (a.residual) {
+      float f[8];
+      r.values(f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += f[j];
+    }
+    store_cols<8>(a.y, row * a.ld_y + col, kType, n, v);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream) {
+  const int64_t blocks = (a.rows * ((a.cols + 7) / 8) + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
+  switch (a.dtype) {
+    case POINTID_FP32: return launch_kernel(dropout_kernel<POINTID_FP32>, grid, dim3(256), 0, stream, a);
+    case POINTID_BF16: return launch_kernel(dropout_kernel<POINTID_BF16>, grid, dim3(256), 0, stream, a);
+  }
+  return launch_kernel(dropout_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
+}
+
+}  // namespace pointid

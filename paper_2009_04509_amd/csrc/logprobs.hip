@@ -1,0 +1,373 @@
+// Log probabilities of given columns, the log of the sum of exponentials, entropy and the most
+// likely columns of each row of logits, and the logits' gradient.
+//
+// With z = scale x, m the row's maximum and d = z - m:
+//   s = sum e^d    lse = m + ln s    logp(t) = d_t - ln s    H = ln s - (sum e^d d) / s
+// Each thread keeps m, s and sum e^d d of the columns it has read (in powers of two: d / ln 2)
+// and brings them to a new maximum when one comes, so that a row is read once.
+#include "internal.h"
+#include "layers_end.h"
+#include "norm.h"
+
+namespace pointid {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kLowest = -3.402823466e38f;
+
+// ---- the most likely columns.  An entry is 64 bits: above, the value's bits as an unsigned
+// number in the order of the values; below, the column (or piece of 8 columns) inverted, so that
+// among equals the lowest column is the largest entry.  0 is no entry.  A NaN counts as minus
+// infinity, -0 as 0.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  v = v != v ? -__builtin_inff() : v + 0.f;
+  const uint32_t b = __float_as_uint(v);
+  return b ^ ((int32_t)b < 0 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t order) {
+  return __uint_as_float(order ^ ((int32_t)order < 0 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ uint64_t entry_of(float v, uint32_t at) { return (uint64_t)order_of(v) << 32 | (uint32_t)~at; }
+
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int x) {
+  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, x, 64), hi = (uint32_t)__shfl_xor((int)(v >> 32), x, 64);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t keep_one(uint64_t v, uint64_t other, bool larger) { return (v > other) == larger ? v : other; }
+// A wave's 64 entries in falling order (a bitonic sort), and the 64 largest of two such lists.
+__device__ __forceinline__ uint64_t sort64(uint64_t v) {
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int k = 2; k <= 64; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j > 0; j /= 2)
+      v = keep_one(v, lane_xor(v, j), ((lane & j) == 0) == ((lane & k) == 0));
+  return v;
+}
+__device__ __forceinline__ uint64_t merge64(uint64_t a, uint64_t b) {
+  const int lane = threadIdx.x % 64;
+  b = lane_xor(b, 63);
+  uint64_t v = a > b ? a : b;
+#pragma unroll
+  for (int j = 32; j > 0; j /= 2) v = keep_one(v, lane_xor(v, j), (lane & j) == 0);
+  return v;
+}
+// The 64 largest of the waves' lists, in the first wave.
+template <int kWaves>
+__device__ __forceinline__ uint64_t merge_waves(uint64_t v, uint64_t (&lists)[kWaves > 1 ? kWaves / 2 * 64 : 1]) {
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+#pragma unroll
+  for (int half = kWaves / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (wave >= half && wave < 2 * half) lists[(wave - half) * 64 + lane] = v;
+    __syncthreads();
+    if (wave < half) v = merge64(v, lists[wave * 64 + lane]);
+  }
+  return v;
+}
+
+// ---- maximum, sum of e^d and of e^d d of some columns; d in powers of two
+struct Sums {
+  float most, s, w;
+};
+// What most is subtracted as: finite, so that no infinity meets itself where all is masked.
+__device__ __forceinline__ float finite_most(float most) { return fmaxf(most, kLowest); }
+// v brought to the maximum `most`, which is no smaller than its own.
+__device__ __forceinline__ void bring_to(Sums* v, float most, float c) {
+  const float d = fmaxf((finite_most(v->most) - finite_most(most)) * c, -1000.f), e = two_to(d);
+  v->w = e * (v->w + d * v->s);
+  v->s = e * v->s;
+  v->most = most;
+}
+__device__ __forceinline__ void add_to(Sums* v, float x, float ref, float c) {
+  const float d = (x - ref) * c, e = two_to(d);       // a NaN, or infinity less itself, stays a NaN
+  v->s += e;
+  v->w += e * fmaxf(d, -1000.f);                      // minus infinity: 0
+}
+
+template <int kWaves>
+__device__ __forceinline__ void block_sums(Sums* v, float c, float (&lds)[kWaves][2]) {
+  float most = v->most;
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) most = fmaxf(most, __shfl_xor(most, x, 64));
+  const int wave = threadIdx.x / 64;
+  if constexpr (kWaves > 1) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) lds[wave][0] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) most = fmaxf(most, lds[i][0]);
+  }
+  bring_to(v, most, c);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    v->s += __shfl_xor(v->s, x, 64);
+    v->w += __shfl_xor(v->w, x, 64);
+  }
+  if constexpr (kWaves > 1) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) lds[wave][0] = v->s, lds[wave][1] = v->w;
+    __syncthreads();
+    v->s = lds[0][0], v->w = lds[0][1];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) v->s += lds[i][0], v->w += lds[i][1];
+  }
+}
+
+// A row's results from its sums: by any thread.
+struct RowEnd {
+  float most, scale, ln_s, lse, entropy;
+  bool empty;                  // every column is masked
+  __device__ __forceinline__ RowEnd(const Sums& v, float scale_) : most(v.most), scale(scale_) {
+    empty = v.s == 0.f;
+    ln_s = logf(v.s);
+    lse = empty ? -__builtin_inff() : most * scale + ln_s;
+    entropy = empty ? 0.f : ln_s - kLn2 * v.w / v.s;
+  }
+  __device__ __forceinline__ float logp(float x) const { return empty ? -__builtin_inff() : (x - most) * scale - ln_s; }
+};
+__device__ __forceinline__ void store_row(const ScanArgs& a, int64_t row, const RowEnd& end, bool has_target, float target) {
+  if (a.logp) a.logp[row] = has_target ? end.logp(target) : 0.f;
+  if (a.lse) a.lse[row] = end.lse;
+  if (a.entropy) a.entropy[row] = end.entropy;
+}
+__device__ __forceinline__ void store_top(const ScanArgs& a, int64_t row, const RowEnd& end, int at, uint64_t entry) {
+  a.top_ids[row * a.top + at] = (int32_t)~(uint32_t)entry;
+  a.top_logp[row * a.top + at] = end.logp(value_of((uint32_t)(entry >> 32)));
+}
+
+constexpr int kListed = 512;   // candidates that shared memory holds
+
+// The k largest entries of columns [first, last) of a row, in falling order in the first wave's
+// lanes.  best: the largest entry of each thread's own pieces (first / 8 + thread + i kThreads),
+// by piece; 0 of none.  The columns that are wanted are all in pieces of the threads with the k
+// largest of these: of any other thread, k threads have a larger one.  So those threads' pieces
+// are read again, and what is at least the k-th of the threads' best is listed; more than the
+// list holds (which takes an order of the values that goes with the threads') is sorted as it
+// is read.
+template <int kType, int kThreads>
+__device__ uint64_t pick_top(const char* x, int64_t first, int64_t last, int k, uint64_t best,
+                             uint64_t (&lists)[kThreads > 64 ? kThreads / 128 * 64 : 1], uint64_t (&listed)[kListed],
+                             uint32_t* count) {
+  constexpr int kWaves = kThreads / 64, kSize = kType == POINTID_FP32 ? 4 : 2;
+  __shared__ uint64_t chosen[kMaxTop];
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  best = merge_waves<kWaves>(sort64(best), lists);
+  __syncthreads();
+  if (threadIdx.x < (unsigned)k) chosen[threadIdx.x] = best;
+  if (threadIdx.x == 0) *count = 0;
+  __syncthreads();
+  int threads = k;
+  while (threads > 0 && chosen[threads - 1] == 0) --threads;   // fewer have any columns
+  const uint64_t least = threads == k ? chosen[k - 1] : 0;
+  const uint32_t base = (uint32_t)(first / 8), pieces = (uint32_t)((last + 7) / 8);
+  const uint32_t each = (pieces - base + kThreads - 1) / kThreads;
+  // whether an entry by column is at least `least`, by piece
+  auto wanted = [&](uint64_t e) {
+    return (e >> 32) > (least >> 32) || ((e >> 32) == (least >> 32) && (~(uint32_t)e) / 8 <= ~(uint32_t)least);
+  };
+  for (uint32_t i = threadIdx.x; i < threads * each; i += kThreads) {
+    const uint32_t of = ~(uint32_t)chosen[i / each], piece = base + (of - base) % kThreads + i % each * kThreads;
+    if (piece >= pieces) continue;
+    Raw8<kType> raw;
+    const int64_t col = (int64_t)piece * 8;
+    const int n = piece_cols(last, col);
+    raw.load(x + col * kSize, n);
+    float v[8];
+    raw.values(v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= n) continue;
+      const uint64_t e = entry_of(v[j], (uint32_t)col + j);
+      if (!wanted(e)) continue;
+      const uint32_t at = atomicAdd(count, 1);
+      if (at < kListed) listed[at] = e;
+    }
+  }
+  __syncthreads();
+  const uint32_t found = *count;
+  uint64_t v = 0;
+  if (found <= kListed) {
+    for (uint32_t at = wave * 64; at < found; at += kThreads) {
+      const uint64_t e = sort64(at + lane < found ? listed[at + lane] : 0);
+      v = at == (uint32_t)wave * 64 ? e : merge64(v, e);
+    }
+  } else {
+    const uint32_t total = threads * each * 8;
+    for (uint32_t at = wave * 64; at < total; at += kThreads) {
+      uint64_t e = 0;
+      const uint32_t i = (at + lane) / 8, j = lane % 8;
+      if (i < threads * each) {
+        const uint32_t of = ~(uint32_t)chosen[i / each], piece = base + (of - base) % kThreads + i % each * kThreads;
+        const int64_t col = (int64_t)piece * 8 + j;
+        if (piece < pieces && col < last) e = entry_of(load_any(x, col, kType), (uint32_t)col);
+        if (!wanted(e)) e = 0;
+      }
+      if (__any(e != 0)) v = merge64(v, sort64(e));
+    }
+  }
+  return merge_waves<kWaves>(v, lists);
+}
+
+// A row (or a split of one) by a block.
+template <int kType, int kThreads>
+__global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2, kWaves = kThreads / 64;
+  __shared__ float lds[kWaves][2];
+  __shared__ uint64_t lists[kThreads > 64 ? kThreads / 128 * 64 : 1], listed[kListed];
+  __shared__ uint32_t count;
+  const float c = a.scale * kLog2e;
+  for (int64_t unit = blockIdx.x; unit < a.rows * a.splits; unit += gridDim.x) {
+    const int64_t row = a.splits == 1 ? unit : unit / a.splits, split = unit - row * a.splits;
+    const int64_t first = split * a.split_cols;
+    const int64_t last = first + a.split_cols < a.cols ? first + a.split_cols : a.cols;
+    const char* const x = a.x.p + row * a.x.ld * kSize;
+    Sums v = {-__builtin_inff(), 0.f, 0.f};
+    float top = -__builtin_inff();
+    uint32_t top_piece = (uint32_t)(first / 8) + threadIdx.x;
+    for (int64_t col = first + threadIdx.x * 8; col < last; col += kThreads * 8) {
+      const int n = piece_cols(last, col);
+      Raw8<kType> raw;
+      raw.load(x + col * kSize, n);
+      float f[8];
+      raw.values(f);
+      float most = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        f[i] = i < n ? f[i] : -__builtin_inff();
+        most = fmaxf(most, f[i]);
+      }
+      if (most > top) top = most, top_piece = (uint32_t)(col / 8);
+      bring_to(&v, fmaxf(v.most, most), c);
+      const float ref = finite_most(v.most);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) add_to(&v, f[i], ref, c);
+    }
+    block_sums<kWaves>(&v, c, lds);
+    uint64_t entry = 0;
+    if (a.top) {
+      const uint64_t best = first + threadIdx.x * 8 < last ? entry_of(top, top_piece) : 0;
+      entry = pick_top<kType, kThreads>(x, first, last, a.top, best, lists, listed, &count);
+    }
+    if (a.splits > 1) {
+      if (threadIdx.x == 0) reinterpret_cast<float4*>(a.part)[unit] = make_float4(v.most, v.s, v.w, 0.f);
+      if (threadIdx.x < (unsigned)a.top) a.part_top[unit * a.top + threadIdx.x] = entry;
+      continue;
+    }
+    const RowEnd end(v, a.scale);
+    if (threadIdx.x == 0) {
+      const int32_t t = a.targets ? a.targets[row] : -1;
+      const bool has = t >= 0 && t < a.cols;
+      store_row(a, row, end, has, has ? load_any(x, t, kType) : 0.f);
+    }
+    if (threadIdx.x < (unsigned)a.top) store_top(a, row, end, threadIdx.x, entry);
+  }
+}
+
+// The splits of a row joined, by a block.
+template <int kType>
+__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a) {
+  __shared__ float lds[4][2];
+  __shared__ uint64_t lists[128];
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const float c = a.scale * kLog2e;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    Sums v = {-__builtin_inff(), 0.f, 0.f};
+    for (int s = threadIdx.x; s < a.splits; s += 256) {
+      const float4 p = reinterpret_cast<const float4*>(a.part)[row * a.splits + s];
+      Sums other = {p.x, p.y, p.z};
+      const float most = fmaxf(v.most, other.most);
+      bring_to(&v, most, c);
+      bring_to(&other, most, c);
+      v.s += other.s;
+      v.w += other.w;
+    }
+    block_sums<4>(&v, c, lds);
+    uint64_t entry = 0;
+    if (a.top) {
+      for (int s = wave; s < a.splits; s += 4)
+        entry = merge64(entry, lane < a.top ? a.part_top[(row * a.splits + s) * a.top + lane] : 0);
+      entry = merge_waves<4>(entry, lists);
+    }
+    const RowEnd end(v, a.scale);
+    if (threadIdx.x == 0) {
+      const int32_t t = a.targets ? a.targets[row] : -1;
+      const bool has = t >= 0 && t < a.cols;
+      store_row(a, row, end, has, has ? load_any(a.x.p, row * a.x.ld + t, kType) : 0.f);
+    }
+    if (threadIdx.x < (unsigned)a.top) store_top(a, row, end, threadIdx.x, entry);
+  }
+}
+
+// dx_j = scale (dlogp ([j = t] - p_j) + dlse p_j - dH p_j (log p_j + H)), p_j = e^(z_j - lse)
+template <int kType>
+__global__ void __launch_bounds__(256) scan_back_kernel(ScanBackArgs a) {
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
+  const int64_t pieces = (a.cols + 7) / 8, total = a.rows * pieces;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)pieces) : i / pieces;
+    const int64_t col = (i - row * pieces) * 8;
+    const int n = piece_cols(a.cols, col);
+    Raw8<kType> raw;
+    raw.load(a.x.p + (row * a.x.ld + col) * kSize, n);
+    float v[8];
+    raw.values(v);
+    const float lse = a.lse[row];
+    const int32_t t = a.targets ? a.targets[row] : -1;
+    const float dlogp = t >= 0 && t < a.cols ? a.dlogp[row] : 0.f;
+    const float on_p = (a.dlse ? a.dlse[row] : 0.f) - dlogp;
+    const float dh = a.dentropy ? a.dentropy[row] : 0.f, h = a.dentropy ? a.entropy[row] : 0.f;
+    const bool empty = lse == -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float logp = v[j] * a.scale - lse, p = two_to(logp * kLog2e);
+      float d = p * (on_p - dh * (fmaxf(logp, -1000.f) + h));
+      if (col + j == t) d += dlogp;
+      v[j] = empty ? 0.f : d * a.scale;
+    }
+    store_cols<8>(a.dx.p, row * a.dx.ld + col, kType, n, v);
+  }
+}
+
+}  // namespace
+
+// Splits of a row, where the rows alone leave CUs idle: of at least 4096 columns.
+int32_t scan_splits(int64_t rows, int64_t cols, int cus) {
+  const int64_t most = (cols + 4095) / 4096, want = (2 * cus + rows - 1) / (rows > 0 ? rows : 1);
+  const int64_t s = most < want ? most : want;
+  return (int32_t)(s < 1 ? 1 : s);
+}
+
+namespace {
+unsigned capped(int64_t blocks) { return (unsigned)(blocks < 65536 ? (blocks > 0 ? blocks : 1) : 65536); }
+}  // namespace
+
+hipError_t launch_logprobs(const ScanArgs& a, hipStream_t stream) {
+  const dim3 grid(capped(a.rows * a.splits));
+  switch (a.dtype) {
+    case POINTID_FP32: return launch_kernel(scan_kernel<POINTID_FP32, 256>, grid, dim3(256), 0, stream, a);
+    case POINTID_BF16: return launch_kernel(scan_kernel<POINTID_BF16, 256>, grid, dim3(256), 0, stream, a);
+  }
+  return launch_kernel(scan_kernel<POINTID_FP16, 256>, grid, dim3(256), 0, stream, a);
+}
+
+hipError_t launch_logprobs_join(const ScanArgs& a, hipStream_t stream) {
+  const dim3 grid(capped(a.rows));
+  switch (a.dtype) {
+    case POINTID_FP32: return launch_kernel(scan_join_kernel<POINTID_FP32>, grid, dim3(256), 0, stream, a);
+    case POINTID_BF16: return launch_kernel(scan_join_kernel<POINTID_BF16>, grid, dim3(256), 0, stream, a);
+  }
+  return launch_kernel(scan_join_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
+}
+
+hipError_t launch_logprobs_back(const ScanBackArgs& a, hipStream_t stream) {
+  const int64_t blocks = (a.rows * ((a.cols + 7) / 8) + 255) / 256;
+  const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
+  switch (a.dtype) {
+    case POINTID_FP32: return launch_kernel(scan_back_kernel<POINTID_FP32>, grid, dim3(256), 0, stream, a);
+    case POINTID_BF16: return launch_kernel(scan_back_kernel<POINTID_BF16>, grid, dim3(256), 0, stream, a);
+  }
+  return launch_kernel(scan_back_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
+}
+
+}  // namespace pointid
