@@ -689,7 +689,7 @@ uint64_t pointid_norm_backward_scratch(pointid_layers l, int64_t m, int64_t n);
  *   entropy = - sum_j p_j ln p_j       p_j = e^(z_j - lse)
  *   top     the `top` largest logits' columns in falling order, the lowest column first among
  *           equals, and their log probabilities
- *   scale     > 0, finite (one over a temperature)
+ *   scale     in [2^-64, 2^64] (one over a temperature)
  *   targets   device int32 [m], optional; a target outside [0, n) is none: logp is 0
  *   logp, lse, entropy  optional fp32 [m]; logp needs targets
  *   top       0..64, at most n; top_ids int32 [m][top], top_logp fp32 [m][top]

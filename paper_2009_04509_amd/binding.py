@@ -1024,40 +1024,57 @@ def _drop(d, device):
     return d.p, d.seed, d.offset, step
 
 
+def _vector(t, name, n, device, dtype=torch.float32):
+    """The address of a vector [n], or None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == (n,)
+            and t.is_contiguous()):
+        _need(t, dtype, name, device)                   # says what is wrong with it
+        raise ValueError(f"{name} must be [{n}]")
+    return t.data_ptr()
+
+
 def _norm(norm, name, n, device):
     """The fields of a norm."""
     if norm is None:
         return 0, 0.0, None, None
-    if norm.kind not in NORMS:
+    kind, weight, bias, eps = norm
+    if kind not in NORMS:
         raise ValueError(f"{name}.kind must be one of {', '.join(NORMS)}")
-    return (NORMS[norm.kind], norm.eps, _bias(norm.weight, f"{name}.weight", n, device),
-            _bias(norm.bias, f"{name}.bias", n, device))
+    return NORMS[kind], eps, _vector(weight, name + ".weight", n, device), _vector(bias, name + ".bias", n, device)
 
 
-def _block(block, dt, m, n, device):
+def _block(block, dt, shape, device):
     if block is None:
         return None
-    out = _matrix(block.out, "block.out", dt, (m, n), device)
+    out = _matrix(block.out, "block.out", dt, shape, device)
+    n = shape[1]
     return _Block(out.data, out.ld, *_norm(block.norm, "block.norm", n, device),
-                  _bias(block.gate, "block.gate", n, device), block.scale, *_drop(block.drop, device))
+                  _vector(block.gate, "block.gate", n, device), block.scale, *_drop(block.drop, device))
 
 
-def _vector(t, name, dtype, m, device):
-    """The address of a vector of the rows, or None."""
-    if t is None:
-        return None
-    _need(t, dtype, name, device)
-    if t.dim() != 1 or t.shape[0] != m:
-        raise ValueError(f"{name} must be [{m}]")
-    return t.data_ptr()
+def _scratch(size, like):
+    """(the memory, its address) of a call's scratch: of its stream's, so that it can be captured."""
+    if size == 0:
+        return None, None
+    t = torch.empty(size, dtype=torch.uint8, device=like.device)
+    return t, t.data_ptr()
 
 
-def _scratch(size, layers, like, *sizes):
-    """(the memory, its bytes) of a call: under capture the graph's own, else the handle's."""
-    if not torch.cuda.is_current_stream_capturing():
-        return None, 0
-    n = size(layers.raw, *sizes)
-    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n else (None, 0)
+def _rows_of_floats(like, rows, n):
+    """float32 vectors [n], in one piece of memory."""
+    if rows == 1:
+        return (like.new_empty((n,), dtype=torch.float32),)
+    return like.new_empty((rows, n), dtype=torch.float32).unbind() if rows else ()
+
+
+def _like(t, given, name, dtype, shape, device):
+    """An output like t, given or made (on the stream that is current), and its descriptor."""
+    if given is not None:
+        return given, _matrix(given, name, dtype, shape, device)
+    t = torch.empty_like(t, memory_format=torch.contiguous_format)
+    return t, _Matrix(t.data_ptr(), shape[1])
 
 
 def pointid_dropout(layers: Layers, x: torch.Tensor, drop: Drop, residual: torch.Tensor | None = None,
@@ -1069,7 +1086,11 @@ def pointid_dropout(layers: Layers, x: torch.Tensor, drop: Drop, residual: torch
     shape = x.shape
     a, r = _matrix(x, "x", dt, shape, dev), _matrix(residual, "residual", dt, shape, dev)
     d = _Drop(*_drop(drop, dev))
-    y, out = _output(y, x, "y", dt, shape, dev, stream)
+
+    def outputs():
+        return _like(x, y, "y", dt, shape, dev)
+
+    y, out = outputs() if stream is None else _make(stream, dev, outputs)
     _check(lib.pointid_dropout(layers.raw, _LAYER_TYPES[dt], shape[0], shape[1], a, d, r, out,
                                _layer_stream(stream, dev)))
     return y
@@ -1090,11 +1111,12 @@ def pointid_norm(layers: Layers, x: torch.Tensor, norm: Norm | None = None, bloc
     if (h is not None and norm is None) or (total is not None and block is None):
         raise ValueError("h needs norm and total needs block")
     a = _matrix(x, "x", dt, shape, dev)
-    after, end = _NormOf(*_norm(norm, "norm", n, dev)) if norm is not None else None, _block(block, dt, m, n, dev)
+    after = _NormOf(*_norm(norm, "norm", n, dev)) if norm is not None else None
+    end = _block(block, dt, shape, dev)
 
     def outputs():
-        return (_output(total, x, "total", dt, shape, dev) if block is not None else (None, None),
-                _output(h, x, "h", dt, shape, dev) if norm is not None else (None, None),
+        return (_like(x, total, "total", dt, shape, dev) if block is not None else (None, None),
+                _like(x, h, "h", dt, shape, dev) if norm is not None else (None, None),
                 x.new_empty((m, 4), dtype=torch.float32) if keep else None)
 
     (total, to_total), (h, to_h), stats = outputs() if stream is None else _make(stream, dev, outputs)
@@ -1114,34 +1136,37 @@ def pointid_norm_backward(layers: Layers, dh: torch.Tensor | None, total: torch.
     given = dh if norm is not None else dtotal
     dt, dev = _layer_type(given, "dh" if norm is not None else "dtotal"), layers.device
     m, n = shape = given.shape
-    a, b = (_matrix(dh, "dh", dt, shape, dev), _matrix(total, "total", dt, shape, dev)) if norm is not None else (None, None)
-    if norm is not None and b is None:
-        raise ValueError("total is needed with norm")
+    a = b = before = None
+    if norm is not None:
+        if total is None:
+            raise ValueError("total is needed with norm")
+        a, b = _matrix(dh, "dh", dt, shape, dev), _matrix(total, "total", dt, shape, dev)
+        before = _NormOf(*_norm(norm, "norm", n, dev))
     c = _matrix(dtotal, "dtotal", dt, shape, dev)
-    before, end = _NormOf(*_norm(norm, "norm", n, dev)) if norm is not None else None, _block(block, dt, m, n, dev)
+    end = _block(block, dt, shape, dev)
     after = block.norm if block is not None else None
+    kept = None
     if norm is not None or after is not None:
         _need(stats, torch.float32, "stats", dev)
-        if tuple(stats.shape) != (m, 4):
+        if stats.shape != (m, 4):
             raise ValueError(f"stats must be [{m}, 4]")
-    else:
-        stats = None
-    params = [norm and norm.weight, norm and norm.bias, after and after.weight, after and after.bias,
-              block and block.gate] if need_params else [None] * 5
+        kept = stats.data_ptr()
+    params = (norm and norm.weight, norm and norm.bias, after and after.weight, after and after.bias,
+              block and block.gate) if need_params else (None,) * 5
     params = [p is not None for p in params]
+    size = lib.pointid_norm_backward_scratch(layers.raw, m, n)
 
     def outputs():
-        return (_output(dx, given, "dx", dt, shape, dev) if need_dx or dx is not None else (None, None),
-                _output(None, given, "dout", dt, shape, dev) if need_dout and block is not None else (None, None),
-                [given.new_empty((n,), dtype=torch.float32) if p else None for p in params],
-                _scratch(lib.pointid_norm_backward_scratch, layers, given, m, n))
+        return (_like(given, dx, "dx", dt, shape, dev) if need_dx or dx is not None else (None, None),
+                _like(given, None, "dout", dt, shape, dev) if need_dout and block is not None else (None, None),
+                _rows_of_floats(given, sum(params), n), _scratch(size, given))
 
-    (dx, to_dx), (dout, to_dout), sums, (scratch, size) = outputs() if stream is None else _make(stream, dev, outputs)
+    (dx, to_dx), (dout, to_dout), sums, (scratch, at) = outputs() if stream is None else _make(stream, dev, outputs)
+    sums = iter(sums)
+    sums = [next(sums) if p else None for p in params]
     grads = _NormGrads(to_dx and to_dx.data, to_dx.ld if to_dx else 0, to_dout and to_dout.data,
-                       to_dout.ld if to_dout else 0, *(p.data_ptr() if p is not None else None for p in sums))
-    _check(lib.pointid_norm_backward(layers.raw, _LAYER_TYPES[dt], m, n, a, b,
-                                     stats.data_ptr() if stats is not None else None, before, end, c, grads,
-                                     scratch.data_ptr() if scratch is not None else None, size,
+                       to_dout.ld if to_dout else 0, *(p if p is None else p.data_ptr() for p in sums))
+    _check(lib.pointid_norm_backward(layers.raw, _LAYER_TYPES[dt], m, n, a, b, kept, before, end, c, grads, at, size,
                                      _layer_stream(stream, dev)))
     return NormGradients(dx, dout, *sums)
 
@@ -1156,24 +1181,22 @@ def pointid_logprobs(layers: Layers, logits: torch.Tensor, targets: torch.Tensor
     dt, dev = _layer_type(logits, "logits"), layers.device
     m, n = logits.shape
     a = _matrix(logits, "logits", dt, (m, n), dev)
-    at = _vector(targets, "targets", torch.int32, m, dev)
+    at = _vector(targets, "targets", m, dev, torch.int32)
     if not 0 <= top <= min(64, n):
         raise ValueError("top must be in [0, 64] and at most n")
+    size = lib.pointid_logprobs_scratch(layers.raw, m, n, top)
 
     def outputs():
-        values = logits.new_empty((1 + (at is not None) + bool(entropy), m), dtype=torch.float32).unbind()
-        best = logits.new_empty((2, m, top), dtype=torch.int32).unbind() if top else None
-        return values, best, _scratch(lib.pointid_logprobs_scratch, layers, logits, m, n, top)
+        return (_rows_of_floats(logits, 1 + (at is not None) + bool(entropy), m),
+                logits.new_empty((m, top), dtype=torch.int32) if top else None,
+                logits.new_empty((m, top), dtype=torch.float32) if top else None, _scratch(size, logits))
 
-    values, best, (scratch, size) = outputs() if stream is None else _make(stream, dev, outputs)
+    values, ids, best, (scratch, scratch_at) = outputs() if stream is None else _make(stream, dev, outputs)
     lse, h, logp = values[0], values[1] if entropy else None, values[-1] if at is not None else None
-    ids, best = (best[0], best[1].view(torch.float32)) if top else (None, None)
     _check(lib.pointid_logprobs(layers.raw, _LAYER_TYPES[dt], m, n, a, scale, at,
                                 logp.data_ptr() if at is not None else None, lse.data_ptr(),
                                 h.data_ptr() if entropy else None, top, ids.data_ptr() if top else None,
-                                best.data_ptr() if top else None,
-                                scratch.data_ptr() if scratch is not None else None, size,
-                                _layer_stream(stream, dev)))
+                                best.data_ptr() if top else None, scratch_at, size, _layer_stream(stream, dev)))
     return LogProbs(logp, lse, h, ids, best)
 
 
@@ -1187,11 +1210,14 @@ def pointid_logprobs_backward(layers: Layers, logits: torch.Tensor, lse: torch.T
     dt, dev = _layer_type(logits, "logits"), layers.device
     m, n = shape = logits.shape
     a = _matrix(logits, "logits", dt, shape, dev)
-    f32 = torch.float32
-    vectors = [_vector(lse, "lse", f32, m, dev), _vector(targets, "targets", torch.int32, m, dev),
-               _vector(dlogp, "dlogp", f32, m, dev), _vector(entropy, "entropy", f32, m, dev),
-               _vector(dentropy, "dentropy", f32, m, dev), _vector(dlse, "dlse", f32, m, dev)]
-    dlogits, out = _output(dlogits, logits, "dlogits", dt, shape, dev, stream)
+    vectors = (_vector(lse, "lse", m, dev), _vector(targets, "targets", m, dev, torch.int32),
+               _vector(dlogp, "dlogp", m, dev), _vector(entropy, "entropy", m, dev),
+               _vector(dentropy, "dentropy", m, dev), _vector(dlse, "dlse", m, dev))
+
+    def outputs():
+        return _like(logits, dlogits, "dlogits", dt, shape, dev)
+
+    dlogits, out = outputs() if stream is None else _make(stream, dev, outputs)
     _check(lib.pointid_logprobs_backward(layers.raw, _LAYER_TYPES[dt], m, n, a, scale, *vectors, out,
                                          _layer_stream(stream, dev)))
     return dlogits

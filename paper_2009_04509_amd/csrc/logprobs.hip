@@ -8,6 +8,7 @@
 #include "internal.h"
 #include "layers_end.h"
 #include "norm.h"
+#include "wave.h"
 
 namespace pointid {
 namespace {
@@ -29,28 +30,33 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ uint64_t entry_of(float v, uint32_t at) { return (uint64_t)order_of(v) << 32 | (uint32_t)~at; }
 
-__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int x) {
-  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, x, 64), hi = (uint32_t)__shfl_xor((int)(v >> 32), x, 64);
-  return (uint64_t)hi << 32 | lo;
+template <int kX>
+__device__ __forceinline__ uint64_t entry_xor(uint64_t v) {
+  return (uint64_t)lane_xor<kX>((uint32_t)(v >> 32)) << 32 | lane_xor<kX>((uint32_t)v);
 }
 __device__ __forceinline__ uint64_t keep_one(uint64_t v, uint64_t other, bool larger) { return (v > other) == larger ? v : other; }
-// A wave's 64 entries in falling order (a bitonic sort), and the 64 largest of two such lists.
-__device__ __forceinline__ uint64_t sort64(uint64_t v) {
+// kFirst, kFirst / 2, .. 1 lanes apart: the last steps of a bitonic sort, each lane of which keeps
+// the larger where it is the lower one of a falling stretch of kStretch lanes or the upper of a
+// rising one
+template <int kFirst, int kStretch>
+__device__ __forceinline__ uint64_t sort_steps(uint64_t v) {
   const int lane = threadIdx.x % 64;
-#pragma unroll
-  for (int k = 2; k <= 64; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2)
-      v = keep_one(v, lane_xor(v, j), ((lane & j) == 0) == ((lane & k) == 0));
+  v = keep_one(v, entry_xor<kFirst>(v), ((lane & kFirst) == 0) == ((lane & kStretch) == 0));
+  if constexpr (kFirst > 1) return sort_steps<kFirst / 2, kStretch>(v);
   return v;
 }
+// A wave's 64 entries in falling order (a bitonic sort), and the 64 largest of two such lists.
+__device__ __forceinline__ uint64_t sort64(uint64_t v) {
+  v = sort_steps<1, 2>(v);
+  v = sort_steps<2, 4>(v);
+  v = sort_steps<4, 8>(v);
+  v = sort_steps<8, 16>(v);
+  v = sort_steps<16, 32>(v);
+  return sort_steps<32, 64>(v);
+}
 __device__ __forceinline__ uint64_t merge64(uint64_t a, uint64_t b) {
-  const int lane = threadIdx.x % 64;
-  b = lane_xor(b, 63);
-  uint64_t v = a > b ? a : b;
-#pragma unroll
-  for (int j = 32; j > 0; j /= 2) v = keep_one(v, lane_xor(v, j), (lane & j) == 0);
-  return v;
+  b = entry_xor<63>(b);
+  return sort_steps<32, 64>(a > b ? a : b);
 }
 // The 64 largest of the waves' lists, in the first wave.
 template <int kWaves>
@@ -66,30 +72,41 @@ __device__ __forceinline__ uint64_t merge_waves(uint64_t v, uint64_t (&lists)[kW
   return v;
 }
 
-// ---- maximum, sum of e^d and of e^d d of some columns; d in powers of two
+// ---- maximum, sum of 2^d and of 2^d d of some columns, d = c (x - maximum) with c = scale / ln 2
+// (the difference first: a column at the maximum adds 1 exactly)
 struct Sums {
   float most, s, w;
 };
-// What most is subtracted as: finite, so that no infinity meets itself where all is masked.
+// What is subtracted: finite, so that no infinity meets itself in a row that is masked whole.
 __device__ __forceinline__ float finite_most(float most) { return fmaxf(most, kLowest); }
+constexpr float kNone = -1000.f;               // 2^kNone is 0, and kNone times it too
 // v brought to the maximum `most`, which is no smaller than its own.
 __device__ __forceinline__ void bring_to(Sums* v, float most, float c) {
-  const float d = fmaxf((finite_most(v->most) - finite_most(most)) * c, -1000.f), e = two_to(d);
+  const float d = fmaxf((finite_most(v->most) - finite_most(most)) * c, kNone), e = two_to(d);
   v->w = e * (v->w + d * v->s);
   v->s = e * v->s;
   v->most = most;
 }
-__device__ __forceinline__ void add_to(Sums* v, float x, float ref, float c) {
-  const float d = (x - ref) * c, e = two_to(d);       // a NaN, or infinity less itself, stays a NaN
-  v->s += e;
-  v->w += e * fmaxf(d, -1000.f);                      // minus infinity: 0
+// 8 values: a NaN, or infinity less itself, stays a NaN; minus infinity adds nothing
+template <bool kEntropy>
+__device__ __forceinline__ void add_to(Sums* v, const float (&x)[8], float ref, float c) {
+  float s = 0.f, w = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float d = (x[i] - ref) * c, e = two_to(d);
+    s += e;
+    if constexpr (kEntropy) w += e * fmaxf(d, kNone);
+  }
+  v->s += s;
+  if constexpr (kEntropy) v->w += w;
+}
+__device__ __forceinline__ float max8(const float (&v)[8]) {
+  return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
 }
 
 template <int kWaves>
 __device__ __forceinline__ void block_sums(Sums* v, float c, float (&lds)[kWaves][2]) {
-  float most = v->most;
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) most = fmaxf(most, __shfl_xor(most, x, 64));
+  float most = lanes_max<64>(v->most);
   const int wave = threadIdx.x / 64;
   if constexpr (kWaves > 1) {
     __syncthreads();
@@ -99,11 +116,8 @@ __device__ __forceinline__ void block_sums(Sums* v, float c, float (&lds)[kWaves
     for (int i = 0; i < kWaves; ++i) most = fmaxf(most, lds[i][0]);
   }
   bring_to(v, most, c);
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) {
-    v->s += __shfl_xor(v->s, x, 64);
-    v->w += __shfl_xor(v->w, x, 64);
-  }
+  v->s = lanes_sum<64>(v->s);
+  v->w = lanes_sum<64>(v->w);
   if constexpr (kWaves > 1) {
     __syncthreads();
     if (threadIdx.x % 64 == 0) lds[wave][0] = v->s, lds[wave][1] = v->w;
@@ -209,10 +223,11 @@ __device__ uint64_t pick_top(const char* x, int64_t first, int64_t last, int k, 
   return merge_waves<kWaves>(v, lists);
 }
 
-// A row (or a split of one) by a block.
-template <int kType, int kThreads>
+// A row (or a split of one) by a block.  kAhead pieces of 8 columns a thread are brought to a new
+// maximum at once, while the next are on their way.
+template <int kType, int kThreads, bool kEntropy>
 __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
-  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2, kWaves = kThreads / 64;
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2, kWaves = kThreads / 64, kAhead = 2;
   __shared__ float lds[kWaves][2];
   __shared__ uint64_t lists[kThreads > 64 ? kThreads / 128 * 64 : 1], listed[kListed];
   __shared__ uint32_t count;
@@ -222,31 +237,55 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
     const int64_t first = split * a.split_cols;
     const int64_t last = first + a.split_cols < a.cols ? first + a.split_cols : a.cols;
     const char* const x = a.x.p + row * a.x.ld * kSize;
+    const int mine = (int)threadIdx.x * 8, width = (int)(last - first);
     Sums v = {-__builtin_inff(), 0.f, 0.f};
     float top = -__builtin_inff();
-    uint32_t top_piece = (uint32_t)(first / 8) + threadIdx.x;
-    for (int64_t col = first + threadIdx.x * 8; col < last; col += kThreads * 8) {
-      const int n = piece_cols(last, col);
-      Raw8<kType> raw;
-      raw.load(x + col * kSize, n);
-      float f[8];
-      raw.values(f);
-      float most = -__builtin_inff();
+    const uint32_t piece0 = (uint32_t)(first / 8) + threadIdx.x;
+    uint32_t top_turn = 0;
+    const char* const at = x + first * kSize;
+    // turns of kAhead pieces a thread; those that are whole for every thread, and one more
+    constexpr int kTurn = kThreads * 8 * kAhead;
+    const int whole = width / kTurn, turns = (width + kTurn - 1) / kTurn;
+    Raw8<kType> raw[kAhead];
+    auto load = [&](int turn) {
+      const char* const p = at + ((int64_t)turn * kTurn + mine) * kSize;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        f[i] = i < n ? f[i] : -__builtin_inff();
-        most = fmaxf(most, f[i]);
+      for (int u = 0; u < kAhead; ++u) {
+        if (turn < whole)
+          raw[u].load(p + u * kThreads * 8 * kSize, 8);
+        else
+          raw[u].load(p + u * kThreads * 8 * kSize, piece_cols(width, turn * kTurn + u * kThreads * 8 + mine));
       }
-      if (most > top) top = most, top_piece = (uint32_t)(col / 8);
-      bring_to(&v, fmaxf(v.most, most), c);
-      const float ref = finite_most(v.most);
+    };
+    load(0);
+    for (int turn = 0; turn < turns; ++turn) {
+      float f[kAhead][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) add_to(&v, f[i], ref, c);
+      for (int u = 0; u < kAhead; ++u) raw[u].values(f[u]);
+      if (turn + 1 < turns) load(turn + 1);
+      if (turn >= whole) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int n = piece_cols(width, turn * kTurn + u * kThreads * 8 + mine);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[u][i] = i < n ? f[u][i] : -__builtin_inff();
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const float m = max8(f[u]);
+        top_turn = m > top ? turn * kAhead + u : top_turn;
+        top = fmaxf(top, m);
+      }
+      if (top > v.most) bring_to(&v, top, c);
+      const float ref = finite_most(top);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) add_to<kEntropy>(&v, f[u], ref, c);
     }
     block_sums<kWaves>(&v, c, lds);
     uint64_t entry = 0;
     if (a.top) {
-      const uint64_t best = first + threadIdx.x * 8 < last ? entry_of(top, top_piece) : 0;
+      const uint64_t best = mine < width ? entry_of(top, piece0 + top_turn * kThreads) : 0;
       entry = pick_top<kType, kThreads>(x, first, last, a.top, best, lists, listed, &count);
     }
     if (a.splits > 1) {
@@ -264,16 +303,75 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
   }
 }
 
+// Rows of at most 8 kLanes columns, each by kLanes lanes that hold 8 of them; the most likely
+// columns one by one.
+template <int kType, int kLanes>
+__global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs a) {
+  constexpr int kSize = kType == POINTID_FP32 ? 4 : 2, kRows = 256 / kLanes;
+  const float c = a.scale * kLog2e;
+  const int lane = threadIdx.x % kLanes, col = lane * 8, n = piece_cols(a.cols, col);
+  for (int64_t row0 = (int64_t)blockIdx.x * kRows; row0 < a.rows; row0 += (int64_t)gridDim.x * kRows) {
+    const int64_t row = row0 + threadIdx.x / kLanes;
+    if (row >= a.rows) continue;
+    const char* const x = a.x.p + row * a.x.ld * kSize;
+    const int32_t target = a.targets ? a.targets[row] : -1;
+    Raw8<kType> raw;
+    raw.load(x + col * kSize, n);
+    float f[8];
+    raw.values(f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? f[i] : -__builtin_inff();
+    Sums v = {lanes_max<kLanes>(max8(f)), 0.f, 0.f};
+    add_to<true>(&v, f, finite_most(v.most), c);
+    v.s = lanes_sum<kLanes>(v.s);
+    v.w = lanes_sum<kLanes>(v.w);
+    const RowEnd end(v, a.scale);
+    const bool has = target >= 0 && target < a.cols;
+    if (has ? target / 8 == lane : lane == 0) {
+      float t = f[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) t = target % 8 == i ? f[i] : t;
+      store_row(a, row, end, has, t);
+    }
+    if (a.top == 0) continue;
+    uint32_t order[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) order[i] = i < n ? order_of(f[i]) : 0;
+    for (int k = 0; k < a.top; ++k) {
+      uint32_t best = 0;
+      int at = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        at = order[i] > best ? i : at;
+        best = order[i] > best ? order[i] : best;
+      }
+      const uint32_t most = over_lanes<kLanes>(best, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+      // the first lane of the row's that has it
+      bool mine = best == most;
+      if constexpr (kLanes > 1) {
+        const uint64_t same = __ballot(mine) >> (threadIdx.x % 64 / kLanes * kLanes);
+        mine = __builtin_ctzll(same) == lane;
+      }
+      if (mine) {
+        store_top(a, row, end, k, (uint64_t)best << 32 | (uint32_t)~(col + at));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) order[i] = at == i ? 0 : order[i];
+      }
+    }
+  }
+}
+
 // The splits of a row joined, by a block.
 template <int kType>
-__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a) {
-  __shared__ float lds[4][2];
-  __shared__ uint64_t lists[128];
+__global__ void __launch_bounds__(512) scan_join_kernel(ScanArgs a) {
+  constexpr int kWaves = 8;
+  __shared__ float lds[kWaves][2];
+  __shared__ uint64_t lists[kWaves / 2 * 64];
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   const float c = a.scale * kLog2e;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     Sums v = {-__builtin_inff(), 0.f, 0.f};
-    for (int s = threadIdx.x; s < a.splits; s += 256) {
+    for (int s = threadIdx.x; s < a.splits; s += kWaves * 64) {
       const float4 p = reinterpret_cast<const float4*>(a.part)[row * a.splits + s];
       Sums other = {p.x, p.y, p.z};
       const float most = fmaxf(v.most, other.most);
@@ -282,12 +380,12 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a) {
       v.s += other.s;
       v.w += other.w;
     }
-    block_sums<4>(&v, c, lds);
+    block_sums<kWaves>(&v, c, lds);
     uint64_t entry = 0;
     if (a.top) {
-      for (int s = wave; s < a.splits; s += 4)
+      for (int s = wave; s < a.splits; s += kWaves)
         entry = merge64(entry, lane < a.top ? a.part_top[(row * a.splits + s) * a.top + lane] : 0);
-      entry = merge_waves<4>(entry, lists);
+      entry = merge_waves<kWaves>(entry, lists);
     }
     const RowEnd end(v, a.scale);
     if (threadIdx.x == 0) {
@@ -342,22 +440,47 @@ namespace {
 unsigned capped(int64_t blocks) { return (unsigned)(blocks < 65536 ? (blocks > 0 ? blocks : 1) : 65536); }
 }  // namespace
 
+namespace {
+template <int kType>
+hipError_t launch_logprobs_of(const ScanArgs& a, hipStream_t stream) {
+  auto few = [&](auto kernel, int lanes) {
+    return launch_kernel(kernel, dim3(capped((a.rows * lanes + 255) / 256)), dim3(256), 0, stream, a);
+  };
+  if (a.cols <= 8) return few(scan_short_kernel<kType, 1>, 1);
+  if (a.cols <= 16) return few(scan_short_kernel<kType, 2>, 2);
+  if (a.cols <= 32) return few(scan_short_kernel<kType, 4>, 4);
+  if (a.cols <= 64) return few(scan_short_kernel<kType, 8>, 8);
+  if (a.cols <= 128) return few(scan_short_kernel<kType, 16>, 16);
+  if (a.cols <= 256) return few(scan_short_kernel<kType, 32>, 32);
+  if (a.cols <= 512) return few(scan_short_kernel<kType, 64>, 64);
+  auto go = [&](auto kernel, int threads) {
+    return launch_kernel(kernel, dim3(capped(a.rows * a.splits)), dim3(threads), 0, stream, a);
+  };
+  // By waves of their own up to 8192 columns, where the rows fill the card so: a block's waves wait
+  // for each other in the choice of the likeliest columns.  With the 8 likeliest, bf16, by waves and
+  // by blocks of 4: 32768 x 4096 80 us and 228, 16384 x 8192 73-79 and 114, 16384 x 16384 171 and
+  // 152, 4096 x 65536 169 and 120.
+  if (a.cols <= 8192 && a.rows > 1024)
+    return a.entropy ? go(scan_kernel<kType, 64, true>, 64) : go(scan_kernel<kType, 64, false>, 64);
+  return a.entropy ? go(scan_kernel<kType, 256, true>, 256) : go(scan_kernel<kType, 256, false>, 256);
+}
+}  // namespace
+
 hipError_t launch_logprobs(const ScanArgs& a, hipStream_t stream) {
-  const dim3 grid(capped(a.rows * a.splits));
   switch (a.dtype) {
-    case POINTID_FP32: return launch_kernel(scan_kernel<POINTID_FP32, 256>, grid, dim3(256), 0, stream, a);
-    case POINTID_BF16: return launch_kernel(scan_kernel<POINTID_BF16, 256>, grid, dim3(256), 0, stream, a);
+    case POINTID_FP32: return launch_logprobs_of<POINTID_FP32>(a, stream);
+    case POINTID_BF16: return launch_logprobs_of<POINTID_BF16>(a, stream);
   }
-  return launch_kernel(scan_kernel<POINTID_FP16, 256>, grid, dim3(256), 0, stream, a);
+  return launch_logprobs_of<POINTID_FP16>(a, stream);
 }
 
 hipError_t launch_logprobs_join(const ScanArgs& a, hipStream_t stream) {
   const dim3 grid(capped(a.rows));
   switch (a.dtype) {
-    case POINTID_FP32: return launch_kernel(scan_join_kernel<POINTID_FP32>, grid, dim3(256), 0, stream, a);
-    case POINTID_BF16: return launch_kernel(scan_join_kernel<POINTID_BF16>, grid, dim3(256), 0, stream, a);
+    case POINTID_FP32: return launch_kernel(scan_join_kernel<POINTID_FP32>, grid, dim3(512), 0, stream, a);
+    case POINTID_BF16: return launch_kernel(scan_join_kernel<POINTID_BF16>, grid, dim3(512), 0, stream, a);
   }
-  return launch_kernel(scan_join_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
+  return launch_kernel(scan_join_kernel<POINTID_FP16>, grid, dim3(512), 0, stream, a);
 }
 
 hipError_t launch_logprobs_back(const ScanBackArgs& a, hipStream_t stream) {

@@ -46,6 +46,7 @@ struct NormArgs {
   float* stats;
   int64_t rows, cols;
   int32_t dtype;
+  int32_t lanes;               // set by the launch: a row's threads
 };
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream);
 
@@ -65,15 +66,17 @@ struct NormBackArgs {
   int32_t blocks;              // of rows
   int64_t rows, cols;
   int32_t dtype;
+  int32_t lanes;               // set by the launch: a row's threads
 };
-// The blocks of rows that leave sums, and whether `means` is needed.
+// The blocks that leave sums, and whether a block holds whole rows; if not, `means` has to be
+// made first.
 struct NormBackPlan {
   int32_t blocks;
-  bool means;
+  bool held;
 };
 NormBackPlan plan_norm_back(const NormBackArgs& a, int cus);
 hipError_t launch_norm_means(const NormBackArgs& a, hipStream_t stream);
-hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t stream);
+hipError_t launch_norm_back(const NormBackArgs& a, bool held, hipStream_t stream);
 hipError_t launch_norm_sums(const NormBackArgs& a, hipStream_t stream);
 
 // ---- logprobs.hip

@@ -3,6 +3,7 @@
 #include "internal.h"
 #include "layers_end.h"
 #include "norm.h"
+#include "wave.h"
 
 namespace pointid {
 namespace {
@@ -120,6 +121,200 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
       store_cols<8>(a.h.p, row * a.h.ld + col, kType, n, t);
     }
     if (a.stats && threadIdx.x == 0)
+      reinterpret_cast<float4*>(a.stats)[row] = make_float4(after.mean, after.r, before.mean, before.r);
+  }
+}
+
+// ---- rows held in registers: a block's threads are groups of `lanes`, each group with a row at
+// a time and each thread with 8 columns of it
+
+constexpr int kMostWaves = 16;
+
+// Sums over a group: 16 lanes (kSmall), or whole waves, which exchange theirs with one barrier of
+// the block a call: the buffers take turns, so that a call's are not written again before the
+// next call's barrier.
+template <bool kSmall>
+struct RowSum {
+  float2 (*waves)[kMostWaves];
+  int first, count;            // the group's waves
+  int turn = 0;
+  __device__ __forceinline__ RowSum(float2 (*w)[kMostWaves], int lanes)
+      : waves(w), first((int)threadIdx.x / lanes * (lanes / 64)), count(lanes / 64) {}
+  __device__ __forceinline__ float2 operator()(float a, float b) {
+    if constexpr (kSmall) return make_float2(lanes_sum<16>(a), lanes_sum<16>(b));
+    a = lanes_sum<64>(a);
+    b = lanes_sum<64>(b);
+    if (count == 1) return make_float2(a, b);
+    const int lane = threadIdx.x % 64;
+    if (lane == 0) waves[turn][threadIdx.x / 64] = make_float2(a, b);
+    __syncthreads();
+    const float2 s = lane % 16 < count ? waves[turn][first + lane % 16] : make_float2(0.f, 0.f);
+    turn ^= 1;
+    return make_float2(lanes_sum<16>(s.x), lanes_sum<16>(s.y));
+  }
+  __device__ __forceinline__ float operator()(float a) {
+    if constexpr (kSmall) return lanes_sum<16>(a);
+    return (*this)(a, 0.f).x;
+  }
+};
+
+// A thread's group; known to be the same for a wave's threads where it is.
+template <bool kSmall>
+__device__ __forceinline__ int group_of(int lanes) {
+  if constexpr (kSmall) return threadIdx.x / 16;
+  return __builtin_amdgcn_readfirstlane((int)threadIdx.x / lanes);
+}
+
+// A thread's 8 columns of one matrix, row after row.  kWhole: rows are whole pieces of 8.
+template <int kType, bool kWhole>
+struct Stream {
+  static constexpr int64_t kSize = kType == POINTID_FP32 ? 4 : 2;
+  char* p;                     // the next row's first column, nullptr without a matrix
+  int64_t step;                // bytes to the group's row after it
+  Raw8<kType> raw;
+  __device__ __forceinline__ Stream(const Rows& m, int64_t row, int64_t rows_on)
+      : p(m.p ? m.p + row * m.ld * kSize : nullptr), step(rows_on * m.ld * kSize) {
+    raw.load(nullptr, 0);
+  }
+  // the next row, if there is one (`here`), on its way; zeros if not
+  __device__ __forceinline__ void load(int col, int n, bool here) {
+    if (!p) return;
+    if constexpr (kWhole) {
+      if (!here) {
+        raw.load(nullptr, 0);
+      } else if (n > 0) {
+        raw.load(p + col * kSize, 8);
+      }
+    } else {
+      raw.load(p + col * kSize, here ? n : 0);
+    }
+    p += step;
+  }
+  __device__ __forceinline__ void store(int col, int n, bool here, const float (&v)[8]) {
+    if (p && here && n > 0) store_cols<8>(p, col, kType, kWhole ? 8 : n, v);
+    p += step;
+  }
+};
+
+// A parameter's 8 columns of a thread from shared memory, where it stands as [2][lanes] pieces
+// of 4 (reads of a wave without bank conflicts).
+__device__ __forceinline__ void share_param(const float* p, float none, float4* to, int lanes, int lane, int col, int n) {
+  float v[8];
+  load_param(p, col, n, none, v);
+  to[lane] = make_float4(v[0], v[1], v[2], v[3]);
+  to[lanes + lane] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void shared_param(const float4* from, int lanes, int lane, float (&v)[8]) {
+  const float4 a = from[lane], b = from[lanes + lane];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+  v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
+// The mean (layer) and 1 / deviation of a row; what is past its n columns does not count.
+template <bool kWhole, class S>
+__device__ __forceinline__ Stats held_stats(const NormOf& norm, float inv, int n, S& row_sum, const float (&v)[8]) {
+  auto counts = [&](int i) { return kWhole ? n > 0 : i < n; };
+  Stats s = {0.f, 1.f};
+  if (norm.kind == POINTID_NORM_LAYER) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += kWhole || counts(i) ? v[i] : 0.f;
+    s.mean = row_sum(kWhole && !counts(0) ? 0.f : sum) * inv;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float d = kWhole || counts(i) ? v[i] - s.mean : 0.f;
+    sum += d * d;
+  }
+  s.r = 1.f / sqrtf(row_sum(kWhole && !counts(0) ? 0.f : sum) * inv + norm.eps);
+  return s;
+}
+
+extern __shared__ float4 shared_floats[];
+
+// Where the parameters stand in shared memory, in blocks of 2 lanes pieces: the biases last, and
+// only where there are any.
+enum { kAfterWeight = 0, kGate = 1, kBeforeWeight = 2, kAfterBias = 3, kBeforeBias = 4 };
+template <class Args>
+__device__ __forceinline__ const float* param_of(const Args& a, int i) {
+  return i == kAfterWeight ? a.after.weight : i == kGate ? a.gate : i == kBeforeWeight ? a.before.weight
+         : i == kAfterBias ? a.after.bias : a.before.bias;
+}
+
+// kShared: the parameters wait in shared memory, for blocks of many rows.  What is not given
+// counts as ones and zeros.
+template <int kType, bool kSmall, bool kWhole, bool kBiases, bool kShared>
+__global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
+  __shared__ float2 waves[2][kMostWaves];
+  const int lanes = kSmall ? 16 : a.lanes, groups = blockDim.x / lanes, group = group_of<kSmall>(lanes);
+  const int lane = threadIdx.x - group * lanes, col = lane * 8, n = piece_cols(a.cols, col);
+  RowSum<kSmall> row_sum(waves, lanes);
+  const DropKey key(a.drop);
+  const float inv = 1.f / (float)a.cols;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  int64_t row = (int64_t)blockIdx.x * groups + group;
+  Stream<kType, kWhole> x(a.x, row, step), o(a.o, row, step), t(a.t, row, step), h(a.h, row, step);
+  o.load(col, n, row < a.rows);
+  x.load(col, n, row < a.rows);
+  if constexpr (kShared) {
+#pragma unroll
+    for (int i = 0; i < (kBiases ? 5 : 3); ++i)
+      if (i % groups == group)
+        share_param(param_of(a, i), i < 3 ? 1.f : 0.f, shared_floats + i * 2 * lanes, lanes, lane, col, n);
+    __syncthreads();
+  }
+  auto param = [&](int i, float (&v)[8]) {
+    if constexpr (kShared)
+      shared_param(shared_floats + i * 2 * lanes, lanes, lane, v);
+    else
+      load_param(param_of(a, i), col, n, i < 3 ? 1.f : 0.f, v);
+  };
+  // every group takes the same number of turns, as the sums need the whole block
+  for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step, row += step) {
+    const bool here = row < a.rows, more = row + step < a.rows;
+    float v[8], s[8], w[8];
+    o.raw.values(v);
+    x.raw.values(s);
+    // the next row is on its way while this one is worked on
+    o.load(col, n, more);
+    x.load(col, n, more);
+    Stats after = {0.f, 1.f}, before = {0.f, 1.f};
+    if (a.o.p) {
+      if (a.after.kind) {
+        after = held_stats<kWhole>(a.after, inv, n, row_sum, v);
+        param(kAfterWeight, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (v[i] - after.mean) * after.r * w[i];
+        if constexpr (kBiases) {
+          param(kAfterBias, w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += w[i];
+        }
+      }
+      if (a.drop.threshold) drop8(a.drop, key, row, col, v);
+      if (a.gate) {
+        param(kGate, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= w[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = a.scale * s[i] + v[i];
+      t.store(col, n, here, s);
+    }
+    if (a.h.p) {
+      before = held_stats<kWhole>(a.before, inv, n, row_sum, s);
+      param(kBeforeWeight, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = (s[i] - before.mean) * before.r * w[i];
+      if constexpr (kBiases) {
+        param(kBeforeBias, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += w[i];
+      }
+      h.store(col, n, here, s);
+    }
+    if (a.stats && lane == 0 && here)
       reinterpret_cast<float4*>(a.stats)[row] = make_float4(after.mean, after.r, before.mean, before.r);
   }
 }
@@ -284,10 +479,143 @@ __global__ void __launch_bounds__(256) norm_back_kernel(NormBackArgs a) {
   }
 }
 
-// The sums of the blocks' sums: 32 columns of one parameter a block, 8 of the partial rows
+// Both passes and the column sums with the rows held in registers; each block takes every
+// gridDim-th set of rows, one of each of its groups, and leaves its sums.  A norm that there is
+// not has the mean 0, the deviation 1, and means of its gradient that count as 0.
+template <int kType, bool kSmall, bool kWhole, bool kBiases, int kMost>
+__global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
+  __shared__ float2 waves[2][kMostWaves];
+  const int lanes = kSmall ? 16 : a.lanes, groups = blockDim.x / lanes, group = group_of<kSmall>(lanes);
+  const int lane = threadIdx.x - group * lanes, col = lane * 8, n = piece_cols(a.cols, col);
+  RowSum<kSmall> row_sum(waves, lanes);
+  const DropKey key(a.drop);
+  const float inv = 1.f / (float)a.cols;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  int64_t row = (int64_t)blockIdx.x * groups + group;
+  Stream<kType, kWhole> dh(a.dh, row, step), t(a.t, row, step), dt(a.dt, row, step), o(a.o, row, step);
+  Stream<kType, kWhole> dx(a.dx, row, step), dout(a.dout, row, step);
+  float4 next;
+  auto load = [&](int64_t r) {
+    const bool here = r < a.rows;
+    dh.load(col, n, here);
+    t.load(col, n, here);
+    dt.load(col, n, here);
+    o.load(col, n, here);
+    next = a.stats && here ? reinterpret_cast<const float4*>(a.stats)[r] : make_float4(0.f, 1.f, 0.f, 1.f);
+  };
+  load(row);
+#pragma unroll
+  for (int i = 0; i < (kBiases ? 4 : 3); ++i)
+    if (i % groups == group)
+      share_param(param_of(a, i), i < 3 ? 1.f : 0.f, shared_floats + i * 2 * lanes, lanes, lane, col, n);
+  __syncthreads();
+  auto param = [&](int i, float (&v)[8]) { shared_param(shared_floats + i * 2 * lanes, lanes, lane, v); };
+  float total[kNormSums][8] = {};
+  for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step, row += step) {
+    const bool here = row < a.rows;
+    float e[8], u[8], d[8], w[8], v[8];
+    const float4 st = a.after.kind ? next : make_float4(0.f, 1.f, next.z, next.w);
+    dh.raw.values(e);
+    t.raw.values(u);
+    dt.raw.values(d);
+    o.raw.values(v);
+    load(row + step);
+    if (a.before.kind) {
+      float se = 0.f, seu = 0.f;
+      param(kBeforeWeight, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u[i] = (u[i] - st.z) * st.w;
+        total[0][i] += e[i] * u[i];
+        if constexpr (kBiases) total[1][i] += e[i];
+        e[i] *= w[i];
+        se += e[i];
+        seu += e[i] * u[i];
+      }
+      const bool layer = a.before.kind == POINTID_NORM_LAYER;
+      const float2 s = layer ? row_sum(se, seu) : make_float2(0.f, row_sum(seu));
+      const float on_u = st.w * (s.y * inv), on_1 = st.w * (s.x * inv);
+      // of columns and rows that do not exist nothing is added
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[i] += st.w * e[i] - on_u * u[i] - on_1;
+        if constexpr (!kWhole) d[i] = i < n && here ? d[i] : 0.f;
+      }
+      if constexpr (kWhole)
+        if (!here || n == 0)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = a.scale * d[i];
+    dx.store(col, n, here, u);
+    if (!a.o.p && !a.dout.p) continue;
+    if (a.drop.threshold) drop8(a.drop, key, row, col, d);
+    param(kAfterWeight, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = (v[i] - st.x) * st.y;
+      u[i] = v[i] * w[i];
+    }
+    if constexpr (kBiases) {
+      float b[8];
+      param(kAfterBias, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] += b[i];
+    }
+    float g[8];
+    param(kGate, g);
+    float sf = 0.f, sfv = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      total[4][i] += d[i] * u[i];
+      d[i] *= g[i];
+      total[2][i] += d[i] * v[i];
+      if constexpr (kBiases) total[3][i] += d[i];
+      d[i] *= w[i];
+      sf += d[i];
+      sfv += d[i] * v[i];
+    }
+    if (!a.dout.p) continue;
+    if (a.after.kind) {
+      const bool layer = a.after.kind == POINTID_NORM_LAYER;
+      const float2 s = layer ? row_sum(sf, sfv) : make_float2(0.f, row_sum(sfv));
+      const float on_v = st.y * (s.y * inv), on_1 = st.y * (s.x * inv);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = st.y * d[i] - on_v * v[i] - on_1;
+    }
+    dout.store(col, n, here, d);
+  }
+  // the groups' sums, in order; by halves, as the parameters stand
+  int wanted = 0, slot = 0;
+  for (int s = 0; s < kNormSums; ++s) wanted += a.out[s] != nullptr;
+#pragma unroll
+  for (int s = 0; s < kNormSums; ++s) {
+    if (!a.out[s]) continue;
+    float* const out = a.part + ((int64_t)blockIdx.x * wanted + slot) * a.cols;
+    ++slot;
+    if (groups > 1) {
+      __syncthreads();
+      float4* const mine = shared_floats + group * 2 * lanes;
+      mine[lane] = make_float4(total[s][0], total[s][1], total[s][2], total[s][3]);
+      mine[lanes + lane] = make_float4(total[s][4], total[s][5], total[s][6], total[s][7]);
+      __syncthreads();
+      if (group != 0) continue;
+      for (int g = 1; g < groups; ++g) {
+        float v[8];
+        shared_param(shared_floats + g * 2 * lanes, lanes, lane, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) total[s][i] += v[i];
+      }
+    }
+    store_cols<8>(out, col, POINTID_FP32, n, total[s]);
+  }
+}
+
+// The sums of the blocks' sums: 32 columns of one parameter a block, 32 of the partial rows
 // at a time, added in order.
-__global__ void __launch_bounds__(256) norm_sums_kernel(NormBackArgs a) {
-  __shared__ float sums[8][33];
+__global__ void __launch_bounds__(1024) norm_sums_kernel(NormBackArgs a) {
+  __shared__ float sums[32][33];
   int wanted = 0, which = 0, at = 0;
   for (int s = 0; s < kNormSums; ++s) {
     if (!a.out[s]) continue;
@@ -299,34 +627,92 @@ __global__ void __launch_bounds__(256) norm_sums_kernel(NormBackArgs a) {
   float t = 0.f;
   if (col < a.cols)
 #pragma unroll 4
-    for (int b = sub; b < a.blocks; b += 8) t += a.part[((int64_t)b * wanted + at) * a.cols + col];
+    for (int b = sub; b < a.blocks; b += 32) t += a.part[((int64_t)b * wanted + at) * a.cols + col];
   sums[sub][c] = t;
   __syncthreads();
   if (sub != 0 || col >= a.cols) return;
   t = 0.f;
 #pragma unroll
-  for (int s = 0; s < 8; ++s) t += sums[s][c];
+  for (int s = 0; s < 32; ++s) t += sums[s][c];
   a.out[which][col] = t;
 }
 
 unsigned row_blocks(int64_t rows) { return (unsigned)(rows < 65536 ? rows : 65536); }
 
+// Columns that a block can hold of a row, 8 a thread.
+constexpr int64_t kHeldCols = 8192;
+// Threads of a row that is held (16, or whole waves), and the groups of them in a block of at
+// most `threads`, or one.
+struct HeldShape {
+  int lanes, groups;
+};
+HeldShape held_shape(int64_t cols, int threads) {
+  const int lanes = cols <= 128 ? 16 : (int)((cols + 511) / 512) * 64;
+  return {lanes, lanes < threads ? threads / lanes : 1};
+}
+// Threads of a block of the backward pass: 768 leave each 168 registers, which the sums of biases
+// and fp32 rows take; 1024 leave 128.  768 and 1024: bf16 16384 x 4096 with biases 160 us and 235,
+// fp32 8192 x 4096 without 166 and 175, bf16 300000 x 100 without 175 and 152.
+int back_threads(int dtype, bool biases, int64_t cols) {
+  return (biases || dtype == POINTID_FP32) && cols <= 6144 ? 768 : 1024;
+}
+
+// f with its template arguments' truth values as constants
+template <class F>
+hipError_t with_flags(bool a, bool b, bool c, F&& f) {
+  auto on = [&](auto x, auto y) { return c ? f(x, y, std::true_type{}) : f(x, y, std::false_type{}); };
+  auto up = [&](auto x) { return b ? on(x, std::true_type{}) : on(x, std::false_type{}); };
+  return a ? up(std::true_type{}) : up(std::false_type{});
+}
+
+template <int kType>
+hipError_t launch_norm_of(NormArgs a, hipStream_t stream) {
+  if (a.cols > kHeldCols) return launch_kernel(norm_kernel<kType>, dim3(row_blocks(a.rows)), dim3(256), 0, stream, a);
+  const HeldShape h = held_shape(a.cols, 256);
+  a.lanes = h.lanes;
+  const bool biases = a.after.bias || a.before.bias;
+  const int64_t need = (a.rows + h.groups - 1) / h.groups;
+  // Many rows: blocks of at least 8 sets of rows, with the parameters in shared memory.  bf16, both
+  // norms and a gate, read from memory for every row and shared: 16384 x 4096 121 us and 104, 8192 x
+  // 4096 59 and 49, 8192 x 8192 150 and 105; fp32 8192 x 4096 113 and 104.
+  const bool shared = need >= 4096;
+  int64_t blocks = need < 65536 ? need : 65536;
+  if (shared) blocks = need / 8 < 4096 ? need / 8 : 4096;
+  auto go = [&](auto kernel, size_t bytes) {
+    return launch_kernel(kernel, dim3((unsigned)blocks), dim3(h.lanes * h.groups), bytes, stream, a);
+  };
+  return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
+    if (shared) return go(norm_rows_kernel<kType, small, whole, bias, true>, (size_t)(biases ? 5 : 3) * h.lanes * 32);
+    return go(norm_rows_kernel<kType, small, whole, bias, false>, 0);
+  });
+}
+
 }  // namespace
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
-  const dim3 grid(row_blocks(a.rows));
   switch (a.dtype) {
-    case POINTID_FP32: return launch_kernel(norm_kernel<POINTID_FP32>, grid, dim3(256), 0, stream, a);
-    case POINTID_BF16: return launch_kernel(norm_kernel<POINTID_BF16>, grid, dim3(256), 0, stream, a);
+    case POINTID_FP32: return launch_norm_of<POINTID_FP32>(a, stream);
+    case POINTID_BF16: return launch_norm_of<POINTID_BF16>(a, stream);
   }
-  return launch_kernel(norm_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
+  return launch_norm_of<POINTID_FP16>(a, stream);
 }
 
+namespace {
+bool has_biases(const NormBackArgs& a) { return a.out[1] || a.out[3] || a.after.bias; }
+}  // namespace
+
 NormBackPlan plan_norm_back(const NormBackArgs& a, int cus) {
-  const int64_t strips = (a.cols + 255) / 256, most = (a.rows + 31) / 32, want = (8 * cus + strips - 1) / strips;
+  const int64_t rows = a.rows, cols = a.cols;
   NormBackPlan p;
-  p.blocks = (int32_t)(most < want ? most : want);
-  p.means = a.before.kind || (a.after.kind && a.dout.p);
+  p.held = cols <= kHeldCols;
+  if (p.held) {
+    const int groups = held_shape(cols, back_threads(a.dtype, has_biases(a), cols)).groups;
+    const int64_t need = (rows + groups - 1) / groups, most = cus;
+    p.blocks = (int32_t)(need < most ? need : most);
+  } else {
+    const int64_t strips = (cols + 255) / 256, most = (rows + 31) / 32, want = (8 * cus + strips - 1) / strips;
+    p.blocks = (int32_t)(most < want ? most : want);
+  }
   return p;
 }
 
@@ -339,19 +725,40 @@ hipError_t launch_norm_means(const NormBackArgs& a, hipStream_t stream) {
   return launch_kernel(norm_means_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
 }
 
-hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.cols + 255) / 256), (unsigned)a.blocks);
+namespace {
+template <int kType>
+hipError_t launch_norm_back_of(NormBackArgs a, bool held, hipStream_t stream) {
+  if (!held)
+    return launch_kernel(norm_back_kernel<kType>, dim3((unsigned)((a.cols + 255) / 256), (unsigned)a.blocks), dim3(256), 0,
+                         stream, a);
+  const bool biases = has_biases(a);
+  const int threads = back_threads(kType, biases, a.cols);
+  const HeldShape h = held_shape(a.cols, threads);
+  a.lanes = h.lanes;
+  const int shared = biases ? 4 : 3;             // the parameters, or the groups' sums
+  return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
+    auto go = [&](auto kernel) {
+      return launch_kernel(kernel, dim3((unsigned)a.blocks), dim3(h.lanes * h.groups),
+                           (size_t)(shared > h.groups ? shared : h.groups) * h.lanes * 32, stream, a);
+    };
+    if (threads == 768) return go(norm_back_rows_kernel<kType, small, whole, bias, 768>);
+    return go(norm_back_rows_kernel<kType, small, whole, bias, 1024>);
+  });
+}
+}  // namespace
+
+hipError_t launch_norm_back(const NormBackArgs& a, bool held, hipStream_t stream) {
   switch (a.dtype) {
-    case POINTID_FP32: return launch_kernel(norm_back_kernel<POINTID_FP32>, grid, dim3(256), 0, stream, a);
-    case POINTID_BF16: return launch_kernel(norm_back_kernel<POINTID_BF16>, grid, dim3(256), 0, stream, a);
+    case POINTID_FP32: return launch_norm_back_of<POINTID_FP32>(a, held, stream);
+    case POINTID_BF16: return launch_norm_back_of<POINTID_BF16>(a, held, stream);
   }
-  return launch_kernel(norm_back_kernel<POINTID_FP16>, grid, dim3(256), 0, stream, a);
+  return launch_norm_back_of<POINTID_FP16>(a, held, stream);
 }
 
 hipError_t launch_norm_sums(const NormBackArgs& a, hipStream_t stream) {
   int wanted = 0;
   for (int s = 0; s < kNormSums; ++s) wanted += a.out[s] != nullptr;
-  return launch_kernel(norm_sums_kernel, dim3((unsigned)((a.cols + 31) / 32), (unsigned)wanted), dim3(256), 0, stream,
+  return launch_kernel(norm_sums_kernel, dim3((unsigned)((a.cols + 31) / 32), (unsigned)wanted), dim3(1024), 0, stream,
                        a);
 }
 

@@ -39,6 +39,10 @@ int check_block(const pointid_block& b) {
   if (!std::isfinite(b.scale)) return set_error(POINTID_EINVAL, "scale must be finite");
   return check_drop(b.drop);
 }
+int check_scale(float scale) {
+  if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return set_error(POINTID_EINVAL, "scale must be in [2^-64, 2^64]");
+  return POINTID_OK;
+}
 int check_scratch(const void* scratch) {
   if (reinterpret_cast<uintptr_t>(scratch) % 256) return set_error(POINTID_EINVAL, "scratch is not aligned to 256 bytes");
   return POINTID_OK;
@@ -142,11 +146,12 @@ int pointid_norm(pointid_layers l, int dtype, int64_t m, int64_t n, const pointi
 
 uint64_t pointid_norm_backward_scratch(pointid_layers l, int64_t m, int64_t n) {
   if (!l || m < 0 || m > kMaxRows || n < 1 || n > kMaxCols) return 0;
+  // the most blocks that any such call has
   NormBackArgs a;
   std::memset(static_cast<void*>(&a), 0, sizeof(a));
-  a.rows = m, a.cols = n;
+  a.rows = m, a.cols = n, a.dtype = POINTID_FP32;
   const NormBackPlan plan = plan_norm_back(a, l->cus);
-  return pad256(means_bytes(m)) + pad256(sums_bytes(plan.blocks, kNormSums, n));
+  return (plan.held ? 0 : pad256(means_bytes(m))) + pad256(sums_bytes(plan.blocks, kNormSums, n));
 }
 
 int pointid_norm_backward(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix* dh,
@@ -200,12 +205,13 @@ int pointid_norm_backward(pointid_layers l, int dtype, int64_t m, int64_t n, con
     Call call(l, static_cast<hipStream_t>(stream), scratch, scratch_bytes);
     const NormBackPlan plan = plan_norm_back(a, l->cus);
     a.blocks = plan.blocks;
-    if (plan.means) call.want(&a.means, means_bytes(m));
+    const bool means = !plan.held && (has(norm) || after);
+    if (means) call.want(&a.means, means_bytes(m));
     if (wanted) call.want(&a.part, sums_bytes(plan.blocks, wanted, n));
     TRY(call.reserve());
     if (m > 0) {
-      if (plan.means) TRY(call.run("norm_means", false, [&] { return launch_norm_means(a, call.stream()); }));
-      TRY(call.run("norm_back", !wanted, [&] { return launch_norm_back(a, call.stream()); }));
+      if (means) TRY(call.run("norm_means", false, [&] { return launch_norm_means(a, call.stream()); }));
+      TRY(call.run("norm_back", !wanted, [&] { return launch_norm_back(a, plan.held, call.stream()); }));
     }
     if (!wanted) return (int)POINTID_OK;
     return call.run("norm_sums", true, [&] { return launch_norm_sums(a, call.stream()); });
@@ -224,7 +230,7 @@ int pointid_logprobs(pointid_layers l, int dtype, int64_t m, int64_t n, const po
                      float* top_logp, void* scratch, uint64_t scratch_bytes, void* stream) {
   return guarded([&] {
     TRY(check_call(l, dtype, m, n));
-    if (!(scale > 0.f) || std::isinf(scale)) return set_error(POINTID_EINVAL, "scale must be positive and finite");
+    TRY(check_scale(scale));
     if (top < 0 || top > kMaxTop || top > n) return set_error(POINTID_EINVAL, "top must be in [0, 64] and at most n");
     TRY(check_scratch(scratch));
     if (m == 0) return (int)POINTID_OK;
@@ -265,7 +271,7 @@ int pointid_logprobs_backward(pointid_layers l, int dtype, int64_t m, int64_t n,
                               const pointid_matrix* dlogits, void* stream) {
   return guarded([&] {
     TRY(check_call(l, dtype, m, n));
-    if (!(scale > 0.f) || std::isinf(scale)) return set_error(POINTID_EINVAL, "scale must be positive and finite");
+    TRY(check_scale(scale));
     if (m == 0) return (int)POINTID_OK;
     TRY(check_matrix(logits, "logits", dtype, m, n));
     TRY(check_matrix(dlogits, "dlogits", dtype, m, n));

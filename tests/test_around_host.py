@@ -178,7 +178,7 @@ def test_binding_refusals(b):
     with pytest.raises(ValueError, match="device"):
         b.pointid_logprobs_backward(layers, x, x[:, 0])
     with pytest.raises(TypeError):
-        b._vector(torch.zeros(2, dtype=torch.int64), "targets", torch.int32, 2, 0)
+        b._vector(torch.zeros(2, dtype=torch.int64), "targets", 2, 0, torch.int32)
     layers._raw = None
 
 

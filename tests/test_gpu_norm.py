@@ -205,6 +205,18 @@ def test_zeros_infinities_and_nans(pid, layers):
     assert (h[0] == 0).all() and h[1].isnan().all() and h[2].isnan().all() and torch.isfinite(h[3:]).all()
 
 
+@pytest.mark.parametrize("n", [72, 9000])
+def test_statistics_of_norms_that_are_not_there_are_not_read(pid, layers, n):
+    for form, absent in ((("rms", None, False, True, 1.0, 0.0), slice(0, 2)), ((None, "layer", True, True, 1.0, 0.0), slice(2, 4))):
+        j = Joint(pid, "bf16", 40, n, form)
+        got = pid.pointid_norm(layers, j.dev(j.x), j.norm(), j.block(), keep=True)
+        stats = got.stats.clone()
+        stats[:, absent] = math.nan
+        back = pid.pointid_norm_backward(layers, j.dev(j.dh) if j.before else None, got.total if j.before else None, stats,
+                                         j.norm(), j.block(), dtotal=j.dev(j.dt))
+        j.check_backward(back, got.stats.cpu(), got.total.cpu() if j.before else None, what=str(form))
+
+
 def test_no_rows(pid, layers):
     x = torch.empty((0, 24), device=DEV)
     norm = pid.Norm("rms", torch.ones(24, device=DEV), torch.ones(24, device=DEV))
