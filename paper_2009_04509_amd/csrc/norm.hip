@@ -165,35 +165,41 @@ __device__ __forceinline__ int group_of(int lanes) {
   return __builtin_amdgcn_readfirstlane((int)threadIdx.x / lanes);
 }
 
-// A thread's 8 columns of one matrix, row after row.  kWhole: rows are whole pieces of 8.
-template <int kType, bool kWhole>
+// A thread's columns of one matrix, row after row: kPieces pieces of 8, a row's threads apart.
+// kWhole: rows are whole pieces of 8.
+template <int kType, bool kWhole, int kPieces>
 struct Stream {
   static constexpr int64_t kSize = kType == POINTID_FP32 ? 4 : 2;
   char* p;                     // the next row's first column, nullptr without a matrix
   int64_t step;                // bytes to the group's row after it
-  Raw8<kType> raw;
+  Raw8<kType> raw[kPieces];
   __device__ __forceinline__ Stream(const Rows& m, int64_t row, int64_t rows_on)
       : p(m.p ? m.p + row * m.ld * kSize : nullptr), step(rows_on * m.ld * kSize) {
-    raw.load(nullptr, 0);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) raw[i].load(nullptr, 0);
   }
   // the next row, if there is one (`here`), on its way; zeros if not
-  __device__ __forceinline__ void load(int col, int n, bool here) {
+  __device__ __forceinline__ void load(const int (&col)[kPieces], const int (&n)[kPieces], bool here) {
     if (!p) return;
-    if constexpr (kWhole) {
-      if (!here) {
-        raw.load(nullptr, 0);
-      } else if (n > 0) {
-        raw.load(p + col * kSize, 8);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      if constexpr (kWhole) {
+        if (!here) {
+          raw[i].load(nullptr, 0);
+        } else if (n[i] > 0) {
+          raw[i].load(p + col[i] * kSize, 8);
+        }
+      } else {
+        raw[i].load(p + col[i] * kSize, here ? n[i] : 0);
       }
-    } else {
-      raw.load(p + col * kSize, here ? n : 0);
     }
     p += step;
   }
-  __device__ __forceinline__ void store(int col, int n, bool here, const float (&v)[8]) {
+  // one piece of the row that `next` goes on from
+  __device__ __forceinline__ void store(int col, int n, bool here, const float (&v)[8]) const {
     if (p && here && n > 0) store_cols<8>(p, col, kType, kWhole ? 8 : n, v);
-    p += step;
   }
+  __device__ __forceinline__ void next() { p += step; }
 };
 
 // A parameter's 8 columns of a thread from shared memory, where it stands as [2][lanes] pieces
@@ -210,24 +216,34 @@ __device__ __forceinline__ void shared_param(const float4* from, int lanes, int 
   v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 
-// The mean (layer) and 1 / deviation of a row; what is past its n columns does not count.
-template <bool kWhole, class S>
-__device__ __forceinline__ Stats held_stats(const NormOf& norm, float inv, int n, S& row_sum, const float (&v)[8]) {
-  auto counts = [&](int i) { return kWhole ? n > 0 : i < n; };
+// The mean (layer) and 1 / deviation of a row; what is past its columns does not count.
+template <bool kWhole, int kPieces, class S>
+__device__ __forceinline__ Stats held_stats(const NormOf& norm, float inv, const int (&n)[kPieces], S& row_sum,
+                                            const float (&v)[kPieces][8]) {
   Stats s = {0.f, 1.f};
   if (norm.kind == POINTID_NORM_LAYER) {
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += kWhole || counts(i) ? v[i] : 0.f;
-    s.mean = row_sum(kWhole && !counts(0) ? 0.f : sum) * inv;
+    for (int p = 0; p < kPieces; ++p) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t += kWhole || i < n[p] ? v[p][i] : 0.f;
+      sum += n[p] > 0 ? t : 0.f;
+    }
+    s.mean = row_sum(sum) * inv;
   }
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float d = kWhole || counts(i) ? v[i] - s.mean : 0.f;
-    sum += d * d;
+  for (int p = 0; p < kPieces; ++p) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float d = kWhole || i < n[p] ? v[p][i] - s.mean : 0.f;
+      t += d * d;
+    }
+    sum += n[p] > 0 ? t : 0.f;
   }
-  s.r = 1.f / sqrtf(row_sum(kWhole && !counts(0) ? 0.f : sum) * inv + norm.eps);
+  s.r = 1.f / sqrtf(row_sum(sum) * inv + norm.eps);
   return s;
 }
 
@@ -244,38 +260,60 @@ __device__ __forceinline__ const float* param_of(const Args& a, int i) {
 
 // kShared: the parameters wait in shared memory, for blocks of many rows.  What is not given
 // counts as ones and zeros.
-template <int kType, bool kSmall, bool kWhole, bool kBiases, bool kShared>
+template <int kType, bool kSmall, bool kWhole, bool kBiases, bool kShared, int kPieces>
 __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
+  static_assert(!kShared || kPieces == 1, "parameters of one piece a thread");
   __shared__ float2 waves[2][kMostWaves];
   const int lanes = kSmall ? 16 : a.lanes, groups = blockDim.x / lanes, group = group_of<kSmall>(lanes);
-  const int lane = threadIdx.x - group * lanes, col = lane * 8, n = piece_cols(a.cols, col);
+  const int lane = threadIdx.x - group * lanes;
+  int col[kPieces], n[kPieces];
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) {
+    col[p] = (p * lanes + lane) * 8;
+    n[p] = piece_cols(a.cols, col[p]);
+  }
   RowSum<kSmall> row_sum(waves, lanes);
   const DropKey key(a.drop);
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
-  Stream<kType, kWhole> x(a.x, row, step), o(a.o, row, step), t(a.t, row, step), h(a.h, row, step);
+  Stream<kType, kWhole, kPieces> x(a.x, row, step), o(a.o, row, step), t(a.t, row, step), h(a.h, row, step);
   o.load(col, n, row < a.rows);
   x.load(col, n, row < a.rows);
   if constexpr (kShared) {
 #pragma unroll
     for (int i = 0; i < (kBiases ? 5 : 3); ++i)
       if (i % groups == group)
-        share_param(param_of(a, i), i < 3 ? 1.f : 0.f, shared_floats + i * 2 * lanes, lanes, lane, col, n);
+        share_param(param_of(a, i), i < 3 ? 1.f : 0.f, shared_floats + i * 2 * lanes, lanes, lane, col[0], n[0]);
     __syncthreads();
   }
-  auto param = [&](int i, float (&v)[8]) {
+  auto param = [&](int i, int p, float (&v)[8]) {
     if constexpr (kShared)
       shared_param(shared_floats + i * 2 * lanes, lanes, lane, v);
     else
-      load_param(param_of(a, i), col, n, i < 3 ? 1.f : 0.f, v);
+      load_param(param_of(a, i), col[p], n[p], i < 3 ? 1.f : 0.f, v);
+  };
+  // (v - mean) r weight + bias
+  auto affine = [&](float (&v)[8], const Stats& s, int weight, int bias, int p) {
+    float w[8];
+    param(weight, p, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (v[i] - s.mean) * s.r * w[i];
+    if constexpr (kBiases) {
+      param(bias, p, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += w[i];
+    }
   };
   // every group takes the same number of turns, as the sums need the whole block
   for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step, row += step) {
     const bool here = row < a.rows, more = row + step < a.rows;
-    float v[8], s[8], w[8];
-    o.raw.values(v);
-    x.raw.values(s);
+    float v[kPieces][8], s[kPieces][8];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      o.raw[p].values(v[p]);
+      x.raw[p].values(s[p]);
+    }
     // the next row is on its way while this one is worked on
     o.load(col, n, more);
     x.load(col, n, more);
@@ -283,36 +321,32 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
     if (a.o.p) {
       if (a.after.kind) {
         after = held_stats<kWhole>(a.after, inv, n, row_sum, v);
-        param(kAfterWeight, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (v[i] - after.mean) * after.r * w[i];
-        if constexpr (kBiases) {
-          param(kAfterBias, w);
+        for (int p = 0; p < kPieces; ++p) affine(v[p], after, kAfterWeight, kAfterBias, p);
+      }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] += w[i];
+      for (int p = 0; p < kPieces; ++p) {
+        if (a.drop.threshold) drop8(a.drop, key, row, col[p], v[p]);
+        if (a.gate) {
+          float w[8];
+          param(kGate, p, w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[p][i] *= w[i];
         }
-      }
-      if (a.drop.threshold) drop8(a.drop, key, row, col, v);
-      if (a.gate) {
-        param(kGate, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= w[i];
+        for (int i = 0; i < 8; ++i) s[p][i] = a.scale * s[p][i] + v[p][i];
+        t.store(col[p], n[p], here, s[p]);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = a.scale * s[i] + v[i];
-      t.store(col, n, here, s);
+      t.next();
     }
     if (a.h.p) {
       before = held_stats<kWhole>(a.before, inv, n, row_sum, s);
-      param(kBeforeWeight, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = (s[i] - before.mean) * before.r * w[i];
-      if constexpr (kBiases) {
-        param(kBeforeBias, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += w[i];
+      for (int p = 0; p < kPieces; ++p) {
+        affine(s[p], before, kBeforeWeight, kBeforeBias, p);
+        h.store(col[p], n[p], here, s[p]);
       }
-      h.store(col, n, here, s);
+      h.next();
     }
     if (a.stats && lane == 0 && here)
       reinterpret_cast<float4*>(a.stats)[row] = make_float4(after.mean, after.r, before.mean, before.r);
@@ -487,20 +521,21 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
   __shared__ float2 waves[2][kMostWaves];
   const int lanes = kSmall ? 16 : a.lanes, groups = blockDim.x / lanes, group = group_of<kSmall>(lanes);
   const int lane = threadIdx.x - group * lanes, col = lane * 8, n = piece_cols(a.cols, col);
+  const int cols[1] = {col}, ns[1] = {n};
   RowSum<kSmall> row_sum(waves, lanes);
   const DropKey key(a.drop);
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
-  Stream<kType, kWhole> dh(a.dh, row, step), t(a.t, row, step), dt(a.dt, row, step), o(a.o, row, step);
-  Stream<kType, kWhole> dx(a.dx, row, step), dout(a.dout, row, step);
+  Stream<kType, kWhole, 1> dh(a.dh, row, step), t(a.t, row, step), dt(a.dt, row, step), o(a.o, row, step);
+  Stream<kType, kWhole, 1> dx(a.dx, row, step), dout(a.dout, row, step);
   float4 next;
   auto load = [&](int64_t r) {
     const bool here = r < a.rows;
-    dh.load(col, n, here);
-    t.load(col, n, here);
-    dt.load(col, n, here);
-    o.load(col, n, here);
+    dh.load(cols, ns, here);
+    t.load(cols, ns, here);
+    dt.load(cols, ns, here);
+    o.load(cols, ns, here);
     next = a.stats && here ? reinterpret_cast<const float4*>(a.stats)[r] : make_float4(0.f, 1.f, 0.f, 1.f);
   };
   load(row);
@@ -515,10 +550,10 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
     const bool here = row < a.rows;
     float e[8], u[8], d[8], w[8], v[8];
     const float4 st = a.after.kind ? next : make_float4(0.f, 1.f, next.z, next.w);
-    dh.raw.values(e);
-    t.raw.values(u);
-    dt.raw.values(d);
-    o.raw.values(v);
+    dh.raw[0].values(e);
+    t.raw[0].values(u);
+    dt.raw[0].values(d);
+    o.raw[0].values(v);
     load(row + step);
     if (a.before.kind) {
       float se = 0.f, seu = 0.f;
@@ -549,6 +584,7 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = a.scale * d[i];
     dx.store(col, n, here, u);
+    dx.next();
     if (!a.o.p && !a.dout.p) continue;
     if (a.drop.threshold) drop8(a.drop, key, row, col, d);
     param(kAfterWeight, w);
@@ -585,6 +621,7 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
       for (int i = 0; i < 8; ++i) d[i] = st.y * d[i] - on_v * v[i] - on_1;
     }
     dout.store(col, n, here, d);
+    dout.next();
   }
   // the groups' sums, in order; by halves, as the parameters stand
   int wanted = 0, slot = 0;
@@ -667,23 +704,25 @@ hipError_t with_flags(bool a, bool b, bool c, F&& f) {
 
 template <int kType>
 hipError_t launch_norm_of(NormArgs a, hipStream_t stream) {
-  if (a.cols > kHeldCols) return launch_kernel(norm_kernel<kType>, dim3(row_blocks(a.rows)), dim3(256), 0, stream, a);
-  const HeldShape h = held_shape(a.cols, 256);
-  a.lanes = h.lanes;
+  if (a.cols > 2 * kHeldCols) return launch_kernel(norm_kernel<kType>, dim3(row_blocks(a.rows)), dim3(256), 0, stream, a);
   const bool biases = a.after.bias || a.before.bias;
+  const bool two = a.cols > kHeldCols;           // pieces a thread
+  const HeldShape h = held_shape(two ? (a.cols + 1) / 2 : a.cols, 256);
+  a.lanes = h.lanes;
   const int64_t need = (a.rows + h.groups - 1) / h.groups;
   // Many rows: blocks of at least 8 sets of rows, with the parameters in shared memory.  bf16, both
   // norms and a gate, read from memory for every row and shared: 16384 x 4096 121 us and 104, 8192 x
   // 4096 59 and 49, 8192 x 8192 150 and 105; fp32 8192 x 4096 113 and 104.
-  const bool shared = need >= 4096;
+  const bool shared = need >= 4096 && !two;
   int64_t blocks = need < 65536 ? need : 65536;
   if (shared) blocks = need / 8 < 4096 ? need / 8 : 4096;
   auto go = [&](auto kernel, size_t bytes) {
     return launch_kernel(kernel, dim3((unsigned)blocks), dim3(h.lanes * h.groups), bytes, stream, a);
   };
   return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
-    if (shared) return go(norm_rows_kernel<kType, small, whole, bias, true>, (size_t)(biases ? 5 : 3) * h.lanes * 32);
-    return go(norm_rows_kernel<kType, small, whole, bias, false>, 0);
+    if (shared) return go(norm_rows_kernel<kType, small, whole, bias, true, 1>, (size_t)(biases ? 5 : 3) * h.lanes * 32);
+    if (two) return go(norm_rows_kernel<kType, false, whole, bias, false, 2>, 0);
+    return go(norm_rows_kernel<kType, small, whole, bias, false, 1>, 0);
   });
 }
 
@@ -741,8 +780,11 @@ hipError_t launch_norm_back_of(NormBackArgs a, bool held, hipStream_t stream) {
       return launch_kernel(kernel, dim3((unsigned)a.blocks), dim3(h.lanes * h.groups),
                            (size_t)(shared > h.groups ? shared : h.groups) * h.lanes * 32, stream, a);
     };
-    if (threads == 768) return go(norm_back_rows_kernel<kType, small, whole, bias, 768>);
-    return go(norm_back_rows_kernel<kType, small, whole, bias, 1024>);
+    if constexpr (bias || kType == POINTID_FP32) {
+      if constexpr (small) return go(norm_back_rows_kernel<kType, small, whole, bias, 768>);
+      if (threads == 768) return go(norm_back_rows_kernel<kType, small, whole, bias, 768>);
+    }
+    if constexpr (!(small && (bias || kType == POINTID_FP32))) return go(norm_back_rows_kernel<kType, small, whole, bias, 1024>);
   });
 }
 }  // namespace

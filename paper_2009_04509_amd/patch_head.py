@@ -1,6 +1,7 @@
 """A small patch classifier trained with the library's layers.
 
     python -m paper_2009_04509_amd.patch_head [--steps N] [--batch B] [--dtype bf16|fp16|fp32] [--kept 8bit|type]
+                                             [--block plain|normed] [--dropout P]
 
 The classifier has the heads of the network of paper §2.2 (softmax over track, shower and
 none, a sigmoid for Michel) on a dense layer over the patch's 2,304 pixels and a gated
@@ -15,6 +16,9 @@ Every layer and gradient is one call of the library.  With ``kept="8bit"`` what 
 reads (x, z1, a1, g, u, h, a2) is kept in 8-bit checkpoints: the pre-activations are
 written so by the forward layers themselves.  Only the loss over the 4 outputs and the
 update of the parameters are torch.
+
+``--block normed`` has norms and dropout around the gated block, and the softmax branch's
+loss and its gradient by the library's log probabilities (NormedPatchHead).
 """
 
 from __future__ import annotations
@@ -143,6 +147,93 @@ class PatchHead:
         return value
 
 
+class NormedPatchHead(PatchHead):
+    """The classifier with norms (root mean square) before and after the gated block, a gate on its
+    output, and dropout as in paper §2.2 after the dense layer and on the block's output:
+
+        a1  = drop(relu(x w1 + b1))
+        n1  = norm(a1, s1)
+        h   = silu(n1 wg) * (n1 wu)
+        t   = a1 + gate * drop(norm(h wd + bd, sa))
+        n2  = norm(t, s2)
+        out = n2 wo + bo
+
+    The norms read what they need for their gradients in its own type.  The masks are made again
+    in the backward pass, from the step's number."""
+
+    def __init__(self, device: int = 0, hidden: int = 512, gated: int = 1536, dtype: str = "bf16", kept: str = "8bit",
+                 seed: int = 0, dropout: float = 0.1):
+        super().__init__(device, hidden, gated, dtype, kept, seed)
+        self.p_drop, self.seed, self.steps = dropout, seed, 0
+        for name, value in (("s1", 1.0), ("sa", 1.0), ("s2", 1.0), ("gate", 0.5)):
+            self.master[name] = torch.full((hidden,), value, device=self.device)
+            self.momentum[name] = torch.zeros_like(self.master[name])
+        self._copy()
+
+    def _drop(self, i: int):
+        """The step's i-th mask."""
+        return pid.Drop(self.p_drop, self.seed, 2 * self.steps + i)
+
+    def forward(self, x: torch.Tensor, train: bool = False):
+        L, p, m = self.layers, self.p, x.shape[0]
+        hidden, gated = p["wg"].shape
+        z1 = self._keep(m, hidden) if train else None
+        g, u = (self._keep(m, gated) if train else None for _ in range(2))
+        a1 = pid.pointid_dense(L, x, p["w1"], p["b1"], "relu", save=z1)
+        if train:
+            a1 = pid.pointid_dropout(L, a1, self._drop(0), y=a1)
+        first = pid.pointid_norm(L, a1, pid.Norm("rms", p["s1"]), keep=train)
+        h = pid.pointid_gated(L, first.h, p["wg"], p["wu"], act="silu", save_g=g, save_u=u)
+        o = pid.pointid_dense(L, h, p["wd"], p["bd"])
+        block = pid.Block(o, pid.Norm("rms", p["sa"]), p["gate"], drop=self._drop(1) if train else None)
+        joint = pid.pointid_norm(L, a1, pid.Norm("rms", p["s2"]), block, keep=train)
+        out = pid.pointid_dense(L, joint.h, p["wo"], p["bo"])
+        if not train:
+            return out
+        return out, {"x": self._kept(x), "z1": z1, "a1": a1, "first": first.stats, "n1": self._kept(first.h), "g": g, "u": u,
+                     "h": self._kept(h), "block": block, "joint": joint, "n2": self._kept(joint.h)}
+
+    def backward(self, dout: torch.Tensor, k: dict) -> dict:
+        L, p = self.layers, self.p
+        dn2, dwo, dbo = pid.pointid_dense_backward(L, dout, k["n2"], p["wo"])
+        j = pid.pointid_norm_backward(L, dn2, k["joint"].total, k["joint"].stats, pid.Norm("rms", p["s2"]), k["block"])
+        dh, dwd, dbd = pid.pointid_dense_backward(L, j.dout, k["h"], p["wd"])
+        dn1, dwg, dwu, _, _ = pid.pointid_gated_backward(L, dh, k["n1"], p["wg"], p["wu"], k["g"], k["u"], "silu")
+        # the residual's gradient joins that through the norm, in its own memory
+        f = pid.pointid_norm_backward(L, dn1, k["a1"], k["first"], pid.Norm("rms", p["s1"]), dtotal=j.dx, dx=j.dx)
+        da1 = pid.pointid_dropout(L, f.dx, self._drop(0), y=f.dx)
+        _, dw1, db1 = pid.pointid_dense_backward(L, da1, k["x"], p["w1"], k["z1"], "relu", need_dx=False)
+        return {"w1": dw1, "b1": db1, "wg": dwg, "wu": dwu, "wd": dwd, "bd": dbd, "wo": dwo, "bo": dbo, "s1": f.dweight,
+                "sa": j.dblock_weight, "s2": j.dweight, "gate": j.dgate}
+
+    def loss_and_gradient(self, out: torch.Tensor, kind: torch.Tensor, michel: torch.Tensor, scale: float):
+        """(mean loss, its gradient by the outputs times ``scale``, in their type)"""
+        n = out.shape[0]
+        kind = kind.to(torch.int32)
+        got = pid.pointid_logprobs(self.layers, out[:, :3], kind)
+        z = out[:, 3].float()
+        value = -got.logp.mean() - (michel * torch.nn.functional.logsigmoid(z) +
+                                    (1 - michel) * torch.nn.functional.logsigmoid(-z)).mean()
+        d = torch.empty_like(out)
+        each = torch.full((n,), -scale / n, device=out.device)
+        pid.pointid_logprobs_backward(self.layers, out[:, :3], got.lse, kind, each, dlogits=d[:, :3])
+        d[:, 3] = (torch.sigmoid(z) - michel) * (scale / n)
+        return value, d
+
+    def step(self, x: torch.Tensor, kind: torch.Tensor, michel: torch.Tensor, rate: float = 0.05,
+             momentum: float = 0.9) -> torch.Tensor:
+        out, kept = self.forward(x.to(self.dtype), train=True)
+        scale = 1024.0
+        value, d = self.loss_and_gradient(out, kind, michel, scale)
+        grads = self.backward(d, kept)
+        self.steps += 1
+        for name, grad in grads.items():
+            self.momentum[name].mul_(momentum).add_(grad.float(), alpha=1 / scale)
+            self.master[name].add_(self.momentum[name], alpha=-rate)
+        self._copy()
+        return value
+
+
 def main(argv=None):
     import argparse
     ap = argparse.ArgumentParser(description="Train a small patch classifier with the library's layers.")
@@ -150,8 +241,11 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=1693)
     ap.add_argument("--dtype", choices=sorted(DTYPES), default="bf16")
     ap.add_argument("--kept", choices=["8bit", "type"], default="8bit")
+    ap.add_argument("--block", choices=["plain", "normed"], default="plain")
+    ap.add_argument("--dropout", type=float, default=0.1, help="of --block normed")
     a = ap.parse_args(argv)
-    model = PatchHead(dtype=a.dtype, kept=a.kept)
+    model = PatchHead(dtype=a.dtype, kept=a.kept) if a.block == "plain" else \
+        NormedPatchHead(dtype=a.dtype, kept=a.kept, dropout=a.dropout)
     g = torch.Generator(device=model.device).manual_seed(1)
     for i in range(a.steps):
         value = model.step(*draw_patches(a.batch, g, model.device))
