@@ -1133,6 +1133,8 @@ def pointid_norm_backward(layers: Layers, dh: torch.Tensor | None, total: torch.
     block: x) and the stats of the forward call, and its norm and block.
 
     Parameters' gradients are float32 [n], of those that are given.  ``dx`` may be dtotal itself."""
+    if norm is None and dh is not None:
+        raise ValueError("dh is the gradient of h, which there is only with norm")
     given = dh if norm is not None else dtotal
     dt, dev = _layer_type(given, "dh" if norm is not None else "dtotal"), layers.device
     m, n = shape = given.shape

@@ -678,6 +678,7 @@ unsigned row_blocks(int64_t rows) { return (unsigned)(rows < 65536 ? rows : 6553
 
 // Columns that a block can hold of a row, 8 a thread.
 constexpr int64_t kHeldCols = 8192;
+constexpr size_t kMostShared = 156 * 1024;     // of a CU's 160 KB, some taken by the sums' exchange
 // Threads of a row that is held (16, or whole waves), and the groups of them in a block of at
 // most `threads`, or one.
 struct HeldShape {
@@ -713,14 +714,15 @@ hipError_t launch_norm_of(NormArgs a, hipStream_t stream) {
   // Many rows: blocks of at least 8 sets of rows, with the parameters in shared memory.  bf16, both
   // norms and a gate, read from memory for every row and shared: 16384 x 4096 121 us and 104, 8192 x
   // 4096 59 and 49, 8192 x 8192 150 and 105; fp32 8192 x 4096 113 and 104.
-  const bool shared = need >= 4096 && !two;
+  const size_t bytes = (size_t)(biases ? 5 : 3) * h.lanes * 32;
+  const bool shared = need >= 4096 && !two && bytes <= kMostShared;
   int64_t blocks = need < 65536 ? need : 65536;
   if (shared) blocks = need / 8 < 4096 ? need / 8 : 4096;
-  auto go = [&](auto kernel, size_t bytes) {
-    return launch_kernel(kernel, dim3((unsigned)blocks), dim3(h.lanes * h.groups), bytes, stream, a);
+  auto go = [&](auto kernel, size_t shared_bytes) {
+    return launch_kernel(kernel, dim3((unsigned)blocks), dim3(h.lanes * h.groups), shared_bytes, stream, a);
   };
   return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
-    if (shared) return go(norm_rows_kernel<kType, small, whole, bias, true, 1>, (size_t)(biases ? 5 : 3) * h.lanes * 32);
+    if (shared) return go(norm_rows_kernel<kType, small, whole, bias, true, 1>, bytes);
     if (two) return go(norm_rows_kernel<kType, false, whole, bias, false, 2>, 0);
     return go(norm_rows_kernel<kType, small, whole, bias, false, 1>, 0);
   });
@@ -774,7 +776,8 @@ hipError_t launch_norm_back_of(NormBackArgs a, bool held, hipStream_t stream) {
   const int threads = back_threads(kType, biases, a.cols);
   const HeldShape h = held_shape(a.cols, threads);
   a.lanes = h.lanes;
-  const int shared = biases ? 4 : 3;             // the parameters, or the groups' sums
+  // the parameters, or the groups' sums: at most 128 KB
+  const int shared = biases ? 4 : 3;
   return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
     auto go = [&](auto kernel) {
       return launch_kernel(kernel, dim3((unsigned)a.blocks), dim3(h.lanes * h.groups),

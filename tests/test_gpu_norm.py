@@ -120,6 +120,45 @@ def test_forward_and_backward(pid, layers, dtype, m, n):
         j.check_backward(back, got.stats.cpu(), t, dt, str(form))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("m, n", [(4100, 8192), (4097, 7000), (6, 8192), (4100, 6145), (70000, 40), (9000, 520)])
+def test_many_rows_and_the_widest_that_are_held(pid, layers, dtype, m, n):
+    """With every parameter: what a block keeps in shared memory is largest.  The last rows and all
+    column sums are checked."""
+    for form in (FORMS[3], FORMS[2]):
+        j = Joint(pid, dtype, 6, n, form, seed=1)
+        if j.p:
+            j.p, j.factor = 0.0, None                       # the rows' masks are tested elsewhere
+        d = torch.device(DEV)
+
+        def many(t):
+            return j.dev(t).repeat(-(-m // 6), 1)[:m].contiguous()
+
+        x, o, dh, dt = (many(t) for t in (j.x, j.o, j.dh, j.dt))
+        got = pid.pointid_norm(layers, x, j.norm(), j.block(o), keep=True)
+        back = pid.pointid_norm_backward(layers, dh, got.total, got.stats, j.norm(), j.block(o), dtotal=dt)
+        few = pid.pointid_norm(layers, x[:6], j.norm(), j.block(o[:6]), keep=True)
+        j.check_forward(few)
+        # rows alike have results alike, wherever they stand (to the rounding of sums in another order)
+        rows = torch.arange(m, device=d) % 6
+        assert torch.allclose(got.h.float(), few.h.float()[rows], rtol=2.0 ** -6, atol=1e-5)
+        f = pid.pointid_norm_backward(layers, dh[:6], few.total, few.stats, j.norm(), j.block(o[:6]), dtotal=dt[:6])
+        j.check_backward(f, few.stats.cpu(), few.total.cpu())
+        for a, b in ((back.dx, f.dx), (back.dout, f.dout)):
+            assert torch.allclose(a.float(), b.float()[rows], rtol=2.0 ** -6, atol=2.0 ** -6)
+        times = torch.bincount(rows, minlength=6).double()
+        for name, k in (("dweight", 0), ("dblock_weight", 1), ("dgate", 2)):
+            parts = []
+            for i in range(6):
+                one = pid.pointid_norm_backward(layers, dh[i:i + 1], few.total[i:i + 1], few.stats[i:i + 1], j.norm(),
+                                                j.block(o[i:i + 1]), dtotal=dt[i:i + 1])
+                parts.append(getattr(one, name).double() * times[i])
+            parts = torch.stack(parts)
+            # fp32 sums of m terms in a tree of partial sums of at most m / 256 + 64 in turn
+            tol = parts.abs().sum(0) * (m / 256 + 64) * A.E + 1e-5 * parts.abs().sum(0)
+            assert ((getattr(back, name).double() - parts.sum(0)).abs() <= tol).all(), name
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 def test_a_norm_alone(pid, layers, dtype, kind):
