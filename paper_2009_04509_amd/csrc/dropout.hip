@@ -2,6 +2,7 @@
 #include "internal.h"
 #include "layers_end.h"
 #include "norm.h"
+#include "passing.h"
 
 namespace pointid {
 namespace {
@@ -16,8 +17,8 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
     const int64_t col = (i - row * pieces) * 8;
     const int n = piece_cols(a.cols, col);
     Raw8<kType> x, r;
-    x.load(a.x + (row * a.ld_x + col) * kSize, n);
-    if (a.residual) r.load(a.residual + (row * a.ld_residual + col) * kSize, n);
+    Passing<kType>::load(&x, a.x + (row * a.ld_x + col) * kSize, n, a.passing);
+    if (a.residual) Passing<kType>::load(&r, a.residual + (row * a.ld_residual + col) * kSize, n, a.passing);
     float v[8];
     x.values(v);
     drop8(a.drop, key, row, col, v);
@@ -27,13 +28,14 @@ __global__ void __launch_bounds__(256) dropout_kernel(DropoutArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += f[j];
     }
-    store_cols<8>(a.y, row * a.ld_y + col, kType, n, v);
+    Passing<kType>::store(a.y + (row * a.ld_y + col) * kSize, n, v, a.passing);
   }
 }
 
 }  // namespace
 
-hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream) {
+hipError_t launch_dropout(DropoutArgs a, hipStream_t stream) {
+  a.passing = passes_cache(a.dtype, a.rows, a.cols, a.residual ? 3 : 2);
   const int64_t blocks = (a.rows * ((a.cols + 7) / 8) + 255) / 256;
   const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
   switch (a.dtype) {

@@ -8,6 +8,7 @@
 #include "internal.h"
 #include "layers_end.h"
 #include "norm.h"
+#include "passing.h"
 #include "wave.h"
 
 namespace pointid {
@@ -398,6 +399,32 @@ __global__ void __launch_bounds__(512) scan_join_kernel(ScanArgs a) {
 }
 
 // dx_j = scale (dlogp ([j = t] - p_j) + dlse p_j - dH p_j (log p_j + H)), p_j = e^(z_j - lse)
+struct BackRow {
+  float lse, dlogp, on_p, dh, h;
+  int32_t target;
+  __device__ __forceinline__ BackRow(const ScanBackArgs& a, int64_t row) {
+    lse = a.lse[row];
+    target = a.targets ? a.targets[row] : -1;
+    dlogp = target >= 0 && target < a.cols ? a.dlogp[row] : 0.f;
+    on_p = (a.dlse ? a.dlse[row] : 0.f) - dlogp;
+    dh = a.dentropy ? a.dentropy[row] : 0.f;
+    h = a.dentropy ? a.entropy[row] : 0.f;
+  }
+  __device__ __forceinline__ void gradient(float scale, int64_t col, float (&v)[8]) const {
+    const bool empty = lse == -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float logp = v[j] * scale - lse, p = two_to(logp * kLog2e);
+      float d = p * (on_p - dh * (fmaxf(logp, kNone) + h));
+      if (col + j == target) d += dlogp;
+      v[j] = empty ? 0.f : d * scale;
+    }
+  }
+};
+
+// Pieces of 8 columns, of any row.  A row's values are read for each piece, from the first cache:
+// blocks of one row that read them once took 49 us for 59 where rows are whole blocks (16384 x 4096
+// bf16), as long at 4096 x 65536, and 66 for 30 at 32768 x 1000.
 template <int kType>
 __global__ void __launch_bounds__(256) scan_back_kernel(ScanBackArgs a) {
   constexpr int kSize = kType == POINTID_FP32 ? 4 : 2;
@@ -407,23 +434,11 @@ __global__ void __launch_bounds__(256) scan_back_kernel(ScanBackArgs a) {
     const int64_t col = (i - row * pieces) * 8;
     const int n = piece_cols(a.cols, col);
     Raw8<kType> raw;
-    raw.load(a.x.p + (row * a.x.ld + col) * kSize, n);
+    Passing<kType>::load(&raw, a.x.p + (row * a.x.ld + col) * kSize, n, a.passing);
     float v[8];
     raw.values(v);
-    const float lse = a.lse[row];
-    const int32_t t = a.targets ? a.targets[row] : -1;
-    const float dlogp = t >= 0 && t < a.cols ? a.dlogp[row] : 0.f;
-    const float on_p = (a.dlse ? a.dlse[row] : 0.f) - dlogp;
-    const float dh = a.dentropy ? a.dentropy[row] : 0.f, h = a.dentropy ? a.entropy[row] : 0.f;
-    const bool empty = lse == -__builtin_inff();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float logp = v[j] * a.scale - lse, p = two_to(logp * kLog2e);
-      float d = p * (on_p - dh * (fmaxf(logp, -1000.f) + h));
-      if (col + j == t) d += dlogp;
-      v[j] = empty ? 0.f : d * a.scale;
-    }
-    store_cols<8>(a.dx.p, row * a.dx.ld + col, kType, n, v);
+    BackRow(a, row).gradient(a.scale, col, v);
+    Passing<kType>::store(a.dx.p + (row * a.dx.ld + col) * kSize, n, v, a.passing);
   }
 }
 
@@ -483,7 +498,8 @@ hipError_t launch_logprobs_join(const ScanArgs& a, hipStream_t stream) {
   return launch_kernel(scan_join_kernel<POINTID_FP16>, grid, dim3(512), 0, stream, a);
 }
 
-hipError_t launch_logprobs_back(const ScanBackArgs& a, hipStream_t stream) {
+hipError_t launch_logprobs_back(ScanBackArgs a, hipStream_t stream) {
+  a.passing = passes_cache(a.dtype, a.rows, a.cols, 2);
   const int64_t blocks = (a.rows * ((a.cols + 7) / 8) + 255) / 256;
   const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384));
   switch (a.dtype) {

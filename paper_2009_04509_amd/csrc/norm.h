@@ -20,8 +20,9 @@ struct DropoutArgs {
   int64_t rows, cols;
   int32_t dtype;
   Drop drop;
+  int32_t passing;             // set by the launch: see Passing
 };
-hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+hipError_t launch_dropout(DropoutArgs a, hipStream_t stream);
 
 // ---- norm.hip
 // u = (v - mean) / deviation, or v / root of the mean square; u weight + bias.
@@ -46,7 +47,7 @@ struct NormArgs {
   float* stats;
   int64_t rows, cols;
   int32_t dtype;
-  int32_t lanes;               // set by the launch: a row's threads
+  int32_t lanes, passing;      // set by the launch: a row's threads, and see Passing
 };
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream);
 
@@ -66,7 +67,7 @@ struct NormBackArgs {
   int32_t blocks;              // of rows
   int64_t rows, cols;
   int32_t dtype;
-  int32_t lanes;               // set by the launch: a row's threads
+  int32_t lanes, passing;      // set by the launch: a row's threads, and see Passing
 };
 // The blocks that leave sums, and whether a block holds whole rows; if not, `means` has to be
 // made first.
@@ -108,7 +109,8 @@ struct ScanBackArgs {
   float scale;
   const int32_t* targets;
   const float *lse, *entropy, *dlogp, *dentropy, *dlse;
+  int32_t passing;             // set by the launch: see Passing
 };
-hipError_t launch_logprobs_back(const ScanBackArgs& a, hipStream_t stream);
+hipError_t launch_logprobs_back(ScanBackArgs a, hipStream_t stream);
 
 }  // namespace pointid

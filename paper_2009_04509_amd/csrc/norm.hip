@@ -3,6 +3,7 @@
 #include "internal.h"
 #include "layers_end.h"
 #include "norm.h"
+#include "passing.h"
 #include "wave.h"
 
 namespace pointid {
@@ -172,9 +173,10 @@ struct Stream {
   static constexpr int64_t kSize = kType == POINTID_FP32 ? 4 : 2;
   char* p;                     // the next row's first column, nullptr without a matrix
   int64_t step;                // bytes to the group's row after it
+  bool passing;
   Raw8<kType> raw[kPieces];
-  __device__ __forceinline__ Stream(const Rows& m, int64_t row, int64_t rows_on)
-      : p(m.p ? m.p + row * m.ld * kSize : nullptr), step(rows_on * m.ld * kSize) {
+  __device__ __forceinline__ Stream(const Rows& m, int64_t row, int64_t rows_on, bool passing_)
+      : p(m.p ? m.p + row * m.ld * kSize : nullptr), step(rows_on * m.ld * kSize), passing(passing_) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) raw[i].load(nullptr, 0);
   }
@@ -187,17 +189,17 @@ struct Stream {
         if (!here) {
           raw[i].load(nullptr, 0);
         } else if (n[i] > 0) {
-          raw[i].load(p + col[i] * kSize, 8);
+          Passing<kType>::load(&raw[i], p + col[i] * kSize, 8, passing);
         }
       } else {
-        raw[i].load(p + col[i] * kSize, here ? n[i] : 0);
+        Passing<kType>::load(&raw[i], p + col[i] * kSize, here ? n[i] : 0, passing);
       }
     }
     p += step;
   }
   // one piece of the row that `next` goes on from
   __device__ __forceinline__ void store(int col, int n, bool here, const float (&v)[8]) const {
-    if (p && here && n > 0) store_cols<8>(p, col, kType, kWhole ? 8 : n, v);
+    if (p && here && n > 0) Passing<kType>::store(p + col * kSize, kWhole ? 8 : n, v, passing);
   }
   __device__ __forceinline__ void next() { p += step; }
 };
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
-  Stream<kType, kWhole, kPieces> x(a.x, row, step), o(a.o, row, step), t(a.t, row, step), h(a.h, row, step);
+  Stream<kType, kWhole, kPieces> x(a.x, row, step, a.passing), o(a.o, row, step, a.passing), t(a.t, row, step, a.passing), h(a.h, row, step, a.passing);
   o.load(col, n, row < a.rows);
   x.load(col, n, row < a.rows);
   if constexpr (kShared) {
@@ -527,8 +529,8 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
-  Stream<kType, kWhole, 1> dh(a.dh, row, step), t(a.t, row, step), dt(a.dt, row, step), o(a.o, row, step);
-  Stream<kType, kWhole, 1> dx(a.dx, row, step), dout(a.dout, row, step);
+  Stream<kType, kWhole, 1> dh(a.dh, row, step, a.passing), t(a.t, row, step, a.passing), dt(a.dt, row, step, a.passing), o(a.o, row, step, a.passing);
+  Stream<kType, kWhole, 1> dx(a.dx, row, step, a.passing), dout(a.dout, row, step, a.passing);
   float4 next;
   auto load = [&](int64_t r) {
     const bool here = r < a.rows;
@@ -708,6 +710,7 @@ hipError_t launch_norm_of(NormArgs a, hipStream_t stream) {
   if (a.cols > 2 * kHeldCols) return launch_kernel(norm_kernel<kType>, dim3(row_blocks(a.rows)), dim3(256), 0, stream, a);
   const bool biases = a.after.bias || a.before.bias;
   const bool two = a.cols > kHeldCols;           // pieces a thread
+  a.passing = passes_cache(kType, a.rows, a.cols, 1 + (a.o.p != nullptr) + (a.t.p != nullptr) + (a.h.p != nullptr));
   const HeldShape h = held_shape(two ? (a.cols + 1) / 2 : a.cols, 256);
   a.lanes = h.lanes;
   const int64_t need = (a.rows + h.groups - 1) / h.groups;
@@ -772,6 +775,9 @@ hipError_t launch_norm_back_of(NormBackArgs a, bool held, hipStream_t stream) {
   if (!held)
     return launch_kernel(norm_back_kernel<kType>, dim3((unsigned)((a.cols + 255) / 256), (unsigned)a.blocks), dim3(256), 0,
                          stream, a);
+  int matrices = 0;
+  for (const Rows* r : {&a.dh, &a.dt, &a.t, &a.o, &a.dx, &a.dout}) matrices += r->p != nullptr;
+  a.passing = passes_cache(kType, a.rows, a.cols, matrices);
   const bool biases = has_biases(a);
   const int threads = back_threads(kType, biases, a.cols);
   const HeldShape h = held_shape(a.cols, threads);
