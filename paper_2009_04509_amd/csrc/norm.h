@@ -109,7 +109,7 @@ struct ScanBackArgs {
   float scale;
   const int32_t* targets;
   const float *lse, *entropy, *dlogp, *dentropy, *dlse;
-  int32_t passing;             // set by the launch: see Passing
+  int32_t lanes, passing;      // set by the launch: a row's threads, and see Passing
 };
 hipError_t launch_logprobs_back(ScanBackArgs a, hipStream_t stream);
 

@@ -91,6 +91,54 @@ def test_top_of_ordered_rows(pid, layers, n, order):
         assert torch.equal(got.top_ids.long().cpu(), ids), (order, top)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("m, n", [(3, 300), (1100, 3000), (3, 70000), (520, 20000)])
+def test_top_of_few_values(pid, layers, dtype, m, n):
+    """Rows of 16-bit values with many equals, of either sign, by every kernel that chooses them."""
+    g = A.gen(n)
+    x = torch.randint(-20, 3, (m, n), generator=g).double() * torch.rand((m, 1), generator=g, dtype=torch.float64)
+    x[1] = torch.where(torch.rand(n, generator=g) < 0.9, -INF, x[1])
+    x = x.to(A.DT[dtype])
+    for top in (1, 7, 64):
+        got = pid.pointid_logprobs(layers, x.to(DEV), top=top)
+        ids = torch.sort(x.double() + 0.0, dim=1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(got.top_ids.long().cpu(), ids), top
+
+
+def test_the_widest_rows(pid, layers):
+    """More pieces than 16 bits count, by one block a row."""
+    m, n = 520, 1 << 20
+    x = torch.zeros((m, n), dtype=torch.bfloat16, device=DEV)
+    at = torch.arange(m, device=DEV) * 2003 + 7
+    x[torch.arange(m, device=DEV), at] = 2
+    x[:, -1] = 1
+    got = pid.pointid_logprobs(layers, x, top=4)
+    want = torch.stack([at, torch.full_like(at, n - 1), torch.zeros_like(at), torch.ones_like(at)], 1)
+    assert torch.equal(got.top_ids.long(), want)
+    lse = math.log(n - 2 + math.e + math.exp(2))
+    assert (got.lse - lse).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("m, n", [(2, 100), (2, 9000), (1100, 5000), (520, 9000)])
+def test_nans_of_both_kinds_hide_nothing(pid, layers, dtype, m, n):
+    """A quiet and a signalling NaN right after a row's largest value, in the same thread's columns."""
+    x = A.rand(A.gen(n), m, n, dtype=dtype)
+    best = torch.arange(m) * 13 % (n - 8) // 8 * 8
+    rows = torch.arange(m)
+    x[rows, best] = 9.0
+    bits = x.view(torch.int16 if dtype != "fp32" else torch.int32)
+    nan = {"bf16": (0x7FC0, 0x7F81), "fp16": (0x7E00, 0x7C01), "fp32": (0x7FC00000, 0x7F800001)}[dtype]
+    for kind in (0, 1):
+        bits[rows, best + 1] = nan[kind]
+        got = pid.pointid_logprobs(layers, x.to(DEV), entropy=True, top=2)
+        assert torch.equal(got.top_ids[:, 0].long().cpu(), best)
+        second = torch.where(torch.isnan(x), -INF, x.double())
+        second[rows, best] = -INF
+        assert torch.equal(got.top_ids[:, 1].long().cpu(), second.max(1).values.view(-1, 1).eq(second).int().argmax(1))
+        assert got.lse.isnan().all() and got.entropy.isnan().all() and got.top_logp.isnan().all()
+
+
 def test_zeros_of_both_signs_are_equal(pid, layers):
     x = torch.zeros((1, 600), device=DEV)
     x[0, :300] = -0.0
