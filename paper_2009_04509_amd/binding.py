@@ -1153,21 +1153,24 @@ def pointid_norm_backward(layers: Layers, dh: torch.Tensor | None, total: torch.
         if stats.shape != (m, 4):
             raise ValueError(f"stats must be [{m}, 4]")
         kept = stats.data_ptr()
-    params = (norm and norm.weight, norm and norm.bias, after and after.weight, after and after.bias,
-              block and block.gate) if need_params else (None,) * 5
-    params = [p is not None for p in params]
+    wanted = [False] * 5
+    if need_params:
+        if norm is not None:
+            wanted[0], wanted[1] = norm.weight is not None, norm.bias is not None
+        if after is not None:
+            wanted[2], wanted[3] = after.weight is not None, after.bias is not None
+        wanted[4] = block is not None and block.gate is not None
     size = lib.pointid_norm_backward_scratch(layers.raw, m, n)
 
     def outputs():
         return (_like(given, dx, "dx", dt, shape, dev) if need_dx or dx is not None else (None, None),
                 _like(given, None, "dout", dt, shape, dev) if need_dout and block is not None else (None, None),
-                _rows_of_floats(given, sum(params), n), _scratch(size, given))
+                iter(_rows_of_floats(given, sum(wanted), n)), _scratch(size, given))
 
-    (dx, to_dx), (dout, to_dout), sums, (scratch, at) = outputs() if stream is None else _make(stream, dev, outputs)
-    sums = iter(sums)
-    sums = [next(sums) if p else None for p in params]
+    (dx, to_dx), (dout, to_dout), made, (scratch, at) = outputs() if stream is None else _make(stream, dev, outputs)
+    sums = [next(made) if w else None for w in wanted]
     grads = _NormGrads(to_dx and to_dx.data, to_dx.ld if to_dx else 0, to_dout and to_dout.data,
-                       to_dout.ld if to_dout else 0, *(p if p is None else p.data_ptr() for p in sums))
+                       to_dout.ld if to_dout else 0, *[p if p is None else p.data_ptr() for p in sums])
     _check(lib.pointid_norm_backward(layers.raw, _LAYER_TYPES[dt], m, n, a, b, kept, before, end, c, grads, at, size,
                                      _layer_stream(stream, dev)))
     return NormGradients(dx, dout, *sums)

@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(256) norm_back_kernel(NormBackArgs a) {
 }
 
 // Both passes and the column sums with the rows held in registers; each block takes every
-// gridDim-th set of rows, one of each of its groups, and leaves its sums.  A norm that there is
+// gridDim-th set of rows, one of each of its groups, and leaves its sums (the only block: the sums).  A norm that there is
 // not has the mean 0, the deviation 1, and means of its gradient that count as 0.
 template <int kType, bool kSmall, bool kWhole, bool kBiases, int kMost>
 __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
 #pragma unroll
   for (int s = 0; s < kNormSums; ++s) {
     if (!a.out[s]) continue;
-    float* const out = a.part + ((int64_t)blockIdx.x * wanted + slot) * a.cols;
+    float* const out = gridDim.x == 1 ? a.out[s] : a.part + ((int64_t)blockIdx.x * wanted + slot) * a.cols;
     ++slot;
     if (groups > 1) {
       __syncthreads();

@@ -151,6 +151,7 @@ uint64_t pointid_norm_backward_scratch(pointid_layers l, int64_t m, int64_t n) {
   std::memset(static_cast<void*>(&a), 0, sizeof(a));
   a.rows = m, a.cols = n, a.dtype = POINTID_FP32;
   const NormBackPlan plan = plan_norm_back(a, l->cus);
+  if (plan.held && plan.blocks <= 1) return 0;
   return (plan.held ? 0 : pad256(means_bytes(m))) + pad256(sums_bytes(plan.blocks, kNormSums, n));
 }
 
@@ -207,13 +208,14 @@ int pointid_norm_backward(pointid_layers l, int dtype, int64_t m, int64_t n, con
     a.blocks = plan.blocks;
     const bool means = !plan.held && (has(norm) || after);
     if (means) call.want(&a.means, means_bytes(m));
-    if (wanted) call.want(&a.part, sums_bytes(plan.blocks, wanted, n));
+    const bool alone = plan.held && plan.blocks == 1;        // its sums are the sums
+    if (wanted && !alone) call.want(&a.part, sums_bytes(plan.blocks, wanted, n));
     TRY(call.reserve());
     if (m > 0) {
       if (means) TRY(call.run("norm_means", false, [&] { return launch_norm_means(a, call.stream()); }));
-      TRY(call.run("norm_back", !wanted, [&] { return launch_norm_back(a, plan.held, call.stream()); }));
+      TRY(call.run("norm_back", !wanted || alone, [&] { return launch_norm_back(a, plan.held, call.stream()); }));
     }
-    if (!wanted) return (int)POINTID_OK;
+    if (!wanted || alone) return (int)POINTID_OK;
     return call.run("norm_sums", true, [&] { return launch_norm_sums(a, call.stream()); });
   });
 }

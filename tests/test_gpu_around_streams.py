@@ -121,15 +121,27 @@ def test_two_threads_share_the_handle(pid, layers):
     assert not fails, fails[:3]
 
 
-def test_under_capture_the_handles_scratch_is_refused(pid, layers):
-    x, w = torch.randn((40, 64), device=DEV), torch.ones(64, device=DEV)
-    got = pid.pointid_norm(layers, x, pid.Norm("rms", w), keep=True)
+@pytest.mark.parametrize("m, refused", [(400, True), (40, False)])
+def test_under_capture_the_handles_scratch_is_refused(pid, layers, m, refused):
+    """Rows of one block alone take none: their sums are the sums."""
+    x, w = torch.randn((m, 64), device=DEV), torch.ones(64, device=DEV)
+    norm = pid.Norm("rms", w)
+    got = pid.pointid_norm(layers, x, norm, keep=True)
+    want = pid.pointid_norm_backward(layers, x, x, got.stats, norm).dweight
     dw = torch.zeros(64, device=DEV)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        rc = pid.lib.pointid_norm_backward(layers.raw, 0, 40, 64, pid._Matrix(x.data_ptr(), 64), pid._Matrix(x.data_ptr(), 64),
+        rc = pid.lib.pointid_norm_backward(layers.raw, 0, m, 64, pid._Matrix(x.data_ptr(), 64), pid._Matrix(x.data_ptr(), 64),
                                            got.stats.data_ptr(), pid._NormOf(1, 1e-5, w.data_ptr(), None), None, None,
                                            pid._NormGrads(None, 0, None, 0, dw.data_ptr()), None, 0,
                                            torch.cuda.current_stream().cuda_stream)
         x.add_(0)
-    assert rc == pid.POINTID_EINVAL and "scratch" in pid.pointid_last_error()
+    if refused:
+        assert rc == pid.POINTID_EINVAL and "scratch" in pid.pointid_last_error()
+        return
+    assert rc == pid.POINTID_OK
+    for _ in range(3):
+        dw.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dw, want)
