@@ -197,11 +197,13 @@ struct Stream {
     }
     p += step;
   }
-  // one piece of the row that `next` goes on from
+  // one piece of the row, and on to the next (a matrix that is not there stays so)
   __device__ __forceinline__ void store(int col, int n, bool here, const float (&v)[8]) const {
     if (p && here && n > 0) Passing<kType>::store(p + col * kSize, kWhole ? 8 : n, v, passing);
   }
-  __device__ __forceinline__ void next() { p += step; }
+  __device__ __forceinline__ void next() {
+    if (p) p += step;
+  }
 };
 
 // A parameter's 8 columns of a thread from shared memory, where it stands as [2][lanes] pieces

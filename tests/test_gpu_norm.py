@@ -178,6 +178,44 @@ def test_a_norm_alone(pid, layers, dtype, kind):
         assert back.dout is None and back.dgate is None and back.dblock_weight is None
 
 
+@pytest.mark.parametrize("m, n", [(3, 40), (9000, 40), (5000, 264), (2500, 1200), (9000, 2050), (40, 9000)])
+def test_only_what_is_asked_for(pid, layers, m, n):
+    """Every output alone, over enough rows for each block to have several, is what it is with the
+    others; and what is not there is nowhere written."""
+    g = A.gen(m + n)
+    x, o, dh, dt = (A.rand(g, m, n).to(DEV) for _ in range(4))
+    w = torch.randn(n, generator=g).to(DEV)
+    norm, block = pid.Norm("rms", w), pid.Block(o, pid.Norm("layer", w, w), w, 0.5, pid.Drop(0.1, 1))
+    full = pid.pointid_norm(layers, x, norm, block, keep=True)
+    M = [pid._Matrix(v.data_ptr(), n) for v in (x, torch.empty_like(x), torch.empty_like(x))]
+    total, h = torch.empty_like(x), torch.empty_like(x)
+    fields, end = pid._NormOf(*pid._norm(norm, "norm", n, 0)), pid._block(block, torch.bfloat16, x.shape, 0)
+    stream = torch.cuda.current_stream().cuda_stream
+    T, H = pid._Matrix(total.data_ptr(), n), pid._Matrix(h.data_ptr(), n)
+    assert pid.lib.pointid_norm(layers.raw, 1, m, n, M[0], fields, end, None, H, None, stream) == pid.POINTID_OK
+    assert pid.lib.pointid_norm(layers.raw, 1, m, n, M[0], None, end, T, None, None, stream) == pid.POINTID_OK
+    assert torch.equal(total, full.total) and torch.equal(h, full.h)
+    every = pid.pointid_norm_backward(layers, dh, full.total, full.stats, norm, block, dtotal=dt)
+    outs = ("dx", "dout", "dweight", "dblock_weight", "dblock_bias", "dgate")
+    made = {k: torch.empty_like(getattr(every, k)) for k in outs}
+    for k in outs:
+        grads = pid._NormGrads()
+        setattr(grads, k, made[k].data_ptr())
+        grads.ld_dx = grads.ld_dout = n
+        assert pid.lib.pointid_norm_backward(layers.raw, 1, m, n, pid._Matrix(dh.data_ptr(), n),
+                                             pid._Matrix(full.total.data_ptr(), n), full.stats.data_ptr(), fields, end,
+                                             pid._Matrix(dt.data_ptr(), n), grads, None, 0, stream) == pid.POINTID_OK
+        if k in ("dx", "dout"):
+            assert torch.equal(made[k], getattr(every, k)), k
+        else:
+            # which sums a block keeps may change how many rows it takes, and so the order of the sums
+            assert torch.allclose(made[k], getattr(every, k), rtol=1e-3, atol=1e-3 * m ** 0.5), k
+    back = pid.pointid_norm_backward(layers, dh, full.total, full.stats, norm, block, dtotal=dt, need_dx=False)
+    assert back.dx is None and torch.equal(back.dout, every.dout) and torch.equal(back.dgate, every.dgate)
+    back = pid.pointid_norm_backward(layers, dh, full.total, full.stats, norm, block, dtotal=dt, need_dout=False)
+    assert back.dout is None and torch.equal(back.dx, every.dx) and torch.equal(back.dweight, every.dweight)
+
+
 def test_no_parameters(pid, layers):
     """weights and biases that are not given are ones and zeros, and have no gradients"""
     x, o = (torch.randn((20, 100), device=DEV) for _ in range(2))
