@@ -570,9 +570,11 @@ int pointid_checkpoint_load(int dtype, int64_t rows, int64_t cols, const pointid
  * beside them in a training step, and the last two when a model is served.  They take the
  * layers' handle and its conventions: matrices of the call's `dtype` with any row pitch,
  * parameters and statistics fp32, 0 <= m <= 2^28 (m == 0: a no-op, but that gradients of
- * parameters are set to 0), 1 <= n <= 2^20, sums in fp32 in a fixed order, results rounded
- * to `dtype` once, the same bits for the same arguments.  Each row's results depend on that
- * row alone, but for gradients of parameters.
+ * parameters are set to 0), 1 <= n <= 2^20, sums in fp32, results rounded to `dtype` once, the
+ * same bits for the same arguments.  Each row's results are those of that row alone, but for
+ * gradients of parameters; the order of a sum depends on the sizes, on alignment to whole pieces
+ * of 8 columns, and on which parameters and outputs there are.  Outputs must not overlap inputs or
+ * each other where nothing else is said.
  *
  * Calls that may take scratch have `scratch`, memory of the caller's of at least
  * `scratch_bytes` = pointid_..._scratch() bytes, aligned to 256, or NULL (and 0) for the
