@@ -670,6 +670,7 @@ typedef struct {
  *   q    = gate * drop(d),  dgate = sum drop(d) norm_after(out)
  *   dout = the norm after the block's gradient from q, and its parameters', as above
  * The means are over a row, the sums over the rows, in a fixed order.
+ * Where no norm follows the block, what is dropped of out adds nothing to dgate, whatever it is.
  *   norm, block  as in the forward call (block->out is needed for a norm after the block and
  *                for dgate)
  *   dh           needed with norm;  total, stats: those of the forward call (without a block,

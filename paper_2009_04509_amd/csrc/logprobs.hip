@@ -241,7 +241,7 @@ __device__ uint64_t pick_top(const char* x, int64_t first, int64_t last, int k, 
       if (j >= n) continue;
       const uint64_t e = entry_of(v[j], (uint32_t)col + j);
       if (!wanted(e)) continue;
-      const uint32_t at = atomicAdd(count, 1);
+      const uint32_t at = atomicAdd(count, 1);   // in any order: they are sorted, and no two are equal
       if (at < kListed) listed[at] = e;
     }
   }

@@ -403,13 +403,20 @@ __device__ __forceinline__ void back8(const NormBackArgs& a, const DropKey& key,
   if (!a.o.p && !a.dout.p) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) b->q[i] = b->d[i];
-  if (a.drop.threshold) drop8(a.drop, key, row, col, b->q);
-  if (a.o.p) {
-    load_row<kType>(a.o, row, col, n, b->u_a);
-    if (a.after.kind)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) b->u_a[i] = (b->u_a[i] - st.x) * st.y;
+  for (int i = 0; i < 8; ++i) b->u_a[i] = 0.f;
+  if (a.o.p) load_row<kType>(a.o, row, col, n, b->u_a);
+  // (o's own infinities do not reach the gate's gradient where they are dropped; a norm's whole row
+  // has them)
+  if (a.drop.threshold) {
+    if (a.after.kind)
+      drop8(a.drop, key, row, col, b->q);
+    else
+      drop8(a.drop, key, row, col, b->q, &b->u_a);
   }
+  if (a.after.kind)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b->u_a[i] = (b->u_a[i] - st.x) * st.y;
 }
 
 // Rows of more than 8192 columns take two passes: the means over each row that its gradients take,
@@ -531,13 +538,13 @@ __global__ void __launch_bounds__(256) norm_back_kernel(NormBackArgs a) {
 
 // Both passes and the column sums with the rows held in registers; each block takes every
 // gridDim-th set of rows, one of each of its groups, and leaves its sums (the only block: the sums):
-// one block a CU, so that there are few sums to add.
+// one block a CU, so that there are few sums to add.  A norm that there is not has the mean 0, the
+// deviation 1, and means of its gradient that count as 0.
 // bf16 16384 x 4096 with dropout (805 MB): 139 us, 5.8 TB/s, the vector units busy 65 %, and 4.8 for the
 // sums.  A branch for each part that a call may lack, and its parameters in registers (167: three waves
 // a SIMD, one block of 512 threads), took 277; both in shared memory and the branches 230.  fp16 1693
 // x 2304, layer norms (47 MB): 21 us, 3.3 rows for each of 512 groups, of which the first waits for
-// memory.  A norm that there is
-// not has the mean 0, the deviation 1, and means of its gradient that count as 0.
+// memory.
 template <int kType, bool kSmall, bool kWhole, bool kBiases, int kMost>
 __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
   __shared__ float2 waves[2][kMostWaves];
@@ -608,7 +615,12 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
     dx.store(col, n, here, u);
     dx.next();
     if (!a.o.p && !a.dout.p) continue;
-    if (a.drop.threshold) drop8(a.drop, key, row, col, d);
+    if (a.drop.threshold) {
+      if (a.after.kind)
+        drop8(a.drop, key, row, col, d);
+      else
+        drop8(a.drop, key, row, col, d, &v);
+    }
     param(kAfterWeight, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -49,14 +49,17 @@ __device__ __forceinline__ void philox(const DropKey& key, uint32_t c0, uint32_t
 }
 
 // v of columns col .. col + 7 (col a multiple of 8) through the dropout.  What is dropped is 0
-// whatever it was, an infinity or NaN too.
-__device__ __forceinline__ void drop8(const Drop& d, const DropKey& key, int64_t row, int64_t col, float (&v)[8]) {
+// whatever it was, an infinity or NaN too; where `with` is given, its values there are 0 as well.
+__device__ __forceinline__ void drop8(const Drop& d, const DropKey& key, int64_t row, int64_t col, float (&v)[8],
+                                      float (*with)[8] = nullptr) {
   uint32_t w[4];
   philox(key, (uint32_t)(col / 8), (uint32_t)row, w);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t bits = i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu;
-    v[i] = bits >= d.threshold ? v[i] * d.scale : 0.f;
+    const bool kept = bits >= d.threshold;
+    v[i] = kept ? v[i] * d.scale : 0.f;
+    if (with) (*with)[i] = kept ? (*with)[i] : 0.f;
   }
 }
 

@@ -294,6 +294,28 @@ def test_statistics_of_norms_that_are_not_there_are_not_read(pid, layers, n):
         j.check_backward(back, got.stats.cpu(), got.total.cpu() if j.before else None, what=str(form))
 
 
+@pytest.mark.parametrize("n", [8, 100, 2048, 9000, 20000])
+def test_infinities_that_are_dropped(pid, layers, n):
+    """A block's output that is an infinity or NaN where it is dropped: nothing of it arrives, nor in
+    the gate's gradient."""
+    m, p = 24, 0.5
+    keep = A.drop_factor(m, n, p, 9, 4) > 0
+    g = A.gen(n)
+    x, dt = (torch.randn((m, n), generator=g).to(DEV) for _ in range(2))
+    o = torch.randn((m, n), generator=g)
+    bad = torch.where(keep, o, torch.where(torch.arange(n) % 2 == 0, math.nan, -math.inf))
+    gate = torch.randn(n, generator=g).to(DEV)
+    for norm in (None, pid.Norm("rms")):
+        results = []
+        for out in (o, bad):
+            block = pid.Block(out.to(DEV), None, gate, 1.0, pid.Drop(p, 9, 4))
+            got = pid.pointid_norm(layers, x, norm, block, keep=True)
+            back = pid.pointid_norm_backward(layers, dt if norm else None, got.total if norm else None, got.stats, norm, block,
+                                             dtotal=dt)
+            results.append([got.total, back.dx, back.dout, back.dgate] + ([got.h] if norm else []))
+        assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(*results))
+
+
 def test_no_rows(pid, layers):
     x = torch.empty((0, 24), device=DEV)
     norm = pid.Norm("rms", torch.ones(24, device=DEV), torch.ones(24, device=DEV))
