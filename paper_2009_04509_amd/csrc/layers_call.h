@@ -22,9 +22,6 @@ constexpr int64_t kMaxRows = int64_t(1) << 28;         // m (a launch has fewer 
 
 inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 inline int size_of(int dtype) { return dtype == POINTID_FP32 ? 4 : 2; }
-inline bool rows_in_16(const void* p, int64_t ld, int dtype) {
-  return aligned16(p) && ld % (dtype == POINTID_FP32 ? 4 : 8) == 0;
-}
 
 // No exception crosses the ABI.
 template <class F>

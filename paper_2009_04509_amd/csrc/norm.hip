@@ -172,9 +172,31 @@ __device__ __forceinline__ int group_of(int lanes) {
   return __builtin_amdgcn_readfirstlane((int)threadIdx.x / lanes);
 }
 
-// A thread's columns of one matrix, row after row: kPieces pieces of 8, a row's threads apart.
-// kWhole: rows are whole pieces of 8.
-template <int kType, bool kWhole, int kPieces>
+// How rows end: with a whole piece of 8 columns; with a ragged one, which is read as the row's last 8
+// columns, a load like the others, and moved into place when it is used; or before the eighth column.
+// (Read value by value, each load would be waited for with all that is on its way beside it: bf16 5280 x
+// 4287, both norms and a gate, 52 us for 73, the gradients 82 for 161; 5280 x 4288 takes 40 and 61.)
+enum { kWhole = 0, kRagged = 1, kTiny = 2 };
+
+// A thread's columns of a row: kPieces pieces of 8, a row's threads apart.
+template <int kEnd, int kPieces>
+struct Columns {
+  int col[kPieces], n[kPieces];  // first column, and how many exist
+  int from[kPieces];             // the column from which on 8 are read
+  bool any_end[kPieces];         // a thread of the wave has less than a whole piece
+  __device__ __forceinline__ Columns(int64_t cols, int lane, int lanes) {
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      col[p] = (p * lanes + lane) * 8;
+      n[p] = piece_cols(cols, col[p]);
+      from[p] = kEnd == kRagged && n[p] < 8 ? (int)cols - 8 : col[p];
+      any_end[p] = __any(n[p] < 8);
+    }
+  }
+};
+
+// A thread's columns of one matrix, row after row.
+template <int kType, int kEnd, int kPieces>
 struct Stream {
   static constexpr int64_t kSize = kType == POINTID_FP32 ? 4 : 2;
   char* p;                     // the next row's first column, nullptr without a matrix
@@ -187,25 +209,45 @@ struct Stream {
     for (int i = 0; i < kPieces; ++i) raw[i].load(nullptr, 0);
   }
   // the next row, if there is one (`here`), on its way; zeros if not
-  __device__ __forceinline__ void load(const int (&col)[kPieces], const int (&n)[kPieces], bool here) {
+  __device__ __forceinline__ void load(const Columns<kEnd, kPieces>& c, bool here) {
     if (!p) return;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      if constexpr (kWhole) {
-        if (!here) {
-          raw[i].load(nullptr, 0);
-        } else if (n[i] > 0) {
-          Passing<kType>::load(&raw[i], p + col[i] * kSize, 8, passing);
-        }
-      } else {
-        Passing<kType>::load(&raw[i], p + col[i] * kSize, here ? n[i] : 0, passing);
-      }
+      if (!here)
+        raw[i].load(nullptr, 0);
+      else if constexpr (kEnd == kTiny)
+        raw[i].load(p + c.col[i] * kSize, c.n[i]);
+      else if (kEnd == kRagged || c.n[i] > 0)
+        Passing<kType>::load(&raw[i], p + c.from[i] * kSize, 8, passing);
     }
     p += step;
   }
+  // the values of a piece, 0 where there is no column
+  __device__ __forceinline__ void values(int i, const Columns<kEnd, kPieces>& c, float (&v)[8]) const {
+    raw[i].values(v);
+    if constexpr (kEnd == kRagged)
+      if (c.any_end[i]) {                        // a branch of the whole wave
+        const int move = c.col[i] - c.from[i];
+        move_down<4>(move, v);
+        move_down<2>(move, v);
+        move_down<1>(move, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k < c.n[i] ? v[k] : 0.f;
+      }
+  }
+  // kBy to the left, in bits: a choice between two places would be one between addresses, in memory
+  template <int kBy>
+  static __device__ __forceinline__ void move_down(int move, float (&v)[8]) {
+    const int mask = (move & kBy) != 0 ? -1 : 0;
+#pragma unroll
+    for (int k = 0; k < 8 - kBy; ++k) {
+      const int here = __float_as_int(v[k]), there = __float_as_int(v[k + kBy]);
+      v[k] = __int_as_float(here ^ ((here ^ there) & mask));
+    }
+  }
   // one piece of the row, and on to the next (a matrix that is not there stays so)
   __device__ __forceinline__ void store(int col, int n, bool here, const float (&v)[8]) const {
-    if (p && here && n > 0) Passing<kType>::store(p + col * kSize, kWhole ? 8 : n, v, passing);
+    if (p && here && n > 0) Passing<kType>::store(p + col * kSize, kEnd == kWhole ? 8 : n, v, passing);
   }
   __device__ __forceinline__ void next() {
     if (p) p += step;
@@ -226,32 +268,40 @@ __device__ __forceinline__ void shared_param(const float4* from, int lanes, int 
   v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 
-// The mean (layer) and 1 / deviation of a row; what is past its columns does not count.
-template <bool kWhole, int kPieces, class S>
-__device__ __forceinline__ Stats held_stats(const NormOf& norm, float inv, const int (&n)[kPieces], S& row_sum,
+// 0 past the n columns of a piece, in the waves that have such.
+__device__ __forceinline__ void zero_past(bool any_end, int n, float (&v)[8]) {
+  if (any_end)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.f;
+}
+
+// The mean (layer) and 1 / deviation of a row, whose values are 0 past its columns.
+template <int kEnd, int kPieces, class S>
+__device__ __forceinline__ Stats held_stats(const NormOf& norm, float inv, const Columns<kEnd, kPieces>& c, S& row_sum,
                                             const float (&v)[kPieces][8]) {
   Stats s = {0.f, 1.f};
+  float sum = 0.f;
   if (norm.kind == POINTID_NORM_LAYER) {
-    float sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += v[p][i];
+    s.mean = row_sum(sum) * inv;
+    sum = 0.f;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      float t = 0.f;
+      float d[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t += kWhole || i < n[p] ? v[p][i] : 0.f;
-      sum += n[p] > 0 ? t : 0.f;
+      for (int i = 0; i < 8; ++i) d[i] = v[p][i] - s.mean;
+      zero_past(c.any_end[p], c.n[p], d);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += d[i] * d[i];
     }
-    s.mean = row_sum(sum) * inv;
-  }
-  float sum = 0.f;
+  } else {
 #pragma unroll
-  for (int p = 0; p < kPieces; ++p) {
-    float t = 0.f;
+    for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float d = kWhole || i < n[p] ? v[p][i] - s.mean : 0.f;
-      t += d * d;
-    }
-    sum += n[p] > 0 ? t : 0.f;
+      for (int i = 0; i < 8; ++i) sum += v[p][i] * v[p][i];
   }
   s.r = 1.f / sqrtf(row_sum(sum) * inv + norm.eps);
   return s;
@@ -259,55 +309,54 @@ __device__ __forceinline__ Stats held_stats(const NormOf& norm, float inv, const
 
 extern __shared__ float4 shared_floats[];
 
-// Where the parameters stand in shared memory, in blocks of 2 lanes pieces: the biases last, and
-// only where there are any.
+// The parameters, in the order in which they stand in shared memory, in blocks of 2 lanes pieces.
 enum { kAfterWeight = 0, kGate = 1, kBeforeWeight = 2, kAfterBias = 3, kBeforeBias = 4 };
+template <int kParam>
+using Which = std::integral_constant<int, kParam>;
 template <class Args>
 __device__ __forceinline__ const float* param_of(const Args& a, int i) {
   return i == kAfterWeight ? a.after.weight : i == kGate ? a.gate : i == kBeforeWeight ? a.before.weight
          : i == kAfterBias ? a.after.bias : a.before.bias;
 }
 
-// kShared: the parameters wait in shared memory, for blocks of many rows.  What is not given
-// counts as ones and zeros.
+// kShared: that many of the parameters wait in shared memory, for blocks of many rows.  What is not
+// given counts as ones and zeros.
 // bf16 16384 x 4096 with both norms and a gate (537 MB): 102 us, 5.3 TB/s, the vector units busy
 // 55 %.  256 threads of two pieces with the parameters in registers took 147 (173 registers: two
 // waves a SIMD), blocks of 1024 threads in two groups 138, parameters from memory 121.
-template <int kType, bool kSmall, bool kWhole, bool kBiases, bool kShared, int kPieces>
+template <int kType, bool kSmall, int kEnd, bool kBiases, int kShared, int kPieces>
 __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
-  static_assert(!kShared || kPieces == 1, "parameters of one piece a thread");
+  static_assert(kShared == 0 || kPieces == 1, "parameters of one piece a thread");
   __shared__ float2 waves[2][kMostWaves];
   const int lanes = kSmall ? 16 : a.lanes, groups = blockDim.x / lanes, group = group_of<kSmall>(lanes);
   const int lane = threadIdx.x - group * lanes;
-  int col[kPieces], n[kPieces];
-#pragma unroll
-  for (int p = 0; p < kPieces; ++p) {
-    col[p] = (p * lanes + lane) * 8;
-    n[p] = piece_cols(a.cols, col[p]);
-  }
+  const Columns<kEnd, kPieces> c(a.cols, lane, lanes);
+  const int (&col)[kPieces] = c.col, (&n)[kPieces] = c.n;
   RowSum<kSmall> row_sum(waves, lanes);
   const DropKey key(a.drop);
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
-  Stream<kType, kWhole, kPieces> x(a.x, row, step, a.passing), o(a.o, row, step, a.passing), t(a.t, row, step, a.passing), h(a.h, row, step, a.passing);
-  o.load(col, n, row < a.rows);
-  x.load(col, n, row < a.rows);
-  if constexpr (kShared) {
+  Stream<kType, kEnd, kPieces> x(a.x, row, step, a.passing), o(a.o, row, step, a.passing);
+  Stream<kType, kEnd, kPieces> t(a.t, row, step, a.passing), h(a.h, row, step, a.passing);
+  o.load(c, row < a.rows);
+  x.load(c, row < a.rows);
+  if constexpr (kShared > 0) {
 #pragma unroll
-    for (int i = 0; i < (kBiases ? 5 : 3); ++i)
+    for (int i = 0; i < kShared; ++i)
       if (i % groups == group)
         share_param(param_of(a, i), i < 3 ? 1.f : 0.f, shared_floats + i * 2 * lanes, lanes, lane, col[0], n[0]);
     __syncthreads();
   }
-  auto param = [&](int i, int p, float (&v)[8]) {
-    if constexpr (kShared)
+  auto param = [&](auto which, int p, float (&v)[8]) {
+    constexpr int i = decltype(which)::value;
+    if constexpr (i < kShared)
       shared_param(shared_floats + i * 2 * lanes, lanes, lane, v);
     else
       load_param(param_of(a, i), col[p], n[p], i < 3 ? 1.f : 0.f, v);
   };
   // (v - mean) r weight + bias
-  auto affine = [&](float (&v)[8], const Stats& s, int weight, int bias, int p) {
+  auto affine = [&](float (&v)[8], const Stats& s, auto weight, auto bias, int p) {
     float w[8];
     param(weight, p, w);
 #pragma unroll
@@ -324,25 +373,28 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
     float v[kPieces][8], s[kPieces][8];
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      o.raw[p].values(v[p]);
-      x.raw[p].values(s[p]);
+      o.values(p, c, v[p]);
+      x.values(p, c, s[p]);
     }
     // the next row is on its way while this one is worked on
-    o.load(col, n, more);
-    x.load(col, n, more);
+    o.load(c, more);
+    x.load(c, more);
     Stats after = {0.f, 1.f}, before = {0.f, 1.f};
     if (a.o.p) {
       if (a.after.kind) {
-        after = held_stats<kWhole>(a.after, inv, n, row_sum, v);
+        after = held_stats(a.after, inv, c, row_sum, v);
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) affine(v[p], after, kAfterWeight, kAfterBias, p);
+        for (int p = 0; p < kPieces; ++p) {
+          affine(v[p], after, Which<kAfterWeight>{}, Which<kAfterBias>{}, p);
+          zero_past(c.any_end[p], n[p], v[p]);
+        }
       }
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
         if (a.drop.threshold) drop8(a.drop, key, row, col[p], v[p]);
         if (a.gate) {
           float w[8];
-          param(kGate, p, w);
+          param(Which<kGate>{}, p, w);
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[p][i] *= w[i];
         }
@@ -353,10 +405,10 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
       t.next();
     }
     if (a.h.p) {
-      before = held_stats<kWhole>(a.before, inv, n, row_sum, s);
+      before = held_stats(a.before, inv, c, row_sum, s);
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
-        affine(s[p], before, kBeforeWeight, kBeforeBias, p);
+        affine(s[p], before, Which<kBeforeWeight>{}, Which<kBeforeBias>{}, p);
         h.store(col[p], n[p], here, s[p]);
       }
       h.next();
@@ -545,26 +597,27 @@ __global__ void __launch_bounds__(256) norm_back_kernel(NormBackArgs a) {
 // a SIMD, one block of 512 threads), took 277; both in shared memory and the branches 230.  fp16 1693
 // x 2304, layer norms (47 MB): 21 us, 3.3 rows for each of 512 groups, of which the first waits for
 // memory.
-template <int kType, bool kSmall, bool kWhole, bool kBiases, int kMost>
+template <int kType, bool kSmall, int kEnd, bool kBiases, int kMost>
 __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
   __shared__ float2 waves[2][kMostWaves];
   const int lanes = kSmall ? 16 : a.lanes, groups = blockDim.x / lanes, group = group_of<kSmall>(lanes);
   const int lane = threadIdx.x - group * lanes, col = lane * 8, n = piece_cols(a.cols, col);
-  const int cols[1] = {col}, ns[1] = {n};
+  const Columns<kEnd, 1> c(a.cols, lane, lanes);
   RowSum<kSmall> row_sum(waves, lanes);
   const DropKey key(a.drop);
   const float inv = 1.f / (float)a.cols;
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
-  Stream<kType, kWhole, 1> dh(a.dh, row, step, a.passing), t(a.t, row, step, a.passing), dt(a.dt, row, step, a.passing), o(a.o, row, step, a.passing);
-  Stream<kType, kWhole, 1> dx(a.dx, row, step, a.passing), dout(a.dout, row, step, a.passing);
+  Stream<kType, kEnd, 1> dh(a.dh, row, step, a.passing), t(a.t, row, step, a.passing);
+  Stream<kType, kEnd, 1> dt(a.dt, row, step, a.passing), o(a.o, row, step, a.passing);
+  Stream<kType, kEnd, 1> dx(a.dx, row, step, a.passing), dout(a.dout, row, step, a.passing);
   float4 next;
   auto load = [&](int64_t r) {
     const bool here = r < a.rows;
-    dh.load(cols, ns, here);
-    t.load(cols, ns, here);
-    dt.load(cols, ns, here);
-    o.load(cols, ns, here);
+    dh.load(c, here);
+    t.load(c, here);
+    dt.load(c, here);
+    o.load(c, here);
     next = a.stats && here ? reinterpret_cast<const float4*>(a.stats)[r] : make_float4(0.f, 1.f, 0.f, 1.f);
   };
   load(row);
@@ -579,10 +632,10 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
     const bool here = row < a.rows;
     float e[8], u[8], d[8], w[8], v[8];
     const float4 st = a.after.kind ? next : make_float4(0.f, 1.f, next.z, next.w);
-    dh.raw[0].values(e);
-    t.raw[0].values(u);
-    dt.raw[0].values(d);
-    o.raw[0].values(v);
+    dh.values(0, c, e);
+    t.values(0, c, u);
+    dt.values(0, c, d);
+    o.values(0, c, v);
     load(row + step);
     if (a.before.kind) {
       float se = 0.f, seu = 0.f;
@@ -599,16 +652,13 @@ __global__ void __launch_bounds__(kMost) norm_back_rows_kernel(NormBackArgs a) {
       const bool layer = a.before.kind == POINTID_NORM_LAYER;
       const float2 s = layer ? row_sum(se, seu) : make_float2(0.f, row_sum(seu));
       const float on_u = st.w * (s.y * inv), on_1 = st.w * (s.x * inv);
-      // of columns and rows that do not exist nothing is added
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        d[i] += st.w * e[i] - on_u * u[i] - on_1;
-        if constexpr (!kWhole) d[i] = i < n && here ? d[i] : 0.f;
-      }
-      if constexpr (kWhole)
-        if (!here || n == 0)
+      for (int i = 0; i < 8; ++i) d[i] += st.w * e[i] - on_u * u[i] - on_1;
+      // columns and rows that do not exist add nothing
+      zero_past(c.any_end[0], n, d);
+      if (!here)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[i] = 0.f;
+        for (int i = 0; i < 8; ++i) d[i] = 0.f;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = a.scale * d[i];
@@ -729,12 +779,17 @@ int back_threads(int dtype, bool biases, int64_t cols) {
   return (biases || dtype == POINTID_FP32) && cols <= 6144 ? 768 : 1024;
 }
 
-// f with its template arguments' truth values as constants
+// f with constants: whether a row has 16 threads, how it ends, whether there are biases.
 template <class F>
-hipError_t with_flags(bool a, bool b, bool c, F&& f) {
-  auto on = [&](auto x, auto y) { return c ? f(x, y, std::true_type{}) : f(x, y, std::false_type{}); };
-  auto up = [&](auto x) { return b ? on(x, std::true_type{}) : on(x, std::false_type{}); };
-  return a ? up(std::true_type{}) : up(std::false_type{});
+hipError_t with_shape(int64_t cols, bool biases, F&& f) {
+  auto up = [&](auto small, auto end) {
+    return biases ? f(small, end, std::true_type{}) : f(small, end, std::false_type{});
+  };
+  const Which<kWhole> whole;
+  const Which<kRagged> ragged;
+  if (cols < 8) return up(std::true_type{}, Which<kTiny>{});
+  if (cols <= 128) return cols % 8 ? up(std::true_type{}, ragged) : up(std::true_type{}, whole);
+  return cols % 8 ? up(std::false_type{}, ragged) : up(std::false_type{}, whole);
 }
 
 template <int kType>
@@ -749,17 +804,26 @@ hipError_t launch_norm_of(NormArgs a, hipStream_t stream) {
   // Many rows: blocks of at least 8 sets of rows, with the parameters in shared memory.  bf16, both
   // norms and a gate, read from memory for every row and shared: 16384 x 4096 121 us and 104, 8192 x
   // 4096 59 and 49, 8192 x 8192 150 and 105; fp32 8192 x 4096 113 and 104.
-  const size_t bytes = (size_t)(biases ? 5 : 3) * h.lanes * 32;
-  const bool shared = need >= 4096 && !two && bytes <= kMostShared;
+  const bool shared = need >= 4096 && !two;
+  // Biases as well where they fit: five against three of five, both norms layer norms with biases and a
+  // gate: bf16 16384 x 2304 80 us and 91, 16384 x 3200 (14 waves a CU) 106 and 111, 8192 x 5120 (10) 93 and
+  // 96; but with 8 or 9 waves a CU too few loads are on their way: 16384 x 4096 154 and 106, 5280 x 4288 71
+  // and 56.  fp32, whose loads are twice as large, 16384 x 4096 204 and 208, 5280 x 4288 79 and 88.
+  auto bytes = [&](int params) { return (size_t)params * h.lanes * 32; };
+  const int waves = (int)(kMostShared / bytes(5)) * (h.lanes * h.groups / 64);
+  const bool five = biases && waves >= (kType == POINTID_FP32 ? 1 : 10);
   int64_t blocks = need < 65536 ? need : 65536;
   if (shared) blocks = need / 8 < 4096 ? need / 8 : 4096;
   auto go = [&](auto kernel, size_t shared_bytes) {
     return launch_kernel(kernel, dim3((unsigned)blocks), dim3(h.lanes * h.groups), shared_bytes, stream, a);
   };
-  return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
-    if (shared) return go(norm_rows_kernel<kType, small, whole, bias, true, 1>, bytes);
-    if (two) return go(norm_rows_kernel<kType, false, whole, bias, false, 2>, 0);
-    return go(norm_rows_kernel<kType, small, whole, bias, false, 1>, 0);
+  return with_shape(a.cols, biases, [&](auto small, auto end, auto bias) {
+    if constexpr (bias)
+      if (shared && five) return go(norm_rows_kernel<kType, small, end, bias, 5, 1>, bytes(5));
+    if (shared) return go(norm_rows_kernel<kType, small, end, bias, 3, 1>, bytes(3));
+    if constexpr (!small)
+      if (two) return go(norm_rows_kernel<kType, false, end, bias, 0, 2>, 0);
+    return go(norm_rows_kernel<kType, small, end, bias, 0, 1>, 0);
   });
 }
 
@@ -816,16 +880,16 @@ hipError_t launch_norm_back_of(NormBackArgs a, bool held, hipStream_t stream) {
   a.lanes = h.lanes;
   // the parameters, or the groups' sums: at most 128 KB
   const int shared = biases ? 4 : 3;
-  return with_flags(a.cols <= 128, a.cols % 8 == 0, biases, [&](auto small, auto whole, auto bias) {
+  return with_shape(a.cols, biases, [&](auto small, auto end, auto bias) {
     auto go = [&](auto kernel) {
       return launch_kernel(kernel, dim3((unsigned)a.blocks), dim3(h.lanes * h.groups),
                            (size_t)(shared > h.groups ? shared : h.groups) * h.lanes * 32, stream, a);
     };
     if constexpr (bias || kType == POINTID_FP32) {
-      if constexpr (small) return go(norm_back_rows_kernel<kType, small, whole, bias, 768>);
-      if (threads == 768) return go(norm_back_rows_kernel<kType, small, whole, bias, 768>);
+      if constexpr (small) return go(norm_back_rows_kernel<kType, small, end, bias, 768>);
+      if (threads == 768) return go(norm_back_rows_kernel<kType, small, end, bias, 768>);
     }
-    if constexpr (!(small && (bias || kType == POINTID_FP32))) return go(norm_back_rows_kernel<kType, small, whole, bias, 1024>);
+    if constexpr (!(small && (bias || kType == POINTID_FP32))) return go(norm_back_rows_kernel<kType, small, end, bias, 1024>);
   });
 }
 }  // namespace

@@ -121,7 +121,8 @@ def test_forward_and_backward(pid, layers, dtype, m, n):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("m, n", [(4100, 8192), (4097, 7000), (6, 8192), (4100, 6145), (70000, 40), (9000, 520)])
+@pytest.mark.parametrize("m, n", [(4100, 8192), (4097, 7000), (6, 8192), (4100, 6145), (70000, 40), (9000, 520),
+                                  (4100, 3587), (4200, 4093), (70000, 13), (20000, 1001)])
 def test_many_rows_and_the_widest_that_are_held(pid, layers, dtype, m, n):
     """With every parameter: what a block keeps in shared memory is largest.  The last rows and all
     column sums are checked."""
@@ -157,6 +158,32 @@ def test_many_rows_and_the_widest_that_are_held(pid, layers, dtype, m, n):
             # fp32 sums of m terms in a tree of partial sums of at most m / 256 + 64 in turn
             tol = parts.abs().sum(0) * (m / 256 + 64) * A.E + 1e-5 * parts.abs().sum(0)
             assert ((getattr(back, name).double() - parts.sum(0)).abs() <= tol).all(), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("n", [2, 7, 9, 15, 127, 129, 505, 515, 1001, 4090, 8191, 8195, 16383])
+def test_rows_that_end_inside_a_piece(pid, layers, dtype, n):
+    """Every matrix between columns of NaN, total in x's place and dx in dtotal's: nothing of what is beside
+    a row is taken or written."""
+    def inside(t):
+        big = torch.full((t.shape[0], n + 11), float("nan"), dtype=A.DT[dtype], device=DEV)
+        big[:, 5:5 + n] = t.to(DEV)
+        return big, big[:, 5:5 + n]
+
+    def around_is_untouched(big):
+        assert torch.isnan(big[:, :5]).all() and torch.isnan(big[:, 5 + n:]).all()
+
+    for i, form in enumerate(FORMS):
+        j = Joint(pid, dtype, 5, n, form, seed=i)
+        (bx, x), (bo, o), (bdh, dh), (bdt, dt) = (inside(t) for t in (j.x, j.o, j.dh, j.dt))
+        bh, h = inside(torch.zeros(5, n))
+        got = pid.pointid_norm(layers, x, j.norm(), j.block(o), total=x, h=h if j.before else None, keep=True)
+        j.check_forward(got, str(form))
+        back = pid.pointid_norm_backward(layers, dh if j.before else None, x if j.before else None, got.stats, j.norm(),
+                                         j.block(o), dtotal=dt, dx=dt)
+        j.check_backward(back, got.stats.cpu(), got.total.cpu() if j.before else None, True, str(form))
+        for big in (bx, bo, bdh, bdt, bh):
+            around_is_untouched(big)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
