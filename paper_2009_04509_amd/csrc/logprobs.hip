@@ -470,10 +470,16 @@ __global__ void __launch_bounds__(512) scan_join_kernel(ScanArgs a) {
 
 // dx_j = scale (dlogp ([j = t] - p_j) + dlse p_j - dH p_j (ln p_j + H)), p_j = e^(z_j - lse), as
 //   q = log2 p_j = x_j scale / ln 2 - lse / ln 2       dx_j = 2^q (on_p - on_pq q) + [j = t] at_target
+// x scale, rounded, less lse
+__device__ __forceinline__ float rounded_less(float x, float scale, float lse) {
+#pragma clang fp contract(off)
+  const float z = x * scale;
+  return z - lse;
+}
 struct BackRow {
   float lse, lse2, at_target, on_p, on_pq;
   int32_t target;
-  bool far;                    // lse / ln 2 may leave the range: x_j scale - lse first
+  bool far;                    // lse is large: see gradient
   // what is read of a row; kept until its turn
   struct Read {
     float lse, dlogp, dlse, dh, h;
@@ -495,13 +501,19 @@ struct BackRow {
     on_pq = r.dh * scale * kLn2;
     lse = empty ? __builtin_inff() : r.lse;                   // p is 0 in a row of nothing
     lse2 = lse * kLog2e;
-    far = !empty && __builtin_fabsf(lse) > 1e37f;
+    far = !empty && __builtin_fabsf(lse) > 1024.f;
   }
   // (fp32: the difference first too, which the roundings of scale / ln 2 and lse / ln 2 are in
-  // otherwise: they double the error of a result that is rounded to 24 bits)
+  // otherwise: they double the error of a result that is rounded to 24 bits.  Of a large lse, whose
+  // own rounding passes that of p, z_j is rounded as the forward pass rounds the largest: what of it
+  // lse cannot hold would be all that is left of the difference, and p past 1, by 2^60 in a bf16 row
+  // of -1e9 alone.)
   template <int kType, bool kEntropy>
   __device__ __forceinline__ void gradient(float scale, float c, int col, float (&v)[8]) const {
-    if (kType == POINTID_FP32 || far) {
+    if (far) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = rounded_less(v[j], scale, lse) * kLog2e;
+    } else if (kType == POINTID_FP32) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(v[j], scale, -lse) * kLog2e;
     } else {
