@@ -103,6 +103,10 @@ __device__ __forceinline__ uint64_t long_entry(uint32_t e, uint32_t first_place)
 struct Sums {
   float most, s, w;
 };
+// A result of `of`, fp32's largest finite value in place of an infinity that is not of's own.
+__device__ __forceinline__ float in_range(float v, float of) {
+  return __builtin_isinf(v) && !__builtin_isinf(of) ? __builtin_copysignf(-kLowest, v) : v;
+}
 // What is subtracted: finite, so that no infinity meets itself in a row that is masked whole.
 __device__ __forceinline__ float finite_most(float most) { return fmaxf(most, kLowest); }
 constexpr float kNone = -1000.f;               // 2^kNone is 0, and kNone times it too
@@ -171,7 +175,8 @@ struct RowEnd {
   __device__ __forceinline__ RowEnd(const Sums& v, float scale_) : most(v.most), scale(scale_) {
     empty = v.s == 0.f;
     ln_s = logf(v.s);
-    lse = empty ? -__builtin_inff() : most * scale + ln_s;
+    // (past fp32's range its end: minus infinity is a row of nothing alone)
+    lse = empty ? -__builtin_inff() : in_range(most * scale + ln_s, most);
     entropy = empty ? 0.f : ln_s - kLn2 * v.w / v.s;
   }
   __device__ __forceinline__ float logp(float x) const { return empty ? -__builtin_inff() : (x - most) * scale - ln_s; }
@@ -470,10 +475,10 @@ __global__ void __launch_bounds__(512) scan_join_kernel(ScanArgs a) {
 
 // dx_j = scale (dlogp ([j = t] - p_j) + dlse p_j - dH p_j (ln p_j + H)), p_j = e^(z_j - lse), as
 //   q = log2 p_j = x_j scale / ln 2 - lse / ln 2       dx_j = 2^q (on_p - on_pq q) + [j = t] at_target
-// x scale, rounded, less lse
+// x scale, rounded and in fp32's range, less lse
 __device__ __forceinline__ float rounded_less(float x, float scale, float lse) {
 #pragma clang fp contract(off)
-  const float z = x * scale;
+  const float z = in_range(x * scale, x);
   return z - lse;
 }
 struct BackRow {

@@ -1,8 +1,8 @@
 """GPU: log probabilities where the log of the sum of exponentials is large: masks of a type's lowest
-value or of -1e9 in every column.
+value or of -1e9 in every column, logits times a scale past fp32's range.
 
 fp32 keeps lse to 2^-24 of itself, so that past 2^24 or so ln of a sum is lost in it: the gradient is
-that of z_j = scale x_j rounded to fp32 and of lse as it stands,
+that of z_j = scale x_j rounded to fp32 (past its range to its largest finite values) and of lse as it stands,
 p_j = e^(z_j - lse), which is 1 where z_j is the row's largest."""
 
 import math
@@ -105,7 +105,10 @@ def check(pid, layers, dtype, m, n, scale):
         s = float(torch.tensor(scale))
         v = (p * on + one * a) * s
         tol = (tp * size + p * (4 * A.E * size + b.abs() * tp / p.clamp(min=1e-300)) + 2 * A.E * (one * a).abs()) * s
-        A.near(dx, v, A.rounded(v, tol + 2 * A.E * v.abs(), dtype), f"dlogits {use}")
+        tol = tol + 2 * A.E * v.abs()
+        if dtype == "fp16":                            # to the nearest: from 65520 on an infinity
+            v = torch.where(v.abs() - tol >= 65520, v.sign() * INF, v)
+        A.near(dx, v, A.rounded(v, tol, dtype), f"dlogits {use}")
 
 
 SIZES = [(12, 3), (12, 70), (12, 500), (12, 900), (1100, 2500), (12, 40000)]
@@ -115,4 +118,12 @@ SIZES = [(12, 3), (12, 70), (12, 500), (12, 900), (1100, 2500), (12, 40000)]
 @pytest.mark.parametrize("m, n", SIZES)
 @pytest.mark.parametrize("scale", [1.0, 0.7])
 def test_large_lse(pid, layers, dtype, m, n, scale):
+    check(pid, layers, dtype, m, n, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("m, n", SIZES)
+@pytest.mark.parametrize("scale", [1.25, 2.0 ** 64])
+def test_past_the_range(pid, layers, dtype, m, n, scale):
+    """An lse that fp32 does not reach is its largest finite value, never that of a row of nothing."""
     check(pid, layers, dtype, m, n, scale)
