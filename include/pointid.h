@@ -698,8 +698,9 @@ uint64_t pointid_norm_backward_scratch(pointid_layers l, int64_t m, int64_t n);
  *   top       0..64, at most n; top_ids int32 [m][top], top_logp fp32 [m][top]
  * A logit of minus infinity is a column that cannot be: p is 0 there, ln p minus infinity.  In a
  * row of nothing else lse and every ln p are minus infinity, entropy is 0 and the top columns are
- * the first ones.  Of other rows an lse past fp32's range is its largest finite value, of either sign.  Plus infinity or a NaN make a row's lse, logp, entropy and top_logp NaN; a
- * NaN's place among the top columns is that of minus infinity.
+ * the first ones.  Of other rows an lse past fp32's range is its largest finite value, of either
+ * sign.  Plus infinity or a NaN make a row's lse, logp, entropy and top_logp NaN; a NaN's place
+ * among the top columns is that of minus infinity.
  * Errors: EINVAL (NULL l, logits or outputs; scale, top, a size, pitch or alignment out of range;
  * scratch too small or not aligned), EUNSUPPORTED (dtype), ENOMEM, EHIP.
  */
@@ -716,9 +717,10 @@ uint64_t pointid_logprobs_scratch(pointid_layers l, int64_t m, int64_t n, int32_
  *   lse       as the forward call left it; entropy too, needed with dentropy
  *   targets   needed with dlogp
  *   dlogits   may be logits itself
- * p_j = e^(z_j - lse) of the fp32 lse, so off by up to 2^-24 |lse| of itself; of an |lse| above 1024 z_j
- * is rounded to fp32 too (past its range to its largest finite value), and p_j at most 1.
- * 0 in rows whose lse is minus infinity.  Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
+ * p_j = e^(z_j - lse) of the fp32 lse, so off by up to 2^-24 |lse| of itself; of an |lse| above
+ * 1024 z_j is rounded to fp32 too (past its range to its largest finite value), and p_j at most 1.
+ * 0 in rows whose lse is minus infinity, whatever their gradients are.
+ * Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.
  */
 int pointid_logprobs_backward(pointid_layers l, int dtype, int64_t m, int64_t n, const pointid_matrix *logits,
                               float scale, const float *lse, const int32_t *targets, const float *dlogp,

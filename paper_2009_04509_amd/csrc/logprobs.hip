@@ -502,8 +502,9 @@ struct BackRow {
     const bool empty = r.lse == -__builtin_inff(), has = r.target >= 0 && r.target < cols && !empty;
     target = has ? r.target : -1;
     at_target = has ? r.dlogp * scale : 0.f;
-    on_p = r.dlse * scale - at_target - r.dh * r.h * scale;
-    on_pq = r.dh * scale * kLn2;
+    // (of a row of nothing 0, as a loss may make an infinity or a NaN of its lse)
+    on_p = empty ? 0.f : r.dlse * scale - at_target - r.dh * r.h * scale;
+    on_pq = empty ? 0.f : r.dh * scale * kLn2;
     lse = empty ? __builtin_inff() : r.lse;                   // p is 0 in a row of nothing
     lse2 = lse * kLog2e;
     far = !empty && __builtin_fabsf(lse) > 1024.f;

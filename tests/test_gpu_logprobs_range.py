@@ -1,5 +1,6 @@
 """GPU: log probabilities where the log of the sum of exponentials is large: masks of a type's lowest
-value or of -1e9 in every column, logits times a scale past fp32's range.
+value or of -1e9 in every column, logits times a scale past fp32's range;
+and the gradients of rows of nothing.
 
 fp32 keeps lse to 2^-24 of itself, so that past 2^24 or so ln of a sum is lost in it: the gradient is
 that of z_j = scale x_j rounded to fp32 (past its range to its largest finite values) and of lse as it stands,
@@ -127,3 +128,26 @@ def test_large_lse(pid, layers, dtype, m, n, scale):
 def test_past_the_range(pid, layers, dtype, m, n, scale):
     """An lse that fp32 does not reach is its largest finite value, never that of a row of nothing."""
     check(pid, layers, dtype, m, n, scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("n", [3, 70, 900, 40000])
+def test_rows_of_nothing_have_no_gradient(pid, layers, dtype, n):
+    """Their lse is minus infinity; what a loss makes of it (a penalty of lse^2: an infinity, or a NaN) does
+    not reach the logits."""
+    x = A.rand(A.gen(n), 4, n, dtype=dtype)
+    x[1] = -INF
+    x[3] = -INF
+    t = torch.tensor([0, 1, -1, n - 1], dtype=torch.int32, device=DEV)
+    X = x.to(DEV)
+    got = pid.pointid_logprobs(layers, X, t, entropy=True)
+    good = torch.ones(4, device=DEV)
+    for bad in (-INF, INF, math.nan):
+        d = good.clone()
+        d[1::2] = bad
+        for args in ((d, None, None, None), (None, got.entropy, d, None), (None, None, None, d), (d, got.entropy, d, d)):
+            dx = pid.pointid_logprobs_backward(layers, X, got.lse, t if args[0] is not None else None, *args)
+            assert (dx[1::2] == 0).all() and torch.isfinite(dx).all(), (bad, dx[1::2])
+            same = pid.pointid_logprobs_backward(layers, X, got.lse, t if args[0] is not None else None,
+                                                 *(good if v is d else v for v in args))
+            assert torch.equal(dx[::2], same[::2])
