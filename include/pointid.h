@@ -613,7 +613,8 @@ int pointid_dropout(pointid_layers l, int dtype, int64_t m, int64_t n, const poi
 /* Norms of rows: u w + b with
  *   RMS    u = x / sqrt(mean(x^2) + eps)
  *   LAYER  u = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps)
- * The squares are summed in fp32: rows whose sum of squares passes its range become 0. */
+ * Both are summed in fp32: rows whose sum of squares passes its range become 0 (u), and rows of a
+ * layer norm whose sum does NaN. */
 enum {
     POINTID_NORM_NONE = 0,
     POINTID_NORM_RMS = 1,

@@ -1,4 +1,5 @@
-"""GPU: layer norms of rows of one value, and of rows whose values differ by little beside their mean."""
+"""GPU: norms of rows of one value, of rows whose values differ by little beside their mean, and of rows
+whose sums pass fp32's range."""
 
 import pytest
 import torch
@@ -63,3 +64,20 @@ def test_the_mean_is_rounded_once(pid, layers, m, n):
     var = (x.double() - mean.view(-1, 1)).square().mean(1) + EPS
     # each difference is exact but for the mean's own rounding, whose square counts
     assert ((got.stats[:, 3].double() * var.sqrt() - 1).abs() <= A.depth(n) * A.E + tol * tol / var).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [100, 1001, 12000, 20000])
+def test_sums_past_the_range(pid, layers, dtype, n):
+    """Of squares: 0 times the weight, whatever the mean; of a layer norm's values: NaN.  The next rows are theirs."""
+    x = torch.randn((6, n), device=DEV)
+    x[0] = torch.where(torch.arange(n, device=DEV) % 2 == 0, 1e30, -1e30)
+    x[1] = 1e30 + 1e28 * x[1].clamp(-1, 1)
+    x[2] = 3e38
+    x = x.to(A.DT[dtype])
+    w, b = (torch.randn(n, device=DEV) for _ in range(2))
+    for kind in ("rms", "layer"):
+        h = pid.pointid_norm(layers, x, pid.Norm(kind, w, b)).h
+        assert torch.equal(h[:2], b.to(h.dtype).expand(2, n)), kind
+        assert h[2].isnan().all() if kind == "layer" else torch.equal(h[2], b.to(h.dtype))
+        assert torch.equal(h[3:], pid.pointid_norm(layers, x[3:], pid.Norm(kind, w, b)).h)
