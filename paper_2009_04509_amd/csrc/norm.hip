@@ -177,6 +177,10 @@ struct RowSum {
   }
 };
 
+// A value that a wave's threads have alike, in a register of the wave's.
+__device__ __forceinline__ float of_wave(float v) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
 // A thread's group; known to be the same for a wave's threads where it is.
 template <bool kSmall>
 __device__ __forceinline__ int group_of(int lanes) {
@@ -362,7 +366,7 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
   const int (&col)[kPieces] = c.col, (&n)[kPieces] = c.n;
   RowSum<kSmall> row_sum(waves, lanes);
   const DropKey key(a.drop);
-  const float inv = 1.f / (float)a.cols;
+  const float cols = of_wave((float)a.cols), inv = of_wave(1.f / (float)a.cols);
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
   Stream<kType, kEnd, kPieces> x(a.x, row, step, a.passing), o(a.o, row, step, a.passing);
@@ -410,7 +414,7 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
     Stats after = {0.f, 1.f}, before = {0.f, 1.f};
     if (a.o.p) {
       if (a.after.kind) {
-        after = held_stats<kType>(a.after, (float)a.cols, inv, c, row_sum, v);
+        after = held_stats<kType>(a.after, cols, inv, c, row_sum, v);
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
           affine(v[p], after, Which<kAfterWeight>{}, Which<kAfterBias>{}, p);
@@ -433,7 +437,7 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(NormArgs a) {
       t.next();
     }
     if (a.h.p) {
-      before = held_stats<kType>(a.before, (float)a.cols, inv, c, row_sum, s);
+      before = held_stats<kType>(a.before, cols, inv, c, row_sum, s);
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
         affine(s[p], before, Which<kBeforeWeight>{}, Which<kBeforeBias>{}, p);
