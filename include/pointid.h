@@ -718,7 +718,7 @@ uint64_t pointid_logprobs_scratch(pointid_layers l, int64_t m, int64_t n, int32_
  *   lse       as the forward call left it; entropy too, needed with dentropy
  *   targets   needed with dlogp
  *   dlogits   may be logits itself
- * p_j = e^(z_j - lse) of the fp32 lse, so off by up to 2^-24 |lse| of itself; of an |lse| above
+ * p_j = e^(z_j - lse) of the fp32 lse, so off by up to 2^-22 |lse| of itself; of an |lse| above
  * 1024 z_j is rounded to fp32 too (past its range to its largest finite value), and p_j at most 1.
  * 0 in rows whose lse is minus infinity, whatever their gradients are.
  * Errors: EINVAL, EUNSUPPORTED (dtype), EHIP.

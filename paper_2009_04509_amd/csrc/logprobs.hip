@@ -7,8 +7,8 @@
 // and brings them to a new maximum when one comes, so that a row is read once.
 //
 // bf16 4096 x 65536 (537 MB) 100 us, 5.4 TB/s, with the 8 likeliest columns 112: near the bytes'
-// time, and near the vector units' too, which the first form kept busy 91 % (an exponential is four
-// instructions' time, and 6 more for each column are the difference, its scale, the clamp and the sums).
+// time, and near the vector units' too, which are busy 80 % of it (an exponential is four instructions'
+// time, and 6 more for each column are the difference, its scale, the clamp and the sums).
 #include "internal.h"
 #include "layers_end.h"
 #include "norm.h"
@@ -379,7 +379,9 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a) {
 }
 
 // Rows of at most 8 kLanes columns, each by kLanes lanes that hold 8 of them; the most likely
-// columns one by one.  fp32 50000 x 3: 3.5 us (a block a row: 280); bf16 500000 x 64 30 us.
+// columns one by one, each a pass over the row's lanes.  fp32 50000 x 3 with the likeliest: 3.5 us (a block a
+// row: 280); bf16 500000 x 64 (64 MB) with 0, 1 and 20 of them 20, 30 and 125, 50000 x 500 with 0, 1, 8
+// and 32 23, 30, 58 and 158.
 template <int kType, int kLanes>
 __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs a) {
   constexpr int kSize = kType == POINTID_FP32 ? 4 : 2, kRows = 256 / kLanes;
@@ -539,7 +541,9 @@ struct BackRow {
 // A strip of 8 columns a thread, row after row: a block's threads are groups of `lanes` (kSmall: a
 // part of a wave, else whole ones), each group with a row at a time, the next row on its way.
 // bf16 4096 x 65536 with an entropy term (1.07 GB) 174 us, 6.2 TB/s; as pieces of any row, whose place
-// is a division and whose row's values are read for each piece, 200 and the vector units busy 86 %.
+// is a division and whose row's values are read for each piece, 200 and the vector units busy 86 %, now 72.
+// Rows of 33 to 63 pieces leave lanes of a wave without one, and a row's end inside a piece is read and
+// written value by value: bf16 100000 x 300 43 us, x 303 49, x 304 32, x 1000 77 (5.2 TB/s).
 template <int kType, bool kSmall, bool kEntropy>
 __global__ void __launch_bounds__(256) scan_back_kernel(ScanBackArgs a) {
   constexpr int64_t kSize = kType == POINTID_FP32 ? 4 : 2;
@@ -602,7 +606,9 @@ hipError_t launch_logprobs_of(const ScanArgs& a, hipStream_t stream) {
   // By waves of their own up to 8192 columns, where the rows fill the card so: a block's waves wait
   // for each other in the choice of the likeliest columns.  With the 8 likeliest, bf16, by waves and
   // by blocks of 4: 32768 x 4096 80 us and 228, 16384 x 8192 73-79 and 114, 16384 x 16384 171 and
-  // 152, 4096 x 65536 169 and 120.
+  // 152, 4096 x 65536 169 and 120; 4096 x 8192 22 and 29, 4096 x 4096 12.4 and 23.5, 2048 x 8192 12.3 and
+  // 15.6, of 1100 rows of 4096 or 8192 both less than the call's host side (11.6).  Without a list they are
+  // alike from 4096 rows of 8192 on (16, 8192 rows 31), and of 4096 columns 9.3 and 10.4.
   if (a.cols <= 8192 && a.rows > 1024)
     return a.entropy ? go(scan_kernel<kType, 64, true>, 64) : go(scan_kernel<kType, 64, false>, 64);
   return a.entropy ? go(scan_kernel<kType, 256, true>, 256) : go(scan_kernel<kType, 256, false>, 256);

@@ -117,7 +117,8 @@ __device__ __forceinline__ Stats stats_of(const NormOf& norm, int64_t cols, floa
   return {0.f, 1.f / sqrtf(s.y / n + norm.eps)};
 }
 
-// Rows of more than 16384 columns: a block a row, which is read once for each sum and once more.
+// Rows of more than 16384 columns: a block a row, which is read once for each sum and once more.  bf16,
+// both norms and a gate, 4096 x 16400 210 us and 4096 x 32768 438 (held, 4096 x 16384 126).
 template <int kType>
 __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   __shared__ float2 waves[4];
@@ -806,7 +807,11 @@ HeldShape held_shape(int64_t cols, int threads) {
 }
 // Threads of a block of the backward pass: 768 leave each 168 registers, which the sums of biases
 // and fp32 rows take; 1024 leave 128.  768 and 1024: bf16 16384 x 4096 with biases 160 us and 235,
-// fp32 8192 x 4096 without 166 and 175, bf16 300000 x 100 without 175 and 152.
+// fp32 8192 x 4096 without 166 and 175, bf16 300000 x 100 without 175 and 152.  Rows of more than 6144
+// columns are a block of more threads, whose 128 registers do not hold these (22 to 40 of them in
+// memory with biases, 6 to 8 without): in the two passes of wider rows they would take longer all the same.
+// Held and in two passes, layer norms with biases, bf16 4096 x 8192 115 us and 185, 1693 x 7168 71 and 79,
+// 4096 x 8191 175 and 329, fp32 4096 x 8192 257 and 304, 1693 x 7168 128 and 128; without, 181 and 300, 80 and 124.
 int back_threads(int dtype, bool biases, int64_t cols) {
   return (biases || dtype == POINTID_FP32) && cols <= 6144 ? 768 : 1024;
 }
@@ -835,7 +840,9 @@ hipError_t launch_norm_of(NormArgs a, hipStream_t stream) {
   const int64_t need = (a.rows + h.groups - 1) / h.groups;
   // Many rows: blocks of at least 8 sets of rows, with the parameters in shared memory.  bf16, both
   // norms and a gate, read from memory for every row and shared: 16384 x 4096 121 us and 104, 8192 x
-  // 4096 59 and 49, 8192 x 8192 150 and 105; fp32 8192 x 4096 113 and 104.
+  // 4096 59 and 49, 8192 x 8192 150 and 105; fp32 8192 x 4096 113 and 104.  Few rows wait for the staging:
+  // 3000 x 4096 23.5 us and 24.5, 4100 x 4096 30.7 and 28.4, 2100 x 8192 41 and 47, 4100 x 8192 78 and 58,
+  // fp32 2100 x 4096 29 and 34, 4100 x 4096 53 and 49.
   const bool shared = need >= 4096 && !two;
   // Biases as well where they fit: five against three of five, both norms layer norms with biases and a
   // gate: bf16 16384 x 2304 80 us and 91, 16384 x 3200 (14 waves a CU) 106 and 111, 8192 x 5120 (10) 93 and
