@@ -179,7 +179,10 @@ struct RowEnd {
     lse = empty ? -__builtin_inff() : in_range(most * scale + ln_s, most);
     entropy = empty ? 0.f : ln_s - kLn2 * v.w / v.s;
   }
-  __device__ __forceinline__ float logp(float x) const { return empty ? -__builtin_inff() : (x - most) * scale - ln_s; }
+  // (halves: the difference of the range's ends is past it, scale times it need not be)
+  __device__ __forceinline__ float logp(float x) const {
+    return empty ? -__builtin_inff() : (0.5f * x - 0.5f * most) * (2.f * scale) - ln_s;
+  }
 };
 __device__ __forceinline__ void store_row(const ScanArgs& a, int64_t row, const RowEnd& end, bool has_target, float target) {
   if (a.logp) a.logp[row] = has_target ? end.logp(target) : 0.f;

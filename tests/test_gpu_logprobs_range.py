@@ -151,3 +151,22 @@ def test_rows_of_nothing_have_no_gradient(pid, layers, dtype, n):
             same = pid.pointid_logprobs_backward(layers, X, got.lse, t if args[0] is not None else None,
                                                  *(good if v is d else v for v in args))
             assert torch.equal(dx[::2], same[::2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [3, 70, 900, 40000])
+@pytest.mark.parametrize("scale", [0.25, 2.0 ** -64])
+def test_columns_further_apart_than_the_range(pid, layers, dtype, n, scale):
+    """Logits whose difference passes fp32's range, their log probability not."""
+    t = torch.finfo(A.DT[dtype])
+    x = A.rand(A.gen(n), 3, n, dtype=dtype)
+    x[:, 0], x[:, 1] = t.max, t.min
+    x[1, 2] = -INF
+    targets = torch.tensor([1, 2, 0], dtype=torch.int32)
+    got = pid.pointid_logprobs(layers, x.to(DEV), targets.to(DEV), scale, entropy=True, top=3)
+    want = A.logprobs64(x.double(), scale, targets, 3)
+    for name in ("lse", "logp", "entropy", "top_logp"):
+        A.near(got[got._fields.index(name)], want[name][0], A.rounded(*want[name], "fp32"), name)
+    low = pid.pointid_logprobs(layers, x.to(DEV), torch.ones(3, dtype=torch.int32, device=DEV), scale)
+    v, tol = A.logprobs64(x.double(), scale, torch.ones(3, dtype=torch.int32), 0)["logp"]
+    A.near(low.logp, v, A.rounded(v, tol, "fp32"), "logp of the lowest")
