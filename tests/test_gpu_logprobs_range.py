@@ -87,7 +87,8 @@ def check(pid, layers, dtype, m, n, scale):
     p = d.exp()
     finite = torch.where(p > 0, d, 0.0)
     # (below 2^10 the kernels may leave z unrounded, or round its factors)
-    near_lse = torch.where(l.abs() < 1024, 4 * A.E * (rounded_logits(x, scale).abs().nan_to_num(posinf=0) + l.abs().nan_to_num(posinf=0)), 0.0)
+    size = rounded_logits(x, scale).abs().nan_to_num(posinf=0) + l.abs().nan_to_num(posinf=0)
+    near_lse = torch.where(l.abs() < 1024, 4 * A.E * size, 0.0)
     tp = p * (6 * A.E + 3 * A.E * finite.abs() + torch.where(p > 0, near_lse, 0.0))
     g = A.gen(n + 1)
     dlogp, dh, dl = (torch.randn(m, generator=g) for _ in range(3))
